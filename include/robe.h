@@ -405,9 +405,151 @@ int robe_last_device_status(robe_handle_t h, void* stream);
 #define ROBE_DBG_GRAD_POS 4
 #define ROBE_DBG_WINDOW 5
 #define ROBE_DBG_LONG_WALK 6
+#define ROBE_DBG_ROW_POS 7 /* position in a tensor of a row operator */
 #define ROBE_DBG_SELFTEST 99
 int robe_debug_status(void* stream);
 int robe_debug_selftest(void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Row operators: what a model does next with the rows it looked up.  They take no ROBE handle.  Element
+ * types are ROBE_F32 and ROBE_BF16 (`dtype`); everything is computed in fp32 and rounded once, to nearest
+ * even, where a result is stored; results are bit-reproducible.  A matrix is a device pointer, aligned to
+ * its elements, and a leading dimension `ld`: the distance of its rows in elements, at least their length
+ * (not looked at for a single row).  16-byte aligned rows are the fastest, any alignment is served.  An output
+ * overlaps no input and no other output unless an entry point says so (ROBE_ERR_INVALID_ARG); columns of
+ * one wider matrix do not overlap.  What stands between the rows of an output is left as it was.
+ * ROBE_ERR_UNSUPPORTED: more than a launch grid can hold.
+ */
+
+/*
+ * robe_dropout - out[r,c] = kept(r,c) ? in[r,c] * s : +0.  The decisions come from a counter-based
+ * generator and are never stored: the gradient of the call is the same call on the gradient of `out`.
+ * With t = floor(65536 p + 1/2) (p to the nearest multiple of 2^-16, so that the expectation is exact)
+ *     kept(r,c) = half(r,c) >= t,     s = 65536 / (65536 - t)
+ * where half(r,c) is 16-bit half c mod 8 (low half of a word first) of the four words that Philox4x32
+ * with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) makes
+ * of the counter (floor(c / 8), r, low and high half of n) under the key (low, high half of seed), with
+ * n = (offset + *step) mod 2^64.  A dropped NaN or infinity gives +0.  The decision does not depend on
+ * dtype, ld or alignment.  t = 65536 drops everything.
+ *   rows, cols  >= 0; rows <= 2^32, cols <= 2^31.   out may be `in` itself (same pointer, same ld).
+ *   p           in [0, 1].
+ *   seed        one per training run, say;  offset  one per call of a step (layer number).
+ *   step        device pointer to one uint64 that the kernel reads when it runs, so that a captured
+ *               graph draws anew in every replay once the caller counts it up; or NULL (0).
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
+ */
+int robe_dropout(const void* in, int64_t in_ld, void* out, int64_t out_ld, int64_t rows, int64_t cols,
+                 int dtype, float p, uint64_t seed, uint64_t offset, const uint64_t* step, void* stream);
+
+typedef struct robe_bias_ctx* robe_bias_t; /* opaque; host memory owned by the library */
+
+/*
+ * robe_bias_create - a learned relative position bias: one learned number per head and bucket of
+ * distances.  Of the S buckets of a side (S = num_buckets; half of it when two_sided) the first
+ * E = floor(S / 2) hold one distance each, 0 .. E-1; bucket E + k, 0 <= k < L = S - E, begins at the
+ * smallest distance n with n^L >= E^(L-k) max_distance^k (found in exact integers, no logarithm): equal
+ * steps of the distance's logarithm from E to max_distance.  The last bucket takes all that is farther.  A
+ * query at position p and a key at position j are r = j - p apart;
+ *     one-sided   bucket(r) = that of max(-r, 0)      (later keys share bucket 0)
+ *     two-sided   bucket(r) = that of |r|, + S for r > 0
+ *   num_buckets   2 .. 128 one-sided; even, 4 .. 256, two-sided.
+ *   max_distance  > E, < 2^31.
+ * The handle is constant after creation: calls on one handle may overlap.
+ */
+int robe_bias_create(robe_bias_t* out, uint32_t num_buckets, uint32_t max_distance, int two_sided);
+int robe_bias_destroy(robe_bias_t b);
+/* robe_bias_num_buckets - num_buckets, or a negative robe_status. */
+int robe_bias_num_buckets(robe_bias_t b);
+/* robe_bias_get_edges - copy out the smallest distance |r| of each bucket (host pointer to num_buckets words; of a
+ * bucket of later keys at least 1). */
+int robe_bias_get_edges(robe_bias_t b, int64_t* edges);
+
+/*
+ * robe_bias_forward - out[n,h,i,j] = rows[bucket(j - (start_n + i)), h]
+ *   rows      fp32 [num_buckets, heads], rows_ld apart: for instance the embeddings, d = heads, of the ids
+ *             0 .. num_buckets-1 of one table, as robe_forward writes them (rows_ld = T*d).
+ *   out       [batch, heads, q_len, k_len]: rows of k_len elements, out_ld apart.
+ *   q_start   position of the first query of every sequence; q_starts, when not NULL, is a device pointer
+ *             to batch positions, one per sequence (key j of every sequence stands at position j): one
+ *             query each with q_starts = lengths - 1 is a decoding step.  Any value, negative ones too.
+ *   causal    0, or 1: where the key is later than the query (r > 0) out is -infinity.
+ *   q_len + k_len < 2^31;  batch < 2^31;  1 <= heads < 2^22.
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
+ */
+int robe_bias_forward(robe_bias_t b, const float* rows, int64_t rows_ld, uint32_t heads, int64_t batch,
+                      int64_t q_len, int64_t k_len, int64_t q_start, const int64_t* q_starts, int causal,
+                      void* out, int64_t out_ld, int dtype, void* stream);
+
+/*
+ * robe_bias_backward - grad_rows[b,h] = sum of grad[n,h,i,j] over all n, i, j with bucket(j - (start_n + i)) = b
+ * (and r <= 0 when causal: what stands in masked places has no effect, NaN included).
+ *   grad        [batch, heads, q_len, k_len], rows grad_ld apart.
+ *   grad_rows   fp32 [num_buckets, heads], grad_rows_ld apart, overwritten (+0 for an empty bucket): what
+ *               robe_backward takes as grad_out.
+ *   workspace   256-byte aligned, robe_bias_backward_workspace_bytes for these sizes (0 for bad arguments).
+ * Errors: as above, and ROBE_ERR_WORKSPACE.
+ */
+size_t robe_bias_backward_workspace_bytes(robe_bias_t b, uint32_t heads, int64_t batch, int64_t q_len,
+                                          int64_t k_len);
+int robe_bias_backward(robe_bias_t b, const void* grad, int64_t grad_ld, uint32_t heads, int64_t batch,
+                       int64_t q_len, int64_t k_len, int64_t q_start, const int64_t* q_starts, int causal,
+                       int dtype, float* grad_rows, int64_t grad_rows_ld, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+#define ROBE_NORM_RMS 0   /* norm(v) = v / sqrt(mean(v^2) + eps)               */
+#define ROBE_NORM_LAYER 1 /* norm(v) = (v - mean(v)) / sqrt(var(v) + eps)      */
+#define ROBE_GATE_NONE 0   /* no gate (1)                                      */
+#define ROBE_GATE_ROW 1    /* one number per row: gate is [rows, 1]            */
+#define ROBE_GATE_VECTOR 2 /* [rows / gate_rows, d]: one vector for gate_rows rows in turn (1: a gate per element) */
+
+/*
+ * robe_residual_forward / robe_residual_backward - the join at which a block's output x enters the rows
+ * again, norms before and after included:
+ *     y      = norm(x) * w_post                        (x where w_post is NULL)
+ *     out    = residual + scale * gate * dropout(y)    (residual NULL: nothing is added to)
+ *     normed = norm(out) * w_pre                       (of out before its rounding; nothing where w_pre is NULL)
+ * Dropout as in robe_dropout (row r, column c of x; p = 0: none).  A join with residual = NULL and
+ * w_post = NULL is the entry of a model: dropout of looked-up rows and the norm before its first block.
+ * out may be residual itself (same pointer, same ld).
+ */
+typedef struct robe_residual_t {
+    int64_t rows, d;   /* rows >= 0, <= 2^32; 1 <= d <= 1048576 */
+    int dtype;         /* of x, residual, gate, out, normed and their gradients; weights and their gradients are fp32 [d] */
+    int norm;          /* ROBE_NORM_*, both norms */
+    float eps, scale;  /* eps >= 0 */
+    int gate;          /* ROBE_GATE_* */
+    int64_t gate_rows; /* ROBE_GATE_VECTOR: divides rows; not looked at otherwise */
+    float p;           /* in [0, 1] */
+    uint64_t seed, offset;
+    const uint64_t* step;
+} robe_residual_t;
+int robe_residual_forward(const robe_residual_t* c, const void* x, int64_t x_ld, const void* residual,
+                          int64_t residual_ld, const void* gate, int64_t gate_ld, const float* w_post,
+                          const float* w_pre, void* out, int64_t out_ld, void* normed, int64_t normed_ld,
+                          void* stream);
+
+/*
+ * The gradients, from x, gate, out (as the forward call stored it; only looked at with w_pre) and the
+ * gradients of out (NULL: zero) and normed (given exactly when w_pre is):
+ *     t = grad_out + dnorm(out; grad_normed w_pre)     grad_residual = t         (NULL: not wanted)
+ *     u = dropout(scale * gate * t)                    grad_x = dnorm(x; u w_post)   (u without w_post)
+ *     grad_gate = sum of scale * dropout(y) * t over what a gate element was used for   (NULL: not wanted)
+ *     grad_w_post = sum over rows of u norm(x)         grad_w_pre = sum over rows of grad_normed norm(out)
+ * with dnorm(v; g) = rstd (g - [mean g] - n mean(g n)), n = norm(v), rstd its factor, [..] with layer norm.
+ * grad_w_post and grad_w_pre are given exactly when their weights are; all outputs are overwritten (the
+ * weights' gradients with +0 when rows is 0).  grad_residual may be grad_out itself (same pointer, same ld).
+ *   gates      rows of the gate for ROBE_GATE_VECTOR, 0 otherwise
+ *   workspace  256-byte aligned, robe_residual_backward_workspace_bytes(rows, d, gates)
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_WORKSPACE, ROBE_ERR_CUDA.
+ */
+size_t robe_residual_backward_workspace_bytes(int64_t rows, int64_t d, int64_t gates);
+int robe_residual_backward(const robe_residual_t* c, const void* grad_out, int64_t grad_out_ld,
+                           const void* grad_normed, int64_t grad_normed_ld, const void* x, int64_t x_ld,
+                           const void* out, int64_t out_ld, const void* gate, int64_t gate_ld,
+                           const float* w_post, const float* w_pre, void* grad_x, int64_t grad_x_ld,
+                           void* grad_residual, int64_t grad_residual_ld, void* grad_gate,
+                           int64_t grad_gate_ld, float* grad_w_post, float* grad_w_pre, void* workspace,
+                           size_t workspace_bytes, void* stream);
 
 /* robe_status_string - static host string for a robe_status value. */
 const char* robe_status_string(int status);

@@ -52,6 +52,12 @@ ROBE_BWD_BINNED = 2
 
 ROBE_STATIC_SCRATCH_BYTES = 32 << 20
 
+ROBE_NORM_RMS = 0
+ROBE_NORM_LAYER = 1
+ROBE_GATE_NONE = 0
+ROBE_GATE_ROW = 1
+ROBE_GATE_VECTOR = 2
+
 ROBE_DBG_SELFTEST = 99
 
 EXPORTS = [
@@ -61,6 +67,9 @@ EXPORTS = [
     "robe_backward_deterministic_static", "robe_backward_adam",
     "robe_forward_keep", "robe_backward_kept", "robe_apply_sgd",
     "robe_debug_status", "robe_debug_selftest", "robe_backward_adagrad",
+    "robe_dropout", "robe_bias_create", "robe_bias_destroy", "robe_bias_num_buckets", "robe_bias_get_edges",
+    "robe_bias_forward", "robe_bias_backward_workspace_bytes", "robe_bias_backward",
+    "robe_residual_forward", "robe_residual_backward_workspace_bytes", "robe_residual_backward",
 ]
 
 if not os.path.exists(LIB_PATH):
@@ -93,15 +102,50 @@ _lib.robe_debug_status.argtypes = [_vp]
 _lib.robe_debug_selftest.argtypes = [_vp]
 _lib.robe_set_status_word.argtypes = [_vp, _vp]
 _lib.robe_last_device_status.argtypes = [_vp, _vp]
+
+
+class _BiasCtx(C.Structure):
+    """What a position-bias handle points to (opaque)."""
+
+
+_BiasHandle = C.POINTER(_BiasCtx)
+
+
+class _Residual(C.Structure):
+    """robe_residual_t"""
+    _fields_ = [("rows", _i64), ("d", _i64), ("dtype", C.c_int), ("norm", C.c_int), ("eps", C.c_float),
+                ("scale", C.c_float), ("gate", C.c_int), ("gate_rows", _i64), ("p", C.c_float), ("seed", _u64),
+                ("offset", _u64), ("step", _vp)]
+
+
+_rows = [_vp, _i64]  # a matrix: pointer and leading dimension
+_lib.robe_dropout.argtypes = _rows * 2 + [_i64, _i64, C.c_int, C.c_float, _u64, _u64, _vp, _vp]
+_lib.robe_bias_create.argtypes = [C.POINTER(_BiasHandle), _u32, _u32, C.c_int]
+_lib.robe_bias_destroy.argtypes = [_BiasHandle]
+_lib.robe_bias_num_buckets.argtypes = [_BiasHandle]
+_lib.robe_bias_get_edges.argtypes = [_BiasHandle, C.POINTER(_i64)]
+_lib.robe_bias_forward.argtypes = [_BiasHandle] + _rows + [_u32] + [_i64] * 4 + [_vp, C.c_int] + _rows + [C.c_int, _vp]
+_lib.robe_bias_backward_workspace_bytes.argtypes = [_BiasHandle, _u32, _i64, _i64, _i64]
+_lib.robe_bias_backward_workspace_bytes.restype = C.c_size_t
+_lib.robe_bias_backward.argtypes = ([_BiasHandle] + _rows + [_u32] + [_i64] * 4 + [_vp, C.c_int, C.c_int] + _rows
+                                    + [_vp, C.c_size_t, _vp])
+_lib.robe_residual_forward.argtypes = [C.POINTER(_Residual)] + _rows * 3 + [_vp, _vp] + _rows * 2 + [_vp]
+_lib.robe_residual_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.robe_residual_backward_workspace_bytes.restype = C.c_size_t
+_lib.robe_residual_backward.argtypes = ([C.POINTER(_Residual)] + _rows * 5 + [_vp, _vp] + _rows * 3
+                                        + [_vp, _vp, _vp, C.c_size_t, _vp])
 _lib.robe_status_string.argtypes = [C.c_int]
 _lib.robe_status_string.restype = C.c_char_p
 for _name in EXPORTS:
-    if _name not in ("robe_backward_workspace_bytes", "robe_status_string"):
+    if not _name.endswith("workspace_bytes") and _name != "robe_status_string":
         getattr(_lib, _name).restype = C.c_int
 
 _native.set_calls(_vp, *(C.cast(getattr(_lib, _name), _vp).value for _name in (
     "robe_set_option", "robe_forward", "robe_forward_keep", "robe_backward", "robe_backward_kept",
     "robe_backward_adam", "robe_backward_adagrad", "robe_apply_sgd")))
+_native.set_row_calls(_BiasHandle, *(C.cast(getattr(_lib, _name), _vp).value for _name in (
+    "robe_dropout", "robe_bias_num_buckets", "robe_bias_forward", "robe_bias_backward", "robe_residual_forward",
+    "robe_residual_backward")))
 _NOT_TAKEN = 1  # from _native: nothing was called
 
 
@@ -284,6 +328,222 @@ def robe_apply_sgd(h, grad_array, lr: float, zero_grad: bool = True, stream=None
         return _check(rc, "robe_apply_sgd")
     _check(_lib.robe_apply_sgd(h, _dev_ptr(grad_array, torch.float32), lr, 1 if zero_grad else 0,
                                _stream_ptr(stream)), "robe_apply_sgd")
+
+
+# ---- row operators: what a model does next with the rows.  Tensors are on the current device; a matrix is a tensor whose
+# last dimension is contiguous and whose others collapse to one (a column slice of a wider one, for instance).
+
+_TYPES = {torch.float32: ROBE_F32, torch.bfloat16: ROBE_BF16}
+
+
+def _here(t, what, dtype=None):
+    """A CUDA tensor of the current device (and element type)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what}: expected a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+    return t
+
+
+def _matrix(t, what, dtype=None):
+    """(pointer, leading dimension, rows, columns)"""
+    _here(t, what, dtype)
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{what}: expected float32 or bfloat16, got {t.dtype}")
+    if t.dim() == 0:
+        raise ValueError(f"{what}: expected a tensor of rows")
+    cols = t.shape[-1]
+    rows = t.numel() // cols if cols else 0
+    if t.numel() == 0:
+        return 0, cols, rows, cols
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last dimension is not contiguous")
+    ld, span = cols, None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if span is None:
+            ld = stride
+            if ld < cols:
+                raise ValueError(f"{what}: rows overlap")
+        elif stride != span:
+            raise ValueError(f"{what}: the rows are not equally far apart")
+        span = stride * size
+    return t.data_ptr(), ld, rows, cols
+
+
+def _matrix_like(t, what, dtype, rows, cols):
+    """Pointer and leading dimension of a matrix of that type and size; of None: (None, 0)."""
+    if t is None:
+        return None, 0
+    p, ld, r, c = _matrix(t, what, dtype)
+    if (r, c) != (rows, cols):
+        raise ValueError(f"{what}: {r} rows of {c}, expected {rows} of {cols}")
+    return p, ld
+
+
+def _vector(t, what, n, dtype=torch.float32):
+    """Pointer of a contiguous vector of n elements; of None: None."""
+    if t is None:
+        return None
+    _here(t, what, dtype)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {n} contiguous elements")
+    return t.data_ptr()
+
+
+def _step_ptr(step):
+    if step is None:
+        return None
+    if _here(step, "step").dtype not in (torch.int64, torch.uint64) or step.numel() != 1:
+        raise TypeError("step: expected one int64 or uint64 element")
+    return step.data_ptr()
+
+
+def robe_dropout(x, out, p: float, seed: int, offset: int = 0, step=None, stream=None) -> None:
+    """out = dropout of the rows x.  The gradient of the call is the same call on the gradient of `out`."""
+    rc = _native.dropout(x, out, p, seed, offset, step, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_dropout")
+    ptr, ld, rows, cols = _matrix(x, "x")
+    out_ptr, out_ld = _matrix_like(out, "out", x.dtype, rows, cols)
+    _check(_lib.robe_dropout(ptr, ld, out_ptr, out_ld, rows, cols, _TYPES[x.dtype], p, seed & (2**64 - 1),
+                             offset & (2**64 - 1), _step_ptr(step), _stream_ptr(stream)), "robe_dropout")
+
+
+def robe_bias_create(num_buckets: int, max_distance: int, two_sided: bool):
+    b = _BiasHandle()
+    if not (0 <= num_buckets < 2**32 and 0 <= max_distance < 2**32):
+        raise RobeError(ROBE_ERR_INVALID_ARG, "robe_bias_create")
+    _check(_lib.robe_bias_create(C.byref(b), num_buckets, max_distance, 1 if two_sided else 0), "robe_bias_create")
+    return b
+
+
+def robe_bias_destroy(b) -> None:
+    _check(_lib.robe_bias_destroy(b), "robe_bias_destroy")
+
+
+def robe_bias_num_buckets(b) -> int:
+    n = int(_lib.robe_bias_num_buckets(b))
+    _check(min(n, 0), "robe_bias_num_buckets")
+    return n
+
+
+def robe_bias_get_edges(b):
+    """Smallest distance of each bucket."""
+    out = (_i64 * robe_bias_num_buckets(b))()
+    _check(_lib.robe_bias_get_edges(b, out), "robe_bias_get_edges")
+    return [int(v) for v in out]
+
+
+def _bias_matrix(t, what):
+    """(pointer, leading dimension, batch, heads, queries, keys) of [batch, heads, queries, keys] or [heads, ..]."""
+    if isinstance(t, torch.Tensor) and t.dim() not in (3, 4):
+        raise ValueError(f"{what}: expected [batch, heads, queries, keys] or [heads, queries, keys]")
+    p, ld, _, _ = _matrix(t, what)
+    n, h, q, k = (1, *t.shape) if t.dim() == 3 else t.shape
+    return p, ld, n, h, q, k
+
+
+def _starts(q_start, batch):
+    """(start of all, pointer to starts)"""
+    if isinstance(q_start, torch.Tensor):
+        return 0, _vector(q_start, "q_start", batch, torch.int64)
+    return q_start, None
+
+
+def robe_bias_forward(b, rows, out, q_start=0, causal: bool = False, stream=None) -> None:
+    """out[n,h,i,j] = rows[bucket(j - (start_n + i)), h]; q_start an int or an int64 tensor of one start per sequence."""
+    rc = _native.bias_forward(b, rows, out, q_start, causal, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_bias_forward")
+    p, ld, n, h, q, k = _bias_matrix(out, "out")
+    table, table_ld = _matrix_like(rows, "rows", torch.float32, robe_bias_num_buckets(b), h)
+    start, starts = _starts(q_start, n)
+    _check(_lib.robe_bias_forward(b, table, table_ld, h, n, q, k, start, starts, 1 if causal else 0, p, ld,
+                                  _TYPES[out.dtype], _stream_ptr(stream)), "robe_bias_forward")
+
+
+def robe_bias_backward_workspace_bytes(b, heads: int, batch: int, q_len: int, k_len: int) -> int:
+    return int(_lib.robe_bias_backward_workspace_bytes(b, heads, batch, q_len, k_len))
+
+
+def robe_bias_backward(b, grad, grad_rows, workspace, q_start=0, causal: bool = False, stream=None) -> None:
+    """grad_rows[b,h] = sum of grad[n,h,i,j] over bucket b."""
+    rc = _native.bias_backward(b, grad, grad_rows, workspace, q_start, causal, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_bias_backward")
+    p, ld, n, h, q, k = _bias_matrix(grad, "grad")
+    table, table_ld = _matrix_like(grad_rows, "grad_rows", torch.float32, robe_bias_num_buckets(b), h)
+    start, starts = _starts(q_start, n)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.robe_bias_backward(b, p, ld, h, n, q, k, start, starts, 1 if causal else 0, _TYPES[grad.dtype], table,
+                                   table_ld, _dev_ptr(workspace), ws_bytes, _stream_ptr(stream)), "robe_bias_backward")
+
+
+def _residual(x, gate, scale, norm, eps, p, seed, offset, step):
+    """robe_residual_t of a call, x's matrix, the gate's (pointer, leading dimension) and (rows, columns)."""
+    ptr, ld, rows, d = _matrix(x, "x")
+    kind, gate_rows, gate_at, gate_size = ROBE_GATE_NONE, 0, (None, 0), (0, 0)
+    if gate is not None:
+        g_ptr, g_ld, g_rows, g_cols = _matrix(gate, "gate", x.dtype)
+        if g_cols == d and g_rows and rows % g_rows == 0:
+            kind, gate_rows = ROBE_GATE_VECTOR, max(1, rows // g_rows)
+        elif g_cols == 1 and g_rows == rows:
+            kind = ROBE_GATE_ROW
+        elif rows == 0 and g_rows == 0:
+            kind, gate_rows = ROBE_GATE_VECTOR, 1
+        else:
+            raise ValueError(f"gate: {g_rows} rows of {g_cols} for {rows} rows of {d}")
+        gate_at, gate_size = (g_ptr, g_ld), (g_rows, g_cols)
+    c = _Residual(rows, d, _TYPES[x.dtype], norm, eps, scale, kind, gate_rows, p, seed & (2**64 - 1),
+                  offset & (2**64 - 1), _step_ptr(step))
+    return c, (ptr, ld), gate_at, gate_size
+
+
+def robe_residual_forward(x, residual, out, normed=None, w_post=None, w_pre=None, gate=None, scale: float = 1.0,
+                          norm: int = ROBE_NORM_RMS, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset: int = 0,
+                          step=None, stream=None) -> None:
+    """out = residual + scale * gate * dropout(norm(x) w_post), normed = norm(out) w_pre.  gate: [rows, 1], [rows, d] or
+    [rows / k, d] (k rows in turn share a vector)."""
+    rc = _native.residual_forward(x, residual, out, normed, w_post, w_pre, gate, scale, norm, eps, p, seed, offset, step,
+                                  stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_residual_forward")
+    c, x_at, gate_at, _ = _residual(x, gate, scale, norm, eps, p, seed, offset, step)
+    like = lambda t, what: _matrix_like(t, what, x.dtype, c.rows, c.d)
+    _check(_lib.robe_residual_forward(C.byref(c), *x_at, *like(residual, "residual"), *gate_at,
+                                      _vector(w_post, "w_post", c.d), _vector(w_pre, "w_pre", c.d), *like(out, "out"),
+                                      *like(normed, "normed"), _stream_ptr(stream)), "robe_residual_forward")
+
+
+def robe_residual_backward_workspace_bytes(rows: int, d: int, gates: int = 0) -> int:
+    """gates: rows of a gate of [rows / k, d]; 0 for no gate or one of [rows, 1]."""
+    return int(_lib.robe_residual_backward_workspace_bytes(rows, d, gates))
+
+
+def robe_residual_backward(grad_out, grad_normed, x, out, grad_x, grad_residual=None, w_post=None, w_pre=None, gate=None,
+                           grad_w_post=None, grad_w_pre=None, grad_gate=None, workspace=None, scale: float = 1.0,
+                           norm: int = ROBE_NORM_RMS, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset: int = 0,
+                           step=None, stream=None) -> None:
+    """Gradients of robe_residual_forward from x, out and gate as that call had and left them."""
+    rc = _native.residual_backward(grad_out, grad_normed, x, out, grad_x, grad_residual, w_post, w_pre, gate, grad_w_post,
+                                   grad_w_pre, grad_gate, workspace, scale, norm, eps, p, seed, offset, step, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_residual_backward")
+    c, x_at, gate_at, gate_size = _residual(x, gate, scale, norm, eps, p, seed, offset, step)
+    like = lambda t, what: _matrix_like(t, what, x.dtype, c.rows, c.d)
+    if grad_gate is not None and gate is None:
+        raise ValueError("grad_gate: there is no gate")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.robe_residual_backward(
+        C.byref(c), *like(grad_out, "grad_out"), *like(grad_normed, "grad_normed"), *x_at, *like(out, "out"), *gate_at,
+        _vector(w_post, "w_post", c.d), _vector(w_pre, "w_pre", c.d), *like(grad_x, "grad_x"),
+        *like(grad_residual, "grad_residual"), *_matrix_like(grad_gate, "grad_gate", x.dtype, *gate_size),
+        _vector(grad_w_post, "grad_w_post", c.d), _vector(grad_w_pre, "grad_w_pre", c.d), _dev_ptr(workspace), ws_bytes,
+        _stream_ptr(stream)), "robe_residual_backward")
 
 
 def robe_debug_status(stream=None) -> int:

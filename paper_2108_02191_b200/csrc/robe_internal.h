@@ -131,6 +131,38 @@ cudaError_t launch_block_keys(const Problem& pb, void* workspace, size_t workspa
 cudaError_t launch_dense_sgd_apply(float* array, float* grad, uint64_t m, float lr, bool zero_grad,
                                    cudaStream_t st);
 
+// ---- row operators (robe_dropout.cu, robe_bias.cu, robe_residual.cu); dtype as Problem::dtype, leading dimensions
+// (ld) in elements.  cudaErrorInvalidValue: more CTAs than a grid has.
+
+struct DropParams;
+cudaError_t launch_dropout(const void* in, int64_t in_ld, void* out, int64_t out_ld, int64_t rows, int64_t cols, int dtype,
+                           const DropParams& drop, cudaStream_t st);
+
+constexpr uint32_t kBiasMaxSide = 128;
+struct BiasBuckets {
+    uint32_t buckets, side;  // of all distances, of one side's (the same unless two-sided)
+    int two_sided;
+    int32_t edges[kBiasMaxSide];  // smallest distance of bucket k of a side; edges[0] = 0, non-decreasing
+};
+struct BiasProblem {
+    BiasBuckets bk;
+    const float* rows;  // device [buckets, heads], forward only
+    int64_t rows_ld;
+    uint32_t heads;
+    int64_t batch, q_len, k_len, q_start;
+    const int64_t* q_starts;  // device [batch] or nullptr
+    int causal;
+};
+cudaError_t launch_bias_forward(const BiasProblem& pb, void* out, int64_t out_ld, int dtype, cudaStream_t st);
+size_t bias_grad_workspace_bytes(uint32_t buckets, uint32_t heads, int64_t batch, int64_t q_len, int64_t k_len);
+cudaError_t launch_bias_backward(const BiasProblem& pb, const void* grad, int64_t grad_ld, int dtype, float* grad_rows,
+                                 int64_t grad_rows_ld, void* workspace, cudaStream_t st);
+
+struct ResidualProblem;
+cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaStream_t st);
+size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates);
+cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void* workspace, cudaStream_t st);
+
 // id / offset range check into the status word
 cudaError_t launch_validate(const Problem& pb, cudaStream_t st);
 

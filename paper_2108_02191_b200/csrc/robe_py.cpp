@@ -31,7 +31,24 @@ struct Calls {
     decltype(&robe_apply_sgd) apply_sgd;
 } calls;
 
-PyObject* handle_type;  // ctypes.c_void_p
+struct RowCalls {
+    decltype(&robe_dropout) dropout;
+    decltype(&robe_bias_num_buckets) bias_num_buckets;
+    decltype(&robe_bias_forward) bias_forward;
+    decltype(&robe_bias_backward) bias_backward;
+    decltype(&robe_residual_forward) residual_forward;
+    decltype(&robe_residual_backward) residual_backward;
+} row_calls;
+
+PyObject* handle_type;       // ctypes.c_void_p
+PyObject* bias_handle_type;  // pointer to the binding's opaque structure
+
+// Rows of a tensor: its last dimension contiguous, the others equally far apart.
+struct Matrix {
+    void* p = nullptr;
+    int64_t ld = 0, rows = 0, cols = 0;
+    int dtype = ROBE_F32;
+};
 
 // Reads the arguments of one call; ok turns false at the first one that is not plainly usable.
 struct Reader {
@@ -99,11 +116,83 @@ struct Reader {
         }
         return (float)v;
     }
-    // a ctypes.c_void_p and nothing else that has a buffer: its buffer is the pointer
-    robe_handle_t handle(int k) {
+    bool truth(int k) {
+        if (args[k] != Py_True && args[k] != Py_False) ok = false;
+        return args[k] == Py_True;
+    }
+    // a tensor of the current device
+    const at::Tensor* local(int k) {
+        if (!THPVariable_Check(args[k])) {
+            ok = false;
+            return nullptr;
+        }
+        const at::Tensor& t = THPVariable_Unpack(args[k]);
+        if (!t.is_cuda() || !t.has_storage() || t.device().index() != c10::cuda::current_device()) {
+            ok = false;
+            return nullptr;
+        }
+        return &t;
+    }
+    Matrix matrix(int k) {
+        Matrix m;
+        const at::Tensor* t = local(k);
+        if (t == nullptr) return m;
+        if (t->scalar_type() == at::kBFloat16) m.dtype = ROBE_BF16;
+        else if (t->scalar_type() != at::kFloat) ok = false;
+        const int64_t dims = t->dim();
+        if (dims == 0 || t->numel() == 0) {  // (the ctypes path takes empty ones)
+            ok = false;
+            return m;
+        }
+        m.cols = t->size(dims - 1);
+        m.rows = t->numel() / m.cols;
+        if (m.cols > 1 && t->stride(dims - 1) != 1) ok = false;
+        m.ld = m.cols;
+        int64_t span = -1;
+        for (int64_t i = dims - 2; i >= 0; --i) {
+            if (t->size(i) == 1) continue;
+            if (span < 0) {
+                m.ld = t->stride(i);
+                if (m.ld < m.cols) ok = false;
+            } else if (t->stride(i) != span) {
+                ok = false;
+            }
+            span = t->stride(i) * t->size(i);
+        }
+        m.p = t->data_ptr();
+        return m;
+    }
+    Matrix matrix_like(int k, const Matrix& of) {
+        if (args[k] == Py_None) return Matrix();
+        const Matrix m = matrix(k);
+        if (m.rows != of.rows || m.cols != of.cols || m.dtype != of.dtype) ok = false;
+        return m;
+    }
+    void* vector_or_null(int k, int64_t n, at::ScalarType type) {
+        if (args[k] == Py_None) return nullptr;
+        const at::Tensor* t = local(k);
+        if (t == nullptr || t->scalar_type() != type || t->numel() != n || !t->is_contiguous()) {
+            ok = false;
+            return nullptr;
+        }
+        return t->data_ptr();
+    }
+    const uint64_t* step(int k) {
+        if (args[k] == Py_None) return nullptr;
+        const at::Tensor* t = local(k);
+        if (t == nullptr || (t->scalar_type() != at::kLong && t->scalar_type() != at::kUInt64) || t->numel() != 1) {
+            ok = false;
+            return nullptr;
+        }
+        return (const uint64_t*)t->data_ptr();
+    }
+    robe_bias_t bias(int k) { return (robe_bias_t)pointer_in(k, bias_handle_type); }
+    robe_handle_t handle(int k) { return (robe_handle_t)pointer_in(k, handle_type); }
+    // a ctypes object of that type and nothing else that has a buffer: its buffer is the pointer
+    void* pointer_in(int k, PyObject* type) {
         Py_buffer b;
-        robe_handle_t h = nullptr;
-        if ((PyObject*)Py_TYPE(args[k]) != handle_type || PyObject_GetBuffer(args[k], &b, PyBUF_SIMPLE) != 0) {
+        void* h = nullptr;
+        if ((PyObject*)Py_TYPE(args[k]) != type || PyObject_GetBuffer(args[k], &b, PyBUF_SIMPLE) != 0) {
             PyErr_Clear();
             ok = false;
             return nullptr;
@@ -285,6 +374,173 @@ PyObject* apply_sgd(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return made([&] { return calls.apply_sgd(h, grad_array, lr, zero, st); });
 }
 
+// (x, out, p, seed, offset, step, stream)
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 7) return not_taken();
+    Reader r{args};
+    const Matrix x = r.matrix(0), out = r.matrix_like(1, x);
+    const float p = r.number(2);
+    const int64_t seed = r.whole(3), offset = r.whole(4);
+    const uint64_t* step = r.step(5);
+    void* st = r.stream(6);
+    if (!r.ok) return not_taken();
+    return made([&] {
+        return row_calls.dropout(x.p, x.ld, out.p, out.ld, x.rows, x.cols, x.dtype, p, (uint64_t)seed, (uint64_t)offset, step, st);
+    });
+}
+
+// What a bias call has: the matrices [batch, heads, queries, keys] (argument `wide`), the rows of the buckets (`rows`) and
+// where the queries start.
+struct Bias {
+    robe_bias_t b;
+    Matrix wide, rows;
+    int64_t batch = 1, heads = 0, q = 0, k = 0, start = 0;
+    const int64_t* starts = nullptr;
+    Bias(Reader& r, int wide_at, int rows_at, int start_at) {
+        b = r.bias(0);
+        wide = r.matrix(wide_at);
+        rows = r.matrix(rows_at);
+        if (!r.ok) return;
+        const at::Tensor& t = THPVariable_Unpack(r.args[wide_at]);
+        const int64_t dims = t.dim();
+        if (dims != 3 && dims != 4) {
+            r.ok = false;
+            return;
+        }
+        if (dims == 4) batch = t.size(0);
+        heads = t.size(dims - 3);
+        q = t.size(dims - 2);
+        k = t.size(dims - 1);
+        if (rows.dtype != ROBE_F32 || rows.cols != heads || rows.rows != row_calls.bias_num_buckets(b)) r.ok = false;
+        if (THPVariable_Check(r.args[start_at])) starts = (const int64_t*)r.vector_or_null(start_at, batch, at::kLong);
+        else start = r.whole(start_at);
+    }
+};
+
+// (b, rows, out, q_start, causal, stream)
+PyObject* bias_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 6) return not_taken();
+    Reader r{args};
+    const Bias a(r, 2, 1, 3);
+    const int causal = r.truth(4);
+    void* st = r.stream(5);
+    if (!r.ok) return not_taken();
+    return made([&] {
+        return row_calls.bias_forward(a.b, (const float*)a.rows.p, a.rows.ld, (uint32_t)a.heads, a.batch, a.q, a.k, a.start,
+                                      a.starts, causal, a.wide.p, a.wide.ld, a.wide.dtype, st);
+    });
+}
+
+// (b, grad, grad_rows, workspace, q_start, causal, stream)
+PyObject* bias_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 7) return not_taken();
+    Reader r{args};
+    size_t ws_bytes = 0;
+    const Bias a(r, 1, 2, 4);
+    void* ws = r.bytes_or_null(3, ws_bytes);
+    const int causal = r.truth(5);
+    void* st = r.stream(6);
+    if (!r.ok) return not_taken();
+    return made([&] {
+        return row_calls.bias_backward(a.b, a.wide.p, a.wide.ld, (uint32_t)a.heads, a.batch, a.q, a.k, a.start, a.starts,
+                                       causal, a.wide.dtype, (float*)a.rows.p, a.rows.ld, ws, ws_bytes, st);
+    });
+}
+
+// The scalars that end a residual call: (scale, norm, eps, p, seed, offset, step), from argument `at` on; the gate's kind goes
+// by its size.
+robe_residual_t residual(Reader& r, int at, const Matrix& x, const Matrix& gate, bool gated) {
+    robe_residual_t c{};
+    c.rows = x.rows;
+    c.d = x.cols;
+    c.dtype = x.dtype;
+    c.scale = r.number(at);
+    const int64_t norm = r.whole(at + 1);
+    if (norm != ROBE_NORM_RMS && norm != ROBE_NORM_LAYER) r.ok = false;
+    c.norm = (int)norm;
+    c.eps = r.number(at + 2);
+    c.p = r.number(at + 3);
+    c.seed = (uint64_t)r.whole(at + 4);
+    c.offset = (uint64_t)r.whole(at + 5);
+    c.step = r.step(at + 6);
+    if (!gated || !r.ok) return c;
+    if (gate.dtype != x.dtype) r.ok = false;
+    if (gate.cols == x.cols && x.rows % gate.rows == 0) {
+        c.gate = ROBE_GATE_VECTOR;
+        c.gate_rows = x.rows / gate.rows;
+    } else if (gate.cols == 1 && gate.rows == x.rows) {
+        c.gate = ROBE_GATE_ROW;
+    } else {
+        r.ok = false;
+    }
+    return c;
+}
+
+// (x, residual, out, normed, w_post, w_pre, gate, scale, norm, eps, p, seed, offset, step, stream)
+PyObject* residual_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 15) return not_taken();
+    Reader r{args};
+    const Matrix x = r.matrix(0), residual_ = r.matrix_like(1, x), out = r.matrix_like(2, x), normed = r.matrix_like(3, x);
+    const float* w_post = (const float*)r.vector_or_null(4, x.cols, at::kFloat);
+    const float* w_pre = (const float*)r.vector_or_null(5, x.cols, at::kFloat);
+    const bool gated = args[6] != Py_None;
+    const Matrix gate = gated ? r.matrix(6) : Matrix();
+    const robe_residual_t c = residual(r, 7, x, gate, gated);
+    void* st = r.stream(14);
+    if (!r.ok) return not_taken();
+    return made([&] {
+        return row_calls.residual_forward(&c, x.p, x.ld, residual_.p, residual_.ld, gate.p, gate.ld, w_post, w_pre, out.p, out.ld,
+                                          normed.p, normed.ld, st);
+    });
+}
+
+// (grad_out, grad_normed, x, out, grad_x, grad_residual, w_post, w_pre, gate, grad_w_post, grad_w_pre, grad_gate, workspace,
+//  scale, norm, eps, p, seed, offset, step, stream)
+PyObject* residual_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 21) return not_taken();
+    Reader r{args};
+    const Matrix x = r.matrix(2), grad_out = r.matrix_like(0, x), grad_normed = r.matrix_like(1, x), out = r.matrix_like(3, x),
+                 grad_x = r.matrix_like(4, x), grad_residual = r.matrix_like(5, x);
+    const float* w_post = (const float*)r.vector_or_null(6, x.cols, at::kFloat);
+    const float* w_pre = (const float*)r.vector_or_null(7, x.cols, at::kFloat);
+    const bool gated = args[8] != Py_None;
+    const Matrix gate = gated ? r.matrix(8) : Matrix();
+    float* grad_w_post = (float*)r.vector_or_null(9, x.cols, at::kFloat);
+    float* grad_w_pre = (float*)r.vector_or_null(10, x.cols, at::kFloat);
+    if (!gated && args[11] != Py_None) r.ok = false;
+    const Matrix grad_gate = gated ? r.matrix_like(11, gate) : Matrix();
+    size_t ws_bytes = 0;
+    void* ws = r.bytes_or_null(12, ws_bytes);
+    const robe_residual_t c = residual(r, 13, x, gate, gated);
+    void* st = r.stream(20);
+    if (!r.ok) return not_taken();
+    return made([&] {
+        return row_calls.residual_backward(&c, grad_out.p, grad_out.ld, grad_normed.p, grad_normed.ld, x.p, x.ld, out.p, out.ld,
+                                           gate.p, gate.ld, w_post, w_pre, grad_x.p, grad_x.ld, grad_residual.p,
+                                           grad_residual.ld, grad_gate.p, grad_gate.ld, grad_w_post, grad_w_pre, ws, ws_bytes,
+                                           st);
+    });
+}
+
+// (the type of a position-bias handle, addresses of the C-ABI functions in the order of RowCalls)
+PyObject* set_row_calls(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    void* p[6];
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "set_row_calls takes a type and six addresses");
+        return nullptr;
+    }
+    for (int k = 0; k < 6; ++k) {
+        p[k] = PyLong_AsVoidPtr(args[k + 1]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    Py_INCREF(args[0]);
+    Py_XSETREF(bias_handle_type, args[0]);
+    row_calls = RowCalls{(decltype(row_calls.dropout))p[0],          (decltype(row_calls.bias_num_buckets))p[1],
+                         (decltype(row_calls.bias_forward))p[2],     (decltype(row_calls.bias_backward))p[3],
+                         (decltype(row_calls.residual_forward))p[4], (decltype(row_calls.residual_backward))p[5]};
+    Py_RETURN_NONE;
+}
+
 // (the type of a handle, addresses of the C-ABI functions in the order of Calls)
 PyObject* set_calls(PyObject*, PyObject* const* args, Py_ssize_t n) {
     void* p[8];
@@ -315,6 +571,12 @@ PyMethodDef methods[] = {
     {"backward_adam", FAST(backward_adam), METH_FASTCALL, "robe_backward_adam"},
     {"backward_adagrad", FAST(backward_adagrad), METH_FASTCALL, "robe_backward_adagrad"},
     {"apply_sgd", FAST(apply_sgd), METH_FASTCALL, "robe_apply_sgd"},
+    {"set_row_calls", FAST(set_row_calls), METH_FASTCALL, "type of a position-bias handle, addresses of the C-ABI functions"},
+    {"dropout", FAST(dropout), METH_FASTCALL, "robe_dropout"},
+    {"bias_forward", FAST(bias_forward), METH_FASTCALL, "robe_bias_forward"},
+    {"bias_backward", FAST(bias_backward), METH_FASTCALL, "robe_bias_backward"},
+    {"residual_forward", FAST(residual_forward), METH_FASTCALL, "robe_residual_forward"},
+    {"residual_backward", FAST(residual_backward), METH_FASTCALL, "robe_residual_backward"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_robe_py", "native marshalling of the binding", -1, methods,

@@ -1,0 +1,121 @@
+// What the row operators (dropout, position bias, residual join) share: element types, 16-byte pieces of a row,
+// and the counter-based generator of the dropout.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "robe_device.cuh"
+
+namespace robe {
+
+// ---- elements.  Everything is computed in fp32; bf16 is widened exactly and rounded once, to nearest even, where
+// a result is stored.
+template <class T>
+constexpr int kPiece = 16 / (int)sizeof(T);  // elements of a 16-byte piece
+
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <class T>
+__device__ __forceinline__ T narrow(float v);
+template <>
+__device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// V consecutive elements as one access of V * sizeof(T) bytes (aligned to that), V a power of two, at most 16 bytes
+template <class T, int V>
+struct alignas(V * sizeof(T)) Pack {
+    T v[V];
+};
+template <int BYTES>
+struct Word;
+template <>
+struct Word<16> { using type = uint4; };
+template <>
+struct Word<8> { using type = uint2; };
+template <>
+struct Word<4> { using type = unsigned; };
+template <>
+struct Word<2> { using type = unsigned short; };
+
+// STREAM: the value is read (written) once and nothing else soon wants its line
+template <bool STREAM, class T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
+    using W = typename Word<V * sizeof(T)>::type;
+    union {
+        W w;
+        Pack<T, V> e;
+    } u;
+    u.w = STREAM ? __ldcs((const W*)p) : __ldca((const W*)p);
+    return u.e;
+}
+template <bool STREAM, class T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& e) {
+    using W = typename Word<V * sizeof(T)>::type;
+    union U {
+        W w;
+        Pack<T, V> e;
+        __device__ U() {}
+    } u;
+    u.e = e;
+    if (STREAM) __stcs((W*)p, u.w);
+    else *(W*)p = u.w;
+}
+
+// ---- generator: Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2,
+// 3", 2011): a block cipher of the counter under the key, so any element's number is had from its position alone.
+struct DropParams {
+    uint32_t threshold;     // of 65536: an element is dropped when its 16 bits are below
+    float scale;            // 65536 / (65536 - threshold), what kept elements are multiplied by
+    uint64_t seed, offset;  // key; upper half of the counter
+    const uint64_t* step;   // device, added to offset, or nullptr
+};
+
+__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint64_t c23, uint64_t key) {
+    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
+    uint32_t c2 = (uint32_t)c23, c3 = (uint32_t)(c23 >> 32);
+#pragma unroll
+    for (int round = 0; round < 10; ++round) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)p0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// The words that columns 8 g .. 8 g + 7 of row r are kept or dropped by: column 8 g + k by half k & 1 (low first) of
+// word k / 2.
+__device__ __forceinline__ uint4 drop_words(uint32_t r, uint32_t g, uint64_t offset, uint64_t seed) {
+    return philox(g, r, offset, seed);
+}
+__device__ __forceinline__ uint64_t drop_offset(const DropParams& d) {
+    return d.offset + (d.step != nullptr ? __ldca((const unsigned long long*)d.step) : 0ull);
+}
+__device__ __forceinline__ bool drop_keeps(const uint4& w, int k, uint32_t threshold) {
+    const uint32_t word = k < 2 ? w.x : k < 4 ? w.y : k < 6 ? w.z : w.w;
+    return ((k & 1) ? word >> 16 : word & 0xFFFFu) >= threshold;
+}
+
+// ---- the residual join: what one call is given
+struct RowsRef {  // rows of a matrix, ld elements apart
+    void* p;
+    int64_t ld;
+};
+struct ResidualProblem {
+    int64_t rows, d;
+    int layer;        // 0: root mean square norm, 1: layer norm
+    float eps, scale;
+    int gate_kind;    // 0 none, 1 a number per row, 2 a vector of d per gate_rows rows
+    int64_t gate_rows;
+    DropParams drop;  // threshold 0: no dropout
+    const float *w_post, *w_pre;  // or nullptr: no norm there
+    RowsRef x, residual, gate, out, normed;  // forward; residual.p may be nullptr (nothing added to)
+    // backward (x, gate and out as above)
+    RowsRef grad_out, grad_normed, grad_x, grad_residual, grad_gate;  // grad_out.p, grad_residual.p, grad_gate.p may be nullptr
+    float *grad_w_post, *grad_w_pre;
+};
+
+}  // namespace robe
