@@ -61,6 +61,28 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& e) {
     else *(W*)p = u.w;
 }
 
+// Copies to shared memory that go on by themselves (BYTES 4, 8 or 16, both sides aligned to it; 2: a plain load and
+// store); what a thread has copied it may read after copies_wait(n), which leaves its n latest groups in flight.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else if constexpr (BYTES >= 4)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+    else
+        *(unsigned short*)to = __ldcs((const unsigned short*)from);
+}
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait(int left) {
+    switch (left) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    }
+}
+
 // ---- generator: Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2,
 // 3", 2011): a block cipher of the counter under the key, so any element's number is had from its position alone.
 struct DropParams {
