@@ -453,7 +453,7 @@ typedef struct robe_bias_ctx* robe_bias_t; /* opaque; host memory owned by the l
  *     one-sided   bucket(r) = that of max(-r, 0)      (later keys share bucket 0)
  *     two-sided   bucket(r) = that of |r|, + S for r > 0
  *   num_buckets   2 .. 128 one-sided; even, 4 .. 256, two-sided.
- *   max_distance  > E, < 2^31.
+ *   max_distance  > E, < 2^30.
  * The handle is constant after creation: calls on one handle may overlap.
  */
 int robe_bias_create(robe_bias_t* out, uint32_t num_buckets, uint32_t max_distance, int two_sided);

@@ -13,69 +13,114 @@ constexpr int kDropThreads = 256;
 struct DropArgs {
     const void* in;
     void* out;
-    int64_t in_ld, out_ld, cols;
-    uint64_t items;   // rows * groups
-    uint64_t groups;  // groups of 8 columns in a row
+    int64_t in_ld, out_ld;
+    uint32_t in_step, out_step;  // bytes between rows, where a call's rows are taken by pieces
+    uint32_t row0;    // number of the first row
+    uint32_t items;   // rows * groups, below 2^31
+    uint32_t groups;  // groups of 8 columns in a row
+    uint32_t tail;    // columns of the last group
     uint64_t magic;   // floor((2^64 - 1) / groups) + 1
     DropParams drop;
 };
 
-// One thread per group of eight columns: one evaluation of the generator decides all of them.
-template <class T, bool ALIGNED>
-__global__ void __launch_bounds__(kDropThreads) dropout_kernel(DropArgs a) {
+// Eight elements by the words of their group.  Products are taken in fp32 and the decision made on them, so that what is
+// dropped is +0 whatever it was.
+__device__ __forceinline__ void drop_eight(uint4 (&e)[1], const uint4& w, const DropParams& d) {  // bf16
+    uint32_t* v = (uint32_t*)e;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float low = widen_low(v[k]) * d.scale, high = widen_high(v[k]) * d.scale;
+        v[k] = narrow2(drop_keeps(w, 2 * k, d) ? low : 0.0f, drop_keeps(w, 2 * k + 1, d) ? high : 0.0f);
+    }
+}
+__device__ __forceinline__ void drop_eight(uint4 (&e)[2], const uint4& w, const DropParams& d) {  // fp32
+    float* v = (float*)e;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = drop_keeps(w, k, d) ? v[k] * d.scale : 0.0f;
+}
+
+// A thread takes groups of eight columns, each decided by one evaluation of the generator: ITEMS of them a CTA's width
+// apart, all loaded before the first is worked on.
+// PIECES: rows are 16-byte aligned and hold whole groups.
+template <class T, bool PIECES, int ITEMS>
+__global__ void __launch_bounds__(kDropThreads, 6) dropout_kernel(DropArgs a) {
+    constexpr int kWords = 8 * sizeof(T) / 16;
     follow();
     const uint64_t offset = drop_offset(a.drop);
-    const uint64_t t = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x;
-    if (t >= a.items) return;
-    const uint64_t r = a.groups == 1 ? t : (t >> 32) == 0 ? __umul64hi(a.magic, t) : t / a.groups;
-    const uint64_t g = t - r * a.groups;
-    const T* in = (const T*)a.in + r * a.in_ld + g * 8;
-    T* out = (T*)a.out + r * a.out_ld + g * 8;
-    const int64_t left = a.cols - (int64_t)g * 8;
-    const uint4 w = drop_words((uint32_t)r, (uint32_t)g, offset, a.drop.seed);
-    if (ALIGNED && left >= 8) {
-        constexpr int V = kPiece<T>;
+    const uint32_t t0 = blockIdx.x * (kDropThreads * ITEMS) + threadIdx.x;
+    uint4 e[ITEMS][kWords];
+    uint32_t row[ITEMS], group[ITEMS];
 #pragma unroll
-        for (int q = 0; q < 8 / V; ++q) {
-            Pack<T, V> e = load_pack<true, T, V>(in + q * V);
+    for (int i = 0; i < ITEMS; ++i) {
+        const uint32_t t = t0 + i * kDropThreads;
+        // t / groups: the upper half of a product (t < 2^32)
+        row[i] = a.groups == 1 ? t : (uint32_t)(((a.magic >> 32) * t + (((a.magic & 0xFFFFFFFFu) * t) >> 32)) >> 32);
+        group[i] = t - row[i] * a.groups;
+        if (PIECES && t < a.items) {
+            const uint4* in = (const uint4*)((const char*)a.in + (uint64_t)row[i] * a.in_step) + group[i] * kWords;
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                e.v[k] = drop_keeps(w, q * V + k, a.drop.threshold) ? narrow<T>(widen(e.v[k]) * a.drop.scale) : narrow<T>(0.0f);
-            store_pack<true, T, V>(out + q * V, e);
+            for (int q = 0; q < kWords; ++q) e[i][q] = __ldcs(in + q);
         }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < left)
-                out[k] = drop_keeps(w, k, a.drop.threshold) ? narrow<T>(widen(in[k]) * a.drop.scale) : narrow<T>(0.0f);
     }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        if (t0 + i * kDropThreads >= a.items) return;
+        const uint4 w = drop_words(a.row0 + row[i], group[i], offset, a.drop);
+        if (PIECES) {
+            drop_eight(e[i], w, a.drop);
+#pragma unroll
+            for (int q = 0; q < kWords; ++q)
+                __stcs((uint4*)((char*)a.out + (uint64_t)row[i] * a.out_step) + group[i] * kWords + q, e[i][q]);
+        } else {
+            const T* in = (const T*)a.in + row[i] * a.in_ld + group[i] * 8ll;
+            T* out = (T*)a.out + row[i] * a.out_ld + group[i] * 8ll;
+            const int left = group[i] + 1 < a.groups ? 8 : (int)a.tail;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) out[k] = narrow<T>(a.drop.none || drop_keeps(w, k, a.drop) ? widen(in[k]) * a.drop.scale : 0.0f);
+        }
+    }
+}
+
+template <class T, bool PIECES>
+void launch(const DropArgs& a, cudaStream_t st) {
+    constexpr int kItems = PIECES ? (sizeof(T) == 2 ? 4 : 2) : 1;
+    // few groups: one a thread, spread over more SMs
+    const bool few = a.items < 148u * 4 * kDropThreads * kItems;
+    const uint32_t per = kDropThreads * (few ? 1 : kItems);
+    launch_next(few ? dropout_kernel<T, PIECES, 1> : dropout_kernel<T, PIECES, kItems>, (a.items + per - 1) / per, kDropThreads, 0,
+                st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_dropout(const void* in, int64_t in_ld, void* out, int64_t out_ld, int64_t rows, int64_t cols, int dtype,
                            const DropParams& drop, cudaStream_t st) {
+    const int64_t size = dtype == 0 ? 4 : 2;
     DropArgs a;
-    a.in = in;
-    a.out = out;
     a.in_ld = in_ld;
     a.out_ld = out_ld;
-    a.cols = cols;
-    a.groups = ((uint64_t)cols + 7) / 8;
-    a.items = (uint64_t)rows * a.groups;
+    a.in_step = (uint32_t)(in_ld * size);
+    a.out_step = (uint32_t)(out_ld * size);
+    a.groups = (uint32_t)((cols + 7) / 8);
+    a.tail = (uint32_t)(cols - (a.groups - 1) * 8ll);
     a.magic = ~0ull / a.groups + 1;
     a.drop = drop;
-    const int64_t size = dtype == 0 ? 4 : 2;
-    const bool aligned = (((uintptr_t)in | (uintptr_t)out) & 15u) == 0 &&
-                         (rows == 1 || (in_ld * size % 16 == 0 && out_ld * size % 16 == 0));
-    const uint64_t grid = (a.items + kDropThreads - 1) / kDropThreads;
-    if (grid >= (1ull << 31)) return cudaErrorInvalidValue;
-    if (dtype == 0)
-        launch_next(aligned ? dropout_kernel<float, true> : dropout_kernel<float, false>, (unsigned)grid, kDropThreads, 0, st, a);
-    else
-        launch_next(aligned ? dropout_kernel<__nv_bfloat16, true> : dropout_kernel<__nv_bfloat16, false>, (unsigned)grid,
-                    kDropThreads, 0, st, a);
-    return cudaGetLastError();
+    const bool pieces = !drop.none && cols % 8 == 0 && (((uintptr_t)in | (uintptr_t)out) & 15u) == 0 &&
+                        (rows == 1 || (in_ld * size % 16 == 0 && out_ld * size % 16 == 0 && in_ld < (1ll << 30) && out_ld < (1ll << 30)));
+    // items are numbered in 32 bits: as many rows a launch as that allows
+    const int64_t most = ((1ll << 31) - 1) / a.groups;
+    for (int64_t r = 0; r < rows; r += most) {
+        a.row0 = (uint32_t)r;
+        a.items = (uint32_t)((rows - r < most ? rows - r : most) * a.groups);
+        a.in = (const char*)in + r * in_ld * size;
+        a.out = (char*)out + r * out_ld * size;
+        if (dtype == 0) pieces ? launch<float, true>(a, st) : launch<float, false>(a, st);
+        else pieces ? launch<__nv_bfloat16, true>(a, st) : launch<__nv_bfloat16, false>(a, st);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace robe

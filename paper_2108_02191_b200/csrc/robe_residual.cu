@@ -48,9 +48,9 @@ __device__ __forceinline__ void row_stats(F&& value, int64_t d, int layer, float
 }
 
 __device__ __forceinline__ float drop_factor(const DropParams& drop, uint64_t offset, int64_t r, int64_t c) {
-    if (drop.threshold == 0) return 1.0f;
-    const uint4 w = drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, drop.seed);
-    return drop_keeps(w, (int)(c & 7), drop.threshold) ? drop.scale : 0.0f;
+    if (drop.none) return 1.0f;
+    const uint4 w = drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, drop);
+    return drop_keeps(w, (int)(c & 7), drop) ? drop.scale : 0.0f;
 }
 __device__ __forceinline__ float dropped(float v, float factor) { return factor == 0.0f ? 0.0f : v * factor; }
 
@@ -146,10 +146,10 @@ struct Ring {
 // What dropout multiplies the elements of a piece by.
 template <int V>
 __device__ __forceinline__ void drop_factors(float (&f)[V], const DropParams& drop, uint64_t offset, int64_t r, int64_t c) {
-    const uint4 w = drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, drop.seed);
+    const uint4 w = drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, drop);
     const int first = (int)(c & 7);
 #pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = drop_keeps(w, first + e, drop.threshold) ? drop.scale : 0.0f;
+    for (int e = 0; e < V; ++e) f[e] = drop_keeps(w, first + e, drop) ? drop.scale : 0.0f;
 }
 // fp32 weights of a piece (16-byte aligned from V = 4 on: the weights are, and columns are multiples of V)
 template <int V>
@@ -246,7 +246,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
 #pragma unroll
                 for (int c = 0; c < V; ++c) v[k][c] = (v[k][c] - mean) * rstd * w[c];
             }
-            if (a.drop.threshold != 0) {
+            if (!a.drop.none) {
                 float f[V];
                 drop_factors<V>(f, a.drop, offset, r, col);
 #pragma unroll
@@ -542,7 +542,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
 #pragma unroll
             for (int c = 0; c < V; ++c) w[c] = f[c] = 1.0f;
             if (post) weights_of<V>(w, a.w_post + col);
-            if (a.drop.threshold != 0) drop_factors<V>(f, a.drop, offset, r, col);
+            if (!a.drop.none) drop_factors<V>(f, a.drop, offset, r, col);
             if (a.gate_kind == 2) {
                 const Pack<T, V> g = ring.read(stage, gate_at, k);
                 Pack<T, V> e;

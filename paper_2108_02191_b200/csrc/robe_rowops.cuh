@@ -21,6 +21,15 @@ __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// two bf16 in a word, low one first
+__device__ __forceinline__ uint32_t narrow2(float low, float high) {
+    uint32_t w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(high), "f"(low));
+    return w;
+}
+__device__ __forceinline__ float widen_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float widen_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
 // V consecutive elements as one access of V * sizeof(T) bytes (aligned to that), V a power of two, at most 16 bytes
 template <class T, int V>
 struct alignas(V * sizeof(T)) Pack {
@@ -85,40 +94,42 @@ __device__ __forceinline__ void copies_wait(int left) {
 
 // ---- generator: Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2,
 // 3", 2011): a block cipher of the counter under the key, so any element's number is had from its position alone.
+constexpr int kRounds = 10;
 struct DropParams {
-    uint32_t threshold;     // of 65536: an element is dropped when its 16 bits are below
-    float scale;            // 65536 / (65536 - threshold), what kept elements are multiplied by
-    uint64_t seed, offset;  // key; upper half of the counter
-    const uint64_t* step;   // device, added to offset, or nullptr
+    uint32_t none;              // 1: nothing is dropped (t = 0), the generator is not asked
+    uint32_t limit;             // (t << 16) - 1: an element is kept when its 16 bits, moved up by 16, are above
+    float scale;                // 65536 / (65536 - t), what kept elements are multiplied by
+    uint32_t keys[kRounds][2];  // the key of every round (made by the host: constants to the kernels)
+    uint64_t offset;            // upper half of the counter
+    const uint64_t* step;       // device, added to offset, or nullptr
 };
-
-__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint64_t c23, uint64_t key) {
-    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
-    uint32_t c2 = (uint32_t)c23, c3 = (uint32_t)(c23 >> 32);
-#pragma unroll
-    for (int round = 0; round < 10; ++round) {
-        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
-        c1 = (uint32_t)p1;
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-        c3 = (uint32_t)p0;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+inline void drop_keys(DropParams& d, uint64_t seed) {
+    for (int k = 0; k < kRounds; ++k) {
+        d.keys[k][0] = (uint32_t)seed + (uint32_t)k * 0x9E3779B9u;
+        d.keys[k][1] = (uint32_t)(seed >> 32) + (uint32_t)k * 0xBB67AE85u;
     }
-    return make_uint4(c0, c1, c2, c3);
 }
 
 // The words that columns 8 g .. 8 g + 7 of row r are kept or dropped by: column 8 g + k by half k & 1 (low first) of
 // word k / 2.
-__device__ __forceinline__ uint4 drop_words(uint32_t r, uint32_t g, uint64_t offset, uint64_t seed) {
-    return philox(g, r, offset, seed);
+__device__ __forceinline__ uint4 drop_words(uint32_t r, uint32_t g, uint64_t offset, const DropParams& d) {
+    uint32_t c0 = g, c1 = r, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ d.keys[k][0];
+        c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ d.keys[k][1];
+        c3 = (uint32_t)p0;
+    }
+    return make_uint4(c0, c1, c2, c3);
 }
 __device__ __forceinline__ uint64_t drop_offset(const DropParams& d) {
     return d.offset + (d.step != nullptr ? __ldca((const unsigned long long*)d.step) : 0ull);
 }
-__device__ __forceinline__ bool drop_keeps(const uint4& w, int k, uint32_t threshold) {
+__device__ __forceinline__ bool drop_keeps(const uint4& w, int k, const DropParams& d) {
     const uint32_t word = k < 2 ? w.x : k < 4 ? w.y : k < 6 ? w.z : w.w;
-    return ((k & 1) ? word >> 16 : word & 0xFFFFu) >= threshold;
+    return ((k & 1) ? word : word << 16) > d.limit;
 }
 
 // ---- the residual join: what one call is given
@@ -132,7 +143,7 @@ struct ResidualProblem {
     float eps, scale;
     int gate_kind;    // 0 none, 1 a number per row, 2 a vector of d per gate_rows rows
     int64_t gate_rows;
-    DropParams drop;  // threshold 0: no dropout
+    DropParams drop;  // none: no dropout
     const float *w_post, *w_pre;  // or nullptr: no norm there
     RowsRef x, residual, gate, out, normed;  // forward; residual.p may be nullptr (nothing added to)
     // backward (x, gate and out as above)

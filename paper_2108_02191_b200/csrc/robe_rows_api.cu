@@ -53,7 +53,7 @@ uint32_t bucket_edge(uint32_t E, uint32_t L, uint32_t far, uint32_t k) {
         p.times_power(n, L);
         return p.at_least(reach);
     };
-    // (the powers' exponents are small and far < 2^31: the root is right to about 1e-14 of itself)
+    // (the powers' exponents are small and far < 2^30: the root is right to about 1e-14 of itself)
     uint32_t n = (uint32_t)(E * std::pow((double)far / E, (double)k / L));
     if (n < 1) n = 1;
     while (n > 1 && reached(n - 1)) --n;
@@ -116,9 +116,11 @@ bool type_ok(int dtype) { return dtype == ROBE_F32 || dtype == ROBE_BF16; }
 
 bool drop_params(float p, uint64_t seed, uint64_t offset, const uint64_t* step, DropParams& d) {
     if (!(p >= 0.0f && p <= 1.0f) || (uintptr_t)step % 8 != 0) return false;
-    d.threshold = (uint32_t)std::floor((double)p * 65536.0 + 0.5);
-    d.scale = d.threshold < 65536 ? (float)(65536.0 / (double)(65536 - d.threshold)) : 0.0f;
-    d.seed = seed;
+    const uint64_t t = (uint64_t)std::floor((double)p * 65536.0 + 0.5);
+    d.none = t == 0;
+    d.limit = (uint32_t)((t << 16) - 1);
+    d.scale = t < 65536 ? (float)(65536.0 / (double)(65536 - t)) : 0.0f;
+    drop_keys(d, seed);
     d.offset = offset;
     d.step = step;
     return true;
@@ -217,7 +219,7 @@ int robe_bias_create(robe_bias_t* out, uint32_t num_buckets, uint32_t max_distan
     const uint32_t side = two_sided ? num_buckets / 2 : num_buckets;
     if (side < 2 || side > kBiasMaxSide) return ROBE_ERR_INVALID_ARG;
     const uint32_t E = side / 2, L = side - E;
-    if (max_distance <= E || max_distance >= (1u << 31)) return ROBE_ERR_INVALID_ARG;
+    if (max_distance <= E || max_distance >= (1u << 30)) return ROBE_ERR_INVALID_ARG;
     robe_bias_ctx* b = new (std::nothrow) robe_bias_ctx();
     if (b == nullptr) return ROBE_ERR_INVALID_ARG;
     b->tag = kBiasTag;

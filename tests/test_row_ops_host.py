@@ -40,7 +40,7 @@ def test_dropout_keeps_the_share_it_says():
 
 
 @pytest.mark.parametrize("two_sided", [False, True])
-@pytest.mark.parametrize("buckets,far", [(2, 2), (4, 3), (32, 128), (32, 129), (6, 1000), (128, 65), (128, 2**31 - 1), (10, 12),
+@pytest.mark.parametrize("buckets,far", [(2, 2), (4, 3), (32, 128), (32, 129), (6, 1000), (128, 65), (128, 2**30 - 1), (10, 12),
                                          (64, 100_000), (30, 128)])
 def test_bucket_edges_are_exact(buckets, far, two_sided):
     if two_sided:
@@ -108,7 +108,7 @@ def test_join_gradients_are_those_of_differences(layer, gate_rows):
 
 
 @pytest.mark.parametrize("args", [(1, 100, 0), (130, 1000, 0), (33, 100, 1), (2, 100, 1), (258, 1000, 1), (32, 16, 0), (32, 8, 1),
-                                  (32, 2**31, 0), (32, 128, 2)])
+                                  (32, 2**30, 0), (32, 128, 2)])
 def test_bias_create_refuses(args):
     b = robe.binding._BiasHandle()
     assert lib().robe_bias_create(C.byref(b), *args) == BAD and not b
