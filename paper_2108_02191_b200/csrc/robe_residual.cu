@@ -89,15 +89,20 @@ __global__ void __launch_bounds__(kJoinThreads) residual_any_kernel(ResidualProb
 
 // ---- rows kept close: `lanes` threads share a row, E elements each, which they copy to shared memory rows ahead and read
 // from there; a thread reads what it copied itself, so nothing but the sums over a row is waited for together.  Up to 512
-// elements (256 backward) a row is a part of a warp's, longer ones a CTA's, up to kMaxLanes E; beyond that the kernels for any length.
+// elements (256 backward) a row is a part of a warp's, longer ones a CTA's, up to kMaxLanes E; beyond that the kernels for any
+// length.
 
 constexpr int kMaxLanes = 512;
 constexpr int kWarpRowThreads = 256;
 
-// Sums of N values over the threads of a row, in each of them.  CTA: by turns in two halves of `scratch`, so that one
-// barrier a sum is enough.
+// Sums of N values over the threads of a row, in each of them.  CTA: by turns in two halves of `scratch` (zero where there
+// is no warp), so that one barrier a sum is enough.
+constexpr int kSums = 3;
+struct Scratch {
+    float4 part[2][kSums][kMaxLanes / 128];
+};
 template <bool CTA, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], int lanes, float (*scratch)[N][kMaxLanes / 32], int& turn) {
+__device__ __forceinline__ void row_sums(float (&v)[kSums], int lanes, Scratch& scratch, int& turn) {
     if (CTA) {
 #pragma unroll
         for (int s = 16; s > 0; s >>= 1)
@@ -106,14 +111,21 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int lanes, float (*scrat
         if (blockDim.x == 32) return;
         if ((threadIdx.x & 31) == 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) scratch[turn][k][threadIdx.x >> 5] = v[k];
+            for (int k = 0; k < N; ++k) ((float*)scratch.part[turn][k])[threadIdx.x >> 5] = v[k];
         __syncthreads();
-        const int warps = blockDim.x >> 5;
+        const int fours = (blockDim.x + 127) >> 7;
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = 0.0f;
-        for (int w = 0; w < warps; ++w)
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[k] += scratch[turn][k][w];
+        for (int k = 0; k < N; ++k) {
+            float4 p = scratch.part[turn][k][0];
+            for (int w = 1; w < fours; ++w) {
+                const float4 q = scratch.part[turn][k][w];
+                p.x += q.x;
+                p.y += q.y;
+                p.z += q.z;
+                p.w += q.w;
+            }
+            v[k] = (p.x + p.y) + (p.z + p.w);
+        }
         turn ^= 1;
     } else {
         for (int s = lanes >> 1; s > 0; s >>= 1)
@@ -121,166 +133,290 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int lanes, float (*scrat
             for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], s);
     }
 }
+template <bool CTA>
+__device__ __forceinline__ void row_sums(float (&v)[kSums], int n, int lanes, Scratch& scratch, int& turn) {
+    if (n == 1) row_sums<CTA, 1>(v, lanes, scratch, turn);
+    else if (n == 2) row_sums<CTA, 2>(v, lanes, scratch, turn);
+    else row_sums<CTA, 3>(v, lanes, scratch, turn);
+}
 
-// The rows' shared memory: [stage][tensor][piece][thread], V elements each.
-template <class T, int V, int NP>
+// A thread's elements of a row: E of them as E / 2 pairs.  They are taken in units of pairs: a piece of V elements, or, where
+// V is 1, two pieces.  Element c of unit u stands in column(u, c).
+template <class T, int V, int E>
 struct Ring {
-    T* base;
-    int tensors, lanes, lane;
-    int64_t d;
+    static constexpr int P = V > 1 ? V / 2 : 1;  // pairs of a unit
+    static constexpr int U = E / (2 * P);        // units
+    static constexpr int NP = E / V;             // pieces
+    T* base;  // [stage][tensor][piece][thread], V elements each
+    int tensors, lanes, lane, d;
+
     __device__ __forceinline__ T* at(int stage, int tensor, int k) const {
-        return base + ((((size_t)stage * tensors + tensor) * NP + k) * blockDim.x + threadIdx.x) * V;
+        return base + (size_t)((((stage * tensors + tensor) * NP + k) * blockDim.x + threadIdx.x) * V);
     }
-    __device__ __forceinline__ int64_t col(int k) const { return (int64_t)(k * lanes + lane) * V; }
+    __device__ __forceinline__ int col(int k) const { return (k * lanes + lane) * V; }
     __device__ __forceinline__ bool has(int k) const { return col(k) < d; }
-    __device__ __forceinline__ void fetch(int stage, int tensor, const T* row) const {
+    // beyond a row's end there are zeros, once and for all
+    __device__ __forceinline__ void clear(int stages) const {
+        for (int s = 0; s < stages * tensors; ++s)
+#pragma unroll
+            for (int k = 0; k < NP; ++k)
+                if (!has(k))
+#pragma unroll
+                    for (int c = 0; c < V; ++c) at(0, s, k)[c] = narrow<T>(0.0f);
+    }
+    __device__ __forceinline__ void fetch(int stage, int tensor, const char* row) const {
 #pragma unroll
         for (int k = 0; k < NP; ++k)
-            if (has(k)) copy_async<V * sizeof(T)>(at(stage, tensor, k), row + col(k));
+            if (has(k)) copy_async<V * sizeof(T)>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
     }
-    __device__ __forceinline__ Pack<T, V> read(int stage, int tensor, int k) const {
-        return *(const Pack<T, V>*)at(stage, tensor, k);
+    __device__ __forceinline__ void zero(int stage, int tensor) const {
+#pragma unroll
+        for (int k = 0; k < NP; ++k)
+#pragma unroll
+            for (int c = 0; c < V; ++c) at(stage, tensor, k)[c] = narrow<T>(0.0f);
+    }
+    __device__ __forceinline__ void read(float2 (&v)[P], int stage, int tensor, int u) const {
+        if constexpr (V == 1) {
+            v[0] = make_float2(widen(*at(stage, tensor, 2 * u)), widen(*at(stage, tensor, 2 * u + 1)));
+        } else {
+            using W = typename Word<V * sizeof(T)>::type;
+            union {
+                W w;
+                uint32_t bits[V * sizeof(T) / 4];
+            } p;
+            p.w = *(const W*)at(stage, tensor, u);
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                if constexpr (sizeof(T) == 2) v[q] = make_float2(widen_low(p.bits[q]), widen_high(p.bits[q]));
+                else v[q] = make_float2(__uint_as_float(p.bits[2 * q]), __uint_as_float(p.bits[2 * q + 1]));
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char* row, const float2 (&v)[P], int u) const {
+        if constexpr (V == 1) {
+            if (has(2 * u)) ((T*)row)[col(2 * u)] = narrow<T>(v[0].x);
+            if (has(2 * u + 1)) ((T*)row)[col(2 * u + 1)] = narrow<T>(v[0].y);
+        } else if (has(u)) {
+            using W = typename Word<V * sizeof(T)>::type;
+            union {
+                W w;
+                uint32_t bits[V * sizeof(T) / 4];
+            } p;
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                if constexpr (sizeof(T) == 2) {
+                    p.bits[q] = narrow2(v[q].x, v[q].y);
+                } else {
+                    p.bits[2 * q] = __float_as_uint(v[q].x);
+                    p.bits[2 * q + 1] = __float_as_uint(v[q].y);
+                }
+            }
+            __stcs((W*)(row + (uint32_t)col(u) * (uint32_t)sizeof(T)), p.w);
+        }
+    }
+    // fp32 weights (16-byte aligned from V = 4 on: the weights are, and columns are multiples of V), 0 beyond the row's end
+    __device__ __forceinline__ void weights(float2 (&w)[P], const float* p, int u) const {
+        if constexpr (V == 1) {
+            w[0].x = has(2 * u) ? __ldca(p + col(2 * u)) : 0.0f;
+            w[0].y = has(2 * u + 1) ? __ldca(p + col(2 * u + 1)) : 0.0f;
+        } else {
+#pragma unroll
+            for (int q = 0; q < P; ++q) w[q] = both(0.0f);
+            if (!has(u)) return;
+            if constexpr (V >= 4) {
+#pragma unroll
+                for (int q = 0; q < P; q += 2) {
+                    const float4 x = __ldca((const float4*)(p + col(u) + 2 * q));
+                    w[q] = make_float2(x.x, x.y);
+                    w[q + 1] = make_float2(x.z, x.w);
+                }
+            } else {
+                w[0] = make_float2(__ldca(p + col(u)), __ldca(p + col(u) + 1));
+            }
+        }
+    }
+    // what an element is kept by when it is above the limit
+    __device__ __forceinline__ void draws(uint32_t (&h)[2 * P], const DropParams& drop, uint64_t offset, uint32_t r, int u) const {
+        if constexpr (V == 1) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int at = col(2 * u + c);
+                const uint4 w = drop_words(r, (uint32_t)at >> 3, offset, drop);
+                const uint32_t word = (at & 4) ? ((at & 2) ? w.w : w.z) : ((at & 2) ? w.y : w.x);
+                h[c] = (at & 1) ? word : word << 16;
+            }
+        } else {
+            const int at = col(u);
+            const uint4 w = drop_words(r, (uint32_t)at >> 3, offset, drop);
+            uint32_t word[4] = {w.x, w.y, w.z, w.w};
+            if constexpr (V <= 4) {
+                word[0] = (at & 4) ? word[2] : word[0];
+                word[1] = (at & 4) ? word[3] : word[1];
+            }
+            if constexpr (V == 2) word[0] = (at & 2) ? word[1] : word[0];
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                h[2 * q] = word[q] << 16;
+                h[2 * q + 1] = word[q];
+            }
+        }
+    }
+};
+__device__ __forceinline__ float2 kept_of(float2 v, const uint32_t* h, uint32_t limit) {
+    return make_float2(h[0] > limit ? v.x : 0.0f, h[1] > limit ? v.y : 0.0f);
+}
+
+// Rows of a tensor by bytes (a row is less than 2^32 bytes from the next where these kernels are used).
+__device__ __forceinline__ char* row_of(const RowsRef& t, uint32_t r, uint32_t size) {
+    return (char*)t.p + (uint64_t)r * ((uint32_t)t.ld * size);
+}
+// A row number that goes up by equal steps, with its gate vector's.
+struct GateRow {
+    uint32_t gate, step_gate;
+    uint64_t in_gate, step_in, gate_rows;
+    __device__ __forceinline__ GateRow(uint32_t r, uint32_t step, uint32_t rows_) : gate_rows(rows_) {
+        gate = r / rows_;
+        in_gate = r - (uint64_t)gate * rows_;
+        step_gate = step / rows_;
+        step_in = step - (uint64_t)step_gate * rows_;
+    }
+    __device__ __forceinline__ void next() {
+        gate += step_gate;
+        in_gate += step_in;
+        if (in_gate >= gate_rows) {
+            in_gate -= gate_rows;
+            ++gate;
+        }
     }
 };
 
-// What dropout multiplies the elements of a piece by.
-template <int V>
-__device__ __forceinline__ void drop_factors(float (&f)[V], const DropParams& drop, uint64_t offset, int64_t r, int64_t c) {
-    const uint4 w = drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, drop);
-    const int first = (int)(c & 7);
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = drop_keeps(w, first + e, drop) ? drop.scale : 0.0f;
-}
-// fp32 weights of a piece (16-byte aligned from V = 4 on: the weights are, and columns are multiples of V)
-template <int V>
-__device__ __forceinline__ void weights_of(float (&w)[V], const float* p) {
-    if constexpr (V >= 4) {
-#pragma unroll
-        for (int q = 0; q < V; q += 4) {
-            const float4 x = __ldca((const float4*)(p + q));
-            w[q] = x.x;
-            w[q + 1] = x.y;
-            w[q + 2] = x.z;
-            w[q + 3] = x.w;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) w[e] = __ldca(p + e);
-    }
-}
-
-template <class T, int V, int NP, bool CTA>
+template <class T, int V, int E, bool CTA>
 __global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
 residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
+    using R = Ring<T, V, E>;
+    constexpr int P = R::P, U = R::U;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
-    __shared__ float scratch[2][1][kMaxLanes / 32];
+    __shared__ Scratch scratch;
     follow();
     const uint64_t offset = drop_offset(a.drop);
     const bool post = a.w_post != nullptr, pre = a.w_pre != nullptr, added = a.residual.p != nullptr;
     const int gate_at = added ? 2 : 1, tensors = gate_at + (a.gate_kind == 2);
-    const Ring<T, V, NP> ring{(T*)ring_bytes, tensors, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), a.d};
-    const int groups = CTA ? 1 : kWarpRowThreads / lanes;
-    const int64_t step = (int64_t)gridDim.x * groups;
-    const int64_t first = (int64_t)blockIdx.x * groups + (CTA ? 0 : threadIdx.x / lanes);
+    const R ring{(T*)ring_bytes, tensors, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), (int)a.d};
+    const uint32_t groups = CTA ? 1 : kWarpRowThreads / lanes, group = CTA ? 0 : threadIdx.x / lanes;
+    const uint32_t step = gridDim.x * groups, rows = (uint32_t)a.rows;
     const float over_d = 1.0f / (float)a.d;
     int turn = 0;
-    auto fetch = [&](int64_t r, int stage) {
-        if (r < a.rows) {
-            ring.fetch(stage, 0, (const T*)a.x.p + r * a.x.ld);
-            if (added) ring.fetch(stage, 1, (const T*)a.residual.p + r * a.residual.ld);
-            if (a.gate_kind == 2) ring.fetch(stage, gate_at, (const T*)a.gate.p + r / a.gate_rows * a.gate.ld);
+    ring.clear(stages);
+    if (CTA) {
+        for (unsigned k = threadIdx.x; k < sizeof(Scratch) / 4; k += blockDim.x) ((float*)&scratch)[k] = 0.0f;
+        __syncthreads();
+    }
+    // (a warp's groups go through as many rows as its first one: sums over lanes need them all)
+    uint64_t leader = (uint64_t)blockIdx.x * groups + (CTA ? 0 : (threadIdx.x & ~31u) / lanes);
+    const uint32_t ahead = CTA ? 0 : group - (threadIdx.x & ~31u) / lanes;
+    uint64_t next = leader + ahead;
+    GateRow gate(next < rows ? (uint32_t)next : 0, step, a.gate_kind == 2 ? (uint32_t)a.gate_rows : 1);
+    auto fetch = [&](int stage) {
+        if (next < rows) {
+            const uint32_t r = (uint32_t)next;
+            ring.fetch(stage, 0, row_of(a.x, r, sizeof(T)));
+            if (added) ring.fetch(stage, 1, row_of(a.residual, r, sizeof(T)));
+            if (a.gate_kind == 2) {
+                ring.fetch(stage, gate_at, row_of(a.gate, gate.gate, sizeof(T)));
+                gate.next();
+            }
         }
+        next += step;
         copies_close();
     };
-    for (int s = 0; s + 1 < stages; ++s) fetch(first + s * step, s);
+    for (int s = 0; s + 1 < stages; ++s) fetch(s);
     int stage = 0;
-    // (a warp's groups go through as many rows as its first one: sums over lanes need them all)
-    const int64_t leader = CTA ? first : (int64_t)blockIdx.x * groups + (threadIdx.x & ~31) / lanes;
-    for (int64_t r0 = leader; r0 < a.rows; r0 += step) {
-        const int64_t r = r0 + (first - leader);
-        const bool here = r < a.rows;
-        fetch(r + (int64_t)(stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+    for (; leader < rows; leader += step) {
+        const bool here = leader + ahead < rows;
+        const uint32_t r = (uint32_t)leader + ahead;
+        fetch(stage == 0 ? stages - 1 : stage - 1);
         copies_wait(stages - 1);
-        float v[NP][V];
+        float2 v[U][P];
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            const Pack<T, V> e = ring.read(stage, 0, k);
-#pragma unroll
-            for (int c = 0; c < V; ++c) v[k][c] = here && ring.has(k) ? widen(e.v[c]) : 0.0f;
-        }
+        for (int u = 0; u < U; ++u) ring.read(v[u], stage, 0, u);
         // norm of the row that v holds (0 beyond d): mean and factor
         auto stats = [&](float& mean, float& rstd) {
-            float s[1];
+            float s[kSums];
             mean = 0.0f;
             if (a.layer) {
-                s[0] = 0.0f;
+                float2 t = both(0.0f);
 #pragma unroll
-                for (int k = 0; k < NP; ++k)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int c = 0; c < V; ++c) s[0] += v[k][c];
+                    for (int q = 0; q < P; ++q) t = add2(t, v[u][q]);
+                s[0] = t.x + t.y;
                 row_sums<CTA, 1>(s, lanes, scratch, turn);
                 mean = s[0] * over_d;
             }
-            s[0] = 0.0f;
+            float2 t = both(0.0f);
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    const float x = v[k][c] - mean;
-                    s[0] += ring.has(k) ? x * x : 0.0f;
+                for (int q = 0; q < P; ++q) {
+                    float2 c = v[u][q];
+                    if (a.layer) {
+                        c = add2(c, both(-mean));
+                        if (!ring.has(V > 1 ? u : 2 * u)) c.x = 0.0f;
+                        if (!ring.has(V > 1 ? u : 2 * u + 1)) c.y = 0.0f;
+                    }
+                    t = fma2(c, c, t);
                 }
+            s[0] = t.x + t.y;
             row_sums<CTA, 1>(s, lanes, scratch, turn);
             rstd = 1.0f / sqrtf(s[0] * over_d + a.eps);
         };
         float mean = 0.0f, rstd = 1.0f;
         if (post) stats(mean, rstd);
         float row_gate = a.scale;
-        if (a.gate_kind == 1 && here) row_gate *= widen(((const T*)a.gate.p)[r * a.gate.ld]);
+        if (a.gate_kind == 1 && here) row_gate *= widen(*(const T*)row_of(a.gate, r, sizeof(T)));
+        if (!a.drop.none) row_gate *= a.drop.scale;
+        char* out = row_of(a.out, r, sizeof(T));
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            if (!ring.has(k) || !here) continue;
-            const int64_t col = ring.col(k);
+        for (int u = 0; u < U; ++u) {
             if (post) {
-                float w[V];
-                weights_of<V>(w, a.w_post + col);
+                float2 w[P];
+                ring.weights(w, a.w_post, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) v[k][c] = (v[k][c] - mean) * rstd * w[c];
+                for (int q = 0; q < P; ++q) v[u][q] = mul2(mul2(add2(v[u][q], both(-mean)), both(rstd)), w[q]);
             }
             if (!a.drop.none) {
-                float f[V];
-                drop_factors<V>(f, a.drop, offset, r, col);
+                uint32_t draws[2 * P];
+                ring.draws(draws, a.drop, offset, r, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) v[k][c] = dropped(v[k][c], f[c]);
+                for (int q = 0; q < P; ++q) v[u][q] = kept_of(v[u][q], draws + 2 * q, a.drop.limit);
             }
-#pragma unroll
-            for (int c = 0; c < V; ++c) v[k][c] *= row_gate;
             if (a.gate_kind == 2) {
-                const Pack<T, V> g = ring.read(stage, gate_at, k);
+                float2 g[P];
+                ring.read(g, stage, gate_at, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) v[k][c] *= widen(g.v[c]);
+                for (int q = 0; q < P; ++q) v[u][q] = mul2(v[u][q], g[q]);
             }
             if (added) {
-                const Pack<T, V> e = ring.read(stage, 1, k);
+                float2 e[P];
+                ring.read(e, stage, 1, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) v[k][c] += widen(e.v[c]);
+                for (int q = 0; q < P; ++q) v[u][q] = fma2(v[u][q], both(row_gate), e[q]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < P; ++q) v[u][q] = mul2(v[u][q], both(row_gate));
             }
-            Pack<T, V> e;
-#pragma unroll
-            for (int c = 0; c < V; ++c) e.v[c] = narrow<T>(v[k][c]);
-            store_pack<true, T, V>((T*)a.out.p + r * a.out.ld + col, e);
+            if (here) ring.store(out, v[u], u);
         }
         if (pre) {
             stats(mean, rstd);
+            char* normed = row_of(a.normed, r, sizeof(T));
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                if (!ring.has(k) || !here) continue;
-                const int64_t col = ring.col(k);
-                float w[V];
-                weights_of<V>(w, a.w_pre + col);
-                Pack<T, V> e;
+            for (int u = 0; u < U; ++u) {
+                float2 w[P];
+                ring.weights(w, a.w_pre, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) e.v[c] = narrow<T>((v[k][c] - mean) * rstd * w[c]);
-                store_pack<true, T, V>((T*)a.normed.p + r * a.normed.ld + col, e);
+                for (int q = 0; q < P; ++q) w[q] = mul2(mul2(add2(v[u][q], both(-mean)), both(rstd)), w[q]);
+                if (here) ring.store(normed, w, u);
             }
         }
         stage = stage + 1 == stages ? 0 : stage + 1;
@@ -397,237 +533,264 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
 
 // One CTA per chunk.  The weights' gradients of a thread's columns are summed in registers over its rows, over the groups of
 // a CTA in shared memory, over the chunks by the kernel below; a gate vector's likewise, or stored when its rows are done.
-template <class T, int V, int NP, bool CTA>
+template <class T, int V, int E, bool CTA>
 __global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
 residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
+    using R = Ring<T, V, E>;
+    constexpr int P = R::P, U = R::U;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
-    __shared__ float scratch[2][3][kMaxLanes / 32];
+    __shared__ Scratch scratch;
     follow();
     const ResidualProblem& a = args.p;
     const uint64_t offset = drop_offset(a.drop);
-    const bool post = a.w_post != nullptr, pre = a.w_pre != nullptr, skip = a.grad_out.p != nullptr;
-    const bool gate_sums = a.gate_kind == 2 && a.grad_gate.p != nullptr && args.chunks.gate_rows > 1;
-    const bool whole_gates = args.chunks.per_gate == 0;
+    const bool post = a.w_post != nullptr, pre = a.w_pre != nullptr, skip = a.grad_out.p != nullptr, vector = a.gate_kind == 2;
+    const bool shared_gate = vector && args.chunks.gate_rows > 1;  // a gate vector of several rows
+    const bool whole_gates = args.chunks.per_gate == 0;            // .. all in this chunk
     const int skip_at = 1, out_at = skip_at + skip, normed_at = out_at + pre, gate_at = normed_at + pre;
-    const int tensors = gate_at + (a.gate_kind == 2);
-    const Ring<T, V, NP> ring{(T*)ring_bytes, tensors, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), a.d};
-    const int groups = CTA ? 1 : kWarpRowThreads / lanes;
-    const int group = CTA ? 0 : threadIdx.x / lanes;
+    const int tensors = gate_at + vector;
+    const R ring{(T*)ring_bytes, tensors, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), (int)a.d};
+    const uint32_t groups = CTA ? 1 : kWarpRowThreads / lanes, group = CTA ? 0 : threadIdx.x / lanes;
     const float over_d = 1.0f / (float)a.d;
-    // the rows of a group: every groups-th of the chunk, or whole gate vectors in turn
-    const int64_t c0 = args.chunks.row0(blockIdx.x), c1 = args.chunks.row1(blockIdx.x);
-    const int64_t block = gate_sums && whole_gates ? args.chunks.gate_rows : 1;
-    auto row_of = [&](int64_t k) {  // k-th row of this group, c1 or more beyond the last
-        return block == 1 ? c0 + k * groups + group : c0 + ((k / block) * groups + group) * block + k % block;
-    };
-    // (as many rounds for all groups: sums over lanes need whole warps)
-    const int64_t rounds = ((c1 - c0 + block - 1) / block + groups - 1) / groups * block;
     int turn = 0;
-    float sum_post[NP][V], sum_pre[NP][V], sum_gate[NP][V];
-#pragma unroll
-    for (int k = 0; k < NP; ++k)
-#pragma unroll
-        for (int c = 0; c < V; ++c) sum_post[k][c] = sum_pre[k][c] = sum_gate[k][c] = 0.0f;
-    auto fetch = [&](int64_t k, int stage) {
-        const int64_t r = row_of(k);
-        if (k < rounds && r < c1) {
-            ring.fetch(stage, 0, (const T*)a.x.p + r * a.x.ld);
-            if (skip) ring.fetch(stage, skip_at, (const T*)a.grad_out.p + r * a.grad_out.ld);
-            if (pre) {
-                ring.fetch(stage, out_at, (const T*)a.out.p + r * a.out.ld);
-                ring.fetch(stage, normed_at, (const T*)a.grad_normed.p + r * a.grad_normed.ld);
-            }
-            if (a.gate_kind == 2) ring.fetch(stage, gate_at, (const T*)a.gate.p + r / a.gate_rows * a.gate.ld);
+    ring.clear(stages);
+    if (CTA) {
+        for (unsigned k = threadIdx.x; k < sizeof(Scratch) / 4; k += blockDim.x) ((float*)&scratch)[k] = 0.0f;
+        __syncthreads();
+    }
+    // the rows of a group: every groups-th of the chunk, or whole gate vectors in turn
+    const uint32_t c0 = (uint32_t)args.chunks.row0(blockIdx.x), c1 = (uint32_t)args.chunks.row1(blockIdx.x);
+    const uint32_t block = shared_gate && whole_gates ? (uint32_t)args.chunks.gate_rows : 1;
+    // (as many rounds for all groups: sums over lanes need whole warps)
+    const uint32_t rounds = ((c1 - c0 + block - 1) / block + groups - 1) / groups * block;
+    struct Place {
+        uint64_t r;
+        uint32_t in_block, gate;
+    };
+    auto advance = [&](Place& p) {
+        ++p.in_block;
+        if (p.in_block == block) {
+            p.in_block = 0;
+            p.r += (uint64_t)(groups - 1) * block;
+            if (block > 1) p.gate += groups;
         }
+        ++p.r;
+    };
+    Place now{c0 + (uint64_t)group * block, 0, 0};
+    if (shared_gate) now.gate = c0 / (uint32_t)args.chunks.gate_rows + (whole_gates ? group : 0);
+    Place next = now;
+    float2 sum_post[U][P], sum_pre[U][P], sum_gate[U][P];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < P; ++q) sum_post[u][q] = sum_pre[u][q] = sum_gate[u][q] = both(0.0f);
+    auto fetch = [&](int stage) {
+        if (next.r < c1) {
+            const uint32_t r = (uint32_t)next.r;
+            ring.fetch(stage, 0, row_of(a.x, r, sizeof(T)));
+            if (skip) ring.fetch(stage, skip_at, row_of(a.grad_out, r, sizeof(T)));
+            if (pre) {
+                ring.fetch(stage, out_at, row_of(a.out, r, sizeof(T)));
+                ring.fetch(stage, normed_at, row_of(a.grad_normed, r, sizeof(T)));
+            }
+            if (vector) ring.fetch(stage, gate_at, row_of(a.gate, shared_gate ? next.gate : r, sizeof(T)));
+        } else {  // no such row: zeros add nothing to the sums
+            for (int k = 0; k < tensors; ++k) ring.zero(stage, k);
+        }
+        advance(next);
         copies_close();
     };
-    for (int s = 0; s + 1 < stages; ++s) fetch(s, s);
+    for (int s = 0; s + 1 < stages; ++s) fetch(s);
     int stage = 0;
-    for (int64_t q = 0; q < rounds; ++q) {
-        const int64_t r = row_of(q);
-        const bool here = r < c1;
-        fetch(q + stages - 1, stage == 0 ? stages - 1 : stage - 1);
+    for (uint32_t round = 0; round < rounds; ++round) {
+        const uint32_t r = (uint32_t)now.r;
+        const bool here = now.r < c1;
+        fetch(stage == 0 ? stages - 1 : stage - 1);
         copies_wait(stages - 1);
-        float x[NP][V], t[NP][V];  // x, then its norm; out, its norm, then the gradient of out
+        float2 x[U][P], t[U][P];  // x, then its norm; out, its norm, then the gradient of out
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            const bool in = here && ring.has(k);
-            const Pack<T, V> e = ring.read(stage, 0, k);
+        for (int u = 0; u < U; ++u) {
+            ring.read(x[u], stage, 0, u);
+            if (pre) ring.read(t[u], stage, out_at, u);
+            else
 #pragma unroll
-            for (int c = 0; c < V; ++c) x[k][c] = in ? widen(e.v[c]) : 0.0f;
-            if (pre) {
-                const Pack<T, V> o = ring.read(stage, out_at, k);
-#pragma unroll
-                for (int c = 0; c < V; ++c) t[k][c] = in ? widen(o.v[c]) : 0.0f;
-            } else {
-#pragma unroll
-                for (int c = 0; c < V; ++c) t[k][c] = 0.0f;
-            }
+                for (int q = 0; q < P; ++q) t[u][q] = both(0.0f);
         }
-        float s[3] = {0.0f, 0.0f, 0.0f};
-        float mean1 = 0.0f, mean2 = 0.0f;
+        float s[kSums];
         if (a.layer) {
+            float2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    s[0] += x[k][c];
-                    s[1] += t[k][c];
+                for (int q = 0; q < P; ++q) {
+                    s1 = add2(s1, x[u][q]);
+                    s2 = add2(s2, t[u][q]);
                 }
-            row_sums<CTA, 3>(s, lanes, scratch, turn);
-            if (post) mean1 = s[0] * over_d;
-            mean2 = s[1] * over_d;
+            s[0] = s1.x + s1.y;
+            s[1] = s2.x + s2.y;
+            row_sums<CTA, 2>(s, lanes, scratch, turn);
+            const float mean1 = post ? s[0] * over_d : 0.0f, mean2 = s[1] * over_d;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int q = 0; q < P; ++q) {
+                    x[u][q] = add2(x[u][q], both(-mean1));
+                    t[u][q] = add2(t[u][q], both(-mean2));
+                    if (!ring.has(V > 1 ? u : 2 * u)) x[u][q].x = t[u][q].x = 0.0f;
+                    if (!ring.has(V > 1 ? u : 2 * u + 1)) x[u][q].y = t[u][q].y = 0.0f;
+                }
         }
-        s[0] = s[1] = s[2] = 0.0f;
+        {
+            float2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
-        for (int k = 0; k < NP; ++k)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int c = 0; c < V; ++c) {
-                x[k][c] = ring.has(k) ? x[k][c] - mean1 : 0.0f;
-                t[k][c] = ring.has(k) ? t[k][c] - mean2 : 0.0f;
-                s[0] += x[k][c] * x[k][c];
-                s[1] += t[k][c] * t[k][c];
-            }
-        row_sums<CTA, 3>(s, lanes, scratch, turn);
-        const float rstd1 = post ? 1.0f / sqrtf(s[0] * over_d + a.eps) : 1.0f;
-        const float rstd2 = pre ? 1.0f / sqrtf(s[1] * over_d + a.eps) : 1.0f;
+                for (int q = 0; q < P; ++q) {
+                    s1 = fma2(x[u][q], x[u][q], s1);
+                    s2 = fma2(t[u][q], t[u][q], s2);
+                }
+            s[0] = s1.x + s1.y;
+            s[1] = s2.x + s2.y;
+        }
+        if (post || pre) row_sums<CTA, 2>(s, lanes, scratch, turn);
+        // (0 for no row: with eps = 0 its factor would be infinite)
+        const float rstd1 = !here ? 0.0f : post ? 1.0f / sqrtf(s[0] * over_d + a.eps) : 1.0f;
+        const float rstd2 = !here ? 0.0f : pre ? 1.0f / sqrtf(s[1] * over_d + a.eps) : 1.0f;
         if (pre) {
-            s[0] = s[1] = s[2] = 0.0f;
+            float2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                if (!ring.has(k) || !here) continue;
-                const Pack<T, V> g = ring.read(stage, normed_at, k);
-                float w[V];
-                weights_of<V>(w, a.w_pre + ring.col(k));
+            for (int u = 0; u < U; ++u) {
+                float2 g[P], w[P];
+                ring.read(g, stage, normed_at, u);
+                ring.weights(w, a.w_pre, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    t[k][c] *= rstd2;
-                    const float gn = widen(g.v[c]);
-                    sum_pre[k][c] += gn * t[k][c];
-                    s[0] += gn * w[c] * t[k][c];
-                    s[1] += gn * w[c];
+                for (int q = 0; q < P; ++q) {
+                    t[u][q] = mul2(t[u][q], both(rstd2));
+                    sum_pre[u][q] = fma2(g[q], t[u][q], sum_pre[u][q]);
+                    w[q] = mul2(g[q], w[q]);
+                    s1 = fma2(w[q], t[u][q], s1);
+                    if (a.layer) s2 = add2(s2, w[q]);
                 }
             }
-            row_sums<CTA, 3>(s, lanes, scratch, turn);
-            const float dot = s[0] * over_d, sum = a.layer ? s[1] * over_d : 0.0f;
+            s[0] = s1.x + s1.y;
+            s[1] = s2.x + s2.y;
+            row_sums<CTA>(s, a.layer ? 2 : 1, lanes, scratch, turn);
+            const float2 dot = both(-s[0] * over_d), mean = both(a.layer ? -s[1] * over_d : 0.0f);
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                if (!ring.has(k) || !here) continue;
-                const Pack<T, V> g = ring.read(stage, normed_at, k);
-                float w[V];
-                weights_of<V>(w, a.w_pre + ring.col(k));
+            for (int u = 0; u < U; ++u) {
+                float2 g[P], w[P];
+                ring.read(g, stage, normed_at, u);
+                ring.weights(w, a.w_pre, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) t[k][c] = rstd2 * (widen(g.v[c]) * w[c] - sum - t[k][c] * dot);
+                for (int q = 0; q < P; ++q) t[u][q] = mul2(fma2(t[u][q], dot, fma2(g[q], w[q], mean)), both(rstd2));
             }
         }
         float row_gate = 1.0f;
-        if (a.gate_kind == 1 && here) row_gate = widen(((const T*)a.gate.p)[r * a.gate.ld]);
-        s[0] = s[1] = s[2] = 0.0f;
+        if (a.gate_kind == 1 && here) row_gate = widen(*(const T*)row_of(a.gate, r, sizeof(T)));
+        const float2 scale = both(a.drop.none ? a.scale : a.scale * a.drop.scale);
+        char* grad_residual = row_of(a.grad_residual, r, sizeof(T));
+        float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            if (!ring.has(k) || !here) continue;
-            const int64_t col = ring.col(k);
+        for (int u = 0; u < U; ++u) {
             if (skip) {
-                const Pack<T, V> e = ring.read(stage, skip_at, k);
+                float2 e[P];
+                ring.read(e, stage, skip_at, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) t[k][c] += widen(e.v[c]);
+                for (int q = 0; q < P; ++q) t[u][q] = add2(t[u][q], e[q]);
             }
-            if (a.grad_residual.p != nullptr) {
-                Pack<T, V> e;
+            if (a.grad_residual.p != nullptr && here) ring.store(grad_residual, t[u], u);
+            float2 w[P];
+            if (post) ring.weights(w, a.w_post, u);
+            uint32_t draws[2 * P];
+            if (!a.drop.none) ring.draws(draws, a.drop, offset, r, u);
+            float2 g[P], gg[P];
+            if (vector) ring.read(g, stage, gate_at, u);
 #pragma unroll
-                for (int c = 0; c < V; ++c) e.v[c] = narrow<T>(t[k][c]);
-                store_pack<true, T, V>((T*)a.grad_residual.p + r * a.grad_residual.ld + col, e);
+            for (int q = 0; q < P; ++q) {
+                x[u][q] = mul2(x[u][q], both(rstd1));
+                float2 y = post ? mul2(x[u][q], w[q]) : x[u][q];
+                float2 st = mul2(t[u][q], scale);
+                if (!a.drop.none) {  // y and what comes back of t, dropped alike
+                    y = kept_of(y, draws + 2 * q, a.drop.limit);
+                    st = kept_of(st, draws + 2 * q, a.drop.limit);
+                }
+                gg[q] = mul2(y, st);
+                t[u][q] = mul2(st, vector ? g[q] : both(row_gate));
             }
-            float w[V], f[V];
+            if (vector) {
+                if (shared_gate)
 #pragma unroll
-            for (int c = 0; c < V; ++c) w[c] = f[c] = 1.0f;
-            if (post) weights_of<V>(w, a.w_post + col);
-            if (!a.drop.none) drop_factors<V>(f, a.drop, offset, r, col);
-            if (a.gate_kind == 2) {
-                const Pack<T, V> g = ring.read(stage, gate_at, k);
-                Pack<T, V> e;
+                    for (int q = 0; q < P; ++q) sum_gate[u][q] = add2(sum_gate[u][q], gg[q]);
+                else if (a.grad_gate.p != nullptr && here) ring.store(row_of(a.grad_gate, r, sizeof(T)), gg, u);
+            } else if (a.gate_kind == 1) {
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    x[k][c] *= rstd1;
-                    const float st = a.scale * t[k][c];
-                    const float gg = dropped(x[k][c] * w[c], f[c]) * st;
-                    sum_gate[k][c] += gg;
-                    e.v[c] = narrow<T>(gg);
-                    t[k][c] = dropped(st * widen(g.v[c]), f[c]);
-                }
-                if (a.grad_gate.p != nullptr && args.chunks.gate_rows == 1)
-                    store_pack<true, T, V>((T*)a.grad_gate.p + r * a.grad_gate.ld + col, e);
-            } else {
-#pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    x[k][c] *= rstd1;
-                    const float st = a.scale * t[k][c];
-                    s[2] += dropped(x[k][c] * w[c], f[c]) * st;
-                    t[k][c] = dropped(st * row_gate, f[c]);
-                }
+                for (int q = 0; q < P; ++q) s2 = add2(s2, gg[q]);
             }
             if (post) {
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    sum_post[k][c] += t[k][c] * x[k][c];
-                    t[k][c] *= w[c];
-                    s[0] += t[k][c] * x[k][c];
-                    s[1] += t[k][c];
+                for (int q = 0; q < P; ++q) {
+                    sum_post[u][q] = fma2(t[u][q], x[u][q], sum_post[u][q]);
+                    t[u][q] = mul2(t[u][q], w[q]);
+                    s0 = fma2(t[u][q], x[u][q], s0);
+                    if (a.layer) s1 = add2(s1, t[u][q]);
                 }
             }
         }
-        if (post || a.gate_kind == 1) row_sums<CTA, 3>(s, lanes, scratch, turn);
+        s[0] = s0.x + s0.y;
+        s[1] = s1.x + s1.y;
+        s[2] = s2.x + s2.y;
+        if (a.gate_kind == 1) row_sums<CTA>(s, 3, lanes, scratch, turn);
+        else if (post) row_sums<CTA>(s, a.layer ? 2 : 1, lanes, scratch, turn);
         if (a.gate_kind == 1 && a.grad_gate.p != nullptr && here && ring.lane == 0)
-            ((T*)a.grad_gate.p)[r * a.grad_gate.ld] = narrow<T>(s[2]);
-        const float dot = post ? s[0] * over_d : 0.0f, sum = post && a.layer ? s[1] * over_d : 0.0f;
-        const bool gate_done = gate_sums && whole_gates && q % block == block - 1 && here;
+            *(T*)row_of(a.grad_gate, r, sizeof(T)) = narrow<T>(s[2]);
+        const float2 dot = both(-s[0] * over_d), mean = both(a.layer ? -s[1] * over_d : 0.0f);
+        char* grad_x = row_of(a.grad_x, r, sizeof(T));
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            if (!ring.has(k) || !here) continue;
-            Pack<T, V> e;
+        for (int u = 0; u < U; ++u) {
+            if (post)
 #pragma unroll
-            for (int c = 0; c < V; ++c) e.v[c] = narrow<T>(post ? rstd1 * (t[k][c] - sum - x[k][c] * dot) : t[k][c]);
-            store_pack<true, T, V>((T*)a.grad_x.p + r * a.grad_x.ld + ring.col(k), e);
-            if (gate_done) {
+                for (int q = 0; q < P; ++q) t[u][q] = mul2(fma2(x[u][q], dot, add2(t[u][q], mean)), both(rstd1));
+            if (here) ring.store(grad_x, t[u], u);
+        }
+        if (shared_gate && whole_gates && now.in_block == block - 1) {  // a gate vector's rows are done
+            char* grad_gate = row_of(a.grad_gate, now.gate, sizeof(T));
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    e.v[c] = narrow<T>(sum_gate[k][c]);
-                    sum_gate[k][c] = 0.0f;
-                }
-                store_pack<true, T, V>((T*)a.grad_gate.p + r / args.chunks.gate_rows * a.grad_gate.ld + ring.col(k), e);
+            for (int u = 0; u < U; ++u) {
+                if (a.grad_gate.p != nullptr && here) ring.store(grad_gate, sum_gate[u], u);
+#pragma unroll
+                for (int q = 0; q < P; ++q) sum_gate[u][q] = both(0.0f);
             }
         }
+        advance(now);
         stage = stage + 1 == stages ? 0 : stage + 1;
     }
     copies_wait(0);
     // the chunk's sums
-    auto store_sums = [&](const float (&v)[NP][V], float* part) {
+    auto store_sums = [&](const float2 (&v)[U][P], float* part) {
         part += blockIdx.x * a.d;
-        if (CTA) {
-#pragma unroll
-            for (int k = 0; k < NP; ++k)
-                if (ring.has(k))
-#pragma unroll
-                    for (int c = 0; c < V; ++c) part[ring.col(k) + c] = v[k][c];
-            return;
+        float* to = part;
+        if (!CTA) {
+            __syncthreads();
+            to = (float*)ring_bytes + group * a.d;  // [groups][d]
         }
-        float* sums = (float*)ring_bytes;  // [groups][d]
-        __syncthreads();
 #pragma unroll
-        for (int k = 0; k < NP; ++k)
-            if (ring.has(k))
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int c = 0; c < V; ++c) sums[group * a.d + ring.col(k) + c] = v[k][c];
+            for (int q = 0; q < P; ++q) {
+                const int k = V > 1 ? u : 2 * u, c = ring.col(k) + 2 * q;
+                if (ring.has(k)) to[V > 1 ? c : ring.col(k)] = v[u][q].x;
+                if (ring.has(V > 1 ? k : k + 1)) to[V > 1 ? c + 1 : ring.col(k + 1)] = v[u][q].y;
+            }
+        if (CTA) return;
         __syncthreads();
-        for (int64_t c = threadIdx.x; c < a.d; c += kWarpRowThreads) {
+        for (int c = threadIdx.x; c < (int)a.d; c += kWarpRowThreads) {
             float s = 0.0f;
-            for (int g = 0; g < groups; ++g) s += sums[g * a.d + c];
+            for (uint32_t g = 0; g < groups; ++g) s += ((float*)ring_bytes)[g * a.d + c];
             part[c] = s;
         }
     };
     if (post) store_sums(sum_post, args.part_post);
     if (pre) store_sums(sum_pre, args.part_pre);
-    if (gate_sums && !whole_gates) store_sums(sum_gate, args.part_gate);
+    if (shared_gate && !whole_gates && a.grad_gate.p != nullptr) store_sums(sum_gate, args.part_gate);
 }
 
 // Columns of [parts][d] summed: blockIdx.y = 0 the weights after the block, 1 those before the next, 2.. gate vectors.
@@ -691,13 +854,17 @@ namespace {
 struct RowPlan {
     int vec;    // elements of a piece
     bool cta;   // a row is a CTA's
-    int lanes;  // threads of a row; 0: too long, the kernels that read rows again
+    int lanes;  // threads of a row; 0: too long or too far apart, the kernels that read rows again
 };
 RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tensors, int size, int warp_elems, int cta_elems) {
     uintptr_t bits = (uintptr_t)(pb.d * size);
+    bool wide = pb.rows >= (1ll << 32);
+    for (const RowsRef& t : {pb.gate, pb.grad_gate}) wide = wide || (t.p != nullptr && t.ld * size >= (1ll << 32));
     for (const RowsRef& t : tensors) {
         bits |= (uintptr_t)t.p;
-        if (t.p != nullptr && pb.rows > 1) bits |= (uintptr_t)(t.ld * size);
+        if (t.p == nullptr || pb.rows <= 1) continue;
+        bits |= (uintptr_t)(t.ld * size);
+        wide = wide || t.ld * size >= (1ll << 32);
     }
     uintptr_t weights = 0;
     for (const float* w : {pb.w_post, pb.w_pre}) weights |= (uintptr_t)w;
@@ -705,7 +872,7 @@ RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tenso
     p.vec = (bits & 15) == 0 && (weights & 15) == 0 ? 16 / size : (bits & 3) == 0 ? 4 / size : 1;
     p.cta = pb.d > 32 * warp_elems;
     const int64_t per = p.cta ? cta_elems : warp_elems;
-    if (pb.d > per * kMaxLanes) {
+    if (pb.d > per * kMaxLanes || wide) {
         p.lanes = 0;
     } else if (p.cta) {
         p.lanes = (int)((pb.d + per - 1) / per + 31) / 32 * 32;
@@ -745,8 +912,8 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
     if (per_sm > 2048 / threads) per_sm = 2048 / threads;
     if (per_sm < 1) per_sm = 1;
     const unsigned grid = (unsigned)(want < 148 * per_sm ? want : 148 * per_sm);
-    if (p.cta) return launch_ring(residual_rows_kernel<T, V, E / V, true>, grid, threads, stage * stages, st, pb, p.lanes, stages);
-    return launch_ring(residual_rows_kernel<T, V, E / V, false>, grid, threads, stage * stages, st, pb, p.lanes, stages);
+    if (p.cta) return launch_ring(residual_rows_kernel<T, V, E, true>, grid, threads, stage * stages, st, pb, p.lanes, stages);
+    return launch_ring(residual_rows_kernel<T, V, E, false>, grid, threads, stage * stages, st, pb, p.lanes, stages);
 }
 
 }  // namespace
@@ -789,8 +956,8 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
         if (smem < sums) smem = sums;
     }
     const unsigned grid = (unsigned)a.chunks.count;
-    if (p.cta) return launch_ring(residual_grad_rows_kernel<T, V, 16 / V, true>, grid, threads, smem, st, a, p.lanes, stages);
-    return launch_ring(residual_grad_rows_kernel<T, V, 8 / V, false>, grid, threads, smem, st, a, p.lanes, stages);
+    if (p.cta) return launch_ring(residual_grad_rows_kernel<T, V, 16, true>, grid, threads, smem, st, a, p.lanes, stages);
+    return launch_ring(residual_grad_rows_kernel<T, V, 8, false>, grid, threads, smem, st, a, p.lanes, stages);
 }
 
 }  // namespace

@@ -30,6 +30,28 @@ __device__ __forceinline__ uint32_t narrow2(float low, float high) {
 __device__ __forceinline__ float widen_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float widen_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Two fp32 operations in one instruction.
+#define ROBE_F2(name, op)                                                                                              \
+    __device__ __forceinline__ float2 name(float2 a, float2 b) {                                                       \
+        float2 d;                                                                                                      \
+        asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n" op " d, a, b;\nmov.b64 {%0, %1}, d;\n}" \
+            : "=f"(d.x), "=f"(d.y)                                                                                     \
+            : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));                                                                 \
+        return d;                                                                                                      \
+    }
+ROBE_F2(add2, "add.rn.f32x2")
+ROBE_F2(mul2, "mul.rn.f32x2")
+#undef ROBE_F2
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 // V consecutive elements as one access of V * sizeof(T) bytes (aligned to that), V a power of two, at most 16 bytes
 template <class T, int V>
 struct alignas(V * sizeof(T)) Pack {
