@@ -6,6 +6,7 @@
 // kept between the passes.  With n = norm(v) and rstd its factor, the gradient through a norm is
 //   d(v) = rstd (g - [mean g] - n mean(g n)),     g = (gradient of the normed row) * weight,   [..]: layer norm only.
 #include <initializer_list>
+#include <type_traits>
 
 #include "robe_internal.h"
 #include "robe_rowops.cuh"
@@ -533,7 +534,7 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
 
 // One CTA per chunk.  The weights' gradients of a thread's columns are summed in registers over its rows, over the groups of
 // a CTA in shared memory, over the chunks by the kernel below; a gate vector's likewise, or stored when its rows are done.
-template <class T, int V, int E, bool CTA>
+template <class T, int V, int E, bool CTA, bool USUAL, int LAYER, int DROP>
 __global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
 residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     using R = Ring<T, V, E>;
@@ -543,7 +544,9 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     follow();
     const ResidualProblem& a = args.p;
     const uint64_t offset = drop_offset(a.drop);
-    const bool post = a.w_post != nullptr, pre = a.w_pre != nullptr, skip = a.grad_out.p != nullptr, vector = a.gate_kind == 2;
+    const bool post = USUAL || a.w_post != nullptr, pre = USUAL || a.w_pre != nullptr, skip = USUAL || a.grad_out.p != nullptr;
+    const bool stream = USUAL || a.grad_residual.p != nullptr, vector = a.gate_kind == 2;
+    const bool layer = USUAL ? LAYER : a.layer, dropping = USUAL ? DROP : !a.drop.none;
     const bool shared_gate = vector && args.chunks.gate_rows > 1;  // a gate vector of several rows
     const bool whole_gates = args.chunks.per_gate == 0;            // .. all in this chunk
     const int skip_at = 1, out_at = skip_at + skip, normed_at = out_at + pre, gate_at = normed_at + pre;
@@ -616,7 +619,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
                 for (int q = 0; q < P; ++q) t[u][q] = both(0.0f);
         }
         float s[kSums];
-        if (a.layer) {
+        if (layer) {
             float2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -668,13 +671,13 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
                     sum_pre[u][q] = fma2(g[q], t[u][q], sum_pre[u][q]);
                     w[q] = mul2(g[q], w[q]);
                     s1 = fma2(w[q], t[u][q], s1);
-                    if (a.layer) s2 = add2(s2, w[q]);
+                    if (layer) s2 = add2(s2, w[q]);
                 }
             }
             s[0] = s1.x + s1.y;
             s[1] = s2.x + s2.y;
-            row_sums<CTA>(s, a.layer ? 2 : 1, lanes, scratch, turn);
-            const float2 dot = both(-s[0] * over_d), mean = both(a.layer ? -s[1] * over_d : 0.0f);
+            row_sums<CTA>(s, layer ? 2 : 1, lanes, scratch, turn);
+            const float2 dot = both(-s[0] * over_d), mean = both(layer ? -s[1] * over_d : 0.0f);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float2 g[P], w[P];
@@ -686,7 +689,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         }
         float row_gate = 1.0f;
         if (a.gate_kind == 1 && here) row_gate = widen(*(const T*)row_of(a.gate, r, sizeof(T)));
-        const float2 scale = both(a.drop.none ? a.scale : a.scale * a.drop.scale);
+        const float2 scale = both(dropping ? a.scale * a.drop.scale : a.scale);
         char* grad_residual = row_of(a.grad_residual, r, sizeof(T));
         float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
@@ -697,11 +700,11 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
 #pragma unroll
                 for (int q = 0; q < P; ++q) t[u][q] = add2(t[u][q], e[q]);
             }
-            if (a.grad_residual.p != nullptr && here) ring.store(grad_residual, t[u], u);
+            if (stream && here) ring.store(grad_residual, t[u], u);
             float2 w[P];
             if (post) ring.weights(w, a.w_post, u);
             uint32_t draws[2 * P];
-            if (!a.drop.none) ring.draws(draws, a.drop, offset, r, u);
+            if (dropping) ring.draws(draws, a.drop, offset, r, u);
             float2 g[P], gg[P];
             if (vector) ring.read(g, stage, gate_at, u);
 #pragma unroll
@@ -709,7 +712,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
                 x[u][q] = mul2(x[u][q], both(rstd1));
                 float2 y = post ? mul2(x[u][q], w[q]) : x[u][q];
                 float2 st = mul2(t[u][q], scale);
-                if (!a.drop.none) {  // y and what comes back of t, dropped alike
+                if (dropping) {  // y and what comes back of t, dropped alike
                     y = kept_of(y, draws + 2 * q, a.drop.limit);
                     st = kept_of(st, draws + 2 * q, a.drop.limit);
                 }
@@ -731,7 +734,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
                     sum_post[u][q] = fma2(t[u][q], x[u][q], sum_post[u][q]);
                     t[u][q] = mul2(t[u][q], w[q]);
                     s0 = fma2(t[u][q], x[u][q], s0);
-                    if (a.layer) s1 = add2(s1, t[u][q]);
+                    if (layer) s1 = add2(s1, t[u][q]);
                 }
             }
         }
@@ -739,10 +742,10 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         s[1] = s1.x + s1.y;
         s[2] = s2.x + s2.y;
         if (a.gate_kind == 1) row_sums<CTA>(s, 3, lanes, scratch, turn);
-        else if (post) row_sums<CTA>(s, a.layer ? 2 : 1, lanes, scratch, turn);
+        else if (post) row_sums<CTA>(s, layer ? 2 : 1, lanes, scratch, turn);
         if (a.gate_kind == 1 && a.grad_gate.p != nullptr && here && ring.lane == 0)
             *(T*)row_of(a.grad_gate, r, sizeof(T)) = narrow<T>(s[2]);
-        const float2 dot = both(-s[0] * over_d), mean = both(a.layer ? -s[1] * over_d : 0.0f);
+        const float2 dot = both(-s[0] * over_d), mean = both(layer ? -s[1] * over_d : 0.0f);
         char* grad_x = row_of(a.grad_x, r, sizeof(T));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -956,8 +959,23 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
         if (smem < sums) smem = sums;
     }
     const unsigned grid = (unsigned)a.chunks.count;
-    if (p.cta) return launch_ring(residual_grad_rows_kernel<T, V, 16, true>, grid, threads, smem, st, a, p.lanes, stages);
-    return launch_ring(residual_grad_rows_kernel<T, V, 8, false>, grid, threads, smem, st, a, p.lanes, stages);
+    // the call of a training step, 16-byte pieces: both norms, both gradients, nothing left to ask in the row loop
+    const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.grad_out.p != nullptr &&
+                       pb.grad_residual.p != nullptr;
+    auto launch = [&](auto cta) {
+        constexpr bool kCta = decltype(cta)::value;
+        constexpr int kE = kCta ? 16 : 8;
+        void (*kernel)(JoinGradArgs, int, int) = residual_grad_rows_kernel<T, V, kE, kCta, false, 0, 0>;
+        if constexpr (V * sizeof(T) == 16) {
+            if (usual)
+                kernel = pb.layer ? (pb.drop.none ? residual_grad_rows_kernel<T, V, kE, kCta, true, 1, 0>
+                                                  : residual_grad_rows_kernel<T, V, kE, kCta, true, 1, 1>)
+                                  : (pb.drop.none ? residual_grad_rows_kernel<T, V, kE, kCta, true, 0, 0>
+                                                  : residual_grad_rows_kernel<T, V, kE, kCta, true, 0, 1>);
+        }
+        return launch_ring(kernel, grid, threads, smem, st, a, p.lanes, stages);
+    };
+    return p.cta ? launch(std::true_type()) : launch(std::false_type());
 }
 
 }  // namespace
