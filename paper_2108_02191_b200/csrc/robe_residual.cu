@@ -6,7 +6,6 @@
 // kept between the passes.  With n = norm(v) and rstd its factor, the gradient through a norm is
 //   d(v) = rstd (g - [mean g] - n mean(g n)),     g = (gradient of the normed row) * weight,   [..]: layer norm only.
 #include <initializer_list>
-#include <type_traits>
 
 #include "robe_internal.h"
 #include "robe_rowops.cuh"
@@ -142,41 +141,50 @@ __device__ __forceinline__ void row_sums(float (&v)[kSums], int n, int lanes, Sc
 }
 
 // A thread's elements of a row: E of them as E / 2 pairs.  They are taken in units of pairs: a piece of V elements, or, where
-// V is 1, two pieces.  Element c of unit u stands in column(u, c).
-template <class T, int V, int E>
+// V is 1, two pieces.  Shared memory is [stage][tensor][piece][thread]; THREADS of a CTA, 0: asked at run time.
+template <class T, int V, int E, int TENSORS, int THREADS>
 struct Ring {
     static constexpr int P = V > 1 ? V / 2 : 1;  // pairs of a unit
     static constexpr int U = E / (2 * P);        // units
     static constexpr int NP = E / V;             // pieces
-    T* base;  // [stage][tensor][piece][thread], V elements each
-    int tensors, lanes, lane, d;
+    static constexpr int kSlot = V * (int)sizeof(T);
+    static constexpr int kThread = kSlot * TENSORS * NP;  // bytes of a thread in a stage
+    char* first;  // the thread's first piece of stage 0
+    int lanes, lane, d;
 
-    __device__ __forceinline__ T* at(int stage, int tensor, int k) const {
-        return base + (size_t)((((stage * tensors + tensor) * NP + k) * blockDim.x + threadIdx.x) * V);
+    __device__ __forceinline__ Ring(unsigned char* bytes, int lanes_, int lane_, int64_t d_)
+        : first((char*)bytes + threadIdx.x * kSlot), lanes(lanes_), lane(lane_), d((int)d_) {}
+    static __device__ __forceinline__ int threads() { return THREADS > 0 ? THREADS : (int)blockDim.x; }
+    __device__ __forceinline__ char* stage(int s) const { return first + s * threads() * kThread; }
+    static __device__ __forceinline__ T* at(char* stage, int tensor, int k) {
+        return (T*)(stage + (tensor * NP + k) * (threads() * kSlot));
     }
     __device__ __forceinline__ int col(int k) const { return (k * lanes + lane) * V; }
     __device__ __forceinline__ bool has(int k) const { return col(k) < d; }
+    __device__ __forceinline__ int col_or_0(int k) const { return has(k) ? col(k) : 0; }
     // beyond a row's end there are zeros, once and for all
     __device__ __forceinline__ void clear(int stages) const {
-        for (int s = 0; s < stages * tensors; ++s)
+        for (int s = 0; s < stages; ++s)
 #pragma unroll
-            for (int k = 0; k < NP; ++k)
-                if (!has(k))
+            for (int t = 0; t < TENSORS; ++t)
 #pragma unroll
-                    for (int c = 0; c < V; ++c) at(0, s, k)[c] = narrow<T>(0.0f);
+                for (int k = 0; k < NP; ++k)
+                    if (!has(k))
+#pragma unroll
+                        for (int c = 0; c < V; ++c) at(stage(s), t, k)[c] = narrow<T>(0.0f);
     }
-    __device__ __forceinline__ void fetch(int stage, int tensor, const char* row) const {
+    __device__ __forceinline__ void fetch(char* stage, int tensor, const char* row) const {
 #pragma unroll
         for (int k = 0; k < NP; ++k)
-            if (has(k)) copy_async<V * sizeof(T)>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
+            if (has(k)) copy_async<kSlot>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
     }
-    __device__ __forceinline__ void zero(int stage, int tensor) const {
+    static __device__ __forceinline__ void zero(char* stage, int tensor) {
 #pragma unroll
         for (int k = 0; k < NP; ++k)
 #pragma unroll
             for (int c = 0; c < V; ++c) at(stage, tensor, k)[c] = narrow<T>(0.0f);
     }
-    __device__ __forceinline__ void read(float2 (&v)[P], int stage, int tensor, int u) const {
+    static __device__ __forceinline__ void read(float2 (&v)[P], char* stage, int tensor, int u) {
         if constexpr (V == 1) {
             v[0] = make_float2(widen(*at(stage, tensor, 2 * u)), widen(*at(stage, tensor, 2 * u + 1)));
         } else {
@@ -215,25 +223,22 @@ struct Ring {
             __stcs((W*)(row + (uint32_t)col(u) * (uint32_t)sizeof(T)), p.w);
         }
     }
-    // fp32 weights (16-byte aligned from V = 4 on: the weights are, and columns are multiples of V), 0 beyond the row's end
+    // fp32 weights (16-byte aligned from V = 4 on: the weights are, and columns are multiples of V); beyond the row's end
+    // some others, which multiply zeros
     __device__ __forceinline__ void weights(float2 (&w)[P], const float* p, int u) const {
         if constexpr (V == 1) {
-            w[0].x = has(2 * u) ? __ldca(p + col(2 * u)) : 0.0f;
-            w[0].y = has(2 * u + 1) ? __ldca(p + col(2 * u + 1)) : 0.0f;
-        } else {
+            w[0] = make_float2(__ldca(p + col_or_0(2 * u)), __ldca(p + col_or_0(2 * u + 1)));
+        } else if constexpr (V >= 4) {
+            const float4* at = (const float4*)(p + col_or_0(u));
 #pragma unroll
-            for (int q = 0; q < P; ++q) w[q] = both(0.0f);
-            if (!has(u)) return;
-            if constexpr (V >= 4) {
-#pragma unroll
-                for (int q = 0; q < P; q += 2) {
-                    const float4 x = __ldca((const float4*)(p + col(u) + 2 * q));
-                    w[q] = make_float2(x.x, x.y);
-                    w[q + 1] = make_float2(x.z, x.w);
-                }
-            } else {
-                w[0] = make_float2(__ldca(p + col(u)), __ldca(p + col(u) + 1));
+            for (int q = 0; q < P; q += 2) {
+                const float4 x = __ldca(at + q / 2);
+                w[q] = make_float2(x.x, x.y);
+                w[q + 1] = make_float2(x.z, x.w);
             }
+        } else {
+            const float* at = p + col_or_0(u);
+            w[0] = make_float2(__ldca(at), __ldca(at + 1));
         }
     }
     // what an element is kept by when it is above the limit
@@ -291,18 +296,19 @@ struct GateRow {
     }
 };
 
-template <class T, int V, int E, bool CTA>
+// USUAL: both norms, something added to, and LAYER, DROP and VECTOR say the rest; otherwise that is asked in the row loop.
+template <class T, int V, int E, bool CTA, bool USUAL, int LAYER, int DROP, int VECTOR>
 __global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
 residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
-    using R = Ring<T, V, E>;
+    using R = Ring<T, V, E, 2 + VECTOR, CTA ? 0 : kWarpRowThreads>;
     constexpr int P = R::P, U = R::U;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
     __shared__ Scratch scratch;
     follow();
     const uint64_t offset = drop_offset(a.drop);
-    const bool post = a.w_post != nullptr, pre = a.w_pre != nullptr, added = a.residual.p != nullptr;
-    const int gate_at = added ? 2 : 1, tensors = gate_at + (a.gate_kind == 2);
-    const R ring{(T*)ring_bytes, tensors, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), (int)a.d};
+    const bool post = USUAL || a.w_post != nullptr, pre = USUAL || a.w_pre != nullptr, added = USUAL || a.residual.p != nullptr;
+    const bool layer = USUAL ? LAYER : a.layer, dropping = USUAL ? DROP : !a.drop.none, vector = USUAL ? VECTOR : a.gate_kind == 2;
+    const R ring(ring_bytes, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), a.d);
     const uint32_t groups = CTA ? 1 : kWarpRowThreads / lanes, group = CTA ? 0 : threadIdx.x / lanes;
     const uint32_t step = gridDim.x * groups, rows = (uint32_t)a.rows;
     const float over_d = 1.0f / (float)a.d;
@@ -316,35 +322,36 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
     uint64_t leader = (uint64_t)blockIdx.x * groups + (CTA ? 0 : (threadIdx.x & ~31u) / lanes);
     const uint32_t ahead = CTA ? 0 : group - (threadIdx.x & ~31u) / lanes;
     uint64_t next = leader + ahead;
-    GateRow gate(next < rows ? (uint32_t)next : 0, step, a.gate_kind == 2 ? (uint32_t)a.gate_rows : 1);
-    auto fetch = [&](int stage) {
+    GateRow gate(next < rows ? (uint32_t)next : 0, step, vector ? (uint32_t)a.gate_rows : 1);
+    auto fetch = [&](char* stage) {
         if (next < rows) {
             const uint32_t r = (uint32_t)next;
             ring.fetch(stage, 0, row_of(a.x, r, sizeof(T)));
             if (added) ring.fetch(stage, 1, row_of(a.residual, r, sizeof(T)));
-            if (a.gate_kind == 2) {
-                ring.fetch(stage, gate_at, row_of(a.gate, gate.gate, sizeof(T)));
+            if (vector) {
+                ring.fetch(stage, 2, row_of(a.gate, gate.gate, sizeof(T)));
                 gate.next();
             }
         }
         next += step;
         copies_close();
     };
-    for (int s = 0; s + 1 < stages; ++s) fetch(s);
-    int stage = 0;
+    for (int s = 0; s + 1 < stages; ++s) fetch(ring.stage(s));
+    int turn_of = 0;
     for (; leader < rows; leader += step) {
         const bool here = leader + ahead < rows;
         const uint32_t r = (uint32_t)leader + ahead;
-        fetch(stage == 0 ? stages - 1 : stage - 1);
+        fetch(ring.stage(turn_of == 0 ? stages - 1 : turn_of - 1));
+        char* stage = ring.stage(turn_of);
         copies_wait(stages - 1);
         float2 v[U][P];
 #pragma unroll
-        for (int u = 0; u < U; ++u) ring.read(v[u], stage, 0, u);
+        for (int u = 0; u < U; ++u) R::read(v[u], stage, 0, u);
         // norm of the row that v holds (0 beyond d): mean and factor
         auto stats = [&](float& mean, float& rstd) {
             float s[kSums];
             mean = 0.0f;
-            if (a.layer) {
+            if (layer) {
                 float2 t = both(0.0f);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -360,7 +367,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
 #pragma unroll
                 for (int q = 0; q < P; ++q) {
                     float2 c = v[u][q];
-                    if (a.layer) {
+                    if (layer) {
                         c = add2(c, both(-mean));
                         if (!ring.has(V > 1 ? u : 2 * u)) c.x = 0.0f;
                         if (!ring.has(V > 1 ? u : 2 * u + 1)) c.y = 0.0f;
@@ -375,7 +382,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
         if (post) stats(mean, rstd);
         float row_gate = a.scale;
         if (a.gate_kind == 1 && here) row_gate *= widen(*(const T*)row_of(a.gate, r, sizeof(T)));
-        if (!a.drop.none) row_gate *= a.drop.scale;
+        if (dropping) row_gate *= a.drop.scale;
         char* out = row_of(a.out, r, sizeof(T));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -383,23 +390,27 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
                 float2 w[P];
                 ring.weights(w, a.w_post, u);
 #pragma unroll
-                for (int q = 0; q < P; ++q) v[u][q] = mul2(mul2(add2(v[u][q], both(-mean)), both(rstd)), w[q]);
+                for (int q = 0; q < P; ++q) {
+                    v[u][q] = mul2(mul2(add2(v[u][q], both(-mean)), both(rstd)), w[q]);
+                    if (layer && !ring.has(V > 1 ? u : 2 * u)) v[u][q].x = 0.0f;
+                    if (layer && !ring.has(V > 1 ? u : 2 * u + 1)) v[u][q].y = 0.0f;
+                }
             }
-            if (!a.drop.none) {
+            if (dropping) {
                 uint32_t draws[2 * P];
                 ring.draws(draws, a.drop, offset, r, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) v[u][q] = kept_of(v[u][q], draws + 2 * q, a.drop.limit);
             }
-            if (a.gate_kind == 2) {
+            if (vector) {
                 float2 g[P];
-                ring.read(g, stage, gate_at, u);
+                R::read(g, stage, 2, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) v[u][q] = mul2(v[u][q], g[q]);
             }
             if (added) {
                 float2 e[P];
-                ring.read(e, stage, 1, u);
+                R::read(e, stage, 1, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) v[u][q] = fma2(v[u][q], both(row_gate), e[q]);
             } else {
@@ -420,7 +431,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
                 if (here) ring.store(normed, w, u);
             }
         }
-        stage = stage + 1 == stages ? 0 : stage + 1;
+        turn_of = turn_of + 1 == stages ? 0 : turn_of + 1;
     }
     copies_wait(0);
 }
@@ -534,10 +545,10 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
 
 // One CTA per chunk.  The weights' gradients of a thread's columns are summed in registers over its rows, over the groups of
 // a CTA in shared memory, over the chunks by the kernel below; a gate vector's likewise, or stored when its rows are done.
-template <class T, int V, int E, bool CTA, bool USUAL, int LAYER, int DROP>
+template <class T, int V, int E, bool CTA, bool USUAL, int LAYER, int DROP, int VECTOR>
 __global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
 residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
-    using R = Ring<T, V, E>;
+    using R = Ring<T, V, E, 4 + VECTOR, CTA ? 0 : kWarpRowThreads>;
     constexpr int P = R::P, U = R::U;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
     __shared__ Scratch scratch;
@@ -545,13 +556,12 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     const ResidualProblem& a = args.p;
     const uint64_t offset = drop_offset(a.drop);
     const bool post = USUAL || a.w_post != nullptr, pre = USUAL || a.w_pre != nullptr, skip = USUAL || a.grad_out.p != nullptr;
-    const bool stream = USUAL || a.grad_residual.p != nullptr, vector = a.gate_kind == 2;
+    const bool stream = USUAL || a.grad_residual.p != nullptr, vector = USUAL ? VECTOR : a.gate_kind == 2;
     const bool layer = USUAL ? LAYER : a.layer, dropping = USUAL ? DROP : !a.drop.none;
     const bool shared_gate = vector && args.chunks.gate_rows > 1;  // a gate vector of several rows
     const bool whole_gates = args.chunks.per_gate == 0;            // .. all in this chunk
-    const int skip_at = 1, out_at = skip_at + skip, normed_at = out_at + pre, gate_at = normed_at + pre;
-    const int tensors = gate_at + vector;
-    const R ring{(T*)ring_bytes, tensors, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), (int)a.d};
+    constexpr int kX = 0, kSkip = 1, kOut = 2, kNormed = 3, kGate = 4;
+    const R ring(ring_bytes, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), a.d);
     const uint32_t groups = CTA ? 1 : kWarpRowThreads / lanes, group = CTA ? 0 : threadIdx.x / lanes;
     const float over_d = 1.0f / (float)a.d;
     int turn = 0;
@@ -586,34 +596,36 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int q = 0; q < P; ++q) sum_post[u][q] = sum_pre[u][q] = sum_gate[u][q] = both(0.0f);
-    auto fetch = [&](int stage) {
+    auto fetch = [&](char* stage) {
         if (next.r < c1) {
             const uint32_t r = (uint32_t)next.r;
-            ring.fetch(stage, 0, row_of(a.x, r, sizeof(T)));
-            if (skip) ring.fetch(stage, skip_at, row_of(a.grad_out, r, sizeof(T)));
+            ring.fetch(stage, kX, row_of(a.x, r, sizeof(T)));
+            if (skip) ring.fetch(stage, kSkip, row_of(a.grad_out, r, sizeof(T)));
             if (pre) {
-                ring.fetch(stage, out_at, row_of(a.out, r, sizeof(T)));
-                ring.fetch(stage, normed_at, row_of(a.grad_normed, r, sizeof(T)));
+                ring.fetch(stage, kOut, row_of(a.out, r, sizeof(T)));
+                ring.fetch(stage, kNormed, row_of(a.grad_normed, r, sizeof(T)));
             }
-            if (vector) ring.fetch(stage, gate_at, row_of(a.gate, shared_gate ? next.gate : r, sizeof(T)));
+            if (vector) ring.fetch(stage, kGate, row_of(a.gate, shared_gate ? next.gate : r, sizeof(T)));
         } else {  // no such row: zeros add nothing to the sums
-            for (int k = 0; k < tensors; ++k) ring.zero(stage, k);
+#pragma unroll
+            for (int k = 0; k < 4 + VECTOR; ++k) R::zero(stage, k);
         }
         advance(next);
         copies_close();
     };
-    for (int s = 0; s + 1 < stages; ++s) fetch(s);
-    int stage = 0;
+    for (int s = 0; s + 1 < stages; ++s) fetch(ring.stage(s));
+    int turn_of = 0;
     for (uint32_t round = 0; round < rounds; ++round) {
         const uint32_t r = (uint32_t)now.r;
         const bool here = now.r < c1;
-        fetch(stage == 0 ? stages - 1 : stage - 1);
+        fetch(ring.stage(turn_of == 0 ? stages - 1 : turn_of - 1));
+        char* stage = ring.stage(turn_of);
         copies_wait(stages - 1);
         float2 x[U][P], t[U][P];  // x, then its norm; out, its norm, then the gradient of out
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            ring.read(x[u], stage, 0, u);
-            if (pre) ring.read(t[u], stage, out_at, u);
+            R::read(x[u], stage, kX, u);
+            if (pre) R::read(t[u], stage, kOut, u);
             else
 #pragma unroll
                 for (int q = 0; q < P; ++q) t[u][q] = both(0.0f);
@@ -663,7 +675,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float2 g[P], w[P];
-                ring.read(g, stage, normed_at, u);
+                R::read(g, stage, kNormed, u);
                 ring.weights(w, a.w_pre, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) {
@@ -681,10 +693,14 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float2 g[P], w[P];
-                ring.read(g, stage, normed_at, u);
+                R::read(g, stage, kNormed, u);
                 ring.weights(w, a.w_pre, u);
 #pragma unroll
-                for (int q = 0; q < P; ++q) t[u][q] = mul2(fma2(t[u][q], dot, fma2(g[q], w[q], mean)), both(rstd2));
+                for (int q = 0; q < P; ++q) {
+                    t[u][q] = mul2(fma2(t[u][q], dot, fma2(g[q], w[q], mean)), both(rstd2));
+                    if (layer && !ring.has(V > 1 ? u : 2 * u)) t[u][q].x = 0.0f;
+                    if (layer && !ring.has(V > 1 ? u : 2 * u + 1)) t[u][q].y = 0.0f;
+                }
             }
         }
         float row_gate = 1.0f;
@@ -696,7 +712,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         for (int u = 0; u < U; ++u) {
             if (skip) {
                 float2 e[P];
-                ring.read(e, stage, skip_at, u);
+                R::read(e, stage, kSkip, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) t[u][q] = add2(t[u][q], e[q]);
             }
@@ -706,7 +722,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
             uint32_t draws[2 * P];
             if (dropping) ring.draws(draws, a.drop, offset, r, u);
             float2 g[P], gg[P];
-            if (vector) ring.read(g, stage, gate_at, u);
+            if (vector) R::read(g, stage, kGate, u);
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 x[u][q] = mul2(x[u][q], both(rstd1));
@@ -764,7 +780,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
             }
         }
         advance(now);
-        stage = stage + 1 == stages ? 0 : stage + 1;
+        turn_of = turn_of + 1 == stages ? 0 : turn_of + 1;
     }
     copies_wait(0);
     // the chunk's sums
@@ -893,7 +909,7 @@ int stages_for(size_t stage_bytes) {
 }
 
 template <class K, class A>
-cudaError_t launch_ring(K* kernel, unsigned grid, int threads, size_t smem, cudaStream_t st, const A& a, int lanes, int stages) {
+cudaError_t launch_ring(K kernel, unsigned grid, int threads, size_t smem, cudaStream_t st, const A& a, int lanes, int stages) {
     if (smem > (40u << 10)) {  // (48 KB with the static part)
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -902,21 +918,39 @@ cudaError_t launch_ring(K* kernel, unsigned grid, int threads, size_t smem, cuda
     return cudaGetLastError();
 }
 
-template <class T, int V>
+// One of the kernels of the usual calls, by layer norm, dropout, gate vectors.
+#define ROBE_USUAL(name, T, V, E, CTA, pb)                                                                           \
+    ((pb).layer ? ((pb).drop.none ? ((pb).gate_kind == 2 ? name<T, V, E, CTA, true, 1, 0, 1> : name<T, V, E, CTA, true, 1, 0, 0>)   \
+                                  : ((pb).gate_kind == 2 ? name<T, V, E, CTA, true, 1, 1, 1> : name<T, V, E, CTA, true, 1, 1, 0>))  \
+                : ((pb).drop.none ? ((pb).gate_kind == 2 ? name<T, V, E, CTA, true, 0, 0, 1> : name<T, V, E, CTA, true, 0, 0, 0>)   \
+                                  : ((pb).gate_kind == 2 ? name<T, V, E, CTA, true, 0, 1, 1> : name<T, V, E, CTA, true, 0, 1, 0>)))
+
+template <class T, int V, bool CTA>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
     constexpr int E = 16;
-    const int threads = p.cta ? p.lanes : kWarpRowThreads;
-    const int tensors = 1 + (pb.residual.p != nullptr) + (pb.gate_kind == 2);
-    const size_t stage = (size_t)tensors * E * sizeof(T) * threads;
+    const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.residual.p != nullptr;
+    const int threads = CTA ? p.lanes : kWarpRowThreads;
+    void (*kernel)(ResidualProblem, int, int) = residual_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
+    int slots = Ring<T, V, E, 3, 0>::kThread;
+    if constexpr (V * sizeof(T) == 16) {
+        if (usual) {
+            kernel = ROBE_USUAL(residual_rows_kernel, T, V, E, CTA, pb);
+            if (pb.gate_kind != 2) slots = Ring<T, V, E, 2, 0>::kThread;
+        }
+    }
+    const size_t stage = (size_t)slots * threads;
     const int stages = stages_for(stage);
-    const int64_t groups = p.cta ? 1 : kWarpRowThreads / p.lanes;
+    const int64_t groups = CTA ? 1 : kWarpRowThreads / p.lanes;
     const int64_t want = (pb.rows + groups - 1) / groups;
     int64_t per_sm = (int64_t)((220u << 10) / (stage * stages + 1024));
     if (per_sm > 2048 / threads) per_sm = 2048 / threads;
     if (per_sm < 1) per_sm = 1;
     const unsigned grid = (unsigned)(want < 148 * per_sm ? want : 148 * per_sm);
-    if (p.cta) return launch_ring(residual_rows_kernel<T, V, E, true>, grid, threads, stage * stages, st, pb, p.lanes, stages);
-    return launch_ring(residual_rows_kernel<T, V, E, false>, grid, threads, stage * stages, st, pb, p.lanes, stages);
+    return launch_ring(kernel, grid, threads, stage * stages, st, pb, p.lanes, stages);
+}
+template <class T, int V>
+cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
+    return p.cta ? launch_forward_rows<T, V, true>(pb, p, st) : launch_forward_rows<T, V, false>(pb, p, st);
 }
 
 }  // namespace
@@ -945,37 +979,34 @@ size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates) {
 
 namespace {
 
-template <class T, int V>
+template <class T, int V, bool CTA>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
+    constexpr int E = CTA ? 16 : 8;
     const ResidualProblem& pb = a.p;
-    const int E = p.cta ? 16 : 8;
-    const int threads = p.cta ? p.lanes : kWarpRowThreads;
-    const int tensors = 1 + (pb.grad_out.p != nullptr) + 2 * (pb.w_pre != nullptr) + (pb.gate_kind == 2);
-    const size_t stage = (size_t)tensors * E * sizeof(T) * threads;
-    const int stages = stages_for(stage);
-    size_t smem = stage * stages;
-    if (!p.cta) {  // (the groups' sums go through the same memory)
-        const size_t sums = (size_t)kWarpRowThreads / p.lanes * pb.d * sizeof(float);
-        if (smem < sums) smem = sums;
-    }
-    const unsigned grid = (unsigned)a.chunks.count;
     // the call of a training step, 16-byte pieces: both norms, both gradients, nothing left to ask in the row loop
     const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.grad_out.p != nullptr &&
                        pb.grad_residual.p != nullptr;
-    auto launch = [&](auto cta) {
-        constexpr bool kCta = decltype(cta)::value;
-        constexpr int kE = kCta ? 16 : 8;
-        void (*kernel)(JoinGradArgs, int, int) = residual_grad_rows_kernel<T, V, kE, kCta, false, 0, 0>;
-        if constexpr (V * sizeof(T) == 16) {
-            if (usual)
-                kernel = pb.layer ? (pb.drop.none ? residual_grad_rows_kernel<T, V, kE, kCta, true, 1, 0>
-                                                  : residual_grad_rows_kernel<T, V, kE, kCta, true, 1, 1>)
-                                  : (pb.drop.none ? residual_grad_rows_kernel<T, V, kE, kCta, true, 0, 0>
-                                                  : residual_grad_rows_kernel<T, V, kE, kCta, true, 0, 1>);
+    const int threads = CTA ? p.lanes : kWarpRowThreads;
+    void (*kernel)(JoinGradArgs, int, int) = residual_grad_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
+    int slots = Ring<T, V, E, 5, 0>::kThread;
+    if constexpr (V * sizeof(T) == 16) {
+        if (usual) {
+            kernel = ROBE_USUAL(residual_grad_rows_kernel, T, V, E, CTA, pb);
+            if (pb.gate_kind != 2) slots = Ring<T, V, E, 4, 0>::kThread;
         }
-        return launch_ring(kernel, grid, threads, smem, st, a, p.lanes, stages);
-    };
-    return p.cta ? launch(std::true_type()) : launch(std::false_type());
+    }
+    const size_t stage = (size_t)slots * threads;
+    const int stages = stages_for(stage);
+    size_t smem = stage * stages;
+    if (!CTA) {  // (the groups' sums go through the same memory)
+        const size_t sums = (size_t)kWarpRowThreads / p.lanes * pb.d * sizeof(float);
+        if (smem < sums) smem = sums;
+    }
+    return launch_ring(kernel, (unsigned)a.chunks.count, threads, smem, st, a, p.lanes, stages);
+}
+template <class T, int V>
+cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
+    return p.cta ? launch_backward_rows<T, V, true>(a, p, st) : launch_backward_rows<T, V, false>(a, p, st);
 }
 
 }  // namespace
