@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kJoinThreads) residual_any_kernel(ResidualProb
 
 constexpr int kMaxLanes = 512;
 constexpr int kWarpRowThreads = 256;
+constexpr int kRowElems = 16, kGradWarpElems = 8;  // elements of a thread
 
 // Sums of N values over the threads of a row, in each of them.  CTA: by turns in two halves of `scratch` (zero where there
 // is no warp), so that one barrier a sum is enough.
@@ -145,8 +146,8 @@ __device__ __forceinline__ void row_sums(float (&v)[kSums], int n, int lanes, Sc
 template <class T, int V, int E, int TENSORS, int THREADS>
 struct Ring {
     static constexpr int P = V > 1 ? V / 2 : 1;  // pairs of a unit
-    static constexpr int U = E / (2 * P);        // units
     static constexpr int NP = E / V;             // pieces
+    static constexpr int U = V > 1 ? NP : NP / 2;  // units
     static constexpr int kSlot = V * (int)sizeof(T);
     static constexpr int kThread = kSlot * TENSORS * NP;  // bytes of a thread in a stage
     char* first;  // the thread's first piece of stage 0
@@ -546,7 +547,7 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
 // One CTA per chunk.  The weights' gradients of a thread's columns are summed in registers over its rows, over the groups of
 // a CTA in shared memory, over the chunks by the kernel below; a gate vector's likewise, or stored when its rows are done.
 template <class T, int V, int E, bool CTA, bool USUAL, int LAYER, int DROP, int VECTOR>
-__global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
+__global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads, CTA ? 1 : VECTOR ? 2 : 3)
 residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     using R = Ring<T, V, E, 4 + VECTOR, CTA ? 0 : kWarpRowThreads>;
     constexpr int P = R::P, U = R::U;
@@ -842,23 +843,28 @@ __global__ void __launch_bounds__(kColumnLanes* kColumnRows) residual_columns_ke
     else (post ? a.grad_w_post : a.grad_w_pre)[c] = (float)s;
 }
 
-constexpr int64_t kMaxChunks = 592;  // four CTAs for each of 148 SMs
+// As many chunks as CTAs are resident at once, so that all end together: rows of a warp's part in CTAs of 256 threads, others
+// in CTAs of a row's threads (128 registers a thread: 512 of them an SM).
+int64_t resident_chunks(int64_t d, bool gates) {
+    if (d <= 32 * kGradWarpElems) return 148 * (gates ? 2 : 3);
+    const int64_t threads = ((d + kRowElems - 1) / kRowElems + 31) / 32 * 32;
+    return 148 * (threads >= 512 ? 1 : 512 / threads);
+}
 
-Chunks chunks_of(int64_t rows, int64_t gates) {
+Chunks chunks_of(int64_t rows, int64_t d, int64_t gates) {
+    const int64_t most = resident_chunks(d, gates > 0);
     Chunks k;
     k.rows = rows;
     k.gate_rows = gates > 0 ? rows / gates : rows;
     k.per_gate = k.gates = k.length = k.count = 0;
     if (rows == 0) return k;
-    int64_t length = (rows + kMaxChunks - 1) / kMaxChunks;
-    if (gates == 0 || k.gate_rows > length) {
-        k.gates = 0;
-        k.per_gate = (k.gate_rows + length - 1) / length;
+    if (gates <= most && (gates == 0 || k.gate_rows > 1)) {
+        k.per_gate = gates > 0 ? most / gates : most;
         k.length = (k.gate_rows + k.per_gate - 1) / k.per_gate;
+        k.per_gate = (k.gate_rows + k.length - 1) / k.length;
         k.count = (gates > 0 ? gates : 1) * k.per_gate;
     } else {
-        k.per_gate = 0;
-        k.gates = (length + k.gate_rows - 1) / k.gate_rows;
+        k.gates = (gates + most - 1) / most;
         k.length = k.gates * k.gate_rows;
         k.count = (rows + k.length - 1) / k.length;
     }
@@ -902,20 +908,12 @@ RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tenso
     return p;
 }
 
-constexpr size_t kRingBytes = 96 << 10;  // of a CTA: two fit an SM
-int stages_for(size_t stage_bytes) {
-    const size_t n = kRingBytes / stage_bytes;
-    return n >= 3 ? 3 : n == 2 ? 2 : 2 * stage_bytes <= (200u << 10) ? 2 : 1;
-}
+int stages_for(size_t stage_bytes) { return 2 * stage_bytes <= (200u << 10) ? 2 : 1; }
 
-template <class K, class A>
-cudaError_t launch_ring(K kernel, unsigned grid, int threads, size_t smem, cudaStream_t st, const A& a, int lanes, int stages) {
-    if (smem > (40u << 10)) {  // (48 KB with the static part)
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
-    launch_next(kernel, grid, threads, smem, st, a, lanes, stages);
-    return cudaGetLastError();
+template <class K>
+cudaError_t allow_shared(K kernel, size_t smem) {
+    if (smem <= (40u << 10)) return cudaSuccess;  // (48 KB with the static part)
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
 }
 
 // One of the kernels of the usual calls, by layer norm, dropout, gate vectors.
@@ -927,7 +925,7 @@ cudaError_t launch_ring(K kernel, unsigned grid, int threads, size_t smem, cudaS
 
 template <class T, int V, bool CTA>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
-    constexpr int E = 16;
+    constexpr int E = kRowElems;
     const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.residual.p != nullptr;
     const int threads = CTA ? p.lanes : kWarpRowThreads;
     void (*kernel)(ResidualProblem, int, int) = residual_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
@@ -940,13 +938,18 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
     }
     const size_t stage = (size_t)slots * threads;
     const int stages = stages_for(stage);
+    cudaError_t e = allow_shared(kernel, stage * stages);
+    if (e != cudaSuccess) return e;
     const int64_t groups = CTA ? 1 : kWarpRowThreads / p.lanes;
-    const int64_t want = (pb.rows + groups - 1) / groups;
-    int64_t per_sm = (int64_t)((220u << 10) / (stage * stages + 1024));
-    if (per_sm > 2048 / threads) per_sm = 2048 / threads;
-    if (per_sm < 1) per_sm = 1;
-    const unsigned grid = (unsigned)(want < 148 * per_sm ? want : 148 * per_sm);
-    return launch_ring(kernel, grid, threads, stage * stages, st, pb, p.lanes, stages);
+    int64_t grid = (pb.rows + groups - 1) / groups;
+    if (grid > 148) {  // CTAs that stay: no more than are resident at once
+        int per_sm = 1;
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, stage * stages);
+        if (e != cudaSuccess) return e;
+        if (grid > 148ll * per_sm) grid = 148ll * per_sm;
+    }
+    launch_next(kernel, (unsigned)grid, threads, stage * stages, st, pb, p.lanes, stages);
+    return cudaGetLastError();
 }
 template <class T, int V>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
@@ -957,7 +960,7 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
 
 cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaStream_t st) {
     const RowPlan p = row_plan(pb, {pb.x, pb.residual, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.out, pb.normed},
-                               dtype == 0 ? 4 : 2, 16, 16);
+                               dtype == 0 ? 4 : 2, kRowElems, kRowElems);
     if (p.lanes > 0) {
         if (dtype == 0) return p.vec == 4 ? launch_forward_rows<float, 4>(pb, p, st) : launch_forward_rows<float, 1>(pb, p, st);
         return p.vec == 8   ? launch_forward_rows<__nv_bfloat16, 8>(pb, p, st)
@@ -972,7 +975,9 @@ cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaSt
 
 size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates) {
     if (rows <= 0 || d <= 0) return 0;
-    const unsigned __int128 bytes = (unsigned __int128)chunks_of(rows, gates).count * d * sizeof(float) * 3;
+    (void)gates;  // (gate vectors are cut into no more chunks)
+    const int64_t most = resident_chunks(d, false);
+    const unsigned __int128 bytes = (unsigned __int128)(rows < most ? rows : most) * d * sizeof(float) * 3;
     if (bytes >= ((unsigned __int128)1 << 62)) return (size_t)1 << 62;
     return ((size_t)bytes + 255) / 256 * 256;
 }
@@ -981,7 +986,7 @@ namespace {
 
 template <class T, int V, bool CTA>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
-    constexpr int E = CTA ? 16 : 8;
+    constexpr int E = CTA ? kRowElems : kGradWarpElems;
     const ResidualProblem& pb = a.p;
     // the call of a training step, 16-byte pieces: both norms, both gradients, nothing left to ask in the row loop
     const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.grad_out.p != nullptr &&
@@ -1002,7 +1007,10 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
         const size_t sums = (size_t)kWarpRowThreads / p.lanes * pb.d * sizeof(float);
         if (smem < sums) smem = sums;
     }
-    return launch_ring(kernel, (unsigned)a.chunks.count, threads, smem, st, a, p.lanes, stages);
+    const cudaError_t e = allow_shared(kernel, smem);
+    if (e != cudaSuccess) return e;
+    launch_next(kernel, (unsigned)a.chunks.count, threads, smem, st, a, p.lanes, stages);
+    return cudaGetLastError();
 }
 template <class T, int V>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
@@ -1014,14 +1022,14 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
 cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void* workspace, cudaStream_t st) {
     JoinGradArgs a;
     a.p = pb;
-    a.chunks = chunks_of(pb.rows, pb.gate_kind == 2 ? pb.rows / pb.gate_rows : 0);
+    a.chunks = chunks_of(pb.rows, pb.d, pb.gate_kind == 2 ? pb.rows / pb.gate_rows : 0);
     a.part_post = (float*)workspace;
     a.part_pre = a.part_post + a.chunks.count * pb.d;
     a.part_gate = a.part_pre + a.chunks.count * pb.d;
     cudaError_t e = cudaSuccess;
     const RowPlan p = row_plan(pb, {pb.x, pb.grad_out, pb.out, pb.grad_normed, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.grad_x,
                                     pb.grad_residual, pb.gate_kind == 2 ? pb.grad_gate : RowsRef{}},
-                               dtype == 0 ? 4 : 2, 8, 16);
+                               dtype == 0 ? 4 : 2, kGradWarpElems, kRowElems);
     if (a.chunks.count == 0) {
     } else if (p.lanes > 0) {
         if (dtype == 0)
