@@ -148,6 +148,7 @@ struct Ring {
     static constexpr int P = V > 1 ? V / 2 : 1;  // pairs of a unit
     static constexpr int NP = E / V;             // pieces
     static constexpr int U = V > 1 ? NP : NP / 2;  // units
+    static constexpr int kPieces = V > 1 ? 1 : 2;  // of a unit
     static constexpr int kSlot = V * (int)sizeof(T);
     static constexpr int kThread = kSlot * TENSORS * NP;  // bytes of a thread in a stage
     char* first;  // the thread's first piece of stage 0
@@ -297,6 +298,17 @@ struct GateRow {
     }
 };
 
+// Adds v to a unit's elements, not to the zeros beyond the row's end.
+template <class R, int P>
+__device__ __forceinline__ void center(const R& ring, float2 (&x)[P], float v, int u) {
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        x[q] = add2(x[q], both(v));
+        if (!ring.has(R::kPieces * u)) x[q].x = 0.0f;
+        if (!ring.has(R::kPieces * u + R::kPieces - 1)) x[q].y = 0.0f;
+    }
+}
+
 // USUAL: both norms, something added to, and LAYER, DROP and VECTOR say the rest; otherwise that is asked in the row loop.
 template <class T, int V, int E, bool CTA, bool USUAL, int LAYER, int DROP, int VECTOR>
 __global__ void __launch_bounds__(CTA ? kMaxLanes : kWarpRowThreads)
@@ -364,17 +376,14 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
             }
             float2 t = both(0.0f);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                float2 c[P];
 #pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    float2 c = v[u][q];
-                    if (layer) {
-                        c = add2(c, both(-mean));
-                        if (!ring.has(V > 1 ? u : 2 * u)) c.x = 0.0f;
-                        if (!ring.has(V > 1 ? u : 2 * u + 1)) c.y = 0.0f;
-                    }
-                    t = fma2(c, c, t);
-                }
+                for (int q = 0; q < P; ++q) c[q] = v[u][q];
+                if (layer) center(ring, c, -mean, u);
+#pragma unroll
+                for (int q = 0; q < P; ++q) t = fma2(c[q], c[q], t);
+            }
             s[0] = t.x + t.y;
             row_sums<CTA, 1>(s, lanes, scratch, turn);
             rstd = 1.0f / sqrtf(s[0] * over_d + a.eps);
@@ -390,12 +399,9 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
             if (post) {
                 float2 w[P];
                 ring.weights(w, a.w_post, u);
+                if (layer) center(ring, v[u], -mean, u);
 #pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    v[u][q] = mul2(mul2(add2(v[u][q], both(-mean)), both(rstd)), w[q]);
-                    if (layer && !ring.has(V > 1 ? u : 2 * u)) v[u][q].x = 0.0f;
-                    if (layer && !ring.has(V > 1 ? u : 2 * u + 1)) v[u][q].y = 0.0f;
-                }
+                for (int q = 0; q < P; ++q) v[u][q] = mul2(mul2(v[u][q], both(rstd)), w[q]);
             }
             if (dropping) {
                 uint32_t draws[2 * P];
@@ -622,41 +628,40 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         fetch(ring.stage(turn_of == 0 ? stages - 1 : turn_of - 1));
         char* stage = ring.stage(turn_of);
         copies_wait(stages - 1);
-        float2 x[U][P], t[U][P];  // x, then its norm; out, its norm, then the gradient of out
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            R::read(x[u], stage, kX, u);
-            if (pre) R::read(t[u], stage, kOut, u);
-            else
-#pragma unroll
-                for (int q = 0; q < P; ++q) t[u][q] = both(0.0f);
-        }
+        float2 t[U][P];  // out, its norm, then the gradient of out
         float s[kSums];
-        if (layer) {
-            float2 s1 = both(0.0f), s2 = both(0.0f);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    s1 = add2(s1, x[u][q]);
-                    s2 = add2(s2, t[u][q]);
-                }
-            s[0] = s1.x + s1.y;
-            s[1] = s2.x + s2.y;
-            row_sums<CTA, 2>(s, lanes, scratch, turn);
-            const float mean1 = post ? s[0] * over_d : 0.0f, mean2 = s[1] * over_d;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    x[u][q] = add2(x[u][q], both(-mean1));
-                    t[u][q] = add2(t[u][q], both(-mean2));
-                    if (!ring.has(V > 1 ? u : 2 * u)) x[u][q].x = t[u][q].x = 0.0f;
-                    if (!ring.has(V > 1 ? u : 2 * u + 1)) x[u][q].y = t[u][q].y = 0.0f;
-                }
-        }
+        float mean1 = 0.0f, mean2 = 0.0f;
         {
+            float2 x[U][P];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                R::read(x[u], stage, kX, u);
+                if (pre) R::read(t[u], stage, kOut, u);
+                else
+#pragma unroll
+                    for (int q = 0; q < P; ++q) t[u][q] = both(0.0f);
+            }
             float2 s1 = both(0.0f), s2 = both(0.0f);
+            if (layer) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int q = 0; q < P; ++q) {
+                        s1 = add2(s1, x[u][q]);
+                        s2 = add2(s2, t[u][q]);
+                    }
+                s[0] = s1.x + s1.y;
+                s[1] = s2.x + s2.y;
+                row_sums<CTA, 2>(s, lanes, scratch, turn);
+                mean1 = post ? s[0] * over_d : 0.0f;
+                mean2 = s[1] * over_d;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    center(ring, x[u], -mean1, u);
+                    center(ring, t[u], -mean2, u);
+                }
+                s1 = s2 = both(0.0f);
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -672,12 +677,15 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         const float rstd1 = !here ? 0.0f : post ? 1.0f / sqrtf(s[0] * over_d + a.eps) : 1.0f;
         const float rstd2 = !here ? 0.0f : pre ? 1.0f / sqrtf(s[1] * over_d + a.eps) : 1.0f;
         if (pre) {
+            // with g the normed row's gradient times the weight: t = (grad_out + rstd g) - rstd (mean(g n) n + [mean g])
+            float2 both_sides[U][P];
             float2 s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                float2 g[P], w[P];
+                float2 g[P], w[P], e[P];
                 R::read(g, stage, kNormed, u);
                 ring.weights(w, a.w_pre, u);
+                if (skip) R::read(e, stage, kSkip, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) {
                     t[u][q] = mul2(t[u][q], both(rstd2));
@@ -685,25 +693,24 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
                     w[q] = mul2(g[q], w[q]);
                     s1 = fma2(w[q], t[u][q], s1);
                     if (layer) s2 = add2(s2, w[q]);
+                    both_sides[u][q] = skip ? fma2(w[q], both(rstd2), e[q]) : mul2(w[q], both(rstd2));
                 }
             }
             s[0] = s1.x + s1.y;
             s[1] = s2.x + s2.y;
             row_sums<CTA>(s, layer ? 2 : 1, lanes, scratch, turn);
-            const float2 dot = both(-s[0] * over_d), mean = both(layer ? -s[1] * over_d : 0.0f);
+            const float dot = -s[0] * over_d * rstd2;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                float2 g[P], w[P];
-                R::read(g, stage, kNormed, u);
-                ring.weights(w, a.w_pre, u);
 #pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    t[u][q] = mul2(fma2(t[u][q], dot, fma2(g[q], w[q], mean)), both(rstd2));
-                    if (layer && !ring.has(V > 1 ? u : 2 * u)) t[u][q].x = 0.0f;
-                    if (layer && !ring.has(V > 1 ? u : 2 * u + 1)) t[u][q].y = 0.0f;
-                }
+                for (int q = 0; q < P; ++q) t[u][q] = fma2(t[u][q], both(dot), both_sides[u][q]);
+                if (layer) center(ring, t[u], -s[1] * over_d * rstd2, u);
             }
+        } else if (skip) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) R::read(t[u], stage, kSkip, u);
         }
+        float2 x[U][P];  // norm of x
         float row_gate = 1.0f;
         if (a.gate_kind == 1 && here) row_gate = widen(*(const T*)row_of(a.gate, r, sizeof(T)));
         const float2 scale = both(dropping ? a.scale * a.drop.scale : a.scale);
@@ -711,12 +718,8 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (skip) {
-                float2 e[P];
-                R::read(e, stage, kSkip, u);
-#pragma unroll
-                for (int q = 0; q < P; ++q) t[u][q] = add2(t[u][q], e[q]);
-            }
+            R::read(x[u], stage, kX, u);
+            if (layer) center(ring, x[u], -mean1, u);
             if (stream && here) ring.store(grad_residual, t[u], u);
             float2 w[P];
             if (post) ring.weights(w, a.w_post, u);
