@@ -386,7 +386,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
             }
             s[0] = t.x + t.y;
             row_sums<CTA, 1>(s, lanes, scratch, turn);
-            rstd = 1.0f / sqrtf(s[0] * over_d + a.eps);
+            rstd = rsqrtf(s[0] * over_d + a.eps);
         };
         float mean = 0.0f, rstd = 1.0f;
         if (post) stats(mean, rstd);
@@ -565,7 +565,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     const bool post = USUAL || a.w_post != nullptr, pre = USUAL || a.w_pre != nullptr, skip = USUAL || a.grad_out.p != nullptr;
     const bool stream = USUAL || a.grad_residual.p != nullptr, vector = USUAL ? VECTOR : a.gate_kind == 2;
     const bool layer = USUAL ? LAYER : a.layer, dropping = USUAL ? DROP : !a.drop.none;
-    const bool shared_gate = vector && args.chunks.gate_rows > 1;  // a gate vector of several rows
+    const bool shared_gate = vector && a.gate_rows > 1;  // a gate vector of several rows
     const bool whole_gates = args.chunks.per_gate == 0;            // .. all in this chunk
     constexpr int kX = 0, kSkip = 1, kOut = 2, kNormed = 3, kGate = 4;
     const R ring(ring_bytes, lanes, CTA ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), a.d);
@@ -579,24 +579,27 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     }
     // the rows of a group: every groups-th of the chunk, or whole gate vectors in turn
     const uint32_t c0 = (uint32_t)args.chunks.row0(blockIdx.x), c1 = (uint32_t)args.chunks.row1(blockIdx.x);
-    const uint32_t block = shared_gate && whole_gates ? (uint32_t)args.chunks.gate_rows : 1;
+    const uint32_t block = shared_gate && whole_gates ? (uint32_t)a.gate_rows : 1;
     // (as many rounds for all groups: sums over lanes need whole warps)
     const uint32_t rounds = ((c1 - c0 + block - 1) / block + groups - 1) / groups * block;
+    // k-th row of this group and its gate vector; none from c1 on
     struct Place {
-        uint64_t r;
-        uint32_t in_block, gate;
+        uint32_t r, in_block, gate;
     };
     auto advance = [&](Place& p) {
-        ++p.in_block;
-        if (p.in_block == block) {
-            p.in_block = 0;
-            p.r += (uint64_t)(groups - 1) * block;
-            if (block > 1) p.gate += groups;
+        if (block == 1) {
+            p.r += groups;
+        } else {
+            ++p.r;
+            if (++p.in_block == block) {
+                p.in_block = 0;
+                p.r += (groups - 1) * block;
+                p.gate += groups;
+            }
         }
-        ++p.r;
     };
-    Place now{c0 + (uint64_t)group * block, 0, 0};
-    if (shared_gate) now.gate = c0 / (uint32_t)args.chunks.gate_rows + (whole_gates ? group : 0);
+    Place now{c0 + group * block, 0, 0};
+    if (shared_gate) now.gate = c0 / (uint32_t)a.gate_rows + (whole_gates ? group : 0);
     Place next = now;
     float2 sum_post[U][P], sum_pre[U][P], sum_gate[U][P];
 #pragma unroll
@@ -605,7 +608,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         for (int q = 0; q < P; ++q) sum_post[u][q] = sum_pre[u][q] = sum_gate[u][q] = both(0.0f);
     auto fetch = [&](char* stage) {
         if (next.r < c1) {
-            const uint32_t r = (uint32_t)next.r;
+            const uint32_t r = next.r;
             ring.fetch(stage, kX, row_of(a.x, r, sizeof(T)));
             if (skip) ring.fetch(stage, kSkip, row_of(a.grad_out, r, sizeof(T)));
             if (pre) {
@@ -623,7 +626,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     for (int s = 0; s + 1 < stages; ++s) fetch(ring.stage(s));
     int turn_of = 0;
     for (uint32_t round = 0; round < rounds; ++round) {
-        const uint32_t r = (uint32_t)now.r;
+        const uint32_t r = now.r;
         const bool here = now.r < c1;
         fetch(ring.stage(turn_of == 0 ? stages - 1 : turn_of - 1));
         char* stage = ring.stage(turn_of);
@@ -674,8 +677,8 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         }
         if (post || pre) row_sums<CTA, 2>(s, lanes, scratch, turn);
         // (0 for no row: with eps = 0 its factor would be infinite)
-        const float rstd1 = !here ? 0.0f : post ? 1.0f / sqrtf(s[0] * over_d + a.eps) : 1.0f;
-        const float rstd2 = !here ? 0.0f : pre ? 1.0f / sqrtf(s[1] * over_d + a.eps) : 1.0f;
+        const float rstd1 = !here ? 0.0f : post ? rsqrtf(s[0] * over_d + a.eps) : 1.0f;
+        const float rstd2 = !here ? 0.0f : pre ? rsqrtf(s[1] * over_d + a.eps) : 1.0f;
         if (pre) {
             // with g the normed row's gradient times the weight: t = (grad_out + rstd g) - rstd (mean(g n) n + [mean g])
             float2 both_sides[U][P];
@@ -886,7 +889,7 @@ struct RowPlan {
 };
 RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tensors, int size, int warp_elems, int cta_elems) {
     uintptr_t bits = (uintptr_t)(pb.d * size);
-    bool wide = pb.rows >= (1ll << 32);
+    bool wide = pb.rows >= (1ll << 30);  // (row numbers are 32 bits, and go past the end)
     for (const RowsRef& t : {pb.gate, pb.grad_gate}) wide = wide || (t.p != nullptr && t.ld * size >= (1ll << 32));
     for (const RowsRef& t : tensors) {
         bits |= (uintptr_t)t.p;
