@@ -5,6 +5,8 @@
 // A bucket is an interval of distances and a distance is one diagonal j - i of a head's matrix, so a matrix holds Q + K - 1
 // different values and its gradient is wanted by diagonals first.  Both kernels work on diagonals: the forward reads a
 // window of the diagonals' values per row, the backward keeps a diagonal's sum in a register while it walks down it.
+#include <type_traits>
+
 #include "robe_internal.h"
 #include "robe_rowops.cuh"
 
@@ -264,7 +266,7 @@ __device__ __forceinline__ void take_piece(float (&v)[kPiece<T>], const uint4* p
 // same all the way, and their sums stay in registers.  A warp's squares, side by side, are copied to shared memory one
 // ahead, in the aligned pieces that they lie in; rows that begin inside a piece are shifted into place when they are read.
 template <class T, bool ALIGNED>
-__global__ void __launch_bounds__(kGradMaxThreads) bias_grad_kernel(BiasGradArgs a) {
+__global__ void __launch_bounds__(kGradMaxThreads, 3) bias_grad_kernel(BiasGradArgs a) {
     constexpr int V = kPiece<T>;
     constexpr int kRow = ALIGNED ? 32 : 33;  // pieces of a row of a warp's squares
     extern __shared__ __align__(16) uint4 pieces[];  // [warp][stage][V][kRow]; afterwards the sums
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(kGradMaxThreads) bias_grad_kernel(BiasGradArgs
     float acc[2 * V - 1], sum[2 * V - 1];
 #pragma unroll
     for (int k = 0; k < 2 * V - 1; ++k) acc[k] = sum[k] = 0.0f;
-    {
+    if (threadIdx.x < a.lanes) {  // (warps beyond only help with the buckets)
         // a lane's lowest diagonal is V delta - (V - 1): beyond it nothing is seen under a causal mask.  What a lane copies
         // the lane before it may read.
         const bool seen = !a.causal || (int64_t)V * delta - (V - 1) - start <= 0;
@@ -391,41 +393,50 @@ __global__ void __launch_bounds__(kGradMaxThreads) bias_grad_kernel(BiasGradArgs
                 }
         }
         copies_wait(0);
-        __syncthreads();
     }
+    __syncthreads();
     // diagonal V delta + k: the lane's own upper half and the next lane's lower one
     float* upper = (float*)pieces;
     float* lower = upper + a.lanes * V;
-    const int at = threadIdx.x * V;
+    if (threadIdx.x < a.lanes) {
+        const int at = threadIdx.x * V;
 #pragma unroll
-    for (int k = 0; k < V; ++k) upper[at + k] = sum[V - 1 + k];
-    lower[at] = 0.0f;
+        for (int k = 0; k < V; ++k) upper[at + k] = sum[V - 1 + k];
+        lower[at] = 0.0f;
 #pragma unroll
-    for (int k = 1; k < V; ++k) lower[at + k] = sum[k - 1];  // diagonals V (delta - 1) + k
+        for (int k = 1; k < V; ++k) lower[at + k] = sum[k - 1];  // diagonals V (delta - 1) + k
+    }
     __syncthreads();
     // lower[V l + k] belongs to upper[V (l - 1) + k]: in terms of diagonals from V (first - 1) on, upper starts at V
     const int64_t base = (int64_t)V * (first - 1);
     const int span = (int)a.lanes * V;
-    for (uint32_t q = warp; q < a.bk.buckets; q += warps) {
-        int64_t from, to;
-        bucket_interval(q, a.bk, edges, a.causal, from, to);
-        from = from + start - base;
-        to = to + start - base;
-        const int d0 = from < 0 ? 0 : from > span + V ? span + V : (int)from;
-        const int d1 = to < 0 ? 0 : to > span + V ? span + V : (int)to;
-        double total = 0.0;
-        if (d0 < d1) {
-            for (int d = d0 + lane; d < d1; d += 32) {
-                float v = 0.0f;
-                if (d < span) v = lower[d];
-                if (d >= V) v += upper[d - V];
-                total += (double)v;
-            }
+    // a bucket is a run of diagonals: so many lanes a bucket that the longest runs are no longer than the many short ones
+    auto join = [&](auto lanes_of_a_bucket) {
+        constexpr uint32_t kShare = decltype(lanes_of_a_bucket)::value, kEach = 32 / kShare;
+        for (uint32_t q0 = warp * kEach; q0 < a.bk.buckets; q0 += warps * kEach) {
+            const uint32_t q = q0 + lane / kShare;
+            int64_t from = 0, to = 0;
+            if (q < a.bk.buckets) bucket_interval(q, a.bk, edges, a.causal, from, to);
+            from = from + start - base;
+            to = to + start - base;
+            const int d0 = from < 0 ? 0 : from > span + V ? span + V : (int)from;
+            const int d1 = q >= a.bk.buckets || to < 0 ? 0 : to > span + V ? span + V : (int)to;
+            double total = 0.0;
+            if (kShare < 32 || d0 < d1) {
+                for (int d = d0 + lane % kShare; d < d1; d += kShare) {
+                    float v = 0.0f;
+                    if (d < span) v = lower[d];
+                    if (d >= V) v += upper[d - V];
+                    total += (double)v;
+                }
 #pragma unroll
-            for (int s = 16; s > 0; s >>= 1) total += __shfl_down_sync(0xFFFFFFFFu, total, s);
+                for (int s = kShare / 2; s > 0; s >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, s);
+            }
+            if (lane % kShare == 0 && q < a.bk.buckets) a.partial[((uint64_t)h * a.bk.buckets + q) * parts + part] = total;
         }
-        if (lane == 0) a.partial[((uint64_t)h * a.bk.buckets + q) * parts + part] = total;
-    }
+    };
+    if (span > 1024) join(std::integral_constant<uint32_t, 32>());
+    else join(std::integral_constant<uint32_t, 8>());
 }
 
 // One warp per (head, bucket): the parts' sums, in a fixed order.
@@ -549,7 +560,7 @@ cudaError_t launch_bias_backward(const BiasProblem& pb, const void* grad, int64_
                                                   : bias_grad_kernel<__nv_bfloat16, false>;
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
-        launch_next(kernel, (unsigned)grid, g.lanes, smem, st, a);
+        launch_next(kernel, (unsigned)grid, g.lanes < 128 ? 128 : g.lanes, smem, st, a);
     }
     launch_next(bias_grad_join_kernel, (unsigned)(pb.heads * pb.bk.buckets), 32, 0, st, a);
     return cudaGetLastError();

@@ -92,6 +92,77 @@ void launch(const DropArgs& a, cudaStream_t st) {
                 st, a);
 }
 
+// Rows laid end to end that are no whole pieces: the elements go by in 16-byte pieces all the same.  A CTA first evaluates the
+// generator for the groups that its elements are of, once each, and leaves the decisions as a string of bits in the order
+// of the elements; a piece then reads its own.
+constexpr int kFlatItems = 4;
+template <class T>
+__global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(DropArgs a, uint64_t elements, uint64_t cols) {
+    constexpr int V = kPiece<T>;
+    constexpr int kTile = kDropThreads * kFlatItems * V;
+    __shared__ uint32_t bits[kTile / 32 + 1];  // (a group may end behind the tile)
+    __shared__ uint64_t place[2];
+    follow();
+    const uint64_t offset = drop_offset(a.drop);
+    const uint64_t base = (uint64_t)blockIdx.x * kTile;
+    const int count = elements - base < kTile ? (int)(elements - base) : kTile;
+    const T* in = (const T*)a.in + base;
+    T* out = (T*)a.out + base;
+    uint4 e[kFlatItems];
+#pragma unroll
+    for (int i = 0; i < kFlatItems; ++i) {
+        const int at = (i * kDropThreads + threadIdx.x) * V;
+        if (at + V <= count) e[i] = __ldcs((const uint4*)(in + at));
+    }
+    for (int k = threadIdx.x; k < kTile / 32 + 1; k += kDropThreads) bits[k] = 0;
+    if (threadIdx.x == 0) {
+        place[0] = base / cols;
+        place[1] = base - place[0] * cols;
+    }
+    __syncthreads();
+    const uint32_t row0 = (uint32_t)place[0], col0 = (uint32_t)place[1];
+    const uint32_t group0 = col0 / 8;
+    // groups from (row0, group0) on, until one begins behind the tile
+    for (uint32_t t = threadIdx.x;; t += kDropThreads) {
+        const uint32_t k = t + group0;
+        const uint32_t r = a.groups == 1 ? k : (uint32_t)(((a.magic >> 32) * k + (((a.magic & 0xFFFFFFFFu) * k) >> 32)) >> 32);
+        const uint32_t g = k - r * a.groups;
+        const int64_t at = (int64_t)((uint64_t)r * cols + g * 8ull) - col0;  // where the group begins in the tile, or before it
+        if (at >= count) break;
+        const uint4 w = drop_words(row0 + r, g, offset, a.drop);
+        uint32_t keep = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) keep |= drop_keeps(w, c, a.drop) ? 1u << c : 0u;
+        if (g + 1 == a.groups) keep &= (1u << a.tail) - 1;
+        const uint32_t first = at < 0 ? keep >> -at : keep << (at & 31);
+        const int word = at < 0 ? 0 : (int)(at >> 5);
+        if (first != 0) atomicOr(&bits[word], first);
+        if (at > 0 && (at & 31) > 24) atomicOr(&bits[word + 1], keep >> (32 - (at & 31)));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFlatItems; ++i) {
+        const int at = (i * kDropThreads + threadIdx.x) * V;
+        if (at >= count) return;
+        const uint32_t keep = bits[at / 32] >> (at & 31);
+        if (at + V <= count) {
+            uint32_t* v = (uint32_t*)&e[i];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (sizeof(T) == 2) {
+                    const float low = widen_low(v[k]) * a.drop.scale, high = widen_high(v[k]) * a.drop.scale;
+                    v[k] = narrow2(keep >> (2 * k) & 1 ? low : 0.0f, keep >> (2 * k + 1) & 1 ? high : 0.0f);
+                } else {
+                    v[k] = __float_as_uint(keep >> k & 1 ? __uint_as_float(v[k]) * a.drop.scale : 0.0f);
+                }
+            }
+            __stcs((uint4*)(out + at), e[i]);
+        } else {
+            for (int k = 0; at + k < count; ++k) out[at + k] = narrow<T>(keep >> k & 1 ? widen(in[at + k]) * a.drop.scale : 0.0f);
+        }
+    }
+}
+
 }  // namespace
 
 cudaError_t launch_dropout(const void* in, int64_t in_ld, void* out, int64_t out_ld, int64_t rows, int64_t cols, int dtype,
@@ -108,6 +179,18 @@ cudaError_t launch_dropout(const void* in, int64_t in_ld, void* out, int64_t out
     a.drop = drop;
     const bool pieces = !drop.none && cols % 8 == 0 && (((uintptr_t)in | (uintptr_t)out) & 15u) == 0 &&
                         (rows == 1 || (in_ld * size % 16 == 0 && out_ld * size % 16 == 0 && in_ld < (1ll << 30) && out_ld < (1ll << 30)));
+    const bool flat = !pieces && !drop.none && (rows == 1 || (in_ld == cols && out_ld == cols)) && (((uintptr_t)in | (uintptr_t)out) & 15u) == 0;
+    if (flat) {
+        a.in = in;
+        a.out = out;
+        const uint64_t elements = (uint64_t)rows * cols;
+        const uint64_t tile = (uint64_t)kDropThreads * kFlatItems * (16 / size);
+        const uint64_t grid = (elements + tile - 1) / tile;
+        if (grid >= (1ull << 31)) return cudaErrorInvalidValue;
+        if (dtype == 0) launch_next(dropout_flat_kernel<float>, (unsigned)grid, kDropThreads, 0, st, a, elements, (uint64_t)cols);
+        else launch_next(dropout_flat_kernel<__nv_bfloat16>, (unsigned)grid, kDropThreads, 0, st, a, elements, (uint64_t)cols);
+        return cudaGetLastError();
+    }
     // items are numbered in 32 bits: as many rows a launch as that allows
     const int64_t most = ((1ll << 31) - 1) / a.groups;
     for (int64_t r = 0; r < rows; r += most) {

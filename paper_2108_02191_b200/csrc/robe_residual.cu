@@ -243,29 +243,57 @@ struct Ring {
             w[0] = make_float2(__ldca(at), __ldca(at + 1));
         }
     }
-    // what an element is kept by when it is above the limit
-    __device__ __forceinline__ void draws(uint32_t (&h)[2 * P], const DropParams& drop, uint64_t offset, uint32_t r, int u) const {
-        if constexpr (V == 1) {
+    // What dropout decides a row's elements by.  The 8 / V lanes whose pieces make up a group of eight columns evaluate the
+    // generator for every 8 / V-th piece each, and hand each other the words.  (A row has that many lanes at least.)
+    static constexpr int kShare = 8 / V;
+    struct Draws {
+        uint4 w[NP / kShare];
+    };
+    __device__ __forceinline__ void draw(Draws& w, const DropParams& drop, uint64_t offset, uint32_t r) const {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int at = col(2 * u + c);
-                const uint4 w = drop_words(r, (uint32_t)at >> 3, offset, drop);
-                const uint32_t word = (at & 4) ? ((at & 2) ? w.w : w.z) : ((at & 2) ? w.y : w.x);
-                h[c] = (at & 1) ? word : word << 16;
-            }
-        } else {
-            const int at = col(u);
-            const uint4 w = drop_words(r, (uint32_t)at >> 3, offset, drop);
-            uint32_t word[4] = {w.x, w.y, w.z, w.w};
-            if constexpr (V <= 4) {
-                word[0] = (at & 4) ? word[2] : word[0];
-                word[1] = (at & 4) ? word[3] : word[1];
-            }
-            if constexpr (V == 2) word[0] = (at & 2) ? word[1] : word[0];
+        for (int e = 0; e < NP / kShare; ++e)
+            w.w[e] = drop_words(r, (uint32_t)col(e * kShare + lane % kShare) >> 3, offset, drop);
+    }
+    // .. of unit u: an element is kept when its number is above the limit.  (All lanes of a warp.)
+    __device__ __forceinline__ void draws(uint32_t (&h)[2 * P], const Draws& w, int u) const {
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
-                h[2 * q] = word[q] << 16;
-                h[2 * q + 1] = word[q];
+        for (int c = 0; c < kPieces; ++c) {
+            const int k = kPieces * u + c;
+            const int at = col(k) & 7;
+            uint4 v;
+            if (kShare == 1) {
+                v = w.w[k];
+            } else {
+                const uint4 mine = w.w[k / kShare];
+                const int from = (threadIdx.x & 31) - lane % kShare + k % kShare;
+                v.x = __shfl_sync(0xFFFFFFFFu, mine.x, from);
+                v.y = __shfl_sync(0xFFFFFFFFu, mine.y, from);
+                v.z = __shfl_sync(0xFFFFFFFFu, mine.z, from);
+                v.w = __shfl_sync(0xFFFFFFFFu, mine.w, from);
+            }
+            if constexpr (V == 8) {
+                const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    h[2 * q] = word[q] << 16;
+                    h[2 * q + 1] = word[q];
+                }
+            } else {
+                const uint32_t low = (at & 4) ? v.z : v.x, high = (at & 4) ? v.w : v.y;
+                if constexpr (V == 4) {
+                    h[0] = low << 16;
+                    h[1] = low;
+                    h[2] = high << 16;
+                    h[3] = high;
+                } else {
+                    const uint32_t word = (at & 2) ? high : low;
+                    if constexpr (V == 2) {
+                        h[0] = word << 16;
+                        h[1] = word;
+                    } else {
+                        h[c] = (at & 1) ? word : word << 16;
+                    }
+                }
             }
         }
     }
@@ -394,6 +422,8 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
         if (a.gate_kind == 1 && here) row_gate *= widen(*(const T*)row_of(a.gate, r, sizeof(T)));
         if (dropping) row_gate *= a.drop.scale;
         char* out = row_of(a.out, r, sizeof(T));
+        typename R::Draws words;
+        if (dropping) ring.draw(words, a.drop, offset, r);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (post) {
@@ -405,7 +435,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
             }
             if (dropping) {
                 uint32_t draws[2 * P];
-                ring.draws(draws, a.drop, offset, r, u);
+                ring.draws(draws, words, u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) v[u][q] = kept_of(v[u][q], draws + 2 * q, a.drop.limit);
             }
@@ -522,7 +552,8 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
             gate_sum = block_sum(gate_sum, scratch);
             if (threadIdx.x == 0) ((T*)a.grad_gate.p)[r * a.grad_gate.ld] = narrow<T>(gate_sum);
         }
-        const int64_t in_gate = r % args.chunks.gate_rows;
+        const int64_t in_gate = r % a.gate_rows;
+        const bool whole_gates = a.gate_rows == 1 || args.chunks.per_gate == 0;
         for (int64_t c = threadIdx.x; c < a.d; c += kJoinThreads) {
             const float t = total(c), f = drop_factor(a.drop, offset, r, c);
             const float n = (widen(x[c]) - mean1) * rstd1;
@@ -536,8 +567,7 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
                 float v = dropped(n * w, f) * (a.scale * t);
                 if (r != r0 && in_gate != 0) v += part_gate[c];
                 part_gate[c] = v;
-                if (args.chunks.per_gate == 0 && in_gate == args.chunks.gate_rows - 1)
-                    ((T*)a.grad_gate.p)[r / args.chunks.gate_rows * a.grad_gate.ld + c] = narrow<T>(v);
+                if (whole_gates && in_gate == a.gate_rows - 1) ((T*)a.grad_gate.p)[r / a.gate_rows * a.grad_gate.ld + c] = narrow<T>(v);
             }
             float gx = u;
             if (a.w_post != nullptr) {
@@ -719,6 +749,8 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         const float2 scale = both(dropping ? a.scale * a.drop.scale : a.scale);
         char* grad_residual = row_of(a.grad_residual, r, sizeof(T));
         float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
+        typename R::Draws words;
+        if (dropping) ring.draw(words, a.drop, offset, r);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             R::read(x[u], stage, kX, u);
@@ -727,7 +759,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
             float2 w[P];
             if (post) ring.weights(w, a.w_post, u);
             uint32_t draws[2 * P];
-            if (dropping) ring.draws(draws, a.drop, offset, r, u);
+            if (dropping) ring.draws(draws, words, u);
             float2 g[P], gg[P];
             if (vector) R::read(g, stage, kGate, u);
 #pragma unroll
@@ -819,33 +851,51 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     if (shared_gate && !whole_gates && a.grad_gate.p != nullptr) store_sums(sum_gate, args.part_gate);
 }
 
-// Columns of [parts][d] summed: blockIdx.y = 0 the weights after the block, 1 those before the next, 2.. gate vectors.
-constexpr int kColumnLanes = 32, kColumnRows = 16;
+// Columns of [parts][d] summed: first the weights after the block, those before the next, then the gate vectors.  A CTA
+// has kColumnThreads / share columns of one of them, `share` threads a column: 16, or 2 for gate vectors of few parts.
+constexpr int kColumnThreads = 512, kColumnBatch = 8;
+
+struct ColumnArgs {
+    JoinGradArgs j;
+    uint32_t weights, weight_tiles;  // sums of weights, CTAs of each
+    int gate_share;
+    uint32_t gate_tiles;
+};
 
 template <class T>
-__global__ void __launch_bounds__(kColumnLanes* kColumnRows) residual_columns_kernel(JoinGradArgs args) {
-    __shared__ double sums[kColumnRows][kColumnLanes];
+__global__ void __launch_bounds__(kColumnThreads) residual_columns_kernel(ColumnArgs args) {
+    __shared__ double sums[kColumnThreads];
     follow();
-    const ResidualProblem& a = args.p;
-    const int lane = threadIdx.x % kColumnLanes, row = threadIdx.x / kColumnLanes;
-    const uint32_t tiles = (uint32_t)((a.d + kColumnLanes - 1) / kColumnLanes);
-    const uint32_t what = blockIdx.x / tiles;
-    const int64_t c = (int64_t)(blockIdx.x % tiles) * kColumnLanes + lane;
-    const int weights = (a.w_post != nullptr) + (a.w_pre != nullptr);
+    const ResidualProblem& a = args.j.p;
+    const uint32_t ahead = args.weights * args.weight_tiles;
+    const bool gate = blockIdx.x >= ahead;
+    const uint32_t block = gate ? blockIdx.x - ahead : blockIdx.x, tiles = gate ? args.gate_tiles : args.weight_tiles;
+    const int share = gate ? args.gate_share : 16, columns = kColumnThreads / share;
+    const uint32_t what = block / tiles;
+    const int lane = threadIdx.x & (columns - 1), row = threadIdx.x / columns;
+    const int64_t c = (int64_t)(block - what * tiles) * columns + lane;
     const bool post = what == 0 && a.w_post != nullptr;
-    const bool gate = (int)what >= weights;
-    const int64_t first = gate ? (what - weights) * args.chunks.per_gate : 0;
-    const int64_t count = gate ? args.chunks.per_gate : args.chunks.count;
-    const float* part = (gate ? args.part_gate : post ? args.part_post : args.part_pre) + first * a.d;
+    const int64_t first = gate ? what * args.j.chunks.per_gate : 0;
+    const int count = (int)(gate ? args.j.chunks.per_gate : args.j.chunks.count);
+    const float* part = (gate ? args.j.part_gate : post ? args.j.part_post : args.j.part_pre) + first * a.d + c;
     double s = 0.0;
     if (c < a.d)
-        for (int64_t k = row; k < count; k += kColumnRows) s += (double)__ldcs(part + k * a.d + c);
-    sums[row][lane] = s;
+        for (int k = row; k < count; k += share * kColumnBatch) {
+            float v[kColumnBatch];
+#pragma unroll
+            for (int q = 0; q < kColumnBatch; ++q) {
+                const int at = k + q * share;
+                v[q] = at < count ? __ldcs(part + at * a.d) : 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < kColumnBatch; ++q) s += (double)v[q];
+        }
+    sums[threadIdx.x] = s;
     __syncthreads();
     if (row != 0 || c >= a.d) return;
     s = 0.0;
-    for (int k = 0; k < kColumnRows; ++k) s += sums[k][lane];
-    if (gate) ((T*)a.grad_gate.p)[(what - weights) * a.grad_gate.ld + c] = narrow<T>((float)s);
+    for (int k = 0; k < share; ++k) s += sums[k * columns + lane];
+    if (gate) ((T*)a.grad_gate.p)[(int64_t)what * a.grad_gate.ld + c] = narrow<T>((float)s);
     else (post ? a.grad_w_post : a.grad_w_pre)[c] = (float)s;
 }
 
@@ -857,16 +907,29 @@ int64_t resident_chunks(int64_t d, bool gates) {
     return 148 * (threads >= 512 ? 1 : 512 / threads);
 }
 
-Chunks chunks_of(int64_t rows, int64_t d, int64_t gates) {
-    const int64_t most = resident_chunks(d, gates > 0);
+// Rows of a CTA at a time.
+int64_t groups_of(int64_t d) {
+    if (d > 32 * kGradWarpElems) return 1;
+    int64_t lanes = 1;
+    while (lanes * kGradWarpElems < d) lanes *= 2;
+    return kWarpRowThreads / lanes;
+}
+
+// gates: gate vectors of more than one row that the rows share, or 0; vector: there is a gate of d columns at all.  The
+// workspace is sized by the same call.
+Chunks chunks_of(int64_t rows, int64_t d, int64_t gates, bool vector) {
+    const int64_t most = resident_chunks(d, vector);
     Chunks k;
     k.rows = rows;
     k.gate_rows = gates > 0 ? rows / gates : rows;
     k.per_gate = k.gates = k.length = k.count = 0;
     if (rows == 0) return k;
-    if (gates <= most && (gates == 0 || k.gate_rows > 1)) {
-        k.per_gate = gates > 0 ? most / gates : most;
+    // whole gate vectors, each by one of a CTA's groups, where there are enough for half of the groups; else a CTA's groups
+    // share one vector's rows (608 vectors of 660 rows of 136: 947 us the first way)
+    if (gates == 0 || 2 * gates < most * groups_of(d)) {
+        k.per_gate = gates == 0 ? most : gates < most ? most / gates : 1;
         k.length = (k.gate_rows + k.per_gate - 1) / k.per_gate;
+        if (k.length < groups_of(d)) k.length = groups_of(d);  // (a row for each of a CTA's groups)
         k.per_gate = (k.gate_rows + k.length - 1) / k.length;
         k.count = (gates > 0 ? gates : 1) * k.per_gate;
     } else {
@@ -881,13 +944,14 @@ Chunks chunks_of(int64_t rows, int64_t d, int64_t gates) {
 
 namespace {
 
-// How a call's rows are cut: V elements an access (16 bytes where every row and length allows, else 4, else one element).
+// How a call's rows are cut: accesses of 16, 8 or 4 bytes, as every row and length allows, or of one element.
 struct RowPlan {
     int vec;    // elements of a piece
     bool cta;   // a row is a CTA's
+    int elems;  // of a thread
     int lanes;  // threads of a row; 0: too long or too far apart, the kernels that read rows again
 };
-RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tensors, int size, int warp_elems, int cta_elems) {
+RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tensors, int size, int warp_elems) {
     uintptr_t bits = (uintptr_t)(pb.d * size);
     bool wide = pb.rows >= (1ll << 30);  // (row numbers are 32 bits, and go past the end)
     for (const RowsRef& t : {pb.gate, pb.grad_gate}) wide = wide || (t.p != nullptr && t.ld * size >= (1ll << 32));
@@ -900,16 +964,20 @@ RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tenso
     uintptr_t weights = 0;
     for (const float* w : {pb.w_post, pb.w_pre}) weights |= (uintptr_t)w;
     RowPlan p;
-    p.vec = (bits & 15) == 0 && (weights & 15) == 0 ? 16 / size : (bits & 3) == 0 ? 4 / size : 1;
+    const bool w16 = (weights & 15) == 0;
+    p.vec = (bits & 15) == 0 && w16 ? 16 / size : (bits & 7) == 0 && (size == 4 || w16) ? 8 / size : (bits & 3) == 0 ? 4 / size : 1;
+    // smaller pieces make longer code of as many elements: half of them where that is enough threads
+    const bool few = p.vec * size < 16 && pb.d <= 8 * kMaxLanes;
+    if (few) warp_elems = 8;
     p.cta = pb.d > 32 * warp_elems;
-    const int64_t per = p.cta ? cta_elems : warp_elems;
-    if (pb.d > per * kMaxLanes || wide) {
+    p.elems = p.cta ? (few ? 8 : kRowElems) : warp_elems;
+    if (pb.d > p.elems * kMaxLanes || wide) {
         p.lanes = 0;
     } else if (p.cta) {
-        p.lanes = (int)((pb.d + per - 1) / per + 31) / 32 * 32;
+        p.lanes = (int)((pb.d + p.elems - 1) / p.elems + 31) / 32 * 32;
     } else {
-        p.lanes = 1;
-        while (p.lanes < 32 && p.lanes * per < pb.d) p.lanes *= 2;
+        p.lanes = p.vec < 8 ? 8 / p.vec : 1;  // (what shares an evaluation of the dropout's generator)
+        while (p.lanes * p.elems < pb.d) p.lanes *= 2;
     }
     return p;
 }
@@ -929,9 +997,8 @@ cudaError_t allow_shared(K kernel, size_t smem) {
                 : ((pb).drop.none ? ((pb).gate_kind == 2 ? name<T, V, E, CTA, true, 0, 0, 1> : name<T, V, E, CTA, true, 0, 0, 0>)   \
                                   : ((pb).gate_kind == 2 ? name<T, V, E, CTA, true, 0, 1, 1> : name<T, V, E, CTA, true, 0, 1, 0>)))
 
-template <class T, int V, bool CTA>
+template <class T, int V, int E, bool CTA>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
-    constexpr int E = kRowElems;
     const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.residual.p != nullptr;
     const int threads = CTA ? p.lanes : kWarpRowThreads;
     void (*kernel)(ResidualProblem, int, int) = residual_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
@@ -959,17 +1026,23 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
 }
 template <class T, int V>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
-    return p.cta ? launch_forward_rows<T, V, true>(pb, p, st) : launch_forward_rows<T, V, false>(pb, p, st);
+    constexpr int kSmall = V * sizeof(T) < 16 ? 8 : kRowElems;
+    if (!p.cta) return p.elems == 8 ? launch_forward_rows<T, V, kSmall, false>(pb, p, st) : launch_forward_rows<T, V, kRowElems, false>(pb, p, st);
+    return p.elems == 8 ? launch_forward_rows<T, V, kSmall, true>(pb, p, st) : launch_forward_rows<T, V, kRowElems, true>(pb, p, st);
 }
 
 }  // namespace
 
 cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaStream_t st) {
     const RowPlan p = row_plan(pb, {pb.x, pb.residual, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.out, pb.normed},
-                               dtype == 0 ? 4 : 2, kRowElems, kRowElems);
+                               dtype == 0 ? 4 : 2, kRowElems);
     if (p.lanes > 0) {
-        if (dtype == 0) return p.vec == 4 ? launch_forward_rows<float, 4>(pb, p, st) : launch_forward_rows<float, 1>(pb, p, st);
+        if (dtype == 0)
+            return p.vec == 4   ? launch_forward_rows<float, 4>(pb, p, st)
+                   : p.vec == 2 ? launch_forward_rows<float, 2>(pb, p, st)
+                                : launch_forward_rows<float, 1>(pb, p, st);
         return p.vec == 8   ? launch_forward_rows<__nv_bfloat16, 8>(pb, p, st)
+               : p.vec == 4 ? launch_forward_rows<__nv_bfloat16, 4>(pb, p, st)
                : p.vec == 2 ? launch_forward_rows<__nv_bfloat16, 2>(pb, p, st)
                             : launch_forward_rows<__nv_bfloat16, 1>(pb, p, st);
     }
@@ -981,18 +1054,20 @@ cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaSt
 
 size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates) {
     if (rows <= 0 || d <= 0) return 0;
-    (void)gates;  // (gate vectors are cut into no more chunks)
-    const int64_t most = resident_chunks(d, false);
-    const unsigned __int128 bytes = (unsigned __int128)(rows < most ? rows : most) * d * sizeof(float) * 3;
+    int64_t count = 0;  // (enough for a gate per row, per element, or none alike)
+    for (const bool vector : {false, true}) {
+        const int64_t n = chunks_of(rows, d, gates < rows ? gates : 0, vector).count;
+        if (n > count) count = n;
+    }
+    const unsigned __int128 bytes = (unsigned __int128)count * d * sizeof(float) * 3;
     if (bytes >= ((unsigned __int128)1 << 62)) return (size_t)1 << 62;
     return ((size_t)bytes + 255) / 256 * 256;
 }
 
 namespace {
 
-template <class T, int V, bool CTA>
+template <class T, int V, int E, bool CTA>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
-    constexpr int E = CTA ? kRowElems : kGradWarpElems;
     const ResidualProblem& pb = a.p;
     // the call of a training step, 16-byte pieces: both norms, both gradients, nothing left to ask in the row loop
     const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.grad_out.p != nullptr &&
@@ -1020,7 +1095,9 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
 }
 template <class T, int V>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
-    return p.cta ? launch_backward_rows<T, V, true>(a, p, st) : launch_backward_rows<T, V, false>(a, p, st);
+    constexpr int kSmall = V * sizeof(T) < 16 ? 8 : kRowElems;
+    if (!p.cta) return launch_backward_rows<T, V, kGradWarpElems, false>(a, p, st);
+    return p.elems == 8 ? launch_backward_rows<T, V, kSmall, true>(a, p, st) : launch_backward_rows<T, V, kRowElems, true>(a, p, st);
 }
 
 }  // namespace
@@ -1028,20 +1105,23 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
 cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void* workspace, cudaStream_t st) {
     JoinGradArgs a;
     a.p = pb;
-    a.chunks = chunks_of(pb.rows, pb.d, pb.gate_kind == 2 ? pb.rows / pb.gate_rows : 0);
+    a.chunks = chunks_of(pb.rows, pb.d, pb.gate_kind == 2 && pb.gate_rows > 1 ? pb.rows / pb.gate_rows : 0, pb.gate_kind == 2);
     a.part_post = (float*)workspace;
     a.part_pre = a.part_post + a.chunks.count * pb.d;
     a.part_gate = a.part_pre + a.chunks.count * pb.d;
     cudaError_t e = cudaSuccess;
     const RowPlan p = row_plan(pb, {pb.x, pb.grad_out, pb.out, pb.grad_normed, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.grad_x,
                                     pb.grad_residual, pb.gate_kind == 2 ? pb.grad_gate : RowsRef{}},
-                               dtype == 0 ? 4 : 2, kGradWarpElems, kRowElems);
+                               dtype == 0 ? 4 : 2, kGradWarpElems);
     if (a.chunks.count == 0) {
     } else if (p.lanes > 0) {
         if (dtype == 0)
-            e = p.vec == 4 ? launch_backward_rows<float, 4>(a, p, st) : launch_backward_rows<float, 1>(a, p, st);
+            e = p.vec == 4   ? launch_backward_rows<float, 4>(a, p, st)
+                : p.vec == 2 ? launch_backward_rows<float, 2>(a, p, st)
+                             : launch_backward_rows<float, 1>(a, p, st);
         else
             e = p.vec == 8   ? launch_backward_rows<__nv_bfloat16, 8>(a, p, st)
+                : p.vec == 4 ? launch_backward_rows<__nv_bfloat16, 4>(a, p, st)
                 : p.vec == 2 ? launch_backward_rows<__nv_bfloat16, 2>(a, p, st)
                              : launch_backward_rows<__nv_bfloat16, 1>(a, p, st);
     } else if (dtype == 0) {
@@ -1050,12 +1130,18 @@ cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void*
         launch_next(residual_grad_any_kernel<__nv_bfloat16>, (unsigned)a.chunks.count, kJoinThreads, 0, st, a);
     }
     if (e != cudaSuccess) return e;
-    const int64_t tiles = (pb.d + kColumnLanes - 1) / kColumnLanes;
-    int64_t sums = (pb.w_post != nullptr) + (pb.w_pre != nullptr);
-    if (pb.gate_kind == 2 && pb.grad_gate.p != nullptr && a.chunks.per_gate > 0) sums += pb.rows / pb.gate_rows;
-    if (sums > 0) {
-        if (dtype == 0) launch_next(residual_columns_kernel<float>, (unsigned)(tiles * sums), kColumnLanes * kColumnRows, 0, st, a);
-        else launch_next(residual_columns_kernel<__nv_bfloat16>, (unsigned)(tiles * sums), kColumnLanes * kColumnRows, 0, st, a);
+    ColumnArgs c;
+    c.j = a;
+    c.weights = (pb.w_post != nullptr) + (pb.w_pre != nullptr);
+    c.weight_tiles = (uint32_t)((pb.d + kColumnThreads / 16 - 1) / (kColumnThreads / 16));
+    c.gate_share = a.chunks.per_gate > 64 ? 16 : 2;
+    c.gate_tiles = (uint32_t)((pb.d + kColumnThreads / c.gate_share - 1) / (kColumnThreads / c.gate_share));
+    int64_t grid = (int64_t)c.weights * c.weight_tiles;
+    if (pb.gate_kind == 2 && pb.gate_rows > 1 && pb.grad_gate.p != nullptr && a.chunks.per_gate > 0)
+        grid += pb.rows / pb.gate_rows * c.gate_tiles;
+    if (grid > 0) {
+        if (dtype == 0) launch_next(residual_columns_kernel<float>, (unsigned)grid, kColumnThreads, 0, st, c);
+        else launch_next(residual_columns_kernel<__nv_bfloat16>, (unsigned)grid, kColumnThreads, 0, st, c);
     }
     return cudaGetLastError();
 }

@@ -50,6 +50,18 @@ def same_bits(a, b):
     return torch.equal(a.contiguous().view(kind), b.contiguous().view(kind))
 
 
+class Workspace:
+    """A workspace of the size asked for, full of old bytes, with others behind it that must stay."""
+
+    def __init__(self, size):
+        self.all = torch.full((size + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda")
+        self.size = size
+        self.own = self.all[:size]
+
+    def kept_within(self):
+        return bool((self.all[self.size:] == 0xA5).all())
+
+
 # ---------------------------------------------------------------- dropout
 
 
@@ -192,9 +204,10 @@ def test_bias_backward(N, H, q, k, start, dtype, causal):
         bits = None
         for how in ("plain", "slice", "odd"):
             got = blank((buckets[0], H), torch.float32, how)
-            ws = torch.full((robe.robe_bias_backward_workspace_bytes(b, H, N, q, k),), 0xA5, dtype=torch.uint8, device="cuda")
+            ws = Workspace(robe.robe_bias_backward_workspace_bytes(b, H, N, q, k))
             placed = place(g.reshape(N * H * q, k), how).unflatten(0, (N, H, q))
-            robe.robe_bias_backward(b, placed, got, ws, start, causal)
+            robe.robe_bias_backward(b, placed, got, ws.own, start, causal)
+            assert ws.kept_within()
             ref.assert_within(got, want, bound, (buckets, how))
             assert surroundings_kept(got)
             bits = got.cpu() if bits is None else bits
@@ -270,7 +283,10 @@ JOINS = [  # rows, d, gate, post, pre, residual, p
     (3, 4097, 1, True, True, True, 0.1), (4, 8192, 4, True, True, True, 0.1), (2, 12_000, "none", True, True, True, 0.1),
     (2, 20_001, 1, True, True, True, 0.1), (3, 40_000, "row", True, True, True, 0.0), (700, 24, 1, True, True, True, 0.1),
     (1500, 40, 750, True, True, True, 0.1), (1201, 12, "none", True, True, True, 0.0), (640, 128, 2, True, True, True, 0.1),
-    (5, 3, "none", True, True, True, 0.0), (1400, 96, 1400, True, True, True, 0.0), (64, 36, 32, True, False, True, 1.0)]
+    (5, 3, "none", True, True, True, 0.0), (1400, 96, 1400, True, True, True, 0.0), (64, 36, 32, True, False, True, 1.0),
+    (900, 47, "row", True, True, True, 0.1), (6080, 24, 10, True, True, True, 0.1), (12_000, 8, 2, True, True, True, 0.0),
+    (3200, 300, 100, True, True, True, 0.1), (1200, 520, 3, True, True, True, 0.1), (300, 909, "none", True, True, True, 0.1),
+    (40, 4100, 5, True, True, True, 0.1), (9, 8191, 1, True, True, True, 0.1), (20_000, 5, 1, True, True, True, 0.2)]
 
 
 @pytest.mark.parametrize("layer", [0, 1])
@@ -312,10 +328,11 @@ def test_residual_backward(rows, d, gate, post, pre, residual, p, dtype, layer):
         got = {"x": blank((rows, d), dtype, how), "residual": blank((rows, d), dtype, how) if residual else None,
                "gate": blank(tuple(t["gate"].shape), dtype, how) if t["gate"] is not None else None,
                "w_post": blank((d,), torch.float32) if post else None, "w_pre": blank((d,), torch.float32) if pre else None}
-        ws = torch.full((robe.robe_residual_backward_workspace_bytes(rows, d, gates),), 0xA5, dtype=torch.uint8, device="cuda")
+        ws = Workspace(robe.robe_residual_backward_workspace_bytes(rows, d, gates))
         robe.robe_residual_backward(place(go, how), place(gn, how), place(t["x"], how), place(out, how), got["x"], got["residual"],
                                     vec(t["w_post"]), vec(t["w_pre"]), place(t["gate"], how), got["w_post"], got["w_pre"],
-                                    got["gate"], ws, 0.7, layer, 1e-5, p, 21, 34)
+                                    got["gate"], ws.own, 0.7, layer, 1e-5, p, 21, 34)
+        assert ws.kept_within()
         for name, v in got.items():
             if v is not None:
                 value, bound = want[name]
@@ -325,7 +342,7 @@ def test_residual_backward(rows, d, gate, post, pre, residual, p, dtype, layer):
             again = {k: None if v is None else torch.empty_like(v) for k, v in got.items()}
             robe.robe_residual_backward(place(go, how), place(gn, how), place(t["x"], how), place(out, how), again["x"],
                                         again["residual"], vec(t["w_post"]), vec(t["w_pre"]), place(t["gate"], how),
-                                        again["w_post"], again["w_pre"], again["gate"], ws, 0.7, layer, 1e-5, p, 21, 34)
+                                        again["w_post"], again["w_pre"], again["gate"], ws.own, 0.7, layer, 1e-5, p, 21, 34)
             bits = all(v is None or same_bits(v, again[k]) for k, v in got.items())
             assert bits
 
