@@ -83,9 +83,9 @@ __global__ void __launch_bounds__(kBiasThreads) bias_few_kernel(BiasArgs a) {
     constexpr int V = kPiece<T>;
     __shared__ HeadValues values;
     follow();
-    const uint32_t kt = blockIdx.x % a.k_tiles;
-    const uint32_t line = blockIdx.x / a.k_tiles;  // (n, h, i)
-    const uint32_t nh = line / (uint32_t)a.q_len;
+    const uint32_t line = a.k_tiles == 1 ? blockIdx.x : blockIdx.x / a.k_tiles;  // (n, h, i)
+    const uint32_t kt = blockIdx.x - line * a.k_tiles;
+    const uint32_t nh = a.q_len == 1 ? line : line / (uint32_t)a.q_len;
     const uint32_t i = line - nh * (uint32_t)a.q_len;
     const uint32_t n = nh / a.heads, h = nh - n * a.heads;
     const int64_t start = start_of(a.q_start, a.q_starts, n);
@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(kBiasThreads) bias_few_kernel(BiasArgs a) {
             for (int k = 0; k < V; ++k) e.v[k] = narrow<T>(values.at(r + k, a));
         }
         if (j >= begin && j + V <= end) {
+            if (!ROBE_CHK(j0 + j >= 0 && j0 + j + V <= a.k_len, ROBE_DBG_ROW_POS)) break;
             store_pack<true, T, V>(row + j, e);
         } else {
 #pragma unroll
@@ -182,6 +183,7 @@ __global__ void __launch_bounds__(kBiasThreads, 8) bias_forward_kernel(BiasArgs 
         for (int g = from; g < to; g += lanes) {
             if (!ROBE_CHK(V + (x & ~(V - 1)) + g * V + V <= U * V, ROBE_DBG_SHARED)) break;
             if (mixed) e = *(const Pack<T, V>*)(window + g * V);
+            if (!ROBE_CHK(g * V >= lead && j0 + g * V - lead + V <= a.k_len, ROBE_DBG_ROW_POS)) break;
             store_pack<true, T, V>(row + g * V, e);
         }
         if (lane == lanes - 1 && to * V < columns + lead && (to > 0 || lead == 0)) {  // the last elements, of no whole piece
@@ -329,6 +331,7 @@ __global__ void __launch_bounds__(kGradMaxThreads, 3) bias_grad_kernel(BiasGradA
                     const char* from = row + (int64_t)g * 16;
 #pragma unroll
                     for (int s = 0; s < V; ++s) {
+                        if (!ROBE_CHK(((uintptr_t)from & ~(uintptr_t)15) >= (uintptr_t)begin && ((uintptr_t)from & ~(uintptr_t)15) + 16 <= (uintptr_t)end, ROBE_DBG_GRAD_POS)) break;
                         copy_async<16>(to + s * kRow, ALIGNED ? from : (const char*)((uintptr_t)from & ~(uintptr_t)15));
                         from += step;
                     }
@@ -336,7 +339,8 @@ __global__ void __launch_bounds__(kGradMaxThreads, 3) bias_grad_kernel(BiasGradA
                 const int last = rb + delta0 + 32;
                 if (!ALIGNED && lane < V && last > 0 && last <= col_groups) {  // the piece behind the last lane's, a row a lane
                     const char* from = row + lane * step + (int64_t)last * 16;
-                    copy_async<16>(to - lane + lane * kRow + 32, (const char*)((uintptr_t)from & ~(uintptr_t)15));
+                    if (ROBE_CHK(((uintptr_t)from & ~(uintptr_t)15) >= (uintptr_t)begin && ((uintptr_t)from & ~(uintptr_t)15) + 16 <= (uintptr_t)end, ROBE_DBG_GRAD_POS))
+                        copy_async<16>(to - lane + lane * kRow + 32, (const char*)((uintptr_t)from & ~(uintptr_t)15));
                 }
             } else if (rb < hi && copied) {
                 const int rows = a.q_len - (int64_t)rb * V < V ? (int)(a.q_len - (int64_t)rb * V) : V;
@@ -400,6 +404,7 @@ __global__ void __launch_bounds__(kGradMaxThreads, 3) bias_grad_kernel(BiasGradA
     float* lower = upper + a.lanes * V;
     if (threadIdx.x < a.lanes) {
         const int at = threadIdx.x * V;
+        static_assert(2 * V * sizeof(float) <= kGradStages * V * sizeof(uint4), "the sums fit the pieces' memory");
 #pragma unroll
         for (int k = 0; k < V; ++k) upper[at + k] = sum[V - 1 + k];
         lower[at] = 0.0f;
@@ -432,7 +437,7 @@ __global__ void __launch_bounds__(kGradMaxThreads, 3) bias_grad_kernel(BiasGradA
 #pragma unroll
                 for (int s = kShare / 2; s > 0; s >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, s);
             }
-            if (lane % kShare == 0 && q < a.bk.buckets) a.partial[((uint64_t)h * a.bk.buckets + q) * parts + part] = total;
+            if (lane % kShare == 0 && q < a.bk.buckets && ROBE_CHK(part < parts && h < a.heads, ROBE_DBG_ROW_POS)) a.partial[((uint64_t)h * a.bk.buckets + q) * parts + part] = total;
         }
     };
     if (span > 1024) join(std::integral_constant<uint32_t, 32>());

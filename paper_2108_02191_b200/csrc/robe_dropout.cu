@@ -65,6 +65,7 @@ __global__ void __launch_bounds__(kDropThreads, 6) dropout_kernel(DropArgs a) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         if (t0 + i * kDropThreads >= a.items) return;
+        if (!ROBE_CHK(group[i] < a.groups && (uint64_t)row[i] * a.groups + group[i] < a.items, ROBE_DBG_ROW_POS)) return;
         const uint4 w = drop_words(a.row0 + row[i], group[i], offset, a.drop);
         if (PIECES) {
             drop_eight(e[i], w, a.drop);
@@ -136,6 +137,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(DropArgs a, 
         if (g + 1 == a.groups) keep &= (1u << a.tail) - 1;
         const uint32_t first = at < 0 ? keep >> -at : keep << (at & 31);
         const int word = at < 0 ? 0 : (int)(at >> 5);
+        if (!ROBE_CHK(at > -8 && g < a.groups && word + 1 < kTile / 32 + 1, ROBE_DBG_SHARED)) break;
         if (first != 0) atomicOr(&bits[word], first);
         if (at > 0 && (at & 31) > 24) atomicOr(&bits[word + 1], keep >> (32 - (at & 31)));
     }

@@ -178,7 +178,7 @@ struct Ring {
     __device__ __forceinline__ void fetch(char* stage, int tensor, const char* row) const {
 #pragma unroll
         for (int k = 0; k < NP; ++k)
-            if (has(k)) copy_async<kSlot>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
+            if (has(k) && ROBE_CHK(col(k) + V <= d, ROBE_DBG_ROW_POS)) copy_async<kSlot>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
     }
     static __device__ __forceinline__ void zero(char* stage, int tensor) {
 #pragma unroll
@@ -207,7 +207,7 @@ struct Ring {
         if constexpr (V == 1) {
             if (has(2 * u)) ((T*)row)[col(2 * u)] = narrow<T>(v[0].x);
             if (has(2 * u + 1)) ((T*)row)[col(2 * u + 1)] = narrow<T>(v[0].y);
-        } else if (has(u)) {
+        } else if (has(u) && ROBE_CHK(col(u) + V <= d, ROBE_DBG_ROW_POS)) {
             using W = typename Word<V * sizeof(T)>::type;
             union {
                 W w;
@@ -367,6 +367,7 @@ residual_rows_kernel(ResidualProblem a, int lanes, int stages) {
     auto fetch = [&](char* stage) {
         if (next < rows) {
             const uint32_t r = (uint32_t)next;
+            if (!ROBE_CHK(!vector || gate.gate == r / a.gate_rows, ROBE_DBG_ROW_POS)) return;
             ring.fetch(stage, 0, row_of(a.x, r, sizeof(T)));
             if (added) ring.fetch(stage, 1, row_of(a.residual, r, sizeof(T)));
             if (vector) {
@@ -639,6 +640,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     auto fetch = [&](char* stage) {
         if (next.r < c1) {
             const uint32_t r = next.r;
+            if (!ROBE_CHK(r >= c0 && r < a.rows && (!shared_gate || next.gate == r / a.gate_rows), ROBE_DBG_ROW_POS)) return;
             ring.fetch(stage, kX, row_of(a.x, r, sizeof(T)));
             if (skip) ring.fetch(stage, kSkip, row_of(a.grad_out, r, sizeof(T)));
             if (pre) {
@@ -824,6 +826,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     copies_wait(0);
     // the chunk's sums
     auto store_sums = [&](const float2 (&v)[U][P], float* part) {
+        if (!ROBE_CHK(blockIdx.x < args.chunks.count, ROBE_DBG_ROW_POS)) return;
         part += blockIdx.x * a.d;
         float* to = part;
         if (!CTA) {
