@@ -394,6 +394,15 @@ def _vector(t, what, n, dtype=torch.float32):
     return t.data_ptr()
 
 
+def _workspace(t):
+    """(pointer, bytes)"""
+    if t is None:
+        return None, 0
+    if not _here(t, "workspace").is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _step_ptr(step):
     if step is None:
         return None
@@ -478,9 +487,8 @@ def robe_bias_backward(b, grad, grad_rows, workspace, q_start=0, causal: bool = 
     p, ld, n, h, q, k = _bias_matrix(grad, "grad")
     table, table_ld = _matrix_like(grad_rows, "grad_rows", torch.float32, robe_bias_num_buckets(b), h)
     start, starts = _starts(q_start, n)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.robe_bias_backward(b, p, ld, h, n, q, k, start, starts, 1 if causal else 0, _TYPES[grad.dtype], table,
-                                   table_ld, _dev_ptr(workspace), ws_bytes, _stream_ptr(stream)), "robe_bias_backward")
+                                   table_ld, *_workspace(workspace), _stream_ptr(stream)), "robe_bias_backward")
 
 
 def _residual(x, gate, scale, norm, eps, p, seed, offset, step):
@@ -537,12 +545,11 @@ def robe_residual_backward(grad_out, grad_normed, x, out, grad_x, grad_residual=
     like = lambda t, what: _matrix_like(t, what, x.dtype, c.rows, c.d)
     if grad_gate is not None and gate is None:
         raise ValueError("grad_gate: there is no gate")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.robe_residual_backward(
         C.byref(c), *like(grad_out, "grad_out"), *like(grad_normed, "grad_normed"), *x_at, *like(out, "out"), *gate_at,
         _vector(w_post, "w_post", c.d), _vector(w_pre, "w_pre", c.d), *like(grad_x, "grad_x"),
         *like(grad_residual, "grad_residual"), *_matrix_like(grad_gate, "grad_gate", x.dtype, *gate_size),
-        _vector(grad_w_post, "grad_w_post", c.d), _vector(grad_w_pre, "grad_w_pre", c.d), _dev_ptr(workspace), ws_bytes,
+        _vector(grad_w_post, "grad_w_post", c.d), _vector(grad_w_pre, "grad_w_pre", c.d), *_workspace(workspace),
         _stream_ptr(stream)), "robe_residual_backward")
 
 

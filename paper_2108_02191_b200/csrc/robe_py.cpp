@@ -186,6 +186,17 @@ struct Reader {
         }
         return (const uint64_t*)t->data_ptr();
     }
+    void* workspace(int k, size_t& n) {
+        n = 0;
+        if (args[k] == Py_None) return nullptr;
+        const at::Tensor* t = local(k);
+        if (t == nullptr || !t->is_contiguous()) {
+            ok = false;
+            return nullptr;
+        }
+        n = (size_t)t->numel() * t->element_size();
+        return t->data_ptr();
+    }
     robe_bias_t bias(int k) { return (robe_bias_t)pointer_in(k, bias_handle_type); }
     robe_handle_t handle(int k) { return (robe_handle_t)pointer_in(k, handle_type); }
     // a ctypes object of that type and nothing else that has a buffer: its buffer is the pointer
@@ -332,7 +343,7 @@ PyObject* backward_adam(PyObject*, PyObject* const* args, Py_ssize_t n) {
     float* m2 = (float*)r.data_or_null(6, at::kFloat);
     const float lr = r.number(7), beta1 = r.number(8), beta2 = r.number(9), eps = r.number(10);
     const int64_t step = r.whole(11);
-    void* ws = r.bytes_or_null(12, ws_bytes);
+    void* ws = r.workspace(12, ws_bytes);
     void* st = r.stream(13);
     if (!r.ok) return not_taken();
     return made([&] {
@@ -437,7 +448,7 @@ PyObject* bias_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Reader r{args};
     size_t ws_bytes = 0;
     const Bias a(r, 1, 2, 4);
-    void* ws = r.bytes_or_null(3, ws_bytes);
+    void* ws = r.workspace(3, ws_bytes);
     const int causal = r.truth(5);
     void* st = r.stream(6);
     if (!r.ok) return not_taken();
@@ -510,7 +521,7 @@ PyObject* residual_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (!gated && args[11] != Py_None) r.ok = false;
     const Matrix grad_gate = gated ? r.matrix_like(11, gate) : Matrix();
     size_t ws_bytes = 0;
-    void* ws = r.bytes_or_null(12, ws_bytes);
+    void* ws = r.workspace(12, ws_bytes);
     const robe_residual_t c = residual(r, 13, x, gate, gated);
     void* st = r.stream(20);
     if (!r.ok) return not_taken();
