@@ -14,8 +14,6 @@ namespace robe {
 
 namespace {
 
-constexpr int kJoinThreads = 256;
-
 // Sum over the CTA's threads, in every thread.
 __device__ __forceinline__ float block_sum(float v, float* scratch) {
 #pragma unroll
@@ -28,42 +26,99 @@ __device__ __forceinline__ float block_sum(float v, float* scratch) {
     return sum;
 }
 
-// ---- rows of any length, one CTA each, read again in every pass over the row: for rows too long for the kernels below
+// ---- rows of any length, one CTA each, read again in every pass over the row: for rows too long for the kernels below.  A
+// thread takes eight columns at a time (one evaluation of the dropout's generator), in 16-byte pieces where PIECES.
 
-// Mean (0 without `layer`) and factor of the norm of a row whose elements `value` gives.
+constexpr int kAnyThreads = 512;
+
+// Eight elements of a row from column c on, zeros beyond its end.
+template <class T, bool PIECES>
+__device__ __forceinline__ void load_eight(float (&v)[8], const T* row, int64_t c, int64_t d) {
+    constexpr int V = kPiece<T>;
+    if (PIECES) {  // (d is a multiple of V)
+#pragma unroll
+        for (int q = 0; q < 8 / V; ++q) {
+            Pack<T, V> e;
+            if (c + q * V < d) e = load_pack<false, T, V>(row + c + q * V);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[q * V + k] = c + q * V < d ? widen(e.v[k]) : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c + k < d ? widen(row[c + k]) : 0.0f;
+    }
+}
+template <class T, bool PIECES>
+__device__ __forceinline__ void store_eight(T* row, const float (&v)[8], int64_t c, int64_t d) {
+    constexpr int V = kPiece<T>;
+    if (PIECES) {
+#pragma unroll
+        for (int q = 0; q < 8 / V; ++q) {
+            Pack<T, V> e;
+#pragma unroll
+            for (int k = 0; k < V; ++k) e.v[k] = narrow<T>(v[q * V + k]);
+            if (c + q * V < d) store_pack<true, T, V>(row + c + q * V, e);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c + k < d) row[c + k] = narrow<T>(v[k]);
+    }
+}
+__device__ __forceinline__ void weights_eight(float (&w)[8], const float* p, int64_t c, int64_t d) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = c + k < d ? __ldca(p + c + k) : 0.0f;
+}
+
+// Mean (0 without `layer`) and factor of the norm of a row whose eight elements from column c on `value` gives.
 template <class F>
 __device__ __forceinline__ void row_stats(F&& value, int64_t d, int layer, float eps, float* scratch, float& mean, float& rstd) {
     mean = 0.0f;
+    float v[8];
     if (layer) {
         float s = 0.0f;
-        for (int64_t c = threadIdx.x; c < d; c += kJoinThreads) s += value(c);
+        for (int64_t c = threadIdx.x * 8; c < d; c += blockDim.x * 8) {
+            value(v, c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
         mean = block_sum(s, scratch) / (float)d;
     }
     float q = 0.0f;
-    for (int64_t c = threadIdx.x; c < d; c += kJoinThreads) {
-        const float v = value(c) - mean;
-        q += v * v;
+    for (int64_t c = threadIdx.x * 8; c < d; c += blockDim.x * 8) {
+        value(v, c);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = v[k] - mean;
+            q += c + k < d ? x * x : 0.0f;
+        }
     }
     rstd = 1.0f / sqrtf(block_sum(q, scratch) / (float)d + eps);
 }
 
-__device__ __forceinline__ float drop_factor(const DropParams& drop, uint64_t offset, int64_t r, int64_t c) {
-    if (drop.none) return 1.0f;
-    const uint4 w = drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, drop);
-    return drop_keeps(w, (int)(c & 7), drop) ? drop.scale : 0.0f;
+// v, as dropout leaves it
+__device__ __forceinline__ void drop_eight_of(float (&v)[8], const ResidualProblem& a, const uint4& w) {
+    if (a.drop.none) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = drop_keeps(w, k, a.drop) ? v[k] * a.drop.scale : 0.0f;
 }
-__device__ __forceinline__ float dropped(float v, float factor) { return factor == 0.0f ? 0.0f : v * factor; }
-
-template <class T>
-__device__ __forceinline__ float gate_of(const ResidualProblem& a, int64_t r, int64_t c) {
-    if (a.gate_kind == 0) return 1.0f;
-    const T* g = (const T*)a.gate.p + r / a.gate_rows * a.gate.ld;
-    return widen(g[a.gate_kind == 1 ? 0 : c]);
+__device__ __forceinline__ uint4 words_eight(const ResidualProblem& a, uint64_t offset, int64_t r, int64_t c) {
+    return a.drop.none ? make_uint4(0, 0, 0, 0) : drop_words((uint32_t)r, (uint32_t)(c >> 3), offset, a.drop);
+}
+template <class T, bool PIECES>
+__device__ __forceinline__ void gate_eight(float (&g)[8], const ResidualProblem& a, int64_t r, int64_t c) {
+    if (a.gate_kind == 2) {
+        load_eight<T, PIECES>(g, (const T*)a.gate.p + r / a.gate_rows * a.gate.ld, c, a.d);
+    } else {
+        const float v = a.gate_kind == 1 ? widen(((const T*)a.gate.p)[r * a.gate.ld]) : 1.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[k] = v;
+    }
 }
 
-template <class T>
-__global__ void __launch_bounds__(kJoinThreads) residual_any_kernel(ResidualProblem a) {
-    __shared__ float scratch[kJoinThreads / 32];
+template <class T, bool PIECES>
+__global__ void __launch_bounds__(kAnyThreads, 2) residual_any_kernel(ResidualProblem a) {
+    __shared__ float scratch[kAnyThreads / 32];
     follow();
     const uint64_t offset = drop_offset(a.drop);
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -71,26 +126,49 @@ __global__ void __launch_bounds__(kJoinThreads) residual_any_kernel(ResidualProb
         const T* residual = a.residual.p != nullptr ? (const T*)a.residual.p + r * a.residual.ld : nullptr;
         float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f;
         if (a.w_post != nullptr)
-            row_stats([&](int64_t c) { return widen(x[c]); }, a.d, a.layer, a.eps, scratch, mean1, rstd1);
-        auto joined = [&](int64_t c) {
-            float y = widen(x[c]);
-            if (a.w_post != nullptr) y = (y - mean1) * rstd1 * a.w_post[c];
-            y = dropped(y, drop_factor(a.drop, offset, r, c)) * a.scale * gate_of<T>(a, r, c);
-            return residual != nullptr ? widen(residual[c]) + y : y;
+            row_stats([&](float (&v)[8], int64_t c) { load_eight<T, PIECES>(v, x, c, a.d); }, a.d, a.layer, a.eps, scratch, mean1, rstd1);
+        auto joined = [&](float (&y)[8], int64_t c) {  // (0 beyond the row's end, as the weights are)
+            float w[8], g[8], e[8];
+            load_eight<T, PIECES>(y, x, c, a.d);
+            if (a.w_post != nullptr) {
+                weights_eight(w, a.w_post, c, a.d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = (y[k] - mean1) * rstd1 * w[k];
+            }
+            drop_eight_of(y, a, words_eight(a, offset, r, c));
+            gate_eight<T, PIECES>(g, a, r, c);
+            if (residual != nullptr) load_eight<T, PIECES>(e, residual, c, a.d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                y[k] = y[k] * a.scale * g[k];
+                if (residual != nullptr) y[k] += e[k];
+            }
         };
         if (a.w_pre != nullptr) row_stats(joined, a.d, a.layer, a.eps, scratch, mean2, rstd2);
-        for (int64_t c = threadIdx.x; c < a.d; c += kJoinThreads) {
-            const float v = joined(c);
-            ((T*)a.out.p)[r * a.out.ld + c] = narrow<T>(v);
-            if (a.w_pre != nullptr) ((T*)a.normed.p)[r * a.normed.ld + c] = narrow<T>((v - mean2) * rstd2 * a.w_pre[c]);
+        for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8) {
+            float v[8], w[8];
+            joined(v, c);
+            store_eight<T, PIECES>((T*)a.out.p + r * a.out.ld, v, c, a.d);
+            if (a.w_pre == nullptr) continue;
+            weights_eight(w, a.w_pre, c, a.d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = (v[k] - mean2) * rstd2 * w[k];
+            store_eight<T, PIECES>((T*)a.normed.p + r * a.normed.ld, v, c, a.d);
         }
     }
 }
 
-// ---- rows kept close: `lanes` threads share a row, E elements each, which they copy to shared memory rows ahead and read
+// ---- rows kept close: `lanes` threads share a row, E elements each, which they copy to shared memory a row ahead and read
 // from there; a thread reads what it copied itself, so nothing but the sums over a row is waited for together.  Up to 512
 // elements (256 backward) a row is a part of a warp's, longer ones a CTA's, up to kMaxLanes E; beyond that the kernels for any
 // length.
+//
+// Measured (16384 rows of 4096 bf16, dropout): forward with a gate per element 127 us (671 MB, 5.3 TB/s; 1156 by the kernel for any
+// length), backward with a gate vector per 1024 rows 210 (805 MB, 3.8 TB/s; 1833).  213 K rows of 128 fp32, layer norm, gate per
+// row: forward 80 us (5.5 TB/s); of 100, backward 107 (4.8 TB/s).  The forward waits for memory; the backward is bound by
+// issue and by its chains of dependent operations (128 registers a thread, so 16 warps an SM, which issue in half of the
+// cycles): 32 elements a thread 241 us, 8 (twice the warps, twice the work per row) 284, the first two sums over a row joined into
+// one 213, scalar for paired operations 327 against 310 at that time, no test of a row's end 219.
 
 // 1 / sqrt(v), to about a rounding: the function's result (within two) and one step of Newton's method.  (A division and a
 // square root, rounded each, took 4 to 10 % of a pass.)
@@ -183,9 +261,19 @@ struct Ring {
                         for (int c = 0; c < V; ++c) at(stage(s), t, k)[c] = narrow<T>(0.0f);
     }
     __device__ __forceinline__ void fetch(char* stage, int tensor, const char* row) const {
+        if constexpr (kSlot == 2) {  // (no asynchronous copy is as small: at least all loads of a row before the first store)
+            unsigned short v[NP];
 #pragma unroll
-        for (int k = 0; k < NP; ++k)
-            if (has(k) && ROBE_CHK(col(k) + V <= d, ROBE_DBG_ROW_POS)) copy_async<kSlot>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
+            for (int k = 0; k < NP; ++k)
+                v[k] = has(k) && ROBE_CHK(col(k) + V <= d, ROBE_DBG_ROW_POS) ? __ldcs((const unsigned short*)row + col(k)) : 0;
+#pragma unroll
+            for (int k = 0; k < NP; ++k) *(unsigned short*)at(stage, tensor, k) = v[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < NP; ++k)
+                if (has(k) && ROBE_CHK(col(k) + V <= d, ROBE_DBG_ROW_POS))
+                    copy_async<kSlot>(at(stage, tensor, k), row + (uint32_t)col(k) * (uint32_t)sizeof(T));
+        }
     }
     static __device__ __forceinline__ void zero(char* stage, int tensor) {
 #pragma unroll
@@ -503,9 +591,12 @@ struct JoinGradArgs {
     float *part_post, *part_pre, *part_gate;  // [chunks][d]
 };
 
-template <class T>
-__global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGradArgs args) {
-    __shared__ float scratch[kJoinThreads / 32];
+// Columns' sums of the chunk in shared memory where they fit (IN_SHARED), else in the workspace: a column is always the same
+// thread's.
+template <class T, bool PIECES, bool IN_SHARED>
+__global__ void __launch_bounds__(kAnyThreads, 1) residual_grad_any_kernel(JoinGradArgs args) {
+    extern __shared__ float shared_sums[];
+    __shared__ float scratch[kAnyThreads / 32];
     follow();
     const ResidualProblem& a = args.p;
     const uint64_t offset = drop_offset(a.drop);
@@ -514,6 +605,11 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
     float* part_post = args.part_post + blockIdx.x * a.d;
     float* part_pre = args.part_pre + blockIdx.x * a.d;
     float* part_gate = args.part_gate + blockIdx.x * a.d;
+    float* sum_post = IN_SHARED ? shared_sums : part_post;
+    float* sum_pre = IN_SHARED ? shared_sums + a.d : part_pre;
+    float* sum_gate = IN_SHARED ? shared_sums + 2 * a.d : part_gate;
+    const bool gate_sums = a.gate_kind == 2 && a.grad_gate.p != nullptr;
+    const bool whole_gates = a.gate_rows == 1 || args.chunks.per_gate == 0;
     for (int64_t r = r0; r < r1; ++r) {
         const T* x = (const T*)a.x.p + r * a.x.ld;
         const T* out = (const T*)a.out.p + r * a.out.ld;
@@ -521,36 +617,73 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
         const T* gn = (const T*)a.grad_normed.p + r * a.grad_normed.ld;
         float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f, dot2 = 0.0f, sum2 = 0.0f;
         if (a.w_pre != nullptr) {
-            row_stats([&](int64_t c) { return widen(out[c]); }, a.d, a.layer, a.eps, scratch, mean2, rstd2);
+            row_stats([&](float (&v)[8], int64_t c) { load_eight<T, PIECES>(v, out, c, a.d); }, a.d, a.layer, a.eps, scratch, mean2, rstd2);
             float dot = 0.0f, sum = 0.0f;
-            for (int64_t c = threadIdx.x; c < a.d; c += kJoinThreads) {
-                const float g = widen(gn[c]) * a.w_pre[c];
-                dot += g * ((widen(out[c]) - mean2) * rstd2);
-                sum += g;
+            for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8) {
+                float g[8], w[8], n[8];
+                load_eight<T, PIECES>(g, gn, c, a.d);
+                load_eight<T, PIECES>(n, out, c, a.d);
+                weights_eight(w, a.w_pre, c, a.d);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    dot += g[k] * w[k] * ((n[k] - mean2) * rstd2);
+                    sum += g[k] * w[k];
+                }
             }
             dot2 = block_sum(dot, scratch) * over_d;
             if (a.layer) sum2 = block_sum(sum, scratch) * over_d;
         }
-        auto total = [&](int64_t c) {  // gradient of `out` from both sides
-            float t = go != nullptr ? widen(go[c]) : 0.0f;
-            if (a.w_pre != nullptr) {
-                const float n = (widen(out[c]) - mean2) * rstd2;
-                t += rstd2 * (widen(gn[c]) * a.w_pre[c] - sum2 - n * dot2);
+        // gradient of `out` from both sides, and the norm of out and its gradient
+        auto total = [&](float (&t)[8], float (&n)[8], float (&g)[8], int64_t c) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = n[k] = g[k] = 0.0f;
+            if (go != nullptr) load_eight<T, PIECES>(t, go, c, a.d);
+            if (a.w_pre == nullptr) return;
+            float w[8];
+            load_eight<T, PIECES>(n, out, c, a.d);
+            load_eight<T, PIECES>(g, gn, c, a.d);
+            weights_eight(w, a.w_pre, c, a.d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                n[k] = (n[k] - mean2) * rstd2;
+                t[k] += rstd2 * (g[k] * w[k] - sum2 - n[k] * dot2);
             }
-            return t;
         };
         if (a.w_post != nullptr)
-            row_stats([&](int64_t c) { return widen(x[c]); }, a.d, a.layer, a.eps, scratch, mean1, rstd1);
+            row_stats([&](float (&v)[8], int64_t c) { load_eight<T, PIECES>(v, x, c, a.d); }, a.d, a.layer, a.eps, scratch, mean1, rstd1);
+        // of eight columns: norm of x, dropped gradient of the norm's row (u), weights, gradient of the gate
+        auto back = [&](const float (&t)[8], float (&n)[8], float (&u)[8], float (&w)[8], float (&gg)[8], int64_t c) {
+            float g[8], y[8];
+            load_eight<T, PIECES>(n, x, c, a.d);
+            if (a.w_post != nullptr) weights_eight(w, a.w_post, c, a.d);
+            gate_eight<T, PIECES>(g, a, r, c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                n[k] = (n[k] - mean1) * rstd1;
+                if (a.w_post == nullptr) w[k] = 1.0f;
+                y[k] = n[k] * w[k];
+                u[k] = t[k] * a.scale * g[k];
+            }
+            const uint4 words = words_eight(a, offset, r, c);
+            drop_eight_of(y, a, words);
+            drop_eight_of(u, a, words);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) gg[k] = y[k] * (a.scale * t[k]);
+        };
         float dot = 0.0f, sum = 0.0f, gate_sum = 0.0f;
-        for (int64_t c = threadIdx.x; c < a.d; c += kJoinThreads) {
-            const float t = total(c), f = drop_factor(a.drop, offset, r, c);
-            const float n = (widen(x[c]) - mean1) * rstd1;
-            const float w = a.w_post != nullptr ? a.w_post[c] : 1.0f;
-            const float g = dropped(t * a.scale * gate_of<T>(a, r, c), f) * w;
-            dot += g * n;
-            sum += g;
-            gate_sum += dropped(n * w, f) * (a.scale * t);
-        }
+        if (a.w_post != nullptr || a.gate_kind == 1)
+            for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8) {
+                float t[8], n2[8], g2[8], n[8], u[8], w[8], gg[8];
+                total(t, n2, g2, c);
+                back(t, n, u, w, gg, c);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (c + k >= a.d) break;
+                    dot += u[k] * w[k] * n[k];
+                    sum += u[k] * w[k];
+                    gate_sum += gg[k];
+                }
+            }
         float dot1 = 0.0f, sum1 = 0.0f;
         if (a.w_post != nullptr) {
             dot1 = block_sum(dot, scratch) * over_d;
@@ -561,31 +694,36 @@ __global__ void __launch_bounds__(kJoinThreads) residual_grad_any_kernel(JoinGra
             if (threadIdx.x == 0) ((T*)a.grad_gate.p)[r * a.grad_gate.ld] = narrow<T>(gate_sum);
         }
         const int64_t in_gate = r % a.gate_rows;
-        const bool whole_gates = a.gate_rows == 1 || args.chunks.per_gate == 0;
-        for (int64_t c = threadIdx.x; c < a.d; c += kJoinThreads) {
-            const float t = total(c), f = drop_factor(a.drop, offset, r, c);
-            const float n = (widen(x[c]) - mean1) * rstd1;
-            const float w = a.w_post != nullptr ? a.w_post[c] : 1.0f;
-            const float u = dropped(t * a.scale * gate_of<T>(a, r, c), f);
-            if (a.w_pre != nullptr) {
-                const float v = widen(gn[c]) * ((widen(out[c]) - mean2) * rstd2);
-                part_pre[c] = (r == r0 ? 0.0f : part_pre[c]) + v;
+        for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8) {
+            float t[8], n2[8], g2[8], n[8], u[8], w[8], gg[8];
+            total(t, n2, g2, c);
+            back(t, n, u, w, gg, c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (c + k >= a.d) break;
+                if (a.w_pre != nullptr) sum_pre[c + k] = (r == r0 ? 0.0f : sum_pre[c + k]) + g2[k] * n2[k];
+                if (gate_sums) {
+                    if (r != r0 && in_gate != 0) gg[k] += sum_gate[c + k];
+                    sum_gate[c + k] = gg[k];
+                }
+                if (a.w_post != nullptr) {
+                    sum_post[c + k] = (r == r0 ? 0.0f : sum_post[c + k]) + u[k] * n[k];
+                    u[k] = rstd1 * (u[k] * w[k] - sum1 - n[k] * dot1);
+                }
             }
-            if (a.gate_kind == 2 && a.grad_gate.p != nullptr) {
-                float v = dropped(n * w, f) * (a.scale * t);
-                if (r != r0 && in_gate != 0) v += part_gate[c];
-                part_gate[c] = v;
-                if (whole_gates && in_gate == a.gate_rows - 1) ((T*)a.grad_gate.p)[r / a.gate_rows * a.grad_gate.ld + c] = narrow<T>(v);
-            }
-            float gx = u;
-            if (a.w_post != nullptr) {
-                part_post[c] = (r == r0 ? 0.0f : part_post[c]) + u * n;
-                gx = rstd1 * (u * w - sum1 - n * dot1);
-            }
-            if (a.grad_residual.p != nullptr) ((T*)a.grad_residual.p)[r * a.grad_residual.ld + c] = narrow<T>(t);
-            ((T*)a.grad_x.p)[r * a.grad_x.ld + c] = narrow<T>(gx);
+            if (gate_sums && whole_gates && in_gate == a.gate_rows - 1)
+                store_eight<T, PIECES>((T*)a.grad_gate.p + r / a.gate_rows * a.grad_gate.ld, gg, c, a.d);
+            if (a.grad_residual.p != nullptr) store_eight<T, PIECES>((T*)a.grad_residual.p + r * a.grad_residual.ld, t, c, a.d);
+            store_eight<T, PIECES>((T*)a.grad_x.p + r * a.grad_x.ld, u, c, a.d);
         }
     }
+    if (!IN_SHARED) return;
+    for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8)
+        for (int64_t k = c; k < c + 8 && k < a.d; ++k) {
+            if (a.w_post != nullptr) part_post[k] = sum_post[k];
+            if (a.w_pre != nullptr) part_pre[k] = sum_pre[k];
+            if (gate_sums && !whole_gates) part_gate[k] = sum_gate[k];
+        }
 }
 
 // One CTA per chunk.  The weights' gradients of a thread's columns are summed in registers over its rows, over the groups of
@@ -961,7 +1099,7 @@ struct RowPlan {
     int elems;  // of a thread
     int lanes;  // threads of a row; 0: too long or too far apart, the kernels that read rows again
 };
-RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tensors, int size, int warp_elems) {
+RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tensors, int size, int warp_elems, bool longer) {
     uintptr_t bits = (uintptr_t)(pb.d * size);
     bool wide = pb.rows >= (1ll << 30);  // (row numbers are 32 bits, and go past the end)
     for (const RowsRef& t : {pb.gate, pb.grad_gate}) wide = wide || (t.p != nullptr && t.ld * size >= (1ll << 32));
@@ -981,6 +1119,7 @@ RowPlan row_plan(const ResidualProblem& pb, std::initializer_list<RowsRef> tenso
     if (few) warp_elems = 8;
     p.cta = pb.d > 32 * warp_elems;
     p.elems = p.cta ? (few ? 8 : kRowElems) : warp_elems;
+    if (longer && p.vec * size == 16 && pb.d > p.elems * kMaxLanes) p.elems = 2 * kRowElems;
     if (pb.d > p.elems * kMaxLanes || wide) {
         p.lanes = 0;
     } else if (p.cta) {
@@ -1013,7 +1152,7 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
     const int threads = CTA ? p.lanes : kWarpRowThreads;
     void (*kernel)(ResidualProblem, int, int) = residual_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
     int slots = Ring<T, V, E, 3, 0>::kThread;
-    if constexpr (V * sizeof(T) == 16) {
+    if constexpr (V * sizeof(T) == 16 && E <= kRowElems) {
         if (usual) {
             kernel = ROBE_USUAL(residual_rows_kernel, T, V, E, CTA, pb);
             if (pb.gate_kind != 2) slots = Ring<T, V, E, 2, 0>::kThread;
@@ -1038,6 +1177,8 @@ template <class T, int V>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
     constexpr int kSmall = V * sizeof(T) < 16 ? 8 : kRowElems;
     if (!p.cta) return p.elems == 8 ? launch_forward_rows<T, V, kSmall, false>(pb, p, st) : launch_forward_rows<T, V, kRowElems, false>(pb, p, st);
+    if constexpr (V * sizeof(T) == 16)
+        if (p.elems == 2 * kRowElems) return launch_forward_rows<T, V, 2 * kRowElems, true>(pb, p, st);
     return p.elems == 8 ? launch_forward_rows<T, V, kSmall, true>(pb, p, st) : launch_forward_rows<T, V, kRowElems, true>(pb, p, st);
 }
 
@@ -1045,7 +1186,7 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
 
 cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaStream_t st) {
     const RowPlan p = row_plan(pb, {pb.x, pb.residual, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.out, pb.normed},
-                               dtype == 0 ? 4 : 2, kRowElems);
+                               dtype == 0 ? 4 : 2, kRowElems, true);
     if (p.lanes > 0) {
         if (dtype == 0)
             return p.vec == 4   ? launch_forward_rows<float, 4>(pb, p, st)
@@ -1056,9 +1197,12 @@ cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaSt
                : p.vec == 2 ? launch_forward_rows<__nv_bfloat16, 2>(pb, p, st)
                             : launch_forward_rows<__nv_bfloat16, 1>(pb, p, st);
     }
-    const unsigned grid = (unsigned)(pb.rows < 148 * 8 ? pb.rows : 148 * 8);
-    if (dtype == 0) launch_next(residual_any_kernel<float>, grid, kJoinThreads, 0, st, pb);
-    else launch_next(residual_any_kernel<__nv_bfloat16>, grid, kJoinThreads, 0, st, pb);
+    const unsigned grid = (unsigned)(pb.rows < 148 * 4 ? pb.rows : 148 * 4);
+    const bool pieces = p.vec * (dtype == 0 ? 4 : 2) == 16;
+    void (*kernel)(ResidualProblem) = dtype == 0 ? (pieces ? residual_any_kernel<float, true> : residual_any_kernel<float, false>)
+                                      : pieces   ? residual_any_kernel<__nv_bfloat16, true>
+                                                 : residual_any_kernel<__nv_bfloat16, false>;
+    launch_next(kernel, grid, kAnyThreads, 0, st, pb);
     return cudaGetLastError();
 }
 
@@ -1075,6 +1219,19 @@ size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates) {
 }
 
 namespace {
+
+template <class T, bool PIECES>
+cudaError_t launch_backward_any(const JoinGradArgs& a, cudaStream_t st) {
+    const size_t sums = (size_t)a.p.d * 3 * sizeof(float);
+    if (sums > (200u << 10)) {
+        launch_next(residual_grad_any_kernel<T, PIECES, false>, (unsigned)a.chunks.count, kAnyThreads, 0, st, a);
+        return cudaGetLastError();
+    }
+    const cudaError_t e = allow_shared(residual_grad_any_kernel<T, PIECES, true>, sums);
+    if (e != cudaSuccess) return e;
+    launch_next(residual_grad_any_kernel<T, PIECES, true>, (unsigned)a.chunks.count, kAnyThreads, sums, st, a);
+    return cudaGetLastError();
+}
 
 template <class T, int V, int E, bool CTA>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
@@ -1122,7 +1279,7 @@ cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void*
     cudaError_t e = cudaSuccess;
     const RowPlan p = row_plan(pb, {pb.x, pb.grad_out, pb.out, pb.grad_normed, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.grad_x,
                                     pb.grad_residual, pb.gate_kind == 2 ? pb.grad_gate : RowsRef{}},
-                               dtype == 0 ? 4 : 2, kGradWarpElems);
+                               dtype == 0 ? 4 : 2, kGradWarpElems, false);
     if (a.chunks.count == 0) {
     } else if (p.lanes > 0) {
         if (dtype == 0)
@@ -1134,10 +1291,11 @@ cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void*
                 : p.vec == 4 ? launch_backward_rows<__nv_bfloat16, 4>(a, p, st)
                 : p.vec == 2 ? launch_backward_rows<__nv_bfloat16, 2>(a, p, st)
                              : launch_backward_rows<__nv_bfloat16, 1>(a, p, st);
-    } else if (dtype == 0) {
-        launch_next(residual_grad_any_kernel<float>, (unsigned)a.chunks.count, kJoinThreads, 0, st, a);
     } else {
-        launch_next(residual_grad_any_kernel<__nv_bfloat16>, (unsigned)a.chunks.count, kJoinThreads, 0, st, a);
+        const bool pieces = p.vec * (dtype == 0 ? 4 : 2) == 16;
+        e = dtype == 0 ? (pieces ? launch_backward_any<float, true>(a, st) : launch_backward_any<float, false>(a, st))
+            : pieces   ? launch_backward_any<__nv_bfloat16, true>(a, st)
+                       : launch_backward_any<__nv_bfloat16, false>(a, st);
     }
     if (e != cudaSuccess) return e;
     ColumnArgs c;

@@ -286,7 +286,9 @@ JOINS = [  # rows, d, gate, post, pre, residual, p
     (5, 3, "none", True, True, True, 0.0), (1400, 96, 1400, True, True, True, 0.0), (64, 36, 32, True, False, True, 1.0),
     (900, 47, "row", True, True, True, 0.1), (6080, 24, 10, True, True, True, 0.1), (12_000, 8, 2, True, True, True, 0.0),
     (3200, 300, 100, True, True, True, 0.1), (1200, 520, 3, True, True, True, 0.1), (300, 909, "none", True, True, True, 0.1),
-    (40, 4100, 5, True, True, True, 0.1), (9, 8191, 1, True, True, True, 0.1), (20_000, 5, 1, True, True, True, 0.2)]
+    (40, 4100, 5, True, True, True, 0.1), (9, 8191, 1, True, True, True, 0.1), (20_000, 5, 1, True, True, True, 0.2),
+    (7, 12_288, 1, True, True, True, 0.1), (600, 8200, 3, True, False, True, 0.1), (300, 8208, 150, True, True, True, 0.0),
+    (5, 30_000, 5, False, True, False, 0.3), (160, 8193, "row", True, True, True, 0.1)]
 
 
 @pytest.mark.parametrize("layer", [0, 1])
