@@ -27,7 +27,8 @@ __device__ __forceinline__ float block_sum(float v, float* scratch) {
 }
 
 // ---- rows of any length, one CTA each, read again in every pass over the row: for rows too long for the kernels below.  A
-// thread takes eight columns at a time (one evaluation of the dropout's generator), in 16-byte pieces where PIECES.
+// thread takes eight columns at a time (one evaluation of the dropout's generator), in 16-byte pieces where PIECES.  Bound by
+// issue: every pass joins the row anew.  4000 rows of 8200 fp32, dropout: backward 670 us (788 MB, 1.2 TB/s).
 
 constexpr int kAnyThreads = 512;
 
@@ -161,7 +162,8 @@ __global__ void __launch_bounds__(kAnyThreads, 2) residual_any_kernel(ResidualPr
 // ---- rows kept close: `lanes` threads share a row, E elements each, which they copy to shared memory a row ahead and read
 // from there; a thread reads what it copied itself, so nothing but the sums over a row is waited for together.  Up to 512
 // elements (256 backward) a row is a part of a warp's, longer ones a CTA's, up to kMaxLanes E; beyond that the kernels for any
-// length.
+// length.  E is 16 (8 backward for parts of a warp, and for small pieces, whose code is longer), 32 for long rows of 16-byte
+// pieces: the bf16 backward then spills, 4000 rows of 12288 390 us, 1218 by the kernel for any length.
 //
 // Measured (16384 rows of 4096 bf16, dropout): forward with a gate per element 127 us (671 MB, 5.3 TB/s; 1156 by the kernel for any
 // length), backward with a gate vector per 1024 rows 210 (805 MB, 3.8 TB/s; 1833).  213 K rows of 128 fp32, layer norm, gate per
@@ -1242,7 +1244,7 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
     const int threads = CTA ? p.lanes : kWarpRowThreads;
     void (*kernel)(JoinGradArgs, int, int) = residual_grad_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
     int slots = Ring<T, V, E, 5, 0>::kThread;
-    if constexpr (V * sizeof(T) == 16) {
+    if constexpr (V * sizeof(T) == 16 && E <= kRowElems) {
         if (usual) {
             kernel = ROBE_USUAL(residual_grad_rows_kernel, T, V, E, CTA, pb);
             if (pb.gate_kind != 2) slots = Ring<T, V, E, 4, 0>::kThread;
@@ -1264,6 +1266,8 @@ template <class T, int V>
 cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaStream_t st) {
     constexpr int kSmall = V * sizeof(T) < 16 ? 8 : kRowElems;
     if (!p.cta) return launch_backward_rows<T, V, kGradWarpElems, false>(a, p, st);
+    if constexpr (V * sizeof(T) == 16 && sizeof(T) == 2)
+        if (p.elems == 2 * kRowElems) return launch_backward_rows<T, V, 2 * kRowElems, true>(a, p, st);
     return p.elems == 8 ? launch_backward_rows<T, V, kSmall, true>(a, p, st) : launch_backward_rows<T, V, kRowElems, true>(a, p, st);
 }
 
@@ -1279,7 +1283,7 @@ cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void*
     cudaError_t e = cudaSuccess;
     const RowPlan p = row_plan(pb, {pb.x, pb.grad_out, pb.out, pb.grad_normed, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.grad_x,
                                     pb.grad_residual, pb.gate_kind == 2 ? pb.grad_gate : RowsRef{}},
-                               dtype == 0 ? 4 : 2, kGradWarpElems, false);
+                               dtype == 0 ? 4 : 2, kGradWarpElems, dtype == 1);
     if (a.chunks.count == 0) {
     } else if (p.lanes > 0) {
         if (dtype == 0)
