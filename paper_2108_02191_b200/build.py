@@ -14,7 +14,7 @@ LIB = os.path.join(_HERE, "librobe.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0",
 ]
 
 
@@ -75,7 +75,7 @@ def build_debug(force: bool = False) -> str:
                 for src in sources():
                     if os.path.basename(src) != "_unity_debug.cu":
                         f.write(f'#include "{os.path.basename(src)}"\n')
-            subprocess.run([nvcc] + NVCC_FLAGS + ["-DROBE_DEBUG", "-o", DEBUG_LIB, unity], check=True)
+            subprocess.run([nvcc] + NVCC_FLAGS + ["--split-compile", "0", "-DROBE_DEBUG", "-o", DEBUG_LIB, unity], check=True)
         finally:
             if os.path.exists(unity):
                 os.unlink(unity)
