@@ -237,7 +237,7 @@ struct Ring {
     static constexpr int U = V > 1 ? NP : NP / 2;  // units
     static constexpr int kPieces = V > 1 ? 1 : 2;  // of a unit
     static constexpr int kSlot = V * (int)sizeof(T);
-    static constexpr int kThread = kSlot * TENSORS * NP;  // bytes of a thread in a stage
+    static constexpr int kThread = TENSORS * E * (int)sizeof(T);  // bytes of a thread in a stage
     char* first;  // the thread's first piece of stage 0
     int lanes, lane, d;
 
@@ -719,13 +719,13 @@ __global__ void __launch_bounds__(kAnyThreads, 1) residual_grad_any_kernel(JoinG
             store_eight<T, PIECES>((T*)a.grad_x.p + r * a.grad_x.ld, u, c, a.d);
         }
     }
-    if (!IN_SHARED) return;
-    for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8)
-        for (int64_t k = c; k < c + 8 && k < a.d; ++k) {
-            if (a.w_post != nullptr) part_post[k] = sum_post[k];
-            if (a.w_pre != nullptr) part_pre[k] = sum_pre[k];
-            if (gate_sums && !whole_gates) part_gate[k] = sum_gate[k];
-        }
+    if constexpr (IN_SHARED)
+        for (int64_t c = threadIdx.x * 8; c < a.d; c += kAnyThreads * 8)
+            for (int64_t k = c; k < c + 8 && k < a.d; ++k) {
+                if (a.w_post != nullptr) part_post[k] = sum_post[k];
+                if (a.w_pre != nullptr) part_pre[k] = sum_pre[k];
+                if (gate_sums && !whole_gates) part_gate[k] = sum_gate[k];
+            }
 }
 
 // One CTA per chunk.  The weights' gradients of a thread's columns are summed in registers over its rows, over the groups of
@@ -1153,11 +1153,11 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
     const bool usual = V * sizeof(T) == 16 && pb.w_post != nullptr && pb.w_pre != nullptr && pb.residual.p != nullptr;
     const int threads = CTA ? p.lanes : kWarpRowThreads;
     void (*kernel)(ResidualProblem, int, int) = residual_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
-    int slots = Ring<T, V, E, 3, 0>::kThread;
+    int slots = 3 * E * (int)sizeof(T);
     if constexpr (V * sizeof(T) == 16 && E <= kRowElems) {
         if (usual) {
             kernel = ROBE_USUAL(residual_rows_kernel, T, V, E, CTA, pb);
-            if (pb.gate_kind != 2) slots = Ring<T, V, E, 2, 0>::kThread;
+            if (pb.gate_kind != 2) slots = 2 * E * (int)sizeof(T);
         }
     }
     const size_t stage = (size_t)slots * threads;
@@ -1243,11 +1243,11 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
                        pb.grad_residual.p != nullptr;
     const int threads = CTA ? p.lanes : kWarpRowThreads;
     void (*kernel)(JoinGradArgs, int, int) = residual_grad_rows_kernel<T, V, E, CTA, false, 0, 0, 1>;
-    int slots = Ring<T, V, E, 5, 0>::kThread;
+    int slots = 5 * E * (int)sizeof(T);
     if constexpr (V * sizeof(T) == 16 && E <= kRowElems) {
         if (usual) {
             kernel = ROBE_USUAL(residual_grad_rows_kernel, T, V, E, CTA, pb);
-            if (pb.gate_kind != 2) slots = Ring<T, V, E, 4, 0>::kThread;
+            if (pb.gate_kind != 2) slots = 4 * E * (int)sizeof(T);
         }
     }
     const size_t stage = (size_t)slots * threads;

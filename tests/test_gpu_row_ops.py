@@ -420,7 +420,112 @@ def test_dropout_in_the_join_is_that_of_the_dropout_call():
         assert same_bits(a, b)
 
 
+# ---------------------------------------------------------------- beyond 32 bits
+
+
+def room(gigabytes):
+    if torch.cuda.mem_get_info()[0] < gigabytes << 30:
+        pytest.skip(f"needs {gigabytes} GB")
+
+
+def test_residual_of_more_than_2_to_31_elements():
+    # the same 1000 rows over and over: the last ones come out as the first
+    d, block, times = 4096, 1000, 530
+    room(40)
+    r = gen(4)
+    some = lambda: torch.randn(block, d, generator=r).bfloat16().cuda()
+    x, residual, go, gn = (some() for _ in range(4))
+    big = lambda t: t.repeat(times, 1)
+    w = (1 + 0.1 * torch.randn(d, generator=r)).cuda()
+    X, R = big(x), big(residual)
+    N = torch.empty_like(X)
+    robe.robe_residual_forward(X, R, R, N, w, w, None, 0.5)  # (in place)
+    assert same_bits(R[-block:], R[:block]) and same_bits(N[-block:], N[:block])
+    small, normed = torch.empty_like(x), torch.empty_like(x)
+    robe.robe_residual_forward(x, residual, small, normed, w, w, None, 0.5)
+    assert same_bits(R[:block], small) and same_bits(N[-block:], normed)
+    del N
+    GO, GN, GX = big(go), big(gn), torch.empty_like(X)
+    g1, g2 = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    ws = torch.empty(robe.robe_residual_backward_workspace_bytes(block * times, d), dtype=torch.uint8, device="cuda")
+    robe.robe_residual_backward(GO, GN, X, R, GX, GO, w, w, None, g1, g2, None, ws, 0.5)
+    assert same_bits(GO[-block:], GO[:block]) and same_bits(GX[-block:], GX[:block])
+    s1, s2, gx, gr = torch.empty(d, device="cuda"), torch.empty(d, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    robe.robe_residual_backward(go, gn, x, small, gx, gr, w, w, None, s1, s2, None, ws, 0.5)
+    assert same_bits(GX[:block], gx) and same_bits(GO[:block], gr)
+    # sums over rows: a thread's chunk (148 CTAs at least share the rows) in fp32, the chunks' in 64 bits
+    chain = (block * times / 148 + 64) * ref.U
+    n1 = x.double() / (x.double().square().mean(1, keepdim=True) + 1e-6).sqrt()
+    for all_rows, few, terms in ((g1, s1, 0.5 * gr.double() * n1), (g2, s2, gn.double() * normed.double() / w)):
+        assert bool(((all_rows.double() - times * few.double()).abs() <= 2 * chain * times * terms.abs().sum(0)).all())
+
+
+def test_bias_of_more_than_2_to_31_places():
+    q = k = 47_000
+    room(16)
+    b = robe.robe_bias_create(32, 1000, False)
+    rows = torch.randn(32, 1, generator=gen(6)).cuda()
+    out = torch.empty(1, 1, q, k, dtype=torch.bfloat16, device="cuda")
+    robe.robe_bias_forward(b, rows, out, 0, True)
+    edges = torch.tensor(robe.robe_bias_get_edges(b)[1:], device="cuda")
+    for i in (0, 1, 20_000, q - 2, q - 1):
+        r = torch.arange(k, device="cuda") - i
+        want = torch.where(r > 0, -math.inf, rows[torch.bucketize((-r).clamp(min=0), edges, right=True), 0]).bfloat16()
+        assert same_bits(out[0, 0, i], want), i
+    # of ones: the number of places of every bucket, exact in 64 bits and rounded once; in fp32 sums of up to 64 ones are exact
+    out.fill_(1.0)
+    got = torch.empty(32, 1, device="cuda")
+    ws = torch.empty(robe.robe_bias_backward_workspace_bytes(b, 1, 1, q, k), dtype=torch.uint8, device="cuda")
+    robe.robe_bias_backward(b, out, got, ws, 0, True)
+    dist = torch.arange(q, device="cuda")
+    want = torch.zeros(32, dtype=torch.float64, device="cuda")
+    want.index_add_(0, torch.bucketize(dist, edges, right=True), (q - dist).double())
+    assert torch.equal(got[:, 0], want.float())
+    robe.robe_bias_destroy(b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_bias_of_long_rows(dtype):
+    # several CTAs along a row, both ways, and a gradient whose diagonals are cut in chunks
+    b = robe.robe_bias_create(16, 200, True)
+    for q, k, start in [(2, 70_001, 69_000), (40, 30_000, 15_000), (6, 25_003, 30_000)]:
+        rows, index = bias_case(2, q, k, (16, 200, True), False, [start], dtype)
+        out = torch.empty(1, 2, q, k, dtype=dtype, device="cuda")
+        robe.robe_bias_forward(b, rows.cuda(), out, start)
+        assert same_bits(out.cpu(), rows[index].permute(0, 3, 1, 2).to(dtype))
+        g = torch.randn(1, 2, q, k, generator=gen(q)).to(dtype)
+        want, bound = bias_grad_reference(g, index, 16)
+        got = torch.empty(16, 2, device="cuda")
+        ws = Workspace(robe.robe_bias_backward_workspace_bytes(b, 2, 1, q, k))
+        robe.robe_bias_backward(b, g.cuda(), got, ws.own, start)
+        ref.assert_within(got, want, bound, (q, k))
+        assert ws.kept_within()
+    robe.robe_bias_destroy(b)
+
+
 # ---------------------------------------------------------------- streams, graphs, together
+
+
+def test_two_streams_at_once_on_one_handle():
+    b = robe.robe_bias_create(32, 128, True)
+    g = [torch.randn(2, 4, 300, 300, generator=gen(n)).cuda() for n in range(2)]
+    size = robe.robe_bias_backward_workspace_bytes(b, 4, 2, 300, 300)
+    alone = []
+    for t in g:
+        got = torch.empty(32, 4, device="cuda")
+        robe.robe_bias_backward(b, t, got, torch.empty(size, dtype=torch.uint8, device="cuda"))
+        alone.append(got)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [torch.empty(32, 4, device="cuda") for _ in g]
+    ws = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in g]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for n in range(2):
+            robe.robe_bias_backward(b, g[n], got[n], ws[n], 0, False, streams[n])
+    torch.cuda.synchronize()
+    assert same_bits(got[0], alone[0]) and same_bits(got[1], alone[1])
+    robe.robe_bias_destroy(b)
 
 
 def test_refusals_of_the_binding():
