@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(kAnyThreads, 2) residual_any_kernel(ResidualPr
 // pieces: the bf16 backward then spills, 4000 rows of 12288 390 us, 1218 by the kernel for any length.
 //
 // Measured (16384 rows of 4096 bf16, dropout): forward with a gate per element 127 us (671 MB, 5.3 TB/s; 1156 by the kernel for any
-// length), backward with a gate vector per 1024 rows 210 (805 MB, 3.8 TB/s; 1833).  213 K rows of 128 fp32, layer norm, gate per
-// row: forward 80 us (5.5 TB/s); of 100, backward 107 (4.8 TB/s).  The forward waits for memory; the backward is bound by
+// length), backward with a gate vector per 1024 rows 207 (805 MB, 3.9 TB/s; 1833).  213 K rows of 128 fp32, layer norm, gate per
+// row: forward 80 us (5.5 TB/s); of 100, backward 103 (5.0 TB/s).  The forward waits for memory; the backward is bound by
 // issue and by its chains of dependent operations (128 registers a thread, so 16 warps an SM, which issue in half of the
 // cycles): 32 elements a thread 241 us, 8 (twice the warps, twice the work per row) 284, the first two sums over a row joined into
 // one 213, scalar for paired operations 327 against 310 at that time, no test of a row's end 219.
@@ -298,6 +298,15 @@ struct Ring {
                 if constexpr (sizeof(T) == 2) v[q] = make_float2(widen_low(p.bits[q]), widen_high(p.bits[q]));
                 else v[q] = make_float2(__uint_as_float(p.bits[2 * q]), __uint_as_float(p.bits[2 * q + 1]));
             }
+        }
+    }
+    // .. straight from memory
+    __device__ __forceinline__ void load(float2 (&v)[P], const char* row, int u) const {
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int k = kPieces * u, c = V > 1 ? col(k) + 2 * q : col(k);
+            v[q].x = has(k) ? widen(((const T*)row)[c]) : 0.0f;
+            v[q].y = has(k + kPieces - 1) ? widen(((const T*)row)[V > 1 ? c + 1 : col(k + 1)]) : 0.0f;
         }
     }
     __device__ __forceinline__ void store(char* row, const float2 (&v)[P], int u) const {
@@ -784,6 +793,17 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int q = 0; q < P; ++q) sum_post[u][q] = sum_pre[u][q] = sum_gate[u][q] = both(0.0f);
+    // the sum that a gate vector's rows share, as the weight's gradient and the gate's
+    auto close_gate = [&](int u, const float2 (&g)[P]) {
+        if (!post) return;
+        float2 w[P];
+        ring.weights(w, a.w_post, u);
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            sum_post[u][q] = fma2(sum_gate[u][q], g[q], sum_post[u][q]);
+            sum_gate[u][q] = mul2(sum_gate[u][q], w[q]);
+        }
+    };
     auto fetch = [&](char* stage) {
         if (next.r < c1) {
             const uint32_t r = next.r;
@@ -897,7 +917,7 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         if (a.gate_kind == 1 && here) row_gate = widen(*(const T*)row_of(a.gate, r, sizeof(T)));
         const float2 scale = both(dropping ? a.scale * a.drop.scale : a.scale);
         char* grad_residual = row_of(a.grad_residual, r, sizeof(T));
-        float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
+        float2 s0 = both(0.0f), s1 = both(0.0f);
         typename R::Draws words;
         if (dropping) ring.draw(words, a.drop, offset, r);
 #pragma unroll
@@ -909,59 +929,67 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
             if (post) ring.weights(w, a.w_post, u);
             uint32_t draws[2 * P];
             if (dropping) ring.draws(draws, words, u);
-            float2 g[P], gg[P];
-            if (vector) R::read(g, stage, kGate, u);
+            // t: what comes back through dropout and scale; a gate that is one number of the row follows after the sums
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 x[u][q] = mul2(x[u][q], both(rstd1));
-                float2 y = post ? mul2(x[u][q], w[q]) : x[u][q];
-                float2 st = mul2(t[u][q], scale);
-                if (dropping) {  // y and what comes back of t, dropped alike
-                    y = kept_of(y, draws + 2 * q, a.drop.limit);
-                    st = kept_of(st, draws + 2 * q, a.drop.limit);
+                t[u][q] = mul2(t[u][q], scale);
+                if (dropping) {
+                    t[u][q] = kept_of(t[u][q], draws + 2 * q, a.drop.limit);
+                    if (!post) x[u][q] = kept_of(x[u][q], draws + 2 * q, a.drop.limit);
                 }
-                gg[q] = mul2(y, st);
-                t[u][q] = mul2(st, vector ? g[q] : both(row_gate));
             }
             if (vector) {
-                if (shared_gate)
+                float2 g[P];
+                R::read(g, stage, kGate, u);
+                if (shared_gate) {  // one sum for two gradients: times the weight it is the gate's, times the gate the weight's
 #pragma unroll
-                    for (int q = 0; q < P; ++q) sum_gate[u][q] = add2(sum_gate[u][q], gg[q]);
-                else if (a.grad_gate.p != nullptr && here) ring.store(row_of(a.grad_gate, r, sizeof(T)), gg, u);
-            } else if (a.gate_kind == 1) {
+                    for (int q = 0; q < P; ++q) sum_gate[u][q] = fma2(t[u][q], x[u][q], sum_gate[u][q]);
+                } else if (a.grad_gate.p != nullptr && here) {
+                    float2 gg[P];
 #pragma unroll
-                for (int q = 0; q < P; ++q) s2 = add2(s2, gg[q]);
-            }
-            if (post) {
-#pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    sum_post[u][q] = fma2(t[u][q], x[u][q], sum_post[u][q]);
-                    t[u][q] = mul2(t[u][q], w[q]);
-                    s0 = fma2(t[u][q], x[u][q], s0);
-                    if (layer) s1 = add2(s1, t[u][q]);
+                    for (int q = 0; q < P; ++q) gg[q] = mul2(post ? mul2(x[u][q], w[q]) : x[u][q], t[u][q]);
+                    ring.store(row_of(a.grad_gate, r, sizeof(T)), gg, u);
                 }
+#pragma unroll
+                for (int q = 0; q < P; ++q) t[u][q] = mul2(t[u][q], g[q]);
+                if (post && !shared_gate)
+#pragma unroll
+                    for (int q = 0; q < P; ++q) sum_post[u][q] = fma2(t[u][q], x[u][q], sum_post[u][q]);
+            } else if (post) {
+#pragma unroll
+                for (int q = 0; q < P; ++q) sum_post[u][q] = fma2(mul2(t[u][q], both(row_gate)), x[u][q], sum_post[u][q]);
+            }
+            if (post)
+#pragma unroll
+                for (int q = 0; q < P; ++q) t[u][q] = mul2(t[u][q], w[q]);
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                s0 = fma2(t[u][q], x[u][q], s0);
+                if (layer) s1 = add2(s1, t[u][q]);
             }
         }
         s[0] = s0.x + s0.y;
         s[1] = s1.x + s1.y;
-        s[2] = s2.x + s2.y;
-        if (a.gate_kind == 1) row_sums<CTA>(s, 3, lanes, scratch, turn);
-        else if (post) row_sums<CTA>(s, layer ? 2 : 1, lanes, scratch, turn);
+        if (post || a.gate_kind == 1) row_sums<CTA>(s, layer && post ? 2 : 1, lanes, scratch, turn);
         if (a.gate_kind == 1 && a.grad_gate.p != nullptr && here && ring.lane == 0)
-            *(T*)row_of(a.grad_gate, r, sizeof(T)) = narrow<T>(s[2]);
+            *(T*)row_of(a.grad_gate, r, sizeof(T)) = narrow<T>(s[0]);
         const float2 dot = both(-s[0] * over_d), mean = both(layer ? -s[1] * over_d : 0.0f);
+        const float2 factor = both(post ? rstd1 * row_gate : row_gate);
         char* grad_x = row_of(a.grad_x, r, sizeof(T));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (post)
 #pragma unroll
-                for (int q = 0; q < P; ++q) t[u][q] = mul2(fma2(x[u][q], dot, add2(t[u][q], mean)), both(rstd1));
+            for (int q = 0; q < P; ++q) t[u][q] = mul2(post ? fma2(x[u][q], dot, add2(t[u][q], mean)) : t[u][q], factor);
             if (here) ring.store(grad_x, t[u], u);
         }
         if (shared_gate && whole_gates && now.in_block == block - 1) {  // a gate vector's rows are done
             char* grad_gate = row_of(a.grad_gate, now.gate, sizeof(T));
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                float2 g[P];
+                R::read(g, stage, kGate, u);
+                close_gate(u, g);
                 if (a.grad_gate.p != nullptr && here) ring.store(grad_gate, sum_gate[u], u);
 #pragma unroll
                 for (int q = 0; q < P; ++q) sum_gate[u][q] = both(0.0f);
@@ -971,6 +999,15 @@ residual_grad_rows_kernel(JoinGradArgs args, int lanes, int stages) {
         turn_of = turn_of + 1 == stages ? 0 : turn_of + 1;
     }
     copies_wait(0);
+    if (shared_gate && !whole_gates) {
+        const char* row = row_of(a.gate, c0 / (uint32_t)a.gate_rows, sizeof(T));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float2 g[P];
+            ring.load(g, row, u);
+            close_gate(u, g);
+        }
+    }
     // the chunk's sums
     auto store_sums = [&](const float2 (&v)[U][P], float* part) {
         if (!ROBE_CHK(blockIdx.x < args.chunks.count, ROBE_DBG_ROW_POS)) return;
