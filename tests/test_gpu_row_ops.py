@@ -506,6 +506,58 @@ def test_bias_of_long_rows(dtype):
 # ---------------------------------------------------------------- streams, graphs, together
 
 
+def test_both_ways_of_calling_give_the_same():
+    # numbers that the native path leaves to ctypes (numpy's), and plain ones
+    import numpy as np
+    x, y = torch.randn(60, 200, generator=gen(1)).cuda(), torch.randn(60, 200, generator=gen(2)).cuda()
+    w = torch.randn(200, generator=gen(3)).cuda()
+    gate = torch.randn(20, 200, generator=gen(4)).cuda()
+    b = robe.robe_bias_create(32, 128, False)
+    rows, start = torch.randn(32, 3, generator=gen(5)).cuda(), torch.tensor([5, 70], device="cuda")
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    results = []
+    for number, truth in ((float, bool), (np.float64, int)):
+        got = [torch.full_like(x, NAN) for _ in range(5)]
+        gg, g1, g2 = torch.full_like(gate, NAN), torch.full_like(w, NAN), torch.full_like(w, NAN)
+        robe.robe_dropout(x, got[0], number(0.25), 7, 8)
+        robe.robe_residual_forward(x, y, got[1], got[2], w, w, gate, number(0.5), 1, 1e-5, 0.1, 2, 3)
+        robe.robe_residual_backward(y, x, x, got[1], got[3], got[4], w, w, gate, g1, g2, gg, ws, number(0.5), 1, 1e-5, 0.1, 2, 3)
+        bias, grad_rows = torch.full((2, 3, 40, 90), NAN, device="cuda"), torch.full_like(rows, NAN)
+        robe.robe_bias_forward(b, rows, bias, start, truth(1))
+        robe.robe_bias_backward(b, bias.nan_to_num(neginf=1.0), grad_rows, ws, start, truth(1))
+        results.append(got + [gg, g1, g2, bias, grad_rows])
+    assert all(same_bits(p, q) for p, q in zip(*results))
+    assert not any(t.isnan().any() for t in results[0])
+    robe.robe_bias_destroy(b)
+
+
+@pytest.mark.parametrize("rows,d", [(5000, 4096), (40_000, 128), (300, 12_288)])
+def test_large_calls_are_captured(rows, d):
+    x, y = (torch.randn(rows, d, device="cuda").bfloat16() for _ in range(2))
+    w = torch.ones(d, device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    out, normed, gx, gr = (torch.empty_like(x) for _ in range(4))
+    g1, g2 = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    ws = torch.empty(robe.robe_residual_backward_workspace_bytes(rows, d), dtype=torch.uint8, device="cuda")
+
+    def both():
+        robe.robe_residual_forward(x, y, out, normed, w, w, None, 0.5, 0, 1e-6, 0.1, 5, 6, step)
+        robe.robe_residual_backward(y, x, x, out, gx, gr, w, w, None, g1, g2, None, ws, 0.5, 0, 1e-6, 0.1, 5, 6, step)
+
+    both()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (out, normed, gx, gr, g1, g2)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for t in (out, normed, gx, gr, g1, g2):
+        t.fill_(NAN)
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(same_bits(a, b) for a, b in zip(want, (out, normed, gx, gr, g1, g2)))
+    del g
+
+
 def test_two_streams_at_once_on_one_handle():
     b = robe.robe_bias_create(32, 128, True)
     g = [torch.randn(2, 4, 300, 300, generator=gen(n)).cuda() for n in range(2)]
