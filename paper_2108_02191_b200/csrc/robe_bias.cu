@@ -306,16 +306,22 @@ __global__ void __launch_bounds__(kGradMaxThreads, 3) bias_grad_kernel(BiasGradA
         int lo = rb0 > -(delta0 + 31) ? rb0 : -(delta0 + 31);  // squares of the warp's lanes
         int hi = rb1 < col_groups - delta0 ? rb1 : col_groups - delta0;
         if (a.causal && (int64_t)V * delta0 - (V - 1) - start > 0) hi = lo;
-        // [lo_in, hi_in): squares of whole rows whose pieces all lie within the tensor: not those of its first row (a piece may
-        // begin before it) nor of its last (a piece may end behind it), where pieces are not the rows' own
-        const int lo_in = !ALIGNED && n == 0 && h == 0 && lo < 1 ? 1 : lo;
-        int hi_in = (int)(a.q_len / V);
-        if ((!ALIGNED || a.k_len % V != 0) && n + 1 == a.batch && h + 1 == a.heads && a.q_len % V == 0) --hi_in;
-        if (hi_in > hi) hi_in = hi;
         const char* begin = (const char*)a.grad;
         const char* end = begin + (((int64_t)a.batch * a.heads * a.q_len - 1) * a.grad_ld + a.k_len) * (int64_t)sizeof(T);
         const char* matrix = begin + ((int64_t)n * a.heads + h) * a.q_len * a.grad_ld * (int64_t)sizeof(T);
         const int64_t step = a.grad_ld * (int64_t)sizeof(T);
+        // [lo_in, hi_in): squares of whole rows whose pieces all lie within the tensor.  Not those of its first row, where pieces
+        // are not the rows' own: one may begin before it.  (A square's rows are 16 bytes at least: the next squares' pieces
+        // do not.)  And none whose last row's last piece ends behind it: rows of few bytes reach that far from other
+        // squares than the last, and from other matrices.
+        const int lo_in = !ALIGNED && n == 0 && h == 0 && lo < 1 ? 1 : lo;
+        int hi_in = (int)(a.q_len / V);
+        if (hi_in > hi) hi_in = hi;
+        auto last_end = [&] {  // of the square above hi_in
+            const uintptr_t last = (uintptr_t)(matrix + ((int64_t)hi_in * V - 1) * step + (ALIGNED ? col_groups - 1 : col_groups) * 16ll);
+            return (last & ~(uintptr_t)15) + 16;
+        };
+        while (hi_in > lo_in && last_end() > (uintptr_t)end) --hi_in;
         uint4* mine = pieces + (size_t)warp * kGradStages * (V * kRow);
         auto copy = [&](uint4* to, const char* from, const char* row) {  // the aligned piece at `from`, if the row has part of it
             if (from + 16 <= row || from >= row + a.k_len * (int64_t)sizeof(T)) return;

@@ -231,6 +231,29 @@ def test_bias_backward_of_sequences_with_starts_of_their_own():
             robe.robe_bias_destroy(b)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k", range(1, 10))
+def test_bias_backward_of_few_keys_reads_its_tensor_alone(k, dtype):
+    # rows of a few bytes, several of which lie in one 16-byte piece: the pieces of the last matrices' rows end at the tensor's
+    # end (on the index-check build a copy that does not is recorded), which is also where its allocation may end
+    b = robe.robe_bias_create(*BUCKETS[0])
+    size = torch.finfo(dtype).bits // 8
+    for N, H, q in [(1, 1, 5), (1, 1, 9), (1, 3, 8), (2, 5, 9), (1, 2, 10), (1, 64, 9), (3, 2, 17), (1, 1, 18), (2, 2, 33), (1, 7, 4)]:
+        _, index = bias_case(H, q, k, BUCKETS[0], False, [q // 2 - k] * N, dtype)
+        g = torch.randn(N, H, q, k, generator=gen(q)).to(dtype)
+        want, bound = bias_grad_reference(g, index, 32)
+        ws = Workspace(robe.robe_bias_backward_workspace_bytes(b, H, N, q, k))
+        for begin in range(0, 16 // size, 3):  # where the tensor begins in a piece; what stands around it is NaN
+            around = torch.full((begin + g.numel() + 64,), NAN, dtype=dtype, device="cuda")
+            placed = around[begin:begin + g.numel()].view(g.shape)
+            placed.copy_(g)
+            got = blank((32, H), torch.float32)
+            robe.robe_bias_backward(b, placed, got, ws.own, q // 2 - k)
+            assert ws.kept_within()
+            ref.assert_within(got, want, bound, (N, H, q, begin))
+    robe.robe_bias_destroy(b)
+
+
 def test_bias_of_nothing():
     b = robe.robe_bias_create(32, 128, True)
     rows = torch.randn(32, 4, device="cuda")
