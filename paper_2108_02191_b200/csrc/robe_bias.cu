@@ -514,7 +514,7 @@ cudaError_t launch_bias_forward(const BiasProblem& pb, void* out, int64_t out_ld
         constexpr int kRow = kBiasThreads * kBiasRowPieces;
         a.k_tiles = (uint32_t)(((pb.k_len + V - 1 + V - 1) / V + kRow - 1) / kRow);  // (rows may begin inside a piece)
         const unsigned __int128 grid = (unsigned __int128)pb.batch * pb.heads * pb.q_len * a.k_tiles;
-        if (grid >= (1u << 31)) return cudaErrorInvalidValue;
+        if (grid >= (1u << 31)) return kGridTooSmall;
         if (dtype == 0) launch_next(bias_few_kernel<float>, (unsigned)grid, kBiasThreads, 0, st, a);
         else launch_next(bias_few_kernel<__nv_bfloat16>, (unsigned)grid, kBiasThreads, 0, st, a);
         return cudaGetLastError();
@@ -525,7 +525,7 @@ cudaError_t launch_bias_forward(const BiasProblem& pb, void* out, int64_t out_ld
     a.lanes_log2 = 0;
     while (a.lanes_log2 < 5 && (1 << a.lanes_log2) < pieces) ++a.lanes_log2;
     const unsigned __int128 grid = (unsigned __int128)pb.batch * pb.heads * a.q_tiles * a.k_tiles;
-    if (grid >= (1u << 31)) return cudaErrorInvalidValue;
+    if (grid >= (1u << 31)) return kGridTooSmall;
     if (dtype == 0) launch_next(bias_forward_kernel<float>, (unsigned)grid, kBiasThreads, 0, st, a);
     else launch_next(bias_forward_kernel<__nv_bfloat16>, (unsigned)grid, kBiasThreads, 0, st, a);
     return cudaGetLastError();
@@ -566,7 +566,7 @@ cudaError_t launch_bias_backward(const BiasProblem& pb, const void* grad, int64_
     a.grad_rows = grad_rows;
     a.grad_rows_ld = grad_rows_ld;
     const unsigned __int128 grid = (unsigned __int128)g.parts * pb.heads;
-    if (grid >= (1u << 31)) return cudaErrorInvalidValue;
+    if (grid >= (1u << 31)) return kGridTooSmall;
     const int64_t size = dtype == 0 ? 4 : 2;
     const bool aligned = ((uintptr_t)grad & 15u) == 0 && grad_ld * size % 16 == 0;
     const size_t smem = (size_t)kGradStages * g.lanes / 32 * V * (aligned ? 32 : 33) * 16;

@@ -190,7 +190,7 @@ cudaError_t launch_dropout(const void* in, int64_t in_ld, void* out, int64_t out
         const uint64_t elements = (uint64_t)rows * cols;
         const uint64_t tile = (uint64_t)kDropThreads * kFlatItems * (16 / size);
         const uint64_t grid = (elements + tile - 1) / tile;
-        if (grid >= (1ull << 31)) return cudaErrorInvalidValue;
+        if (grid >= (1ull << 31)) return kGridTooSmall;
         if (dtype == 0) launch_next(dropout_flat_kernel<float>, (unsigned)grid, kDropThreads, 0, st, a, elements, (uint64_t)cols);
         else launch_next(dropout_flat_kernel<__nv_bfloat16>, (unsigned)grid, kDropThreads, 0, st, a, elements, (uint64_t)cols);
         return cudaGetLastError();

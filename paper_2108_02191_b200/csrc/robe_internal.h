@@ -132,8 +132,9 @@ cudaError_t launch_dense_sgd_apply(float* array, float* grad, uint64_t m, float 
                                    cudaStream_t st);
 
 // ---- row operators (robe_dropout.cu, robe_bias.cu, robe_residual.cu); dtype as Problem::dtype, leading dimensions
-// (ld) in elements.  cudaErrorInvalidValue: more CTAs than a grid has.
+// (ld) in elements.  They return a runtime's error (which stays for cudaGetLastError or not), or kGridTooSmall.
 
+constexpr cudaError_t kGridTooSmall = (cudaError_t)-1;  // more CTAs than a grid has: nothing was launched; no code of the runtime's
 struct DropParams;
 cudaError_t launch_dropout(const void* in, int64_t in_ld, void* out, int64_t out_ld, int64_t rows, int64_t cols, int dtype,
                            const DropParams& drop, cudaStream_t st);

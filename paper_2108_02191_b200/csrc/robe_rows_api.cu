@@ -128,8 +128,8 @@ bool drop_params(float p, uint64_t seed, uint64_t offset, const uint64_t* step, 
 
 int rows_status(cudaError_t e) {
     if (e == cudaSuccess) return ROBE_OK;
-    if (e == cudaErrorInvalidValue) return ROBE_ERR_UNSUPPORTED;
-    (void)cudaGetLastError();
+    if (e == kGridTooSmall) return ROBE_ERR_UNSUPPORTED;
+    (void)cudaGetLastError();  // (a call that only asked or set something leaves its error there: the next launch would find it)
     return ROBE_ERR_CUDA;
 }
 

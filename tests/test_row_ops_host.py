@@ -2,6 +2,8 @@
 checks of the C ABI and of the binding."""
 import ctypes as C
 import math
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -230,6 +232,70 @@ def test_column_slices_of_one_matrix_do_not_overlap():
     assert go(0x100000 + 60) == BAD and go(0x100000 + 68) == BAD and go(0x100000 + 3 * 128 + 60) == BAD
     if not torch.cuda.is_available():  # a launch without a device is an error of its own, after all checks
         assert go(0x100000 + 64) == robe.ROBE_ERR_CUDA and go(0x100000 - 64) == robe.ROBE_ERR_CUDA
+
+
+STUBS = r"""
+#include <cuda_runtime.h>
+#include <cstdio>
+static cudaError_t told, left;  // what the helpers return, and the runtime's error that it leaves
+static cudaError_t take_left() {
+    const cudaError_t e = left;
+    left = cudaSuccess;
+    return e;
+}
+#define cudaGetLastError take_left
+#include "robe_rows_api.cu"
+namespace robe {
+// launch helpers that fail as told, the runtime's error left set as by a call that only asks or sets something
+cudaError_t fail() {
+    left = told == kGridTooSmall ? cudaSuccess : told;
+    return told;
+}
+cudaError_t launch_dropout(const void*, int64_t, void*, int64_t, int64_t, int64_t, int, const DropParams&, cudaStream_t) { return fail(); }
+cudaError_t launch_bias_forward(const BiasProblem&, void*, int64_t, int, cudaStream_t) { return fail(); }
+size_t bias_grad_workspace_bytes(uint32_t, uint32_t, int64_t, int64_t, int64_t) { return 0; }
+cudaError_t launch_bias_backward(const BiasProblem&, const void*, int64_t, int, float*, int64_t, void*, cudaStream_t) { return fail(); }
+cudaError_t launch_residual_forward(const ResidualProblem&, int, cudaStream_t) { return fail(); }
+size_t residual_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
+cudaError_t launch_residual_backward(const ResidualProblem&, int, void*, cudaStream_t) { return fail(); }
+}
+int main() {
+    char* p = (char*)0x100000;
+    float* w = (float*)(p + 0x10000);
+    robe_bias_t b;
+    robe_bias_create(&b, 32, 128, 0);
+    robe_residual_t c = {4, 8, ROBE_F32, 0, 1e-6f, 1.0f, 0, 0, 0.0f, 0, 0, nullptr};
+    const cudaError_t all[] = {cudaErrorInvalidValue, cudaErrorInvalidConfiguration, kGridTooSmall};
+    for (cudaError_t e : all) {
+        told = e;
+        for (int call = 0; call < 5; ++call) {
+            const int rc = call == 0   ? robe_dropout(p, 8, p + 4096, 8, 4, 8, ROBE_F32, 0.1f, 1, 2, nullptr, nullptr)
+                           : call == 1 ? robe_bias_forward(b, w, 4, 4, 1, 2, 8, 0, nullptr, 0, p, 8, ROBE_F32, nullptr)
+                           : call == 2 ? robe_bias_backward(b, p, 8, 4, 1, 2, 8, 0, nullptr, 0, ROBE_F32, w, 4, nullptr, 0, nullptr)
+                           : call == 3 ? robe_residual_forward(&c, p, 8, nullptr, 0, nullptr, 0, nullptr, nullptr, p + 4096, 8, nullptr, 0, nullptr)
+                                       : robe_residual_backward(&c, p, 8, nullptr, 0, p + 4096, 8, nullptr, 0, nullptr, 0, nullptr, nullptr,
+                                                                p + 8192, 8, nullptr, 0, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr);
+            printf("%d %d %d\n", (int)e, rc, (int)left);
+        }
+    }
+}
+"""
+
+
+def test_errors_of_the_runtime_are_told_from_a_grids_limit_and_not_left_behind(tmp_path):
+    # the C ABI's own source over launch helpers that fail: whatever the runtime answers is an error of its own, "unsupported"
+    # only what a grid does not hold, and no error stays for the call after
+    from paper_2108_02191_b200 import build
+    src, exe = tmp_path / "status.cu", str(tmp_path / "status")
+    src.write_text(STUBS)
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    subprocess.run([nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, "-o", exe, str(src)], check=True)
+    lines = subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split("\n")
+    got = [tuple(int(v) for v in line.split()) for line in lines if line]
+    assert len(got) == 15
+    for told, status, left in got:
+        assert status == (robe.ROBE_ERR_UNSUPPORTED if told == -1 else robe.ROBE_ERR_CUDA), (told, status)
+        assert left == 0, (told, left)
 
 
 # ---------------------------------------------------------------- the binding
