@@ -372,6 +372,60 @@ def test_residual_backward(rows, d, gate, post, pre, residual, p, dtype, layer):
             assert bits
 
 
+def whole_numbers(shape, most, seed, dtype=torch.float32):
+    """-most .. most without 0, on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = torch.randint(1, most + 1, shape, generator=g, device="cuda")
+    return (n * (2 * torch.randint(0, 2, shape, generator=g, device="cuda") - 1)).to(dtype)
+
+
+def exact_sums(rows, d, gate, dtype, layer, p, how):
+    """Rows of +-1 without eps: a norm is the row itself, and with weights after the join of 0 the gradients of weights and gates are
+    sums of whole numbers, none of them 0 without dropout: a row that is lost or taken twice shows in every column."""
+    assert float((torch.tensor(1.0) / d) * d) == 1.0  # (the kernels multiply by 1 / d)
+    if layer:  # as many of either sign in a row
+        assert d % 2 == 0
+        columns = 1.0 - 2.0 * (torch.arange(d, device="cuda") % 2)
+        x, out = (whole_numbers((rows, 1), 1, n) * columns for n in (1, 2))
+    else:
+        x, out = (whole_numbers((rows, d), 1, n) for n in (1, 2))
+    x, out = x.to(dtype), out.to(dtype)
+    t, gn = whole_numbers((rows, d), 3, 3, dtype), whole_numbers((rows, d), 3, 4, dtype)
+    shape = {"none": None, "row": (rows, 1)}.get(gate, (rows // gate, d) if isinstance(gate, int) else None)
+    g = whole_numbers(shape, 2, 5, dtype) if shape else None
+    w_post, w_pre = whole_numbers((d,), 2, 6), torch.zeros(d, device="cuda")
+    got = {"w_post": blank((d,), torch.float32), "w_pre": blank((d,), torch.float32),
+           "gate": blank(shape, dtype, how) if shape else None}
+    ws = Workspace(robe.robe_residual_backward_workspace_bytes(rows, d, rows // gate if isinstance(gate, int) else 0))
+    robe.robe_residual_backward(place(t, how), place(gn, how), place(x, how), place(out, how), blank((rows, d), dtype, how),
+                                blank((rows, d), dtype, how), w_post, w_pre, place(g, how), got["w_post"], got["w_pre"], got["gate"],
+                                ws.own, 0.5, layer, 0.0, p, 7, 8)
+    assert ws.kept_within()
+    assert torch.equal(got["w_pre"].double(), (gn * out).sum(0, dtype=torch.float64))
+    s = 0.5 * t.float() * x.float()
+    if p:  # (a half is dropped: twice what is kept)
+        s = torch.where(ref.kept(rows, d, p, 7, 8).cuda(), ref.drop_scale(p) * s, torch.zeros((), device="cuda"))
+    per = gate if isinstance(gate, int) else 1
+    of_rows = s if g is None else s * g.float().repeat_interleave(per, 0)
+    assert torch.equal(got["w_post"].double(), of_rows.sum(0, dtype=torch.float64))
+    if g is not None:
+        s = s * w_post
+        want = s.sum(1, keepdim=True, dtype=torch.float64) if gate == "row" else s.reshape(-1, per, d).sum(1, dtype=torch.float64)
+        assert torch.equal(got["gate"].double(), want.to(dtype).double())
+
+
+@pytest.mark.parametrize("how", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,gate,layer,p", [
+    (1, 8, 1, 0, 0.0), (20_000, 5, 1, 0, 0.0), (20_001, 5, "none", 0, 0.0), (12_000, 8, 2, 0, 0.0), (120_000, 8, 2, 1, 0.0),
+    (6080, 24, 10, 0, 0.0), (1500, 40, 750, 0, 0.0), (1201, 12, "none", 1, 0.0), (31_003, 100, "row", 1, 0.0), (50_000, 128, 1000, 0, 0.0),
+    (41_041, 136, 41, 0, 0.0), (7001, 257, "none", 0, 0.0), (9999, 520, 3, 0, 0.0), (2900, 520, 29, 0, 0.5), (3000, 1024, 1500, 0, 0.0),
+    (2003, 4096, "none", 1, 0.0), (4097, 264, 17, 0, 0.5), (500, 8200, 250, 0, 0.0), (449, 8200, "row", 0, 0.5), (300, 12_288, 1, 0, 0.0),
+    (400, 20_001, 8, 0, 0.0), (297, 30_000, "none", 0, 0.5)])
+def test_residual_sums_of_whole_numbers(rows, d, gate, layer, p, dtype, how):
+    exact_sums(rows, d, gate, dtype, layer, p, how)
+
+
 @pytest.mark.parametrize("rows,d,gate", [(50, 128, "none"), (6, 4096, 1), (5, 213, "row"), (2, 20_001, "none")])
 def test_residual_in_place(rows, d, gate):
     # the sum over the residual, the residual's gradient over the output's: the same bits as into buffers of their own
