@@ -540,7 +540,8 @@ int robe_residual_forward(const robe_residual_t* c, const void* x, int64_t x_ld,
  * weights' gradients with +0 when rows is 0).  grad_residual may be grad_out itself (same pointer, same ld).
  *   gates      rows of the gate for ROBE_GATE_VECTOR, 0 otherwise
  *   workspace  256-byte aligned, robe_residual_backward_workspace_bytes(rows, d, gates)
- * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_WORKSPACE, ROBE_ERR_CUDA.
+ * Sums over rows are fp32 sums of at most 256 rows a thread, joined over at most 256 threads in fp32 and beyond in fp64.
+ * Errors of both: ROBE_ERR_INVALID_ARG, ROBE_ERR_CUDA; of the backward also ROBE_ERR_WORKSPACE, ROBE_ERR_UNSUPPORTED.
  */
 size_t robe_residual_backward_workspace_bytes(int64_t rows, int64_t d, int64_t gates);
 int robe_residual_backward(const robe_residual_t* c, const void* grad_out, int64_t grad_out_ld,

@@ -1102,9 +1102,13 @@ int64_t groups_of(int64_t d) {
     return kWarpRowThreads / lanes;
 }
 
-// gates: gate vectors of more than one row that the rows share, or 0; vector: there is a gate of d columns at all.  The
-// workspace is sized by the same call.
-Chunks chunks_of(int64_t rows, int64_t d, int64_t gates, bool vector) {
+// Rows that a thread sums in fp32 at most, whatever the call's: a sum of n like terms is off by up to n / 2 of its last places, and
+// from 2^24 on takes nothing in.  The chunks' sums are joined in 64 bits.
+constexpr int64_t kChainRows = 256;
+
+// gates: gate vectors of more than one row that the rows share, or 0; vector: there is a gate of d columns at all; again: for the
+// kernel that reads rows again.  The workspace is sized by the same call.
+Chunks chunks_of(int64_t rows, int64_t d, int64_t gates, bool vector, bool again) {
     int64_t most = resident_chunks(d, vector);
     // .. but four rows of each beyond two a SM: fewer chunks' sums to join (1578 rows of 312 fp32 36 -> 26 us, 2000 of 1024 bf16
     // 34 -> 27)
@@ -1114,16 +1118,23 @@ Chunks chunks_of(int64_t rows, int64_t d, int64_t gates, bool vector) {
     k.gate_rows = gates > 0 ? rows / gates : rows;
     k.per_gate = k.gates = k.length = k.count = 0;
     if (rows == 0) return k;
+    // groups that are sure to share a chunk's rows (at least 8 lanes a row where pieces are of one element)
+    const int64_t sharing = again ? 1 : groups_of(d) < kWarpRowThreads / 8 ? groups_of(d) : kWarpRowThreads / 8;
     // whole gate vectors, each by one of a CTA's groups, where there are enough for half of the groups; else a CTA's groups
     // share one vector's rows (608 vectors of 660 rows of 136: 947 us the first way)
-    if (gates == 0 || 2 * gates < most * groups_of(d)) {
+    if (gates == 0 || 2 * gates < most * groups_of(d) || k.gate_rows > kChainRows) {
         k.per_gate = gates == 0 ? most : gates < most ? most / gates : 1;
         k.length = (k.gate_rows + k.per_gate - 1) / k.per_gate;
         if (k.length < groups_of(d)) k.length = groups_of(d);  // (a row for each of a CTA's groups)
+        // longer than a chain: so many times the chunks, all alike
+        const int64_t times = (k.length + kChainRows * sharing - 1) / (kChainRows * sharing);
+        k.length = (k.length + times - 1) / times;
         k.per_gate = (k.gate_rows + k.length - 1) / k.length;
         k.count = (gates > 0 ? gates : 1) * k.per_gate;
     } else {
         k.gates = (gates + most - 1) / most;
+        const int64_t chain = kChainRows / k.gate_rows * sharing, times = (k.gates + chain - 1) / chain;
+        k.gates = (k.gates + times - 1) / times;
         k.length = k.gates * k.gate_rows;
         k.count = (rows + k.length - 1) / k.length;
     }
@@ -1250,11 +1261,12 @@ cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaSt
 
 size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates) {
     if (rows <= 0 || d <= 0) return 0;
-    int64_t count = 0;  // (enough for a gate per row, per element, or none alike)
-    for (const bool vector : {false, true}) {
-        const int64_t n = chunks_of(rows, d, gates < rows ? gates : 0, vector).count;
-        if (n > count) count = n;
-    }
+    int64_t count = 0;  // (enough for a gate per row, per element, or none alike, and for either kernel)
+    for (const bool vector : {false, true})
+        for (const bool again : {false, true}) {
+            const int64_t n = chunks_of(rows, d, gates < rows ? gates : 0, vector, again).count;
+            if (n > count) count = n;
+        }
     const unsigned __int128 bytes = (unsigned __int128)count * d * sizeof(float) * 3;
     if (bytes >= ((unsigned __int128)1 << 62)) return (size_t)1 << 62;
     return ((size_t)bytes + 255) / 256 * 256;
@@ -1316,14 +1328,25 @@ cudaError_t launch_backward_rows(const JoinGradArgs& a, const RowPlan& p, cudaSt
 cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void* workspace, cudaStream_t st) {
     JoinGradArgs a;
     a.p = pb;
-    a.chunks = chunks_of(pb.rows, pb.d, pb.gate_kind == 2 && pb.gate_rows > 1 ? pb.rows / pb.gate_rows : 0, pb.gate_kind == 2);
-    a.part_post = (float*)workspace;
-    a.part_pre = a.part_post + a.chunks.count * pb.d;
-    a.part_gate = a.part_pre + a.chunks.count * pb.d;
-    cudaError_t e = cudaSuccess;
     const RowPlan p = row_plan(pb, {pb.x, pb.grad_out, pb.out, pb.grad_normed, pb.gate_kind == 2 ? pb.gate : RowsRef{}, pb.grad_x,
                                     pb.grad_residual, pb.gate_kind == 2 ? pb.grad_gate : RowsRef{}},
                                dtype == 0 ? 4 : 2, kGradWarpElems, dtype == 1);
+    a.chunks = chunks_of(pb.rows, pb.d, pb.gate_kind == 2 && pb.gate_rows > 1 ? pb.rows / pb.gate_rows : 0, pb.gate_kind == 2,
+                         p.lanes == 0);
+    a.part_post = (float*)workspace;
+    a.part_pre = a.part_post + a.chunks.count * pb.d;
+    a.part_gate = a.part_pre + a.chunks.count * pb.d;
+    ColumnArgs c;
+    c.j = a;
+    c.weights = (pb.w_post != nullptr) + (pb.w_pre != nullptr);
+    c.weight_tiles = (uint32_t)((pb.d + kColumnThreads / 16 - 1) / (kColumnThreads / 16));
+    c.gate_share = a.chunks.per_gate > 64 ? 16 : 2;
+    c.gate_tiles = (uint32_t)((pb.d + kColumnThreads / c.gate_share - 1) / (kColumnThreads / c.gate_share));
+    int64_t grid = (int64_t)c.weights * c.weight_tiles;
+    if (pb.gate_kind == 2 && pb.gate_rows > 1 && pb.grad_gate.p != nullptr && a.chunks.per_gate > 0)
+        grid += pb.rows / pb.gate_rows * c.gate_tiles;
+    if (grid >= (1ll << 31)) return kGridTooSmall;
+    cudaError_t e = cudaSuccess;
     if (a.chunks.count == 0) {
     } else if (p.lanes > 0) {
         if (dtype == 0)
@@ -1342,15 +1365,6 @@ cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void*
                        : launch_backward_any<__nv_bfloat16, false>(a, st);
     }
     if (e != cudaSuccess) return e;
-    ColumnArgs c;
-    c.j = a;
-    c.weights = (pb.w_post != nullptr) + (pb.w_pre != nullptr);
-    c.weight_tiles = (uint32_t)((pb.d + kColumnThreads / 16 - 1) / (kColumnThreads / 16));
-    c.gate_share = a.chunks.per_gate > 64 ? 16 : 2;
-    c.gate_tiles = (uint32_t)((pb.d + kColumnThreads / c.gate_share - 1) / (kColumnThreads / c.gate_share));
-    int64_t grid = (int64_t)c.weights * c.weight_tiles;
-    if (pb.gate_kind == 2 && pb.gate_rows > 1 && pb.grad_gate.p != nullptr && a.chunks.per_gate > 0)
-        grid += pb.rows / pb.gate_rows * c.gate_tiles;
     if (grid > 0) {
         if (dtype == 0) launch_next(residual_columns_kernel<float>, (unsigned)grid, kColumnThreads, 0, st, c);
         else launch_next(residual_columns_kernel<__nv_bfloat16>, (unsigned)grid, kColumnThreads, 0, st, c);

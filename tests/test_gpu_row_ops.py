@@ -561,6 +561,23 @@ def test_bias_of_more_than_2_to_31_places():
     robe.robe_bias_destroy(b)
 
 
+@pytest.mark.parametrize("rows,d,scale", [(148 * 16 * 2000, 264, 1.01922607421875), (148 * 1600, 8200, 1.27313232421875)])
+def test_residual_sums_of_many_rows(rows, d, scale):
+    # ones without eps, all terms are the scale: a single sum of 1600 of this one in fp32 is off by 400 U, of 2000 of that by 500 U.
+    # 256 rows in fp32 (256 U), the rest in 64 bits, one rounding of the sum, one of a gate's scale
+    room(3 * rows * d * 4 >> 30)
+    x = torch.ones(rows, d, device="cuda")
+    gx, w, gate = torch.empty_like(x), torch.ones(d, device="cuda"), torch.ones(4, d, device="cuda")
+    for gates in (0, 4):
+        gw, gg = torch.empty(d, device="cuda"), torch.empty_like(gate)
+        ws = torch.empty(robe.robe_residual_backward_workspace_bytes(rows, d, gates), dtype=torch.uint8, device="cuda")
+        robe.robe_residual_backward(x, None, x, None, gx, None, w, None, gate if gates else None, gw, None, gg if gates else None, ws,
+                                    scale, 0, 0.0)
+        for got, terms in [(gw, rows)] + ([(gg, rows // 4)] if gates else []):
+            off = (got.double() - terms * scale).abs().max() / (terms * scale)
+            assert off <= 258 * ref.U, (gates, terms, float(off) / ref.U)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_bias_of_long_rows(dtype):
     # several CTAs along a row, both ways, and a gradient whose diagonals are cut in chunks

@@ -224,6 +224,27 @@ def test_residual_arguments():
     assert robe.robe_residual_backward_workspace_bytes(-1, 16, 0) == 0
 
 
+@pytest.mark.parametrize("rows,d,gates", [(530_000, 4096, 0), (1 << 32, 300, 0), (1 << 32, 1 << 20, 0), (1 << 28, 512, 4), (1 << 28, 512, 1 << 19),
+                                          (1 << 28, 512, 1 << 22), (1 << 30, 8, 0), (1 << 30, 8, 1 << 15), (1 << 30, 100, 1 << 29)])
+def test_residual_sums_are_cut_so_that_no_thread_adds_up_many_rows(rows, d, gates):
+    # the sums of every chunk are in the workspace, three of d fp32 each.  Rows of over 256 elements are one thread's after the
+    # other; of shorter ones at least a 32nd of a chunk's
+    chunks = robe.robe_residual_backward_workspace_bytes(rows, d, gates) // (12 * d)
+    assert chunks * 256 * (1 if d > 256 else 32) >= rows
+    assert chunks * 12 * d * 16 <= rows * d * 6  # and stay a small part of the call's tensors
+
+
+def test_residual_beyond_a_grid():
+    # the joining kernel would have 2^23 gate vectors of 2^12 CTAs each; (addresses are never reached)
+    rows, d = 1 << 32, 1 << 20
+    at = lambda k: C.c_void_p(k << 55)
+    c = robe.binding._Residual(rows, d, 1, 0, 1e-6, 1.0, 2, 512, 0.0, 0, 0, None)
+    need = robe.robe_residual_backward_workspace_bytes(rows, d, rows // 512)
+    rc = lib().robe_residual_backward(C.byref(c), at(1), d, None, 0, at(2), d, None, 0, at(3), d, None, None, at(4), d, None, 0, at(5), d,
+                                      None, None, at(6), need, None)
+    assert rc == robe.ROBE_ERR_UNSUPPORTED
+
+
 def test_column_slices_of_one_matrix_do_not_overlap():
     # rows of [8, 32]: the first 16 columns and the last 16; one column in common is refused
     c = robe.binding._Residual(8, 16, 0, 0, 1e-6, 1.0, 0, 0, 0.0, 1, 2, None)
