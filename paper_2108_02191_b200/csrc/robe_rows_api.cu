@@ -191,6 +191,9 @@ bool residual_problem(const robe_residual_t* c, ResidualProblem& pb, int64_t& ga
     return drop_params(c->p, c->seed, c->offset, c->step, pb.drop);
 }
 
+// the counter that dropout's decisions go by: read by every CTA when it starts
+Span counter(const uint64_t* step) { return Span{step, 1, step != nullptr, 1, 8}; }
+
 RowsRef ref(const Span& s) { return RowsRef{(void*)s.p, s.ld}; }
 
 }  // namespace robe_rows_api_detail
@@ -201,9 +204,10 @@ extern "C" {
 int robe_dropout(const void* in, int64_t in_ld, void* out, int64_t out_ld, int64_t rows, int64_t cols,
                  int dtype, float p, uint64_t seed, uint64_t offset, const uint64_t* step, void* stream) {
     if (!type_ok(dtype) || rows < 0 || cols < 0 || rows > (1ll << 32) || cols > (1ll << 31)) return ROBE_ERR_INVALID_ARG;
-    const Span from{in, in_ld, rows, cols, size_of(dtype)}, to{out, out_ld, rows, cols, size_of(dtype)};
+    const Span from{in, in_ld, rows, cols, size_of(dtype)}, to{out, out_ld, rows, cols, size_of(dtype)}, at = counter(step);
     Checked c;
     c.reads(from);
+    c.reads(at);
     c.writes(to);
     DropParams drop;
     if (!c.ok(&to, &from) || !drop_params(p, seed, offset, step, drop)) return ROBE_ERR_INVALID_ARG;
@@ -315,9 +319,9 @@ int robe_residual_forward(const robe_residual_t* c, const void* x, int64_t x_ld,
     const int64_t n = c->rows, d = c->d, e = size_of(c->dtype);
     const Span sx{x, x_ld, n, d, e}, sr{residual, residual_ld, residual != nullptr ? n : 0, d, e},
         sg{gate, gate_ld, gates, gate_cols, e}, s1{w_post, d, w_post != nullptr, d, 4}, s2{w_pre, d, w_pre != nullptr, d, 4},
-        so{out, out_ld, n, d, e}, sn{normed, normed_ld, w_pre != nullptr ? n : 0, d, e};
+        so{out, out_ld, n, d, e}, sn{normed, normed_ld, w_pre != nullptr ? n : 0, d, e}, at = counter(c->step);
     Checked k;
-    for (const Span* s : {&sx, &sr, &sg, &s1, &s2}) k.reads(*s);
+    for (const Span* s : {&sx, &sr, &sg, &s1, &s2, &at}) k.reads(*s);
     for (const Span* s : {&so, &sn}) k.writes(*s);
     if (!k.ok(&so, &sr)) return ROBE_ERR_INVALID_ARG;
     if (n == 0) return ROBE_OK;
@@ -357,13 +361,13 @@ int robe_residual_backward(const robe_residual_t* c, const void* grad_out, int64
         s1{w_post, d, w_post != nullptr, d, 4}, s2{w_pre, d, w_pre != nullptr, d, 4},
         gx{grad_x, grad_x_ld, n, d, e}, gr{grad_residual, grad_residual_ld, grad_residual != nullptr ? n : 0, d, e},
         gg{grad_gate, grad_gate_ld, grad_gate != nullptr ? gates : 0, gate_cols, e},
-        g1{grad_w_post, d, grad_w_post != nullptr, d, 4}, g2{grad_w_pre, d, grad_w_pre != nullptr, d, 4};
+        g1{grad_w_post, d, grad_w_post != nullptr, d, 4}, g2{grad_w_pre, d, grad_w_pre != nullptr, d, 4}, at = counter(c->step);
     const size_t need = residual_workspace_bytes(n, d, c->gate == ROBE_GATE_VECTOR ? gates : 0);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return ROBE_ERR_WORKSPACE;
     if (((uintptr_t)workspace & 255u) != 0) return ROBE_ERR_WORKSPACE;
     const Span scratch{workspace, 1, 1, need < ((size_t)1 << 60) ? (int64_t)need : 0, 1};
     Checked k;
-    for (const Span* s : {&sgo, &sgn, &sx, &so, &sg, &s1, &s2}) k.reads(*s);
+    for (const Span* s : {&sgo, &sgn, &sx, &so, &sg, &s1, &s2, &at}) k.reads(*s);
     for (const Span* s : {&gx, &gr, &gg, &g1, &g2, &scratch}) k.writes(*s);
     if (!k.ok(&gr, &sgo)) return ROBE_ERR_INVALID_ARG;
     pb.w_post = w_post;

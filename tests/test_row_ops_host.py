@@ -224,6 +224,21 @@ def test_residual_arguments():
     assert robe.robe_residual_backward_workspace_bytes(-1, 16, 0) == 0
 
 
+def test_a_step_counter_within_what_a_call_writes_is_refused():
+    # every CTA reads the counter when it starts, others have written by then
+    at = lambda k: C.c_void_p(0x100000 * k)
+    assert lib().robe_dropout(at(1), 16, at(2), 16, 8, 16, 0, 0.1, 1, 2, 0x200000 + 504, None) == BAD
+    assert lib().robe_dropout(at(1), 16, at(1), 16, 8, 16, 0, 0.1, 1, 2, 0x100000, None) == BAD  # in place too
+    for step in (0x600000, 0x700008):  # out, normed
+        c = robe.binding._Residual(8, 16, 0, 0, 1e-6, 1.0, 0, 0, 0.1, 1, 2, step)
+        assert lib().robe_residual_forward(C.byref(c), at(1), 16, at(2), 16, None, 0, at(4), at(5), at(6), 16, at(7), 16, None) == BAD
+    need = robe.robe_residual_backward_workspace_bytes(8, 16, 0)
+    for step in (0x800000, 0x900100, 0xB00000, 0xC00038, 0xD00000 + need - 8):  # gradients of x, residual, both weights; workspace
+        c = robe.binding._Residual(8, 16, 0, 0, 1e-6, 1.0, 0, 0, 0.1, 1, 2, step)
+        assert lib().robe_residual_backward(C.byref(c), at(1), 16, at(2), 16, at(3), 16, at(4), 16, None, 0, at(6), at(7), at(8), 16,
+                                            at(9), 16, None, 0, at(11), at(12), at(13), need, None) == BAD
+
+
 @pytest.mark.parametrize("rows,d,gates", [(530_000, 4096, 0), (1 << 32, 300, 0), (1 << 32, 1 << 20, 0), (1 << 28, 512, 4), (1 << 28, 512, 1 << 19),
                                           (1 << 28, 512, 1 << 22), (1 << 30, 8, 0), (1 << 30, 8, 1 << 15), (1 << 30, 100, 1 << 29)])
 def test_residual_sums_are_cut_so_that_no_thread_adds_up_many_rows(rows, d, gates):
