@@ -533,7 +533,8 @@ int robe_residual_forward(const robe_residual_t* c, const void* x, int64_t x_ld,
  * gradients of out (NULL: zero) and normed (given exactly when w_pre is):
  *     t = grad_out + dnorm(out; grad_normed w_pre)     grad_residual = t         (NULL: not wanted)
  *     u = dropout(scale * gate * t)                    grad_x = dnorm(x; u w_post)   (u without w_post)
- *     grad_gate = sum of scale * dropout(y) * t over what a gate element was used for   (NULL: not wanted)
+ *     grad_gate = sum of scale * dropout(y) * t over what a gate element was used for   (NULL: not wanted;
+                    a dropped element adds +0, whatever t is there)
  *     grad_w_post = sum over rows of u norm(x)         grad_w_pre = sum over rows of grad_normed norm(out)
  * with dnorm(v; g) = rstd (g - [mean g] - n mean(g n)), n = norm(v), rstd its factor, [..] with layer norm.
  * grad_w_post and grad_w_pre are given exactly when their weights are; all outputs are overwritten (the

@@ -679,7 +679,8 @@ __global__ void __launch_bounds__(kAnyThreads, 1) residual_grad_any_kernel(JoinG
             drop_eight_of(y, a, words);
             drop_eight_of(u, a, words);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) gg[k] = y[k] * (a.scale * t[k]);
+            for (int k = 0; k < 8; ++k)  // (of what is dropped +0, whatever t is there)
+                gg[k] = a.drop.none || drop_keeps(words, k, a.drop) ? y[k] * (a.scale * t[k]) : 0.0f;
         };
         float dot = 0.0f, sum = 0.0f, gate_sum = 0.0f;
         if (a.w_post != nullptr || a.gate_kind == 1)

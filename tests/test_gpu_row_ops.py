@@ -463,6 +463,30 @@ def test_residual_gate_and_block_output_from_one_projection():
         ref.assert_within(got, *want[name], name)
 
 
+@pytest.mark.parametrize("how", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("rows,d,gate", [(40, 64, "row"), (40, 64, 1), (40, 64, 4), (12, 4096, 1), (12, 4096, "row"), (6, 20_001, "row"),
+                                         (6, 20_001, 1), (6, 20_001, 3), (4, 30_000, 2)])
+def test_residual_backward_of_what_is_not_a_number_where_it_is_dropped(rows, d, gate, post, dtype, how):
+    # the block's and the gate's gradients are as if there were zeros; the residual's is what came in
+    t = join_inputs(rows, d, dtype, gate, post, False, True, 3)
+    keep = ref.kept(rows, d, 0.5, 5, 9)
+    go = torch.randn(rows, d, generator=gen(4)).to(dtype)
+    results = []
+    for fill in (0.0, NAN, math.inf):
+        g = torch.where(keep, go, torch.tensor(fill, dtype=dtype))
+        gx, gr, gg = blank((rows, d), dtype, how), blank((rows, d), dtype, how), blank(tuple(t["gate"].shape), dtype, how)
+        gw = blank((d,), torch.float32) if post else None
+        ws = Workspace(robe.robe_residual_backward_workspace_bytes(rows, d, rows // gate if gate != "row" else 0))
+        robe.robe_residual_backward(place(g, how), None, place(t["x"], how), None, gx, gr, place(t["w_post"]), None,
+                                    place(t["gate"], how), gw, None, gg, ws.own, 0.7, 0, 1e-5, 0.5, 5, 9)
+        torch.testing.assert_close(gr.cpu(), g, rtol=0, atol=0, equal_nan=True)  # (a NaN rounded to bf16 has other bits)
+        results.append([gx.cpu(), gg.cpu()] + ([gw.cpu()] if post else []))
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
 def test_residual_of_no_rows():
     for d in (16, 4096):
         e = torch.empty(0, d, device="cuda")
