@@ -426,6 +426,16 @@ def test_residual_sums_of_whole_numbers(rows, d, gate, layer, p, dtype, how):
     exact_sums(rows, d, gate, dtype, layer, p, how)
 
 
+@pytest.mark.parametrize("how", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,gate", [(480_000, 264, 100), (700_001, 264, "none"), (330_000, 264, 275), (3_700_003, 8, "none"),
+                                         (3_700_000, 5, "row"), (2_000_000, 12, 250), (29_700, 8200, 100), (22_500, 8200, 300),
+                                         (40_001, 8200, "none")])
+def test_residual_sums_of_whole_numbers_in_chunks_cut_by_their_length(rows, d, gate, dtype, how):
+    room(12 * rows * d * 4 + (4 << 30) >> 30)
+    exact_sums(rows, d, gate, dtype, 0, 0.0, how)
+
+
 @pytest.mark.parametrize("rows,d,gate", [(50, 128, "none"), (6, 4096, 1), (5, 213, "row"), (2, 20_001, "none")])
 def test_residual_in_place(rows, d, gate):
     # the sum over the residual, the residual's gradient over the output's: the same bits as into buffers of their own
