@@ -343,7 +343,7 @@ PyObject* backward_adam(PyObject*, PyObject* const* args, Py_ssize_t n) {
     float* m2 = (float*)r.data_or_null(6, at::kFloat);
     const float lr = r.number(7), beta1 = r.number(8), beta2 = r.number(9), eps = r.number(10);
     const int64_t step = r.whole(11);
-    void* ws = r.workspace(12, ws_bytes);
+    void* ws = r.bytes_or_null(12, ws_bytes);
     void* st = r.stream(13);
     if (!r.ok) return not_taken();
     return made([&] {

@@ -79,3 +79,11 @@ def test_index_check_run_picks_every_test_of_a_kernel_path():
     left = {t for t in tests if not any(w.strip() in t for w in words)}
     assert {t for t in left if not re.search(r"full_size|full_batch|whole_array|reduced_batch|cfg5|cfg2|errors|refuse|validate|empty|share_one_array|"
                                              r"bf16|huge_ids|max_array|many_tables_and_large", t)} == set()
+
+
+def test_lookup_calls_read_their_workspaces_alike():
+    # a workspace of the lookup's backward may be on any device that the handle's array is on, whatever the current one; only the
+    # row operators ask for the current device
+    text = open(os.path.join(CSRC, "robe_py.cpp")).read()
+    calls = text[text.index("PyObject* forward("):text.index("PyObject* dropout(")]
+    assert calls.count("r.bytes_or_null(") == 4 and "r.workspace(" not in calls
