@@ -1230,7 +1230,7 @@ cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cud
 template <class T, int V>
 cudaError_t launch_forward_rows(const ResidualProblem& pb, const RowPlan& p, cudaStream_t st) {
     constexpr int kSmall = V * sizeof(T) < 16 ? 8 : kRowElems;
-    if (!p.cta) return p.elems == 8 ? launch_forward_rows<T, V, kSmall, false>(pb, p, st) : launch_forward_rows<T, V, kRowElems, false>(pb, p, st);
+    if (!p.cta) return launch_forward_rows<T, V, kSmall, false>(pb, p, st);  // (rows this short: small pieces always take 8)
     if constexpr (V * sizeof(T) == 16)
         if (p.elems == 2 * kRowElems) return launch_forward_rows<T, V, 2 * kRowElems, true>(pb, p, st);
     return p.elems == 8 ? launch_forward_rows<T, V, kSmall, true>(pb, p, st) : launch_forward_rows<T, V, kRowElems, true>(pb, p, st);
