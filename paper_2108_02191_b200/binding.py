@@ -551,6 +551,11 @@ def robe_residual_backward(grad_out, grad_normed, x, out, grad_x, grad_residual=
         *like(grad_residual, "grad_residual"), *_matrix_like(grad_gate, "grad_gate", x.dtype, *gate_size),
         _vector(grad_w_post, "grad_w_post", c.d), _vector(grad_w_pre, "grad_w_pre", c.d), *_workspace(workspace),
         _stream_ptr(stream)), "robe_residual_backward")
+    if c.rows == 0 and grad_gate is not None and grad_gate.numel() > 0:
+        # gate vectors of no rows each, which the C ABI (rows / gate_rows of them) does not know of: everything dropped is zeros
+        p_gate, ld, rows, cols = _matrix(grad_gate, "grad_gate")
+        _check(_lib.robe_dropout(p_gate, ld, p_gate, ld, rows, cols, c.dtype, 1.0, 0, 0, None, _stream_ptr(stream)),
+               "robe_residual_backward")
 
 
 def robe_debug_status(stream=None) -> int:

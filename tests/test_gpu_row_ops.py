@@ -507,6 +507,21 @@ def test_residual_of_no_rows():
         assert torch.equal(g1, torch.zeros_like(g1)) and torch.equal(g2, torch.zeros_like(g2))
 
 
+@pytest.mark.parametrize("how", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_residual_gate_vectors_of_no_rows(dtype, how):
+    # sequences of length zero, a gate vector each: the gates' gradients are zero, not what stood there
+    e = torch.empty(0, 21, dtype=dtype, device="cuda")
+    gate, gg = place(torch.ones(5, 21, dtype=dtype), how), blank((5, 21), dtype, how)
+    w, gw = torch.ones(21, device="cuda"), torch.full((21,), NAN, device="cuda")
+    robe.robe_residual_forward(e, e, e.clone(), None, w, None, gate)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    robe.robe_residual_backward(e, None, e, None, e.clone(), None, w, None, gate, gw, None, gg, stream=side)
+    side.synchronize()
+    assert same_bits(gg, torch.zeros_like(gg)) and surroundings_kept(gg) and same_bits(gw, torch.zeros_like(gw))
+
+
 def test_residual_rows_of_zeros_and_of_infinities():
     # eps alone under the root; an infinite element makes its own row NaN and no other
     x = torch.randn(6, 128, generator=gen(3))
