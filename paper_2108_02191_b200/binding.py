@@ -460,6 +460,8 @@ def _starts(q_start, batch):
     """(start of all, pointer to starts)"""
     if isinstance(q_start, torch.Tensor):
         return 0, _vector(q_start, "q_start", batch, torch.int64)
+    if not -2**63 <= q_start < 2**63:  # (ctypes would take it modulo 2^64)
+        raise ValueError(f"q_start: {q_start} is beyond 64 bits")
     return q_start, None
 
 
@@ -476,6 +478,8 @@ def robe_bias_forward(b, rows, out, q_start=0, causal: bool = False, stream=None
 
 
 def robe_bias_backward_workspace_bytes(b, heads: int, batch: int, q_len: int, k_len: int) -> int:
+    if not (0 <= heads < 2**32 and all(-2**63 <= n < 2**63 for n in (batch, q_len, k_len))):
+        return 0
     return int(_lib.robe_bias_backward_workspace_bytes(b, heads, batch, q_len, k_len))
 
 
@@ -506,6 +510,8 @@ def _residual(x, gate, scale, norm, eps, p, seed, offset, step):
         else:
             raise ValueError(f"gate: {g_rows} rows of {g_cols} for {rows} rows of {d}")
         gate_at, gate_size = (g_ptr, g_ld), (g_rows, g_cols)
+    if norm not in (ROBE_NORM_RMS, ROBE_NORM_LAYER):
+        raise RobeError(ROBE_ERR_INVALID_ARG, "norm")
     c = _Residual(rows, d, _TYPES[x.dtype], norm, eps, scale, kind, gate_rows, p, seed & (2**64 - 1),
                   offset & (2**64 - 1), _step_ptr(step))
     return c, (ptr, ld), gate_at, gate_size
@@ -529,6 +535,8 @@ def robe_residual_forward(x, residual, out, normed=None, w_post=None, w_pre=None
 
 def robe_residual_backward_workspace_bytes(rows: int, d: int, gates: int = 0) -> int:
     """gates: rows of a gate of [rows / k, d]; 0 for no gate or one of [rows, 1]."""
+    if not all(-2**63 <= n < 2**63 for n in (rows, d, gates)):
+        return 0
     return int(_lib.robe_residual_backward_workspace_bytes(rows, d, gates))
 
 

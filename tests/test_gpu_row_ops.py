@@ -755,6 +755,26 @@ def test_refusals_of_the_binding():
     robe.robe_bias_destroy(b)
 
 
+def test_numbers_beyond_the_c_abis_are_refused():
+    x, w = torch.zeros(4, 8, device="cuda"), torch.ones(8, device="cuda")
+    b = robe.robe_bias_create(32, 128, False)
+    bias, rows = torch.full((1, 4, 8, 8), NAN, device="cuda"), torch.zeros(32, 4, device="cuda")
+    ws = torch.empty(robe.robe_bias_backward_workspace_bytes(b, 4, 1, 8, 8), dtype=torch.uint8, device="cuda")
+    for start in (2**63, -2**63 - 1, 2**64 + 5):
+        with pytest.raises(ValueError):
+            robe.robe_bias_forward(b, rows, bias, start)
+        with pytest.raises(ValueError):
+            robe.robe_bias_backward(b, bias, rows, ws, start)
+    assert bias.isnan().all()
+    for norm in (2, -1, 2**32, 2**32 + 1, 2**64):
+        with pytest.raises(robe.RobeError):
+            robe.robe_residual_forward(x, None, torch.zeros_like(x), w_post=w, norm=norm)
+    for start in (2**63 - 1, -2**63):  # the last ones that there are
+        robe.robe_bias_forward(b, rows, bias, start)
+        assert not bias.any()
+    robe.robe_bias_destroy(b)
+
+
 def test_calls_on_another_stream():
     side = torch.cuda.Stream()
     x = torch.randn(3000, 128, generator=gen(1)).cuda()

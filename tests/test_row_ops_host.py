@@ -170,6 +170,15 @@ def test_bias_workspace_is_small():
     robe.robe_bias_destroy(b)
 
 
+def test_workspace_sizes_of_numbers_beyond_the_c_abis():
+    b = robe.robe_bias_create(32, 128, True)
+    for args in [(2**32 + 4, 1, 8, 8), (4, 2**64 + 1, 8, 8), (4, 1, 2**64 + 8, 8), (4, 1, 8, 2**64 + 8), (-4, 1, 8, 8)]:
+        assert robe.robe_bias_backward_workspace_bytes(b, *args) == 0, args
+    robe.robe_bias_destroy(b)
+    for args in [(2**64 + 8, 16, 0), (8, 2**64 + 16, 0), (8, 16, 2**64 + 2), (8, 16, -1)]:
+        assert robe.robe_residual_backward_workspace_bytes(*args) == 0, args
+
+
 def test_dropout_arguments():
     def call(src=P, src_ld=10, out=Q, out_ld=10, rows=4, cols=10, dtype=0, p=0.1, step=None):
         return lib().robe_dropout(src, src_ld, out, out_ld, rows, cols, dtype, p, 1, 2, step, None)
