@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kBiasThreads) bias_few_kernel(BiasArgs a) {
 // A tile of a head's matrix: the values of its diagonals go to shared memory once, then every 16-byte piece of every row is
 // a window of them.  The window of a row starts anywhere, so the values are kept kPiece times, copy s from diagonal s on:
 // whatever the start, one copy has the window on a 16-byte boundary.  A tile beyond the borders needs none of that.  16 matrices
-// of 2048 x 2048 bf16 (134 MB written) 23.6 us, 5.7 TB/s; with the borders searched in 64 bits 30.
+// of 2048 x 2048 bf16 (134 MB written) 24.1 us, 5.6 TB/s; with the borders searched in 64 bits 30.
 template <class T>
 __global__ void __launch_bounds__(kBiasThreads, 8) bias_forward_kernel(BiasArgs a) {
     constexpr int V = kPiece<T>;
@@ -269,7 +269,7 @@ __device__ __forceinline__ void take_piece(float (&v)[kPiece<T>], const uint4* p
 // square) and moves from each to the next one down and to the right: the 2 V - 1 diagonals that cross its squares are the
 // same all the way, and their sums stay in registers.  A warp's squares, side by side, are copied to shared memory one
 // ahead, in the aligned pieces that they lie in; rows that begin inside a piece are shifted into place when they are read.  16 x 16 matrices of 2048 x 2048
-// bf16 (2.1 GB read): 339 us, 6.3 TB/s, which is what a copy reaches; loads into registers 437 (too few under way), three
+// bf16 (2.1 GB read): 341 us, 6.3 TB/s, which is what a copy reaches; loads into registers 437 (too few under way), three
 // squares ahead 348 (fewer CTAs).  4 x 12 of 777 x 1001, masked: 23 us, of which the walk's 8 steps and the sums by buckets
 // are latency.
 template <class T, bool ALIGNED>

@@ -165,9 +165,9 @@ __global__ void __launch_bounds__(kAnyThreads, 2) residual_any_kernel(ResidualPr
 // length.  E is 16 (8 backward for parts of a warp, and for small pieces, whose code is longer), 32 for long rows of 16-byte
 // pieces: the bf16 backward then spills, 4000 rows of 12288 390 us, 1218 by the kernel for any length.
 //
-// Measured (16384 rows of 4096 bf16, dropout): forward with a gate per element 127 us (671 MB, 5.3 TB/s; 1156 by the kernel for any
+// Measured (16384 rows of 4096 bf16, dropout): forward with a gate per element 130 us (671 MB, 5.2 TB/s; 1156 by the kernel for any
 // length), backward with a gate vector per 1024 rows 207 (805 MB, 3.9 TB/s; 1833).  213 K rows of 128 fp32, layer norm, gate per
-// row: forward 80 us (5.5 TB/s); of 100, backward 103 (5.0 TB/s).  The forward waits for memory; the backward is bound by
+// row: forward 80 us (5.5 TB/s); of 100, backward 108 (4.7 TB/s).  The forward waits for memory; the backward is bound by
 // issue and by its chains of dependent operations (128 registers a thread, so 16 warps an SM, which issue in half of the
 // cycles): 32 elements a thread 241 us, 8 (twice the warps, twice the work per row) 284, the first two sums over a row joined into
 // one 213, scalar for paired operations 327 against 310 at that time, no test of a row's end 219.
@@ -1087,8 +1087,10 @@ __global__ void __launch_bounds__(kColumnThreads) residual_columns_kernel(Column
     else (post ? a.grad_w_post : a.grad_w_pre)[c] = (float)s;
 }
 
-// As many chunks as CTAs are resident at once, so that all end together: rows of a warp's part in CTAs of 256 threads, others
-// in CTAs of a row's threads (128 registers a thread: 512 of them an SM).
+// As many chunks as CTAs are resident at once by their registers, so that all end together: rows of a warp's part in CTAs of 256
+// threads, others in CTAs of a row's threads (128 registers a thread: 512 of them an SM).  That is how many are resident in
+// the usual bf16 calls.  Shared memory is not looked at: where a CTA's stages take more of it (fp32 rows of a CTA: 64 KB a stage
+// at 256 threads), the chunks go by in more than one wave.
 int64_t resident_chunks(int64_t d, bool gates) {
     if (d <= 32 * kGradWarpElems) return 148 * (gates ? 2 : 3);
     const int64_t threads = ((d + kRowElems - 1) / kRowElems + 31) / 32 * 32;
