@@ -553,6 +553,121 @@ int robe_residual_backward(const robe_residual_t* c, const void* grad_out, int64
                            int64_t grad_gate_ld, float* grad_w_post, float* grad_w_pre, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Plain tables, as they stand beside the hashed array in a model: [vocab, d] rows of their own.
+ */
+
+/*
+ * robe_table_forward - out[r,:] = scale * table[ids[r],:], +0 where ids[r] is not in 0 .. vocab-1 (a padding id of -1).
+ *   table       fp32 or bf16 (table_dtype), rows table_ld apart;  out  fp32 or bf16 (out_dtype), whichever the table has.
+ *   ids         device pointer to rows ids, ROBE_I64 or ROBE_I32 (index_type), aligned to their size.
+ *   rows  >= 0, < 2^62;  0 <= vocab < 2^31;  1 <= d <= 1048576.
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
+ */
+int robe_table_forward(const void* table, int64_t table_ld, int64_t vocab, int64_t d, int table_dtype, const void* ids,
+                       int index_type, int64_t rows, float scale, void* out, int64_t out_ld, int out_dtype, void* stream);
+
+/*
+ * robe_table_backward - the gradient of a table: with S_v the sum of the rows of grad whose id is v, in fp32,
+ *     accumulate 0    grad_table[v,:] = scale * S_v           (every row is written, +0 where no id is v)
+ *     accumulate 1    grad_table[v,:] = fma(scale, S_v, grad_table[v,:])   (rows without an id keep their bits)
+ * The second form also adds to what another use of the table has left (a tied output layer), and on an fp32 table itself, with
+ * scale = -lr * (the forward's scale), it is the step of plain SGD.
+ *   grad        [rows, d], fp32 or bf16 (dtype), grad_ld apart.
+ *   skip        an id whose row gets no gradient (-1: none); ids outside the table never do.
+ *   grad_table  fp32 [vocab, d], grad_table_ld apart.
+ *   workspace   256-byte aligned, robe_table_backward_workspace_bytes(rows, vocab, d) (0 for bad arguments).
+ *   rows < 2^31.
+ * A sum's order follows from the sizes and ids alone: fp32 sums of at most 256 rows in the order of the call, joined in fp64.
+ * Errors: as above, and ROBE_ERR_WORKSPACE.
+ */
+size_t robe_table_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t d);
+int robe_table_backward(const void* grad, int64_t grad_ld, int dtype, const void* ids, int index_type, int64_t rows,
+                        float scale, int64_t skip, int accumulate, float* grad_table, int64_t grad_table_ld, int64_t vocab,
+                        int64_t d, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Rows in 8 bits.  A row of d columns is codes, one byte each, and an fp32 scale for every `group` columns (the last group may be
+ * shorter): what a code stands for is its own value times its group's scale.  With m the group's largest magnitude,
+ *     scale = max(m, 2^-90) / Q,    code = round(v * (1 / scale))
+ * where each operation is rounded to nearest even, in fp32 but for the last, so that codes and scales follow bit for
+ * bit from the values.  ROBE_E4M3: Q = 448, codes are floats with four bits of exponent and three of fraction; ROBE_I8: Q = 127, whole
+ * numbers.  A group that holds a NaN or an infinity reads back as NaN throughout.
+ *   group   1 .. 256, or d (one scale a row; 0 means d).  Number of scales of a row: ceil(d / group).
+ */
+#define ROBE_E4M3 2
+#define ROBE_I8 3
+
+/*
+ * robe_residual_quantize - robe_residual_forward without a norm of x, gate and dropout, whose `normed` leaves in 8 bits:
+ *     out    = residual + scale * x              (residual NULL: nothing is added to; out NULL: not stored)
+ *     normed = norm(out) * w_pre                 (of out before its rounding; w_pre NULL: out itself, no norm)
+ *     codes, scales = normed in 8 bits
+ * The gradient is robe_residual_backward's, from out as this call stored it, with the gradient of normed passed straight through
+ * the rounding to codes.  out may be residual itself (same pointer, same ld).
+ *   rows >= 0, <= 2^32;  1 <= d <= 1048576;  dtype  of x, residual and out;  norm  ROBE_NORM_*.
+ *   codes   [rows, d] bytes, codes_ld apart;  scales  [rows, ceil(d / group)], scales_ld apart.
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_CUDA.
+ */
+int robe_residual_quantize(int64_t rows, int64_t d, int dtype, int norm, float eps, float scale, const void* x, int64_t x_ld,
+                           const void* residual, int64_t residual_ld, const float* w_pre, void* out, int64_t out_ld, void* codes,
+                           int64_t codes_ld, int code_type, int64_t group, float* scales, int64_t scales_ld, void* stream);
+
+/*
+ * A cache of rows in 8 bits, in pages of page_rows rows.  Row t of sequence s (t from 0) stands at position p = starts[s] + t and lies
+ * in row p mod page_rows of page pages[s, floor(p / page_rows)]; it has no place where p is negative, beyond the page table, or
+ * the page's number is not in 0 .. num_pages-1.  The call's rows are the sequences' one after the other: those of s
+ * are offsets[s] .. offsets[s+1]-1 of them (offsets non-decreasing); without offsets every sequence has equally many.
+ */
+typedef struct robe_cache_t {
+    void* codes;                      /* [num_pages, page_rows, d] bytes: rows codes_ld apart, pages codes_page */
+    int64_t codes_ld, codes_page;
+    float* scales;                    /* [num_pages, page_rows, ceil(d / group)] */
+    int64_t scales_ld, scales_page;
+    int64_t num_pages, page_rows;     /* < 2^31 each */
+    int64_t d, group;                 /* as above */
+    int code_type;                    /* ROBE_E4M3, ROBE_I8 */
+    const int32_t* pages;             /* device [batch, max_pages], pages_ld apart */
+    int64_t pages_ld, batch, max_pages;
+    const int64_t* offsets;           /* device [batch + 1], or NULL */
+    const int64_t* starts;            /* device [batch], or NULL: 0 */
+} robe_cache_t;
+
+/*
+ * robe_cache_write - rows [n, d] into their places; rows without a place, before offsets[0] and from offsets[batch] on are
+ * not written anywhere.  Two rows of a call with the same place (a page that two sequences write to) leave there some mixture
+ * of the two: shared pages are for reading.
+ * robe_cache_read  - the other way: out[r,:] = code * scale, +0 for a row without a place; rows before offsets[0] and from
+ * offsets[batch] on are left as they were.
+ *   rows / out   fp32 or bf16 (dtype), ld apart;  0 <= n <= 2^32 (a multiple of batch where offsets is NULL).
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
+ */
+int robe_cache_write(const robe_cache_t* c, const void* rows, int64_t rows_ld, int64_t n, int dtype, void* stream);
+int robe_cache_read(const robe_cache_t* c, void* out, int64_t out_ld, int64_t n, int dtype, void* stream);
+
+/*
+ * robe_cache_attention - attention of one new token of each sequence over its rows in two such caches.  The query of sequence s stands
+ * at position starts[s] (its own key and value have been written there); query head h reads head h / (q_heads / heads) of the cache, which
+ * is columns head * dim .. of a row:
+ *     x_j = scale * q[s,h,:] . K_j + (bias ? bias_rows[bucket(j - starts[s]), h] : 0)      0 <= j <= starts[s]
+ *     out[s,h,:] = sum_j exp(x_j) V_j / sum_j exp(x_j)
+ * over the positions that have a place; +0 where there is none (starts[s] < 0, say).  bucket as in robe_bias_forward.
+ *   keys, values   caches with the same code type, pages, sizes and strides; group = dim, d = heads * dim; offsets NULL;
+ *                  codes 16-byte aligned (pointer, codes_ld and codes_page); scales as robe_cache_write leaves them.
+ *   q, out         bf16 [batch * q_heads, dim], a row for every sequence and head, ld apart.  dim 32, 64, 96, 128 or 256; heads divides q_heads.
+ *   bias           handle or NULL;  bias_rows  fp32 [num_buckets, q_heads], bias_ld apart.
+ *   workspace      256-byte aligned, robe_cache_attention_workspace_bytes(batch, heads, q_heads, dim, max_pages * page_rows)
+ *                  bytes (0 for bad arguments); one call at a time.
+ *   max_pages * page_rows < 2^31 - 2^16;  batch * q_heads < 2^31.
+ * Scores, the divisor and the sums are fp32; a weight is rounded to 11 bits relative to itself, where it is above 2^-14 of the largest.
+ * How the sum over a sequence is cut follows from all lengths of the call; the same call gives the same bits.
+ * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_WORKSPACE, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
+ */
+size_t robe_cache_attention_workspace_bytes(int64_t batch, int64_t heads, int64_t q_heads, int64_t dim, int64_t positions);
+int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, const void* q, int64_t q_ld, int64_t q_heads,
+                         float scale, robe_bias_t bias, const float* bias_rows, int64_t bias_ld, void* out, int64_t out_ld,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
 /* robe_status_string - static host string for a robe_status value. */
 const char* robe_status_string(int status);
 

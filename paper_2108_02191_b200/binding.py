@@ -31,6 +31,8 @@ ROBE_ERR_UNSUPPORTED = -5
 
 ROBE_F32 = 0
 ROBE_BF16 = 1
+ROBE_E4M3 = 2
+ROBE_I8 = 3
 
 ROBE_OPT_SIGN = 1
 ROBE_OPT_BWD_MODE = 2
@@ -70,6 +72,8 @@ EXPORTS = [
     "robe_dropout", "robe_bias_create", "robe_bias_destroy", "robe_bias_num_buckets", "robe_bias_get_edges",
     "robe_bias_forward", "robe_bias_backward_workspace_bytes", "robe_bias_backward",
     "robe_residual_forward", "robe_residual_backward_workspace_bytes", "robe_residual_backward",
+    "robe_table_forward", "robe_table_backward_workspace_bytes", "robe_table_backward", "robe_residual_quantize",
+    "robe_cache_write", "robe_cache_read", "robe_cache_attention_workspace_bytes", "robe_cache_attention",
 ]
 
 if not os.path.exists(LIB_PATH):
@@ -118,6 +122,14 @@ class _Residual(C.Structure):
                 ("offset", _u64), ("step", _vp)]
 
 
+class _Cache(C.Structure):
+    """robe_cache_t"""
+    _fields_ = [("codes", _vp), ("codes_ld", _i64), ("codes_page", _i64), ("scales", _vp), ("scales_ld", _i64),
+                ("scales_page", _i64), ("num_pages", _i64), ("page_rows", _i64), ("d", _i64), ("group", _i64),
+                ("code_type", C.c_int), ("pages", _vp), ("pages_ld", _i64), ("batch", _i64), ("max_pages", _i64),
+                ("offsets", _vp), ("starts", _vp)]
+
+
 _rows = [_vp, _i64]  # a matrix: pointer and leading dimension
 _lib.robe_dropout.argtypes = _rows * 2 + [_i64, _i64, C.c_int, C.c_float, _u64, _u64, _vp, _vp]
 _lib.robe_bias_create.argtypes = [C.POINTER(_BiasHandle), _u32, _u32, C.c_int]
@@ -134,6 +146,19 @@ _lib.robe_residual_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
 _lib.robe_residual_backward_workspace_bytes.restype = C.c_size_t
 _lib.robe_residual_backward.argtypes = ([C.POINTER(_Residual)] + _rows * 5 + [_vp, _vp] + _rows * 3
                                         + [_vp, _vp, _vp, C.c_size_t, _vp])
+_lib.robe_table_forward.argtypes = _rows + [_i64, _i64, C.c_int, _vp, C.c_int, _i64, C.c_float] + _rows + [C.c_int, _vp]
+_lib.robe_table_backward_workspace_bytes.argtypes = [_i64] * 3
+_lib.robe_table_backward_workspace_bytes.restype = C.c_size_t
+_lib.robe_table_backward.argtypes = (_rows + [C.c_int, _vp, C.c_int, _i64, C.c_float, _i64, C.c_int] + _rows + [_i64, _i64, _vp,
+                                     C.c_size_t, _vp])
+_lib.robe_residual_quantize.argtypes = ([_i64, _i64, C.c_int, C.c_int, C.c_float, C.c_float] + _rows * 2 + [_vp] + _rows * 2
+                                        + [C.c_int, _i64] + _rows + [_vp])
+_lib.robe_cache_write.argtypes = [C.POINTER(_Cache)] + _rows + [_i64, C.c_int, _vp]
+_lib.robe_cache_read.argtypes = [C.POINTER(_Cache)] + _rows + [_i64, C.c_int, _vp]
+_lib.robe_cache_attention_workspace_bytes.argtypes = [_i64] * 5
+_lib.robe_cache_attention_workspace_bytes.restype = C.c_size_t
+_lib.robe_cache_attention.argtypes = ([C.POINTER(_Cache)] * 2 + _rows + [_i64, C.c_float, _BiasHandle] + _rows * 2
+                                      + [_vp, C.c_size_t, _vp])
 _lib.robe_status_string.argtypes = [C.c_int]
 _lib.robe_status_string.restype = C.c_char_p
 for _name in EXPORTS:
@@ -145,7 +170,8 @@ _native.set_calls(_vp, *(C.cast(getattr(_lib, _name), _vp).value for _name in (
     "robe_backward_adam", "robe_backward_adagrad", "robe_apply_sgd")))
 _native.set_row_calls(_BiasHandle, *(C.cast(getattr(_lib, _name), _vp).value for _name in (
     "robe_dropout", "robe_bias_num_buckets", "robe_bias_forward", "robe_bias_backward", "robe_residual_forward",
-    "robe_residual_backward")))
+    "robe_residual_backward", "robe_table_forward", "robe_table_backward", "robe_residual_quantize", "robe_cache_write",
+    "robe_cache_read", "robe_cache_attention")))
 _NOT_TAKEN = 1  # from _native: nothing was called
 
 
@@ -334,6 +360,7 @@ def robe_apply_sgd(h, grad_array, lr: float, zero_grad: bool = True, stream=None
 # last dimension is contiguous and whose others collapse to one (a column slice of a wider one, for instance).
 
 _TYPES = {torch.float32: ROBE_F32, torch.bfloat16: ROBE_BF16}
+_BYTES = (torch.uint8,)
 
 
 def _here(t, what, dtype=None):
@@ -347,10 +374,10 @@ def _here(t, what, dtype=None):
     return t
 
 
-def _matrix(t, what, dtype=None):
+def _matrix(t, what, dtype=None, types=_TYPES):
     """(pointer, leading dimension, rows, columns)"""
     _here(t, what, dtype)
-    if t.dtype not in _TYPES:
+    if t.dtype not in types:
         raise TypeError(f"{what}: expected float32 or bfloat16, got {t.dtype}")
     if t.dim() == 0:
         raise ValueError(f"{what}: expected a tensor of rows")
@@ -374,11 +401,11 @@ def _matrix(t, what, dtype=None):
     return t.data_ptr(), ld, rows, cols
 
 
-def _matrix_like(t, what, dtype, rows, cols):
+def _matrix_like(t, what, dtype, rows, cols, types=_TYPES):
     """Pointer and leading dimension of a matrix of that type and size; of None: (None, 0)."""
     if t is None:
         return None, 0
-    p, ld, r, c = _matrix(t, what, dtype)
+    p, ld, r, c = _matrix(t, what, dtype, types)
     if (r, c) != (rows, cols):
         raise ValueError(f"{what}: {r} rows of {c}, expected {rows} of {cols}")
     return p, ld
@@ -564,6 +591,186 @@ def robe_residual_backward(grad_out, grad_normed, x, out, grad_x, grad_residual=
         p_gate, ld, rows, cols = _matrix(grad_gate, "grad_gate")
         _check(_lib.robe_dropout(p_gate, ld, p_gate, ld, rows, cols, c.dtype, 1.0, 0, 0, None, _stream_ptr(stream)),
                "robe_residual_backward")
+
+
+# ---- plain tables
+
+def _id_list(t, rows):
+    """(pointer, index type) of a contiguous tensor of that many ids"""
+    if _here(t, "ids").dtype not in (torch.int64, torch.int32):
+        raise TypeError(f"ids: expected int64 or int32, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError("ids: expected a contiguous tensor")
+    if t.numel() != rows:
+        raise ValueError(f"ids: {t.numel()} for {rows} rows")
+    return t.data_ptr(), ROBE_I32 if t.dtype == torch.int32 else ROBE_I64
+
+
+def robe_table_forward(table, ids, out, scale: float = 1.0, stream=None) -> None:
+    """out[r,:] = scale * table[ids[r],:]; +0 for ids outside the table.  table [vocab, d]; ids of any shape, out [.., d]."""
+    rc = _native.table_forward(table, ids, out, scale, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_table_forward")
+    p, ld, vocab, d = _matrix(table, "table")
+    to, to_ld, rows, cols = _matrix(out, "out")
+    if cols != d:
+        raise ValueError(f"out: rows of {cols}, expected {d}")
+    _check(_lib.robe_table_forward(p, ld, vocab, d, _TYPES[table.dtype], *_id_list(ids, rows), rows, scale, to, to_ld,
+                                   _TYPES[out.dtype], _stream_ptr(stream)), "robe_table_forward")
+
+
+def robe_table_backward_workspace_bytes(rows: int, vocab: int, d: int) -> int:
+    if not all(-2**63 <= n < 2**63 for n in (rows, vocab, d)):
+        return 0
+    return int(_lib.robe_table_backward_workspace_bytes(rows, vocab, d))
+
+
+def robe_table_backward(grad, ids, grad_table, workspace, scale: float = 1.0, accumulate: bool = False, skip: int = -1,
+                        stream=None) -> None:
+    """grad_table[v,:] = scale * sum of the rows of grad whose id is v; accumulate: added to what is there.  skip: an id without
+    a gradient."""
+    rc = _native.table_backward(grad, ids, grad_table, workspace, scale, accumulate, skip, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_table_backward")
+    p, ld, rows, cols = _matrix(grad, "grad")
+    to, to_ld, vocab, d = _matrix(grad_table, "grad_table", torch.float32)
+    if cols != d:
+        raise ValueError(f"grad: rows of {cols}, expected {d}")
+    if not -2**63 <= skip < 2**63:
+        raise ValueError(f"skip: {skip} is beyond 64 bits")
+    _check(_lib.robe_table_backward(p, ld, _TYPES[grad.dtype], *_id_list(ids, rows), rows, scale, skip, 1 if accumulate else 0, to,
+                                    to_ld, vocab, d, *_workspace(workspace), _stream_ptr(stream)), "robe_table_backward")
+
+
+# ---- rows in 8 bits: codes are float8_e4m3fn or int8 tensors, a scale for every `group` columns (0: for every row)
+
+_CODES = {torch.float8_e4m3fn: ROBE_E4M3, torch.int8: ROBE_I8}
+
+
+def _group(d, group):
+    """(columns of a group, groups of a row)"""
+    if not 0 <= group < 2**63:
+        raise RobeError(ROBE_ERR_INVALID_ARG, "group")
+    g = group or max(d, 1)
+    return group, -(-d // g)
+
+
+def _collapsed(t, what, keep):
+    """Elements of the dimensions from `keep` on, which have to be contiguous."""
+    n = 1
+    for size, stride in zip(reversed(t.shape[keep:]), reversed(t.stride()[keep:])):
+        if size != 1 and stride != n:
+            raise ValueError(f"{what}: the dimensions of a row are not contiguous")
+        n *= size
+    return n
+
+
+def _code_rows(t, what, rows, d):
+    """(pointer, leading dimension, type) of a matrix of codes"""
+    if _here(t, what).dtype not in _CODES:
+        raise TypeError(f"{what}: expected float8_e4m3fn or int8, got {t.dtype}")
+    return *_matrix_like(t.view(torch.uint8), what, None, rows, d, _BYTES), _CODES[t.dtype]
+
+
+def _paged(t, what, types):
+    """(pointer, leading dimension, distance of pages, pages, rows of a page, columns) of [pages, page_rows, ..]"""
+    if _here(t, what).dtype not in types:
+        raise TypeError(f"{what}: got {t.dtype}")
+    if t.dim() < 3:
+        raise ValueError(f"{what}: expected [pages, rows of a page, columns]")
+    cols = _collapsed(t, what, 2)
+    ld = t.stride(1) if t.shape[1] > 1 else cols
+    page = t.stride(0) if t.shape[0] > 1 else ld * t.shape[1]
+    return t.data_ptr(), ld, page, t.shape[0], t.shape[1], cols
+
+
+def _cache(codes, scales, pages, offsets, starts, group):
+    p, ld, page, num, rows, d = _paged(codes, "codes", _CODES)
+    group, groups = _group(d, group)
+    s, s_ld, s_page, s_num, s_rows, s_cols = _paged(scales, "scales", (torch.float32,))
+    if (s_num, s_rows, s_cols) != (num, rows, groups):
+        raise ValueError(f"scales: [{s_num}, {s_rows}, {s_cols}], expected [{num}, {rows}, {groups}]")
+    if _here(pages, "pages", torch.int32).dim() != 2:
+        raise ValueError("pages: expected [batch, pages of a sequence]")
+    batch, most = pages.shape
+    if most > 1 and pages.stride(1) != 1:
+        raise ValueError("pages: the last dimension is not contiguous")
+    return _Cache(p, ld, page, s, s_ld, s_page, num, rows, d, group, _CODES[codes.dtype], pages.data_ptr(),
+                  pages.stride(0) if batch > 1 else most, batch, most, _vector(offsets, "offsets", batch + 1, torch.int64),
+                  _vector(starts, "starts", batch, torch.int64))
+
+
+def robe_residual_quantize(x, residual, out, codes, scales, w_pre=None, group: int = 0, scale: float = 1.0,
+                           norm: int = ROBE_NORM_RMS, eps: float = 1e-6, stream=None) -> None:
+    """out = residual + scale * x; codes, scales = norm(out) w_pre in 8 bits.  residual, out, w_pre may be None."""
+    rc = _native.residual_quantize(x, residual, out, codes, scales, w_pre, group, scale, norm, eps, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_residual_quantize")
+    p, ld, rows, d = _matrix(x, "x")
+    group, groups = _group(d, group)
+    if norm not in (ROBE_NORM_RMS, ROBE_NORM_LAYER):
+        raise RobeError(ROBE_ERR_INVALID_ARG, "norm")
+    like = lambda t, what: _matrix_like(t, what, x.dtype, rows, d)
+    code_p, code_ld, code_type = _code_rows(codes, "codes", rows, d)
+    _check(_lib.robe_residual_quantize(rows, d, _TYPES[x.dtype], norm, eps, scale, p, ld, *like(residual, "residual"),
+                                       _vector(w_pre, "w_pre", d), *like(out, "out"), code_p, code_ld, code_type, group,
+                                       *_matrix_like(_here(scales, "scales"), "scales", torch.float32, rows, groups),
+                                       _stream_ptr(stream)), "robe_residual_quantize")
+
+
+def robe_cache_write(rows, codes, scales, pages, offsets=None, starts=None, group: int = 0, stream=None) -> None:
+    """rows [n, d] of the sequences into their places: codes [pages, page_rows, d], scales [pages, page_rows, d / group], pages int32
+    [batch, most], offsets int64 [batch + 1] (None: equally many rows each), starts int64 [batch] (None: 0)."""
+    rc = _native.cache_write(rows, codes, scales, pages, offsets, starts, group, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_cache_write")
+    c = _cache(codes, scales, pages, offsets, starts, group)
+    p, ld, n, d = _matrix(rows, "rows")
+    if d != c.d:
+        raise ValueError(f"rows: of {d}, expected {c.d}")
+    _check(_lib.robe_cache_write(C.byref(c), p, ld, n, _TYPES[rows.dtype], _stream_ptr(stream)), "robe_cache_write")
+
+
+def robe_cache_read(codes, scales, pages, out, offsets=None, starts=None, group: int = 0, stream=None) -> None:
+    """out [n, d]: the sequences' rows from their places, +0 where there is none."""
+    rc = _native.cache_read(codes, scales, pages, out, offsets, starts, group, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_cache_read")
+    c = _cache(codes, scales, pages, offsets, starts, group)
+    p, ld, n, d = _matrix(out, "out")
+    if d != c.d:
+        raise ValueError(f"out: rows of {d}, expected {c.d}")
+    _check(_lib.robe_cache_read(C.byref(c), p, ld, n, _TYPES[out.dtype], _stream_ptr(stream)), "robe_cache_read")
+
+
+def robe_cache_attention_workspace_bytes(batch: int, heads: int, q_heads: int, dim: int, positions: int) -> int:
+    """positions: that the page table has room for (pages of a sequence x rows of a page)."""
+    if not all(-2**63 <= n < 2**63 for n in (batch, heads, q_heads, dim, positions)):
+        return 0
+    return int(_lib.robe_cache_attention_workspace_bytes(batch, heads, q_heads, dim, positions))
+
+
+def robe_cache_attention(q, keys, key_scales, values, value_scales, pages, starts, out, workspace, scale: float, bias=None,
+                         bias_rows=None, stream=None) -> None:
+    """Attention of the query at position starts[s] of each sequence over the rows 0 .. starts[s] of a cache of keys and one of values.
+    q, out bf16 [batch, q_heads, dim]; bias: a position-bias handle with bias_rows [buckets, q_heads]."""
+    rc = _native.cache_attention(q, keys, key_scales, values, value_scales, pages, starts, out, workspace, scale, bias, bias_rows, stream)
+    if rc != _NOT_TAKEN:
+        return _check(rc, "robe_cache_attention")
+    if _here(q, "q", torch.bfloat16).dim() != 3:
+        raise ValueError("q: expected [batch, query heads, columns of a head]")
+    p, ld, rows, dim = _matrix(q, "q")
+    batch, q_heads = q.shape[:2]
+    if starts is None:
+        raise ValueError("starts: expected int64 [batch]")
+    k, v = (_cache(c, s, pages, None, starts, dim) for c, s in ((keys, key_scales), (values, value_scales)))
+    if k.batch != batch:
+        raise ValueError(f"pages: of {k.batch} sequences, expected {batch}")
+    to, to_ld = _matrix_like(_here(out, "out"), "out", torch.bfloat16, rows, dim)
+    table, table_ld = (None, 0) if bias is None else _matrix_like(_here(bias_rows, "bias_rows"), "bias_rows", torch.float32,
+                                                                  robe_bias_num_buckets(bias), q_heads)
+    _check(_lib.robe_cache_attention(C.byref(k), C.byref(v), p, ld, q_heads, scale, bias, table, table_ld, to, to_ld,
+                                     *_workspace(workspace), _stream_ptr(stream)), "robe_cache_attention")
 
 
 def robe_debug_status(stream=None) -> int:

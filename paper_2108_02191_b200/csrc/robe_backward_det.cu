@@ -1270,6 +1270,21 @@ void launch_apply(const ApplyArgs& aa, const uint32_t* K, const uint32_t* V, con
 
 }  // namespace
 
+size_t sort_counts_bytes() { return (size_t)kRadix * kSortMaxGrid * sizeof(uint32_t); }
+size_t sort_totals_bytes() { return kRadix * sizeof(uint32_t); }
+
+int launch_sort_pairs(uint32_t* const (&keys)[2], uint32_t* const (&vals)[2], uint64_t n, uint32_t bits, uint32_t* counts,
+                      uint32_t* totals, cudaStream_t st) {
+    const uint32_t npass = (bits + 7) / 8;
+    const uint32_t bpp = (bits + npass - 1) / npass;
+    const SortPlan sp = make_plan(n, bpp);
+    int in = 0;
+    for (uint32_t shift = 0; shift < bits; shift += bpp, in ^= 1)
+        launch_sort_pass<true>(sp, keys[in], vals[in], keys[in ^ 1], vals[in ^ 1], counts, totals, shift,
+                               bits - shift < bpp ? bits - shift : bpp, st);
+    return in;
+}
+
 size_t det_workspace_bytes(const MapParams& mp, int64_t nbags, int64_t nnz, bool bags) {
     (void)nbags;
     const uint64_t nb = (uint64_t)nnz * mp.C;

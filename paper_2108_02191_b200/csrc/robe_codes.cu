@@ -1,0 +1,665 @@
+// Rows in 8 bits: the residual join whose norm leaves as codes with scales, and a paged cache of such rows, written and
+// read back.  Formulas of codes and scales: robe_codes.cuh.  All of it moves data once and is bound by memory; the sums and
+// largest magnitudes that it takes stay in registers and shuffles.
+#include <initializer_list>
+#include <type_traits>
+
+#include "robe_codes.cuh"
+#include "robe_internal.h"
+
+namespace robe {
+
+namespace {
+
+constexpr int kCodeThreads = 256;
+constexpr int kJoinMost = 512;       // threads a row
+constexpr int64_t kGroupMost = 256;  // columns of a group that lanes of one warp hold; beyond: one scale a row
+
+// Eight columns of a row, loaded and stored by pieces of P elements; where fewer than eight are left, one by one.
+template <class T>
+struct Eight {
+    T e[8];
+};
+template <class T, int P>
+constexpr int kStep = P * (int)sizeof(T) > 16 ? kPiece<T> : P;
+template <class T, int P>
+__device__ __forceinline__ void load_eight(Eight<T>& r, const T* p, int count) {
+    constexpr int S = kStep<T, P>;
+    if (count == 8) {
+#pragma unroll
+        for (int q = 0; q < 8 / S; ++q) {
+            const Pack<T, S> e = load_pack<true, T, S>(p + q * S);
+#pragma unroll
+            for (int k = 0; k < S; ++k) r.e[q * S + k] = e.v[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r.e[k] = k < count ? p[k] : narrow<T>(0.0f);
+    }
+}
+template <class T, int P>
+__device__ __forceinline__ void store_eight(const float (&v)[8], T* p, int count) {
+    constexpr int S = kStep<T, P>;
+    if (count == 8) {
+#pragma unroll
+        for (int q = 0; q < 8 / S; ++q) {
+            Pack<T, S> e;
+#pragma unroll
+            for (int k = 0; k < S; ++k) e.v[k] = narrow<T>(v[q * S + k]);
+            store_pack<true, T, S>(p + q * S, e);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < count) p[k] = narrow<T>(v[k]);
+    }
+}
+// eight codes, by pieces of `piece` bytes
+__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t low, uint32_t high, int count, int piece) {
+    if (count == 8 && piece == 8) {
+        *(uint2*)p = make_uint2(low, high);
+    } else if (count == 8 && piece == 4) {
+        ((uint32_t*)p)[0] = low;
+        ((uint32_t*)p)[1] = high;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < count) p[k] = (uint8_t)((k < 4 ? low : high) >> (8 * (k % 4)));
+    }
+}
+template <bool I8>
+__device__ __forceinline__ void store_codes(uint8_t* p, const float (&v)[8], float factor, int count, int piece) {
+    store_codes(p, codes_of<I8>(v, factor), codes_of<I8>(v + 4, factor), count, piece);
+}
+__device__ __forceinline__ uint32_t largest_of(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = max(m, magnitude(v[k]));
+    return m;
+}
+
+// ---- where columns lie: a unit is eight columns of one group; `lanes` units (a power of two) hold a group, those behind its end
+// nothing.  With one scale a row the units follow one another and the whole row is the group.
+struct Columns {
+    int64_t d;
+    uint32_t group, shift, units;  // shift: of lanes; units: of a row
+    int whole;                     // one scale a row
+};
+__device__ __forceinline__ int64_t columns_of(const Columns& c, uint32_t unit, int& count) {
+    const int64_t begin = (int64_t)(unit >> c.shift) * c.group;
+    const int64_t end = begin + c.group < c.d ? begin + c.group : c.d;
+    const int64_t col = begin + (int64_t)(unit & ((1u << c.shift) - 1u)) * 8;
+    const int64_t left = end - col;
+    count = unit >= c.units || left <= 0 ? 0 : left < 8 ? (int)left : 8;
+    return col;
+}
+Columns columns(int64_t d, int64_t group) {
+    Columns c;
+    c.d = d;
+    c.whole = group > kGroupMost;
+    if (c.whole) group = 8;
+    c.group = (uint32_t)group;
+    c.shift = 0;
+    while ((8ll << c.shift) < group) ++c.shift;
+    c.units = (uint32_t)((d + group - 1) / group) << c.shift;
+    return c;
+}
+
+// ---------------------------------------------------------------- the join
+
+struct QuantizeArgs {
+    int64_t rows;
+    Columns c;
+    int layer;
+    float eps, scale;
+    const float* w;
+    RowsRef x, residual, out, codes, scales;
+    int code_piece, w_pieces;
+    uint32_t threads;  // of a row
+    // a cache takes the codes: rows of the call lie where `at` says
+    int cached;
+    CachePlaces at;
+    int64_t codes_page, scales_page;
+};
+
+// where row r's codes and scales go; false: nowhere
+__device__ __forceinline__ bool codes_row(const QuantizeArgs& a, int64_t r, uint8_t*& codes, float*& scales) {
+    int64_t code = r * a.codes.ld, scale = r * a.scales.ld;
+    if (a.cached) {
+        const CacheRow at = cache_row(a.at, r);
+        if (at.page < 0) return false;
+        code = at.page * a.codes_page + at.row * a.codes.ld;
+        scale = at.page * a.scales_page + at.row * a.scales.ld;
+    }
+    codes = (uint8_t*)a.codes.p + code;
+    scales = (float*)a.scales.p + scale;
+    return true;
+}
+// eight weights
+__device__ __forceinline__ void load_weights(float (&w)[8], const QuantizeArgs& a, int64_t col, int count) {
+    if (a.w_pieces && count == 8) {
+        const float4 p = __ldca((const float4*)(a.w + col)), q = __ldca((const float4*)(a.w + col) + 1);
+        w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
+        w[4] = q.x; w[5] = q.y; w[6] = q.z; w[7] = q.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = k < count ? __ldca(a.w + col + k) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ float add_over(float v, uint32_t lanes) {
+    for (uint32_t o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+__device__ __forceinline__ uint32_t most_over(uint32_t v, uint32_t lanes) {
+    for (uint32_t o = 1; o < lanes; o <<= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
+// over the threads of a row: lanes of a warp, or whole warps that meet in shared memory (one word a warp)
+__device__ __forceinline__ float add_over_row(float v, uint32_t threads, float* words) {
+    if (threads <= 32) return add_over(v, threads);
+    v = add_over(v, 32);
+    const uint32_t warp = threadIdx.x / 32, per = threads / 32, first = warp / per * per;
+    if (threadIdx.x % 32 == 0) words[warp] = v;
+    __syncthreads();
+    v = 0.0f;
+    for (uint32_t k = 0; k < per; ++k) v += words[first + k];
+    return v;
+}
+__device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t threads, uint32_t* words) {
+    if (threads <= 32) return most_over(v, threads);
+    v = most_over(v, 32);
+    const uint32_t warp = threadIdx.x / 32, per = threads / 32, first = warp / per * per;
+    if (threadIdx.x % 32 == 0) words[warp] = v;
+    __syncthreads();
+    v = 0;
+    for (uint32_t k = 0; k < per; ++k) v = max(v, words[first + k]);
+    return v;
+}
+
+// A row in the registers of its threads, K units each; the next row's loads are under way while one is worked on.
+template <class T, int P, int K, bool I8>
+__global__ void __launch_bounds__(kJoinMost) quantize_rows_kernel(QuantizeArgs a) {
+    __shared__ float sums[2][2][kJoinMost / 32];  // (two rows' turns: a barrier of the next row stands between a read and the next write)
+    __shared__ uint32_t most[2][kJoinMost / 32];
+    constexpr bool kAhead = K * sizeof(T) <= 8;
+    follow();
+    const uint32_t per_cta = blockDim.x / a.threads;
+    const uint32_t t = threadIdx.x % a.threads;
+    const int64_t stride = (int64_t)gridDim.x * per_cta;
+    int64_t col[K];
+    int count[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) col[j] = columns_of(a.c, t + j * a.threads, count[j]);
+    Eight<T> x[K], y[K];
+    auto load = [&](int64_t r) {
+        if (r >= a.rows) return;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (count[j] == 0) continue;
+            if (!ROBE_CHK(col[j] + count[j] <= a.c.d, ROBE_DBG_ROW_POS)) continue;
+            load_eight<T, P>(x[j], (const T*)a.x.p + r * a.x.ld + col[j], count[j]);
+            if (a.residual.p != nullptr) load_eight<T, P>(y[j], (const T*)a.residual.p + r * a.residual.ld + col[j], count[j]);
+        }
+    };
+    int64_t r = (int64_t)blockIdx.x * per_cta + threadIdx.x / a.threads;
+    load(r);
+    int turn = 0;
+    for (int64_t base = (int64_t)blockIdx.x * per_cta; base < a.rows; base += stride, r += stride, turn ^= 1) {
+        const bool on = r < a.rows;
+        float v[K][8];
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float s = a.scale * widen(x[j].e[k]);
+                v[j][k] = !on || count[j] == 0 ? 0.0f : a.residual.p != nullptr ? widen(y[j].e[k]) + s : s;
+            }
+        if (kAhead) load(r + stride);
+        if (a.out.p != nullptr && on) {
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (count[j] > 0) store_eight<T, P>(v[j], (T*)a.out.p + r * a.out.ld + col[j], count[j]);
+        }
+        if (a.w != nullptr) {
+            if (a.layer) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum += v[j][k];
+                const float mean = add_over_row(sum, a.threads, sums[turn][0]) / (float)a.c.d;
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[j][k] = k < count[j] ? v[j][k] - mean : 0.0f;
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum = fmaf(v[j][k], v[j][k], sum);
+            const float factor = 1.0f / sqrtf(add_over_row(sum, a.threads, sums[turn][1]) / (float)a.c.d + a.eps);
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                if (count[j] == 0) continue;
+                float w[8];
+                load_weights(w, a, col[j], count[j]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[j][k] = v[j][k] * factor * w[k];
+            }
+        }
+        uint8_t* codes = nullptr;
+        float* scales = nullptr;
+        const bool to = on && codes_row(a, r, codes, scales);
+        GroupScale whole{};
+        if (a.c.whole) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < K; ++j) m = max(m, largest_of(v[j]));
+            whole = group_scale(most_over_row(m, a.threads, most[turn]), I8 ? kLargestI8 : kLargestE4m3);
+            if (to && t == 0) scales[0] = whole.scale;
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            GroupScale g = whole;
+            if (!a.c.whole) {
+                g = group_scale(most_over(largest_of(v[j]), 1u << a.c.shift), I8 ? kLargestI8 : kLargestE4m3);
+                const uint32_t unit = t + j * a.threads;
+                if (to && count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
+            }
+            if (to && count[j] > 0) store_codes<I8>(codes + col[j], v[j], g.factor, count[j], a.code_piece);
+        }
+        if (!kAhead) load(r + stride);
+    }
+}
+
+// Rows of any length, a CTA each, read again for every step: statistics, the largest magnitude of a whole row, codes.
+template <class T, int P, bool I8>
+__global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a) {
+    __shared__ float sums[2][kJoinMost / 32];
+    __shared__ uint32_t most[kJoinMost / 32];
+    follow();
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        uint8_t* codes = nullptr;
+        float* scales = nullptr;
+        const bool to = codes_row(a, r, codes, scales);
+        if (!to && a.out.p == nullptr) continue;  // (the same for the whole CTA)
+        auto joined = [&](float (&v)[8], uint32_t unit, int64_t& col) {
+            int count;
+            col = columns_of(a.c, unit, count);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+            if (count == 0 || !ROBE_CHK(col + count <= a.c.d, ROBE_DBG_ROW_POS)) return 0;
+            Eight<T> x, y;
+            load_eight<T, P>(x, (const T*)a.x.p + r * a.x.ld + col, count);
+            if (a.residual.p != nullptr) load_eight<T, P>(y, (const T*)a.residual.p + r * a.residual.ld + col, count);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float s = a.scale * widen(x.e[k]);
+                if (k < count) v[k] = a.residual.p != nullptr ? widen(y.e[k]) + s : s;
+            }
+            return count;
+        };
+        float mean = 0.0f, factor = 1.0f;
+        if (a.w != nullptr) {
+            if (a.layer) {
+                float sum = 0.0f, v[8];
+                int64_t col;
+                for (uint32_t u = threadIdx.x; u < a.c.units; u += kJoinMost) {
+                    joined(v, u, col);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum += v[k];
+                }
+                mean = add_over_row(sum, kJoinMost, sums[0]) / (float)a.c.d;
+            }
+            float sum = 0.0f, v[8];
+            int64_t col;
+            for (uint32_t u = threadIdx.x; u < a.c.units; u += kJoinMost) {
+                const int count = joined(v, u, col);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < count) sum = fmaf(v[k] - mean, v[k] - mean, sum);
+            }
+            factor = 1.0f / sqrtf(add_over_row(sum, kJoinMost, sums[1]) / (float)a.c.d + a.eps);
+        }
+        auto normed = [&](float (&n)[8], const float (&v)[8], int64_t col, int count) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n[k] = v[k];
+            if (a.w == nullptr || count == 0) return;
+            float w[8];
+            load_weights(w, a, col, count);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n[k] = k < count ? (v[k] - mean) * factor * w[k] : 0.0f;
+        };
+        GroupScale whole{};
+        if (a.c.whole) {
+            uint32_t m = 0;
+            for (uint32_t u = threadIdx.x; u < a.c.units; u += kJoinMost) {
+                float v[8], n[8];
+                int64_t col;
+                const int count = joined(v, u, col);
+                normed(n, v, col, count);
+                m = max(m, largest_of(n));
+            }
+            whole = group_scale(most_over_row(m, kJoinMost, most), I8 ? kLargestI8 : kLargestE4m3);
+            if (to && threadIdx.x == 0) scales[0] = whole.scale;
+        }
+        // (out may be the residual itself: every element is read for the last time by the thread that then writes it)
+        for (uint32_t u0 = 0; u0 < a.c.units; u0 += kJoinMost) {
+            const uint32_t u = u0 + threadIdx.x;
+            float v[8], n[8];
+            int64_t col;
+            const int count = joined(v, u, col);
+            normed(n, v, col, count);
+            if (a.out.p != nullptr && count > 0) store_eight<T, P>(v, (T*)a.out.p + r * a.out.ld + col, count);
+            GroupScale g = whole;
+            if (!a.c.whole) {
+                g = group_scale(most_over(largest_of(n), 1u << a.c.shift), I8 ? kLargestI8 : kLargestE4m3);
+                if (to && count > 0 && (u & ((1u << a.c.shift) - 1u)) == 0) scales[u >> a.c.shift] = g.scale;
+            }
+            if (to && count > 0) store_codes<I8>(codes + col, n, g.factor, count, a.code_piece);
+        }
+        __syncthreads();  // the words of the sums are read until here
+    }
+}
+
+// elements of a piece that rows, groups and addresses allow
+int piece_for(const Columns& c, int most, int64_t size, std::initializer_list<const RowsRef*> all, int64_t rows) {
+    for (int v = most; v > 1; v /= 2) {
+        bool ok = c.group % v == 0;
+        for (const RowsRef* m : all)
+            if (m->p != nullptr) ok = ok && (uintptr_t)m->p % (v * size) == 0 && (rows <= 1 || m->ld * size % (v * size) == 0);
+        if (ok) return v;
+    }
+    return 1;
+}
+
+template <class T, int P, bool I8>
+cudaError_t launch_quantize(QuantizeArgs& a, bool in_registers, cudaStream_t st) {
+    const uint32_t units = a.c.units;
+    if (!in_registers || units > 4 * kJoinMost) {
+        const int64_t grid = a.rows < 148 * 8 ? a.rows : 148 * 8;
+        launch_next(quantize_long_kernel<T, P, I8>, (unsigned)grid, kJoinMost, 0, st, a);
+        return cudaGetLastError();
+    }
+    const int K = units <= 64 ? 1 : units <= 2 * kJoinMost ? 2 : 4;
+    uint32_t threads = (units + K - 1) / K;
+    if (threads <= 32) {
+        uint32_t p = 1;
+        while (p < threads) p *= 2;
+        threads = p < (1u << a.c.shift) ? 1u << a.c.shift : p;
+    } else {
+        threads = (threads + 31) / 32 * 32;
+    }
+    a.threads = threads;
+    const uint32_t block = threads >= 128 ? threads : 128 / threads * threads;
+    const int64_t per = block / threads;
+    const int64_t ctas = (a.rows + per - 1) / per;
+    auto launch = [&](auto kernel) {
+        int resident = 1;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, (int)block, 0) != cudaSuccess || resident < 1) resident = 1;
+        const int64_t most = 148ll * resident;
+        launch_next(kernel, (unsigned)(ctas < most ? ctas : most), block, 0, st, a);
+    };
+    if (K == 1) launch(quantize_rows_kernel<T, P, 1, I8>);
+    else if (K == 2) launch(quantize_rows_kernel<T, P, 2, I8>);
+    else launch(quantize_rows_kernel<T, P, 4, I8>);
+    return cudaGetLastError();
+}
+template <class T>
+cudaError_t launch_quantize(QuantizeArgs& a, int i8, bool in_registers, cudaStream_t st) {
+    constexpr int kMost = kPiece<T>;
+    const int piece = piece_for(a.c, kMost, sizeof(T), {&a.x, &a.residual, &a.out}, a.rows);
+    auto go = [&](auto eight) {
+        constexpr bool I8 = decltype(eight)::value;
+        if (piece == kMost) return launch_quantize<T, kMost, I8>(a, in_registers, st);
+        if (kMost == 8 && piece == 4) return launch_quantize<T, 4, I8>(a, in_registers, st);
+        if (piece == 2) return launch_quantize<T, 2, I8>(a, in_registers, st);
+        return launch_quantize<T, 1, I8>(a, in_registers, st);
+    };
+    return i8 ? go(std::true_type{}) : go(std::false_type{});
+}
+
+// ---------------------------------------------------------------- the cache
+
+struct CacheArgs {
+    CacheProblem c;
+    Columns cols;
+    RowsRef rows;
+    int64_t n;
+    uint32_t per_cta;  // rows
+    uint32_t units;    // of a row: eight columns (write), W columns (read)
+    uint64_t magic;    // of units
+    uint64_t group_magic;
+    int code_piece;
+};
+struct Place {
+    int64_t code, scale;  // of the row's first; code -1: none, -2: of no sequence
+};
+constexpr int kCacheRows = 256;  // most rows of a CTA
+
+// the places of the CTA's rows
+__device__ __forceinline__ void find_places(const CacheArgs& a, Place* places, int64_t first, uint32_t rows) {
+    for (uint32_t k = threadIdx.x; k < rows; k += kCodeThreads) {
+        const CacheRow at = cache_row(a.c.at, first + k);
+        Place p{at.page, 0};
+        if (at.page >= 0) {
+            p.code = at.page * a.c.codes.page_ld + at.row * a.c.codes.ld;
+            p.scale = at.page * a.c.scales.page_ld + at.row * a.c.scales.ld;
+        }
+        places[k] = p;
+    }
+    __syncthreads();
+}
+
+template <class T, int P, bool I8, int ITEMS>
+__global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) {
+    __shared__ Place places[kCacheRows];
+    follow();
+    const int64_t first = (int64_t)blockIdx.x * a.per_cta;
+    const uint32_t rows = a.n - first < a.per_cta ? (uint32_t)(a.n - first) : a.per_cta;
+    find_places(a, places, first, rows);
+    const uint32_t items = rows * a.units;
+    for (uint32_t base = 0; base < items; base += kCodeThreads * ITEMS) {
+        Eight<T> e[ITEMS];
+        int count[ITEMS];
+        int64_t col[ITEMS];
+        uint32_t row[ITEMS], unit[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t t = base + i * kCodeThreads + threadIdx.x;
+            row[i] = divide(t, a.units, a.magic);
+            unit[i] = t - row[i] * a.units;
+            count[i] = 0;
+            if (t < items) col[i] = columns_of(a.cols, unit[i], count[i]);
+            if (count[i] > 0 && places[row[i]].code < 0) count[i] = 0;
+            if (count[i] > 0) load_eight<T, P>(e[i], (const T*)a.rows.p + (first + row[i]) * a.rows.ld + col[i], count[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = count[i] > 0 ? widen(e[i].e[k]) : 0.0f;
+            const GroupScale g = group_scale(most_over(largest_of(v), 1u << a.cols.shift), I8 ? kLargestI8 : kLargestE4m3);
+            if (count[i] == 0) continue;
+            const Place at = places[row[i]];
+            if (!ROBE_CHK(col[i] + count[i] <= a.cols.d, ROBE_DBG_ROW_POS)) continue;
+            if ((unit[i] & ((1u << a.cols.shift) - 1u)) == 0) ((float*)a.c.scales.p)[at.scale + (unit[i] >> a.cols.shift)] = g.scale;
+            store_codes<I8>((uint8_t*)a.c.codes.p + at.code + col[i], v, g.factor, count[i], a.code_piece);
+        }
+    }
+}
+
+// W columns a thread: one access of W bytes, W a power of two that divides the group
+template <int W>
+struct CodeWords {
+    uint32_t w[W < 4 ? 1 : W / 4];
+    __device__ __forceinline__ void load(const uint8_t* p) {
+        if constexpr (W == 16) {
+            const uint4 q = __ldcs((const uint4*)p);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (W == 8) {
+            const uint2 q = __ldcs((const uint2*)p);
+            w[0] = q.x; w[1] = q.y;
+        } else if constexpr (W == 4) {
+            w[0] = __ldcs((const uint32_t*)p);
+        } else {
+            w[0] = __ldcs(p);
+        }
+    }
+};
+template <class T, int W, bool I8, int ITEMS>
+__global__ void __launch_bounds__(kCodeThreads) cache_read_kernel(CacheArgs a) {
+    __shared__ Place places[kCacheRows];
+    follow();
+    const int64_t first = (int64_t)blockIdx.x * a.per_cta;
+    const uint32_t rows = a.n - first < a.per_cta ? (uint32_t)(a.n - first) : a.per_cta;
+    find_places(a, places, first, rows);
+    const uint32_t items = rows * a.units;
+    for (uint32_t base = 0; base < items; base += kCodeThreads * ITEMS) {
+        CodeWords<W> e[ITEMS];
+        float scale[ITEMS];
+        uint32_t row[ITEMS], col[ITEMS];
+        int64_t code[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t t = base + i * kCodeThreads + threadIdx.x;
+            row[i] = divide(t, a.units, a.magic);
+            col[i] = (t - row[i] * a.units) * W;
+            code[i] = -2;
+            if (t < items) {
+                const Place at = places[row[i]];
+                code[i] = at.code;
+                if (at.code >= 0 && ROBE_CHK(col[i] + W <= (uint64_t)a.c.d, ROBE_DBG_ROW_POS)) {
+                    e[i].load((const uint8_t*)a.c.codes.p + at.code + col[i]);
+                    scale[i] = __ldca((const float*)a.c.scales.p + at.scale + divide(col[i], (uint32_t)a.c.group, a.group_magic));
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (code[i] == -2) continue;
+            float v[W < 4 ? 4 : W];
+#pragma unroll
+            for (int q = 0; q < (W < 4 ? 1 : W / 4); ++q) values_of<I8>(e[i].w[q], v + 4 * q);
+            T* to = (T*)a.rows.p + (first + row[i]) * a.rows.ld + col[i];
+            constexpr int S = W * (int)sizeof(T) > 16 ? kPiece<T> : W;
+#pragma unroll
+            for (int q = 0; q < W / S; ++q) {
+                Pack<T, S> o;
+#pragma unroll
+                for (int k = 0; k < S; ++k) o.v[k] = narrow<T>(code[i] >= 0 ? v[q * S + k] * scale[i] : 0.0f);
+                store_pack<true, T, S>(to + q * S, o);
+            }
+        }
+    }
+}
+
+// rows of a CTA: about `items` units a thread, spread over the SMs where there are few
+uint32_t rows_per_cta(int64_t n, uint32_t units, int items) {
+    int64_t rows = (int64_t)kCodeThreads * items / units;
+    if (rows > n / (148 * 2)) rows = n / (148 * 2);
+    return (uint32_t)(rows < 1 ? 1 : rows > kCacheRows ? kCacheRows : rows);
+}
+
+template <class T, bool I8>
+cudaError_t launch_write(CacheArgs& a, cudaStream_t st) {
+    constexpr int kMost = kPiece<T>;
+    const int piece = piece_for(a.cols, kMost, sizeof(T), {&a.rows}, a.n);
+    const int64_t grid = (a.n + a.per_cta - 1) / a.per_cta;
+    if (grid >= (1ll << 31)) return kGridTooSmall;
+    auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)grid, kCodeThreads, 0, st, a); };
+    if (piece == kMost) launch(cache_write_kernel<T, kMost, I8, 4>);
+    else if (kMost == 8 && piece == 4) launch(cache_write_kernel<T, 4, I8, 2>);
+    else if (piece == 2) launch(cache_write_kernel<T, 2, I8, 2>);
+    else launch(cache_write_kernel<T, 1, I8, 2>);
+    return cudaGetLastError();
+}
+
+template <class T, bool I8>
+cudaError_t launch_read(CacheArgs& a, int width, cudaStream_t st) {
+    const int64_t grid = (a.n + a.per_cta - 1) / a.per_cta;
+    if (grid >= (1ll << 31)) return kGridTooSmall;
+    auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)grid, kCodeThreads, 0, st, a); };
+    if (width == 16) launch(cache_read_kernel<T, 16, I8, 2>);
+    else if (width == 8) launch(cache_read_kernel<T, 8, I8, 4>);
+    else if (width == 4) launch(cache_read_kernel<T, 4, I8, 4>);
+    else launch(cache_read_kernel<T, 1, I8, 4>);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_residual_quantize(const QuantizeProblem& pb, int dtype, cudaStream_t st) {
+    QuantizeArgs a{};
+    a.rows = pb.rows;
+    a.c = columns(pb.d, pb.group);
+    a.layer = pb.layer;
+    a.eps = pb.eps;
+    a.scale = pb.scale;
+    a.w = pb.w;
+    a.x = pb.x;
+    a.residual = pb.residual;
+    a.out = pb.out;
+    a.codes = pb.codes;
+    a.scales = pb.scales;
+    a.code_piece = piece_for(a.c, 8, 1, {&a.codes}, pb.rows);
+    a.w_pieces = (uintptr_t)pb.w % 16 == 0 && a.c.group % 4 == 0;
+    return dtype == 0 ? launch_quantize<float>(a, pb.i8, true, st) : launch_quantize<__nv_bfloat16>(a, pb.i8, true, st);
+}
+
+cudaError_t launch_cache_write(const CacheProblem& pb, const void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st) {
+    const Columns cols = columns(pb.d, pb.group);
+    const RowsRef codes{pb.codes.p, pb.codes.ld}, codes_pages{pb.codes.p, pb.codes.page_ld};
+    const int code_piece = piece_for(cols, 8, 1, {&codes, &codes_pages}, 2);
+    if (cols.whole) {  // one scale a row, over more columns than a warp holds: as the join does it
+        QuantizeArgs a{};
+        a.rows = n;
+        a.c = cols;
+        a.scale = 1.0f;
+        a.x = RowsRef{(void*)rows, rows_ld};
+        a.codes = codes;
+        a.scales = RowsRef{pb.scales.p, pb.scales.ld};
+        a.codes_page = pb.codes.page_ld;
+        a.scales_page = pb.scales.page_ld;
+        a.code_piece = code_piece;
+        a.cached = 1;
+        a.at = pb.at;
+        return dtype == 0 ? launch_quantize<float>(a, pb.i8, false, st) : launch_quantize<__nv_bfloat16>(a, pb.i8, false, st);
+    }
+    CacheArgs a{};
+    a.c = pb;
+    a.cols = cols;
+    a.rows = RowsRef{(void*)rows, rows_ld};
+    a.n = n;
+    a.units = cols.units;
+    a.magic = magic_of(a.units);
+    a.code_piece = code_piece;
+    a.per_cta = rows_per_cta(n, a.units, 4);
+    if (dtype == 0) return pb.i8 ? launch_write<float, true>(a, st) : launch_write<float, false>(a, st);
+    return pb.i8 ? launch_write<__nv_bfloat16, true>(a, st) : launch_write<__nv_bfloat16, false>(a, st);
+}
+
+cudaError_t launch_cache_read(const CacheProblem& pb, void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st) {
+    const int64_t size = dtype == 0 ? 4 : 2;
+    int width = 16;
+    for (; width > 1; width = width == 4 ? 1 : width / 2) {
+        const int64_t bytes = width * size > 16 ? 16 : width * size;
+        if (pb.d % width == 0 && pb.group % width == 0 && (uintptr_t)pb.codes.p % width == 0 && pb.codes.ld % width == 0 &&
+            pb.codes.page_ld % width == 0 && (uintptr_t)rows % bytes == 0 && (n <= 1 || rows_ld * size % bytes == 0))
+            break;
+    }
+    CacheArgs a{};
+    a.c = pb;
+    a.rows = RowsRef{rows, rows_ld};
+    a.n = n;
+    a.units = (uint32_t)(pb.d / width);
+    a.magic = magic_of(a.units);
+    a.group_magic = magic_of((uint32_t)pb.group);
+    a.per_cta = rows_per_cta(n, a.units, width == 16 ? 2 : 4);
+    if (dtype == 0) return pb.i8 ? launch_read<float, true>(a, width, st) : launch_read<float, false>(a, width, st);
+    return pb.i8 ? launch_read<__nv_bfloat16, true>(a, width, st) : launch_read<__nv_bfloat16, false>(a, width, st);
+}
+
+}  // namespace robe

@@ -126,6 +126,13 @@ void block_key_buffers(const Problem& pb, void* workspace, uint32_t** keys, uint
 cudaError_t launch_block_keys(const Problem& pb, void* workspace, size_t workspace_bytes,
                               cudaStream_t st);
 
+// Stable sort of n < 2^32 pairs by the low `bits` bits of their keys, from the first buffers to those whose number is
+// returned; counts, totals: sort_counts_bytes and sort_totals_bytes of device memory (robe_backward_det.cu).
+size_t sort_counts_bytes();
+size_t sort_totals_bytes();
+int launch_sort_pairs(uint32_t* const (&keys)[2], uint32_t* const (&vals)[2], uint64_t n, uint32_t bits, uint32_t* counts,
+                      uint32_t* totals, cudaStream_t st);
+
 // dense SGD apply of the data-parallel step: array[j] = fma(-lr, grad[j], array[j]) for j < m,
 // grad zeroed afterwards when zero_grad
 cudaError_t launch_dense_sgd_apply(float* array, float* grad, uint64_t m, float lr, bool zero_grad,
@@ -163,6 +170,30 @@ struct ResidualProblem;
 cudaError_t launch_residual_forward(const ResidualProblem& pb, int dtype, cudaStream_t st);
 size_t residual_workspace_bytes(int64_t rows, int64_t d, int64_t gates);
 cudaError_t launch_residual_backward(const ResidualProblem& pb, int dtype, void* workspace, cudaStream_t st);
+
+// ---- plain tables (robe_table.cu)
+struct TableProblem {
+    const void* table;  // forward only
+    int64_t table_ld, vocab, d;
+    int dtype;          // of the table (forward), of the gradient rows (backward)
+    IdList ids;
+    int64_t rows;
+    float scale;
+};
+cudaError_t launch_table_forward(const TableProblem& pb, void* out, int64_t out_ld, int out_dtype, cudaStream_t st);
+size_t table_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d);
+cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int64_t grad_ld, int64_t skip, int accumulate, float* grad_table,
+                                  int64_t grad_table_ld, void* workspace, cudaStream_t st);
+
+// ---- rows in 8 bits (robe_codes.cu), attention over a cache of them (robe_attend.cu)
+struct QuantizeProblem;
+struct CacheProblem;
+struct AttendProblem;
+cudaError_t launch_residual_quantize(const QuantizeProblem& pb, int dtype, cudaStream_t st);
+cudaError_t launch_cache_write(const CacheProblem& pb, const void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st);
+cudaError_t launch_cache_read(const CacheProblem& pb, void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st);
+size_t attend_workspace_bytes(int64_t batch, int64_t heads, int64_t q_heads, int64_t dim, int64_t positions);
+cudaError_t launch_attend(const AttendProblem& pb, void* workspace, cudaStream_t st);
 
 // id / offset range check into the status word
 cudaError_t launch_validate(const Problem& pb, cudaStream_t st);

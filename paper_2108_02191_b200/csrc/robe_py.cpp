@@ -38,6 +38,12 @@ struct RowCalls {
     decltype(&robe_bias_backward) bias_backward;
     decltype(&robe_residual_forward) residual_forward;
     decltype(&robe_residual_backward) residual_backward;
+    decltype(&robe_table_forward) table_forward;
+    decltype(&robe_table_backward) table_backward;
+    decltype(&robe_residual_quantize) residual_quantize;
+    decltype(&robe_cache_write) cache_write;
+    decltype(&robe_cache_read) cache_read;
+    decltype(&robe_cache_attention) cache_attention;
 } row_calls;
 
 PyObject* handle_type;       // ctypes.c_void_p
@@ -139,6 +145,22 @@ struct Reader {
         if (t == nullptr) return m;
         if (t->scalar_type() == at::kBFloat16) m.dtype = ROBE_BF16;
         else if (t->scalar_type() != at::kFloat) ok = false;
+        return matrix_of(t, m);
+    }
+    Matrix codes(int k) {
+        Matrix m;
+        const at::Tensor* t = local(k);
+        if (t == nullptr) return m;
+        m.dtype = code_type(t);
+        return matrix_of(t, m);
+    }
+    int code_type(const at::Tensor* t) {
+        if (t->scalar_type() == at::kFloat8_e4m3fn) return ROBE_E4M3;
+        if (t->scalar_type() != at::kChar) ok = false;
+        return ROBE_I8;
+    }
+    // where a tensor's rows lie; m has its type
+    Matrix matrix_of(const at::Tensor* t, Matrix m) {
         const int64_t dims = t->dim();
         if (dims == 0 || t->numel() == 0) {  // (the ctypes path takes empty ones)
             ok = false;
@@ -196,6 +218,69 @@ struct Reader {
         }
         n = (size_t)t->numel() * t->element_size();
         return t->data_ptr();
+    }
+    // ids of a contiguous tensor of the current device, n of them
+    const void* id_list(int k, int64_t n, int& type) {
+        const at::Tensor* t = local(k);
+        if (t == nullptr) return nullptr;
+        if (t->scalar_type() == at::kLong) type = ROBE_I64;
+        else if (t->scalar_type() == at::kInt) type = ROBE_I32;
+        else ok = false;
+        if (!t->is_contiguous() || t->numel() != n) ok = false;
+        return t->data_ptr();
+    }
+    // [pages, page_rows, ..] with contiguous rows
+    struct Paged {
+        void* p = nullptr;
+        int64_t ld = 0, page = 0, pages = 0, rows = 0, cols = 1;
+    };
+    Paged paged(const at::Tensor* t) {
+        Paged m;
+        const int64_t dims = t->dim();
+        if (dims < 3 || t->numel() == 0) {  // (the ctypes path takes empty ones)
+            ok = false;
+            return m;
+        }
+        for (int64_t i = dims - 1; i >= 2; --i) {
+            if (t->size(i) != 1 && t->stride(i) != m.cols) ok = false;
+            m.cols *= t->size(i);
+        }
+        m.p = t->data_ptr();
+        m.pages = t->size(0);
+        m.rows = t->size(1);
+        m.ld = m.rows > 1 ? t->stride(1) : m.cols;
+        m.page = m.pages > 1 ? t->stride(0) : m.ld * m.rows;
+        return m;
+    }
+    // a cache of the tensors (codes, scales, pages) of those arguments; offsets, starts: argument or -1
+    robe_cache_t cache(int codes_at, int scales_at, int pages_at, int offsets_at, int starts_at, int64_t group) {
+        robe_cache_t c{};
+        const at::Tensor *codes = local(codes_at), *scales = local(scales_at), *pages = local(pages_at);
+        if (!ok) return c;
+        c.code_type = code_type(codes);
+        if (scales->scalar_type() != at::kFloat || pages->scalar_type() != at::kInt || pages->dim() != 2 || pages->numel() == 0) ok = false;
+        if (!ok) return c;
+        const Paged k = paged(codes), s = paged(scales);
+        if (!ok) return c;
+        if (group < 0 || s.pages != k.pages || s.rows != k.rows || s.cols != (group == 0 ? 1 : (k.cols + group - 1) / group)) ok = false;
+        if (pages->size(1) > 1 && pages->stride(1) != 1) ok = false;
+        c.codes = k.p;
+        c.codes_ld = k.ld;
+        c.codes_page = k.page;
+        c.scales = (float*)s.p;
+        c.scales_ld = s.ld;
+        c.scales_page = s.page;
+        c.num_pages = k.pages;
+        c.page_rows = k.rows;
+        c.d = k.cols;
+        c.group = group;
+        c.pages = (const int32_t*)pages->data_ptr();
+        c.batch = pages->size(0);
+        c.max_pages = pages->size(1);
+        c.pages_ld = c.batch > 1 ? pages->stride(0) : c.max_pages;
+        if (offsets_at >= 0) c.offsets = (const int64_t*)vector_or_null(offsets_at, c.batch + 1, at::kLong);
+        if (starts_at >= 0) c.starts = (const int64_t*)vector_or_null(starts_at, c.batch, at::kLong);
+        return c;
     }
     robe_bias_t bias(int k) { return (robe_bias_t)pointer_in(k, bias_handle_type); }
     robe_handle_t handle(int k) { return (robe_handle_t)pointer_in(k, handle_type); }
@@ -533,14 +618,117 @@ PyObject* residual_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// (table, ids, out, scale, stream)
+PyObject* table_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 5) return not_taken();
+    Reader r{args};
+    const Matrix table = r.matrix(0), out = r.matrix(2);
+    int type = ROBE_I64;
+    const void* ids = r.id_list(1, out.rows, type);
+    const float scale = r.number(3);
+    void* st = r.stream(4);
+    if (!r.ok || out.cols != table.cols) return not_taken();
+    return made([&] {
+        return row_calls.table_forward(table.p, table.ld, table.rows, table.cols, table.dtype, ids, type, out.rows, scale, out.p, out.ld,
+                                       out.dtype, st);
+    });
+}
+
+// (grad, ids, grad_table, workspace, scale, accumulate, skip, stream)
+PyObject* table_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return not_taken();
+    Reader r{args};
+    const Matrix grad = r.matrix(0), table = r.matrix(2);
+    int type = ROBE_I64;
+    size_t ws_bytes = 0;
+    const void* ids = r.id_list(1, grad.rows, type);
+    void* ws = r.workspace(3, ws_bytes);
+    const float scale = r.number(4);
+    const int accumulate = r.truth(5);
+    const int64_t skip = r.whole(6);
+    void* st = r.stream(7);
+    if (!r.ok || grad.cols != table.cols || table.dtype != ROBE_F32) return not_taken();
+    return made([&] {
+        return row_calls.table_backward(grad.p, grad.ld, grad.dtype, ids, type, grad.rows, scale, skip, accumulate, (float*)table.p, table.ld,
+                                        table.rows, table.cols, ws, ws_bytes, st);
+    });
+}
+
+// (x, residual, out, codes, scales, w_pre, group, scale, norm, eps, stream)
+PyObject* residual_quantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 11) return not_taken();
+    Reader r{args};
+    const Matrix x = r.matrix(0), residual_ = r.matrix_like(1, x), out = r.matrix_like(2, x), codes = r.codes(3), scales = r.matrix(4);
+    const float* w = (const float*)r.vector_or_null(5, x.cols, at::kFloat);
+    const int64_t group = r.whole(6);
+    const float scale = r.number(7);
+    const int64_t norm = r.whole(8);
+    const float eps = r.number(9);
+    void* st = r.stream(10);
+    if (!r.ok || group < 0 || (norm != ROBE_NORM_RMS && norm != ROBE_NORM_LAYER)) return not_taken();
+    const int64_t groups = group == 0 ? 1 : x.cols / group + (x.cols % group != 0);
+    if (codes.rows != x.rows || codes.cols != x.cols || scales.dtype != ROBE_F32 || scales.rows != x.rows || scales.cols != groups) return not_taken();
+    return made([&] {
+        return row_calls.residual_quantize(x.rows, x.cols, x.dtype, (int)norm, eps, scale, x.p, x.ld, residual_.p, residual_.ld, w, out.p,
+                                           out.ld, codes.p, codes.ld, codes.dtype, group, (float*)scales.p, scales.ld, st);
+    });
+}
+
+// (rows, codes, scales, pages, offsets, starts, group, stream)
+PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return not_taken();
+    Reader r{args};
+    const Matrix rows = r.matrix(0);
+    const robe_cache_t c = r.cache(1, 2, 3, 4, 5, r.whole(6));
+    void* st = r.stream(7);
+    if (!r.ok || rows.cols != c.d) return not_taken();
+    return made([&] { return row_calls.cache_write(&c, rows.p, rows.ld, rows.rows, rows.dtype, st); });
+}
+
+// (codes, scales, pages, out, offsets, starts, group, stream)
+PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return not_taken();
+    Reader r{args};
+    const Matrix out = r.matrix(3);
+    const robe_cache_t c = r.cache(0, 1, 2, 4, 5, r.whole(6));
+    void* st = r.stream(7);
+    if (!r.ok || out.cols != c.d) return not_taken();
+    return made([&] { return row_calls.cache_read(&c, out.p, out.ld, out.rows, out.dtype, st); });
+}
+
+// (q, keys, key_scales, values, value_scales, pages, starts, out, workspace, scale, bias, bias_rows, stream)
+PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 13 || args[6] == Py_None) return not_taken();
+    Reader r{args};
+    const Matrix q = r.matrix(0), out = r.matrix(7);
+    if (!r.ok || q.dtype != ROBE_BF16 || out.dtype != ROBE_BF16 || out.rows != q.rows || out.cols != q.cols) return not_taken();
+    const at::Tensor& t = THPVariable_Unpack(args[0]);
+    if (t.dim() != 3) return not_taken();
+    const int64_t q_heads = t.size(1);
+    const robe_cache_t k = r.cache(1, 2, 5, -1, 6, q.cols), v = r.cache(3, 4, 5, -1, 6, q.cols);
+    size_t ws_bytes = 0;
+    void* ws = r.workspace(8, ws_bytes);
+    const float scale = r.number(9);
+    const bool biased = args[10] != Py_None;
+    const robe_bias_t b = biased ? r.bias(10) : nullptr;
+    const Matrix rows = biased ? r.matrix(11) : Matrix();
+    void* st = r.stream(12);
+    if (!r.ok || k.batch != t.size(0)) return not_taken();
+    if (biased && (rows.dtype != ROBE_F32 || rows.cols != q_heads || rows.rows != row_calls.bias_num_buckets(b))) return not_taken();
+    return made([&] {
+        return row_calls.cache_attention(&k, &v, q.p, q.ld, q_heads, scale, b, (const float*)rows.p, rows.ld, out.p, out.ld, ws, ws_bytes, st);
+    });
+}
+
 // (the type of a position-bias handle, addresses of the C-ABI functions in the order of RowCalls)
 PyObject* set_row_calls(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[6];
-    if (n != 7) {
-        PyErr_SetString(PyExc_TypeError, "set_row_calls takes a type and six addresses");
+    constexpr int kCalls = 12;
+    void* p[kCalls];
+    if (n != kCalls + 1) {
+        PyErr_SetString(PyExc_TypeError, "set_row_calls takes a type and twelve addresses");
         return nullptr;
     }
-    for (int k = 0; k < 6; ++k) {
+    for (int k = 0; k < kCalls; ++k) {
         p[k] = PyLong_AsVoidPtr(args[k + 1]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -548,7 +736,10 @@ PyObject* set_row_calls(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_XSETREF(bias_handle_type, args[0]);
     row_calls = RowCalls{(decltype(row_calls.dropout))p[0],          (decltype(row_calls.bias_num_buckets))p[1],
                          (decltype(row_calls.bias_forward))p[2],     (decltype(row_calls.bias_backward))p[3],
-                         (decltype(row_calls.residual_forward))p[4], (decltype(row_calls.residual_backward))p[5]};
+                         (decltype(row_calls.residual_forward))p[4], (decltype(row_calls.residual_backward))p[5],
+                         (decltype(row_calls.table_forward))p[6],    (decltype(row_calls.table_backward))p[7],
+                         (decltype(row_calls.residual_quantize))p[8], (decltype(row_calls.cache_write))p[9],
+                         (decltype(row_calls.cache_read))p[10],      (decltype(row_calls.cache_attention))p[11]};
     Py_RETURN_NONE;
 }
 
@@ -588,6 +779,12 @@ PyMethodDef methods[] = {
     {"bias_backward", FAST(bias_backward), METH_FASTCALL, "robe_bias_backward"},
     {"residual_forward", FAST(residual_forward), METH_FASTCALL, "robe_residual_forward"},
     {"residual_backward", FAST(residual_backward), METH_FASTCALL, "robe_residual_backward"},
+    {"table_forward", FAST(table_forward), METH_FASTCALL, "robe_table_forward"},
+    {"table_backward", FAST(table_backward), METH_FASTCALL, "robe_table_backward"},
+    {"residual_quantize", FAST(residual_quantize), METH_FASTCALL, "robe_residual_quantize"},
+    {"cache_write", FAST(cache_write), METH_FASTCALL, "robe_cache_write"},
+    {"cache_read", FAST(cache_read), METH_FASTCALL, "robe_cache_read"},
+    {"cache_attention", FAST(cache_attention), METH_FASTCALL, "robe_cache_attention"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_robe_py", "native marshalling of the binding", -1, methods,

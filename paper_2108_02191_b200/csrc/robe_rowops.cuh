@@ -154,6 +154,12 @@ __device__ __forceinline__ bool drop_keeps(const uint4& w, int k, const DropPara
     return ((k & 1) ? word : word << 16) > d.limit;
 }
 
+// k / by for any 32-bit k, by a product
+__device__ __forceinline__ uint32_t divide(uint32_t k, uint32_t by, uint64_t magic) {
+    return by == 1 ? k : (uint32_t)__umul64hi(magic, k);
+}
+inline uint64_t magic_of(uint32_t by) { return by > 1 ? ~0ull / by + 1 : 0; }
+
 // ---- the residual join: what one call is given
 struct RowsRef {  // rows of a matrix, ld elements apart
     void* p;
