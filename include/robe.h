@@ -658,7 +658,7 @@ int robe_cache_read(const robe_cache_t* c, void* out, int64_t out_ld, int64_t n,
  *   bias           handle or NULL;  bias_rows  fp32 [num_buckets, q_heads], bias_ld apart.
  *   workspace      256-byte aligned, robe_cache_attention_workspace_bytes(batch, heads, q_heads, dim, max_pages * page_rows)
  *                  bytes (0 for bad arguments); one call at a time.
- *   max_pages * page_rows < 2^31 - 2^16;  batch * q_heads < 2^31.
+ *   max_pages * page_rows < 2^31 - 2^16;  batch * q_heads < 2^31;  codes of a cache within 64 GB, scales within 16 (ROBE_ERR_UNSUPPORTED).
  * Scores, the divisor and the sums are fp32; a weight is rounded to 11 bits relative to itself, where it is above 2^-14 of the largest.
  * How the sum over a sequence is cut follows from all lengths of the call; the same call gives the same bits.
  * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_WORKSPACE, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.

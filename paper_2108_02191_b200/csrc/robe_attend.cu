@@ -3,10 +3,12 @@
 //     out = sum_j exp(s_j) V_j / sum_j exp(s_j).
 //
 // Bound by memory: 2 (dim + 4) bytes per key and head of the cache, each read once, for 4 dim operations per query head.  A warp
-// takes 16 keys at a time, straight from the cache into the registers of the matrix instructions (m16n8k16, fp16 with fp32
-// sums): codes of 8 bits are exact in fp16, and since the order of a sum's terms is free, a thread loads 16 consecutive bytes
-// of a key and calls them what the instruction wants of it; the transposed values come of one byte permutation per pair of
-// keys, which the widening needs anyway.  Keys' scales multiply the scores; values' scales go into the weights:
+// works on 32 keys at a time (16 where heads have 256 columns) with m16n8k16 instructions (fp16, fp32 sums): a single token has at most as many query heads to a head
+// of the cache as such an instruction has rows, so the tensor cores' larger tiles would stay empty.  Codes of 8 bits are exact in
+// fp16.  Since the order of a sum's terms is free, a thread reads 16 consecutive bytes of a key and calls them what the instruction
+// wants of it, and the transposed values come of one byte permutation per pair of keys, which the widening needs anyway.
+// Keys and values are copied ahead to shared memory, each warp for itself, in pieces of 16 bytes that are shuffled so that both
+// ways of reading them meet no bank twice.  Keys' scales multiply the scores; values' scales go into the weights:
 //     w_j = exp2(x_j - m) sv_j with m the running maximum of x_j + log2(sv_j)  (x_j = s_j log2(e)),
 // so that weights are at most 1 and are rounded to fp16 relative to the largest CONTRIBUTION (half a step is 2^-12 of a
 // weight down to 2^-14 of the largest, 2^-25 of the largest below: the result is bf16), while the divisor
@@ -14,9 +16,9 @@
 // The new tokens' queries are taken to fp16 after an exact division by a power of two (of the row's largest element):
 // bf16 has fewer fraction bits than fp16, so elements down to 2^-16 of the largest stay exact.
 //
-// Work is split over the cache's length by what is really there: a first kernel cuts the sequences, whose lengths it reads,
-// into spans of equal length (at least kSpanLeast keys, as many spans as CTAs are resident), a second one takes a
-// span and a head of the cache per CTA, and a third one joins the spans of a sequence.
+// Work is split over the cache's length by what is really there: the sequences, whose lengths only the device knows, are cut
+// into spans of equal length (by every CTA for itself, or by a kernel of its own where they are many), a CTA takes a span and a
+// head of the cache in turn, and another kernel joins the spans of a sequence.
 #include "robe_codes.cuh"
 #include "robe_internal.h"
 
@@ -26,14 +28,20 @@ namespace {
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = 32 * kAttendWarps;
-constexpr int kTile = 16;                              // keys of a warp's step
-constexpr uint32_t kSpanStep = kTile * kAttendWarps;   // spans are multiples of this
-constexpr uint32_t kSpanLeast = 4 * kSpanStep;
+template <int DIM>
+constexpr int kTile = DIM > 128 ? 16 : 32;             // keys of a warp's step
+constexpr uint32_t kSpanStep = 128;                    // spans are multiples of this, a step of four warps
+constexpr uint32_t kSpanLeast = 2 * kSpanStep;
+// From kSpanMany keys a CTA on, several spans of about kSpanLong are made for each, so that CTAs end together (64 sequences of up to 8191
+// keys, 8 heads of 128: spans of about 512 147 us, 1024 139, 2048 139).
+constexpr uint32_t kSpanMany = 1536, kSpanLong = 1024;
 constexpr int kHeads = 16;                             // query heads of a CTA
 constexpr int kPlanThreads = 1024;
-constexpr uint32_t kAttendCtas = 148 * 4;              // most CTAs
+constexpr uint32_t kPlanWarp = 256;                    // sequences of a call that a warp of each CTA plans for itself
+constexpr uint32_t kAttendCtas = 148 * 8;              // most CTAs
+constexpr uint32_t kSpansPerCta = 8;                   // most spans that are made for a CTA
 
-// What the first kernel leaves: spans before sequence n in first[n], and their length.
+// What the first kernel leaves: the spans' length, and spans before sequence n in first[n].
 struct AttendPlan {
     uint32_t span;
     uint32_t pad[63];
@@ -43,17 +51,65 @@ struct AttendArgs {
     uint32_t blocks;       // heads of the cache x blocks of kHeads of their query heads
     uint32_t head_blocks;  // blocks per head of the cache
     uint32_t group;        // query heads per head of the cache
+    uint32_t rows;         // query heads of the largest block
     uint32_t ctas;         // that spans are made for, at most kAttendCtas
-    uint64_t page_magic;
+    uint32_t page_magic, page_shift;  // key / page_rows = (key * magic >> 32) >> shift, for pages of more than one row
     uint32_t positions;    // that the page table has room for
-    AttendPlan* plan;
-    uint32_t* first;  // [batch + 1]
-    float* parts;     // [spans x blocks][kHeads][dim + 2]
+    uint32_t code_page, code_ld;    // pieces of 16 bytes
+    uint32_t scale_page, scale_ld;  // elements
+    AttendPlan* plan;  // nullptr: few sequences, every CTA plans for itself
+    uint32_t* first;   // [batch + 1]
+    float* parts;     // [spans x blocks][rows][dim + 4]
 };
 
 __device__ __forceinline__ uint32_t length_of(const AttendArgs& a, int64_t n) {
     const int64_t pos = __ldca(a.p.at.starts + n);
     return pos < 0 ? 0 : pos >= (int64_t)a.positions ? a.positions : (uint32_t)pos + 1;
+}
+
+// length of the spans for that many keys in all
+__device__ __forceinline__ uint32_t span_of(const AttendArgs& a, unsigned long long keys) {
+    const unsigned long long each = (keys * a.blocks + a.ctas - 1) / a.ctas;
+    unsigned long long many = each < kSpanMany ? 1 : each / kSpanLong;
+    many = many < kSpansPerCta ? many : kSpansPerCta;
+    const unsigned long long span = ((each + many - 1) / many + kSpanStep - 1) / kSpanStep * kSpanStep;
+    return span < kSpanLeast ? kSpanLeast : (uint32_t)span;
+}
+// The plan of a call of at most kPlanWarp sequences, by the CTA's first warp: first[0 .. batch] and behind them the spans' length.
+__device__ __forceinline__ void plan_in_cta(const AttendArgs& a, uint32_t* first) {
+    constexpr uint32_t kEach = kPlanWarp / 32;
+    if (threadIdx.x < 32) {
+        const uint32_t batch = (uint32_t)a.p.at.batch, n0 = threadIdx.x * kEach;
+        uint32_t length[kEach];
+        unsigned long long keys = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) {
+            length[k] = n0 + k < batch ? length_of(a, n0 + k) : 0;
+            keys += length[k];
+        }
+        for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xFFFFFFFFu, keys, o);
+        const uint32_t span = span_of(a, keys);
+        uint32_t mine = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) {
+            length[k] = (length[k] + span - 1) / span;
+            mine += length[k];
+        }
+        uint32_t before = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, before, o);
+            if (threadIdx.x >= (uint32_t)o) before += b;
+        }
+        before -= mine;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) {
+            if (n0 + k <= batch) first[n0 + k] = before;
+            before += length[k];
+        }
+        if (threadIdx.x == 31 && batch == kPlanWarp) first[batch] = before;
+        if (threadIdx.x == 0) first[kPlanWarp + 1] = span;
+    }
+    __syncthreads();
 }
 
 __global__ void __launch_bounds__(kPlanThreads) attend_plan_kernel(AttendArgs a) {
@@ -71,13 +127,11 @@ __global__ void __launch_bounds__(kPlanThreads) attend_plan_kernel(AttendArgs a)
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
     if (threadIdx.x % 32 == 0) atomicAdd(&keys, mine);  // (whole numbers: the order does not matter)
     __syncthreads();
-    const unsigned long long each = (keys * a.blocks + a.ctas - 1) / a.ctas;
-    unsigned long long span = (each + kSpanStep - 1) / kSpanStep * kSpanStep;
-    span = span < kSpanLeast ? kSpanLeast : span;
-    if (threadIdx.x == 0) a.plan->span = (uint32_t)span;
+    const uint32_t span = span_of(a, keys);
+    if (threadIdx.x == 0) a.plan->span = span;
     for (int64_t base = 0; base < a.p.at.batch; base += kPlanThreads) {
         const int64_t n = base + threadIdx.x;
-        const uint32_t v = n < a.p.at.batch ? (uint32_t)((length_of(a, n) + span - 1) / span) : 0;
+        const uint32_t v = n < a.p.at.batch ? (length_of(a, n) + span - 1) / span : 0;
         uint32_t sum = v;
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, sum, o);
@@ -127,69 +181,133 @@ __device__ __forceinline__ uint32_t pair_of_words(uint32_t a, uint32_t b, int k)
     return widen_pair<I8>(__byte_perm(a, b, I8 ? (k | (4 + k) << 8) | 0 : k | (4 + k) << 4));
 }
 
-// Bytes of a key that thread t of four loads: 16 of every 64, then a quarter of what is left; word w of them starts at
+__device__ __forceinline__ float exp2_of(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float log2_of(float v) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float most_nan(float a, float b) {  // NaN where either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// copies to shared memory; bytes 0: zeros are written and nothing is read
+__device__ __forceinline__ void copy_piece(uint32_t to, const void* from, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_word(uint32_t to, const void* from, uint32_t bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
+// Where byte `at` of key `row` of a step lies.  Rows of 64, 128 and 256 bytes: pieces of 16 bytes change places within 128 so
+// that eight lanes of either way of reading (two keys x four pieces; four keys, two apart, x two pieces) meet all banks.
+template <int DIM>
+__device__ __forceinline__ uint32_t place_of(uint32_t row, uint32_t at) {
+    constexpr uint32_t kPieces = DIM / 16;
+    const uint32_t piece = row * kPieces + at / 16;
+    uint32_t turn = 0;
+    if (kPieces == 8 || kPieces == 16) turn = (row >> 1 & 3) << 1 ^ (row & 1) << 2;
+    else if (kPieces == 4) turn = (row >> 1 & 3) << 1;
+    return (piece ^ turn) * 16 + at % 16;
+}
+// reads of shared memory by its own addresses
+__device__ __forceinline__ void read_words(uint32_t* w, uint32_t at, int words) {
+    if (words == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+    else if (words == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+}
+// The columns of a key that thread t of four has: 16 of every 64, then a quarter of what is left; word w of them starts at
 template <int DIM>
 __device__ __forceinline__ constexpr int key_column(int t, int w) {
     return w < DIM / 64 * 4 ? w / 4 * 64 + t * 16 + w % 4 * 4 : DIM / 64 * 64 + t * (DIM % 64 / 4) + (w - DIM / 64 * 4) * 4;
 }
-template <int DIM>
-__device__ __forceinline__ void load_key(uint32_t (&w)[DIM / 16], const uint8_t* p, int t) {
-#pragma unroll
-    for (int i = 0; i < DIM / 64; ++i) {
-        const uint4 q = __ldcs((const uint4*)(p + i * 64 + t * 16));
-        w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
-    }
-#pragma unroll
-    for (int k = DIM / 64 * 4; k < DIM / 16; ++k) w[k] = __ldcs((const uint32_t*)(p + key_column<DIM>(t, k)));
-}
-// .. of a value that thread g of eight loads: 16 of every 128, then an eighth of what is left; column k of them is
+// .. of a value that thread g of eight has: 16 of every 128, then an eighth of what is left; column k of them is
 template <int DIM>
 __device__ __forceinline__ constexpr int value_column(int g, int k) {
     return k < DIM / 128 * 16 ? k / 16 * 128 + g * 16 + k % 16 : DIM / 128 * 128 + g * (DIM % 128 / 8) + (k - DIM / 128 * 16);
 }
+// Reads of a row, and the words that come in one.
 template <int DIM>
-__device__ __forceinline__ void load_value(uint32_t (&w)[DIM / 32], const uint8_t* p, int g) {
-#pragma unroll
-    for (int i = 0; i < DIM / 128; ++i) {
-        const uint4 q = __ldcs((const uint4*)(p + i * 128 + g * 16));
-        w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
-    }
-    if (DIM % 128 == 64) {
-        const uint2 q = __ldcs((const uint2*)(p + DIM / 128 * 128 + g * 8));
-        w[DIM / 128 * 4] = q.x; w[DIM / 128 * 4 + 1] = q.y;
-    } else {
-#pragma unroll
-        for (int k = DIM / 128 * 4; k < DIM / 32; ++k) w[k] = __ldcs((const uint32_t*)(p + value_column<DIM>(g, k * 4)));
-    }
-}
+__device__ __forceinline__ constexpr int key_words(int read) { return read < DIM / 64 ? 4 : 2; }
+template <int DIM>
+__device__ __forceinline__ constexpr int value_words(int read) { return read < DIM / 128 ? 4 : DIM % 128 == 64 ? 2 : 1; }
+template <int DIM>
+constexpr int kKeyReads = DIM / 64 + (DIM % 64 ? 1 : 0);
+template <int DIM>
+constexpr int kValueReads = DIM / 128 + (DIM % 128 == 64 ? 1 : DIM % 128 / 32);
+
+// A warp's steps ahead in shared memory: keys, values, and their scales.
+constexpr int kStages = 2;
+template <int DIM>
+struct AttendStage {
+    uint8_t keys[kTile<DIM> * DIM], values[kTile<DIM> * DIM];
+    float key_scales[kTile<DIM>], value_scales[kTile<DIM>];
+};
+template <int DIM>
+struct AttendSmem {
+    union {
+        AttendStage<DIM> stages[kAttendWarps][kStages];
+        // after the last step: what a warp has, [kHeads][DIM + 4] in the place of its stages
+        float parts[kAttendWarps][kStages * sizeof(AttendStage<DIM>) / 4];
+    };
+    static_assert(kStages * sizeof(AttendStage<DIM>) >= kHeads * (DIM + 4) * 4, "a warp's part has room in its stages");
+    float warp_most[kAttendWarps][kHeads], warp_sum[kAttendWarps][kHeads];
+    int32_t edges[kBiasMaxSide];
+    uint32_t first[kPlanWarp + 2];
+    float bias[][kHeads + 1];  // as many rows as a side has buckets
+};
 
 // WIDE: more than eight query heads to a CTA.
 template <int DIM, bool I8, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     constexpr int N = WIDE ? 2 : 1;  // blocks of eight query heads
+    constexpr int T = kTile<DIM>, S = kStages;
+    constexpr uint32_t kStep = T * kAttendWarps;
     constexpr float kLog2e = 1.4426950408889634f;
     constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: keys whose values have no scale count in the divisor too
-    __shared__ float joined[kHeads][DIM + 4];
-    __shared__ float warp_most[kAttendWarps][kHeads], warp_sum[kAttendWarps][kHeads];
-    __shared__ float bias[kBiasMaxSide][kHeads + 1];
-    __shared__ int32_t edges[kBiasMaxSide];
+    extern __shared__ __align__(128) uint8_t memory[];
+    AttendSmem<DIM>& sm = *(AttendSmem<DIM>*)memory;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     follow();
-    const uint32_t span = a.plan->span;
     const uint32_t batch = (uint32_t)a.p.at.batch;
-    const uint32_t items = __ldca(a.first + batch) * a.blocks;
+    if (a.plan == nullptr) plan_in_cta(a, sm.first);
+    const uint32_t* const firsts = a.plan == nullptr ? sm.first : a.first;
+    const uint32_t span = a.plan == nullptr ? sm.first[kPlanWarp + 1] : a.plan->span;
+    const uint32_t items = firsts[batch] * a.blocks;
     const uint32_t side = a.p.biased ? a.p.bk.side : 0;
-    for (uint32_t k = threadIdx.x; k < side; k += kAttendThreads) edges[k] = a.p.bk.edges[k];
+    for (uint32_t k = threadIdx.x; k < side; k += kAttendThreads) sm.edges[k] = a.p.bk.edges[k];
+    // where a lane copies to and reads from, in a stage
+    constexpr bool kPlain = 32 % (DIM / 16) == 0;  // (a lane's pieces are the same piece of different rows)
+    const uint32_t stages = (uint32_t)__cvta_generic_to_shared(sm.stages[warp]);
+    const uint8_t* const key_codes = (const uint8_t*)a.p.key_codes.p + (kPlain ? lane % (DIM / 16) * 16 : 0);
+    const uint8_t* const value_codes = (const uint8_t*)a.p.value_codes.p + (kPlain ? lane % (DIM / 16) * 16 : 0);
+    uint32_t copy_at[T * DIM / 512], key_at[kKeyReads<DIM>], value_at[2][kValueReads<DIM>];
+#pragma unroll
+    for (int i = 0; i < T * DIM / 512; ++i) copy_at[i] = place_of<DIM>((lane + 32 * i) / (DIM / 16), (lane + 32 * i) % (DIM / 16) * 16);
+    // (rows eight apart are turned alike: their distance is 8 DIM)
+#pragma unroll
+    for (int i = 0; i < kKeyReads<DIM>; ++i) key_at[i] = place_of<DIM>(g, key_column<DIM>(t, 4 * i));
+#pragma unroll
+    for (int i = 0; i < kValueReads<DIM>; ++i) {
+        const int column = i <= DIM / 128 ? value_column<DIM>(g, 16 * i) : value_column<DIM>(g, DIM / 128 * 16 + (i - DIM / 128) * 4);
+        value_at[0][i] = T * DIM + place_of<DIM>(2 * t, column);
+        value_at[1][i] = T * DIM + place_of<DIM>(2 * t + 1, column);
+    }
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t piece = item / a.blocks, block = item - piece * a.blocks;
         uint32_t n = 0;
         for (uint32_t hi = batch; hi - n > 1;) {  // first[n] <= piece < first[n + 1] (sequences without keys have no piece)
             const uint32_t mid = (n + hi) / 2;
-            if (__ldca(a.first + mid) <= piece) n = mid;
+            if (firsts[mid] <= piece) n = mid;
             else hi = mid;
         }
-        const uint32_t pieces = __ldca(a.first + n + 1) - __ldca(a.first + n);
-        const uint32_t split = piece - __ldca(a.first + n);
+        const uint32_t pieces = firsts[n + 1] - firsts[n];
+        const uint32_t split = piece - firsts[n];
         const uint32_t length = length_of(a, n);
         const int64_t pos = __ldca(a.p.at.starts + n);
         const uint32_t begin = split * span, end = length - begin < span ? length : begin + span;
@@ -197,11 +315,52 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
         const uint32_t q0 = (block - head * a.head_blocks) * kHeads;  // first of its query heads
         const uint32_t in_block = a.group - q0 < (uint32_t)kHeads ? a.group - q0 : (uint32_t)kHeads;
         const int64_t q_row = (int64_t)n * a.p.q_heads + head * a.group + q0;
+
+        // a step's copies: lane l knows where key l lies (of 16: l + 16 too)
+        const int32_t* pages = a.p.at.pages + (int64_t)n * a.p.at.pages_ld;
+        uint32_t next_row = 0;  // of its page: the key whose page was asked for last
+        auto page_of = [&](uint32_t first_key) -> int32_t {
+            const uint32_t j = first_key + lane % T;
+            const uint32_t k = a.p.at.page_rows == 1 ? j : __umulhi(j, a.page_magic) >> a.page_shift;
+            next_row = j - k * a.p.at.page_rows;
+            return j < end ? __ldca(pages + k) : -1;
+        };
+        const uint32_t head_code = head * (DIM / 16);
+        auto copy_step = [&](int32_t page, uint32_t stage) -> unsigned {  // keys that have a place
+            const bool there = page >= 0 && page < a.p.at.num_pages;
+            const unsigned mask = __ballot_sync(0xFFFFFFFFu, there);
+            const uint32_t at = there ? page * a.code_page + (next_row * a.code_ld + head_code) : 0;
+            const uint32_t scale_at = there ? page * a.scale_page + (next_row * a.scale_ld + head) : 0;
+            const uint32_t to = stages + stage * (uint32_t)sizeof(AttendStage<DIM>);
+#pragma unroll
+            for (int i = 0; i < T * DIM / 512; ++i) {
+                const uint32_t r = (lane + 32 * i) / (DIM / 16);
+                const uint32_t from = __shfl_sync(0xFFFFFFFFu, at, r) + (kPlain ? 0 : (lane + 32 * i) % (DIM / 16));
+                const uint32_t bytes = (mask >> r & 1) * 16;
+                copy_piece(to + copy_at[i], key_codes + (uint64_t)from * 16, bytes);
+                copy_piece(to + copy_at[i] + T * DIM, value_codes + (uint64_t)from * 16, bytes);
+            }
+            const uint32_t scales = to + 2 * T * DIM + lane * 4, bytes = there ? 4 : 0;
+            copy_word(scales, (const float*)(T == 32 || lane < 16 ? a.p.key_scales.p : a.p.value_scales.p) + scale_at, bytes);
+            if (T == 32) copy_word(scales + 128, (const float*)a.p.value_scales.p + scale_at, bytes);
+            return mask;
+        };
+        uint32_t key0 = begin + warp * T;
+        unsigned there[S - 1];
+        int32_t next_page = page_of(key0);
+#pragma unroll
+        for (int k = 0; k < S - 1; ++k) {
+            there[k] = copy_step(next_page, k);
+            copies_close();
+            next_page = page_of(key0 + (k + 1) * kStep);
+        }
+
         for (uint32_t k = threadIdx.x; k < side * kHeads; k += kAttendThreads) {
             const uint32_t b = k / kHeads, h = k % kHeads;
-            bias[b][h] = h < in_block ? __ldca(a.p.bias + b * a.p.bias_ld + head * a.group + q0 + h) * kLog2e : 0.0f;
+            sm.bias[b][h] = h < in_block ? __ldca(a.p.bias + b * a.p.bias_ld + head * a.group + q0 + h) * kLog2e : 0.0f;
         }
         // queries: rows g and g + 8 of the instruction's first operand
+        const bool q_pieces = ((uintptr_t)a.p.q.p | (uint64_t)a.p.q.ld * 2) % 8 == 0;
         uint32_t q[N][DIM / 16][2];
         float q_factor[N];
 #pragma unroll
@@ -211,9 +370,21 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
             const __nv_bfloat16* from = (const __nv_bfloat16*)a.p.q.p + (q_row + h) * a.p.q.ld;
             uint32_t most = 0;
 #pragma unroll
-            for (int w = 0; w < DIM / 16; ++w)
+            for (int w = 0; w < DIM / 16; ++w) {
+                const __nv_bfloat16* four = from + key_column<DIM>(t, w);
+                uint2 v = make_uint2(0, 0);
+                if (on && q_pieces) {
+                    v = __ldca((const uint2*)four);
+                } else if (on) {
+                    const unsigned short* one = (const unsigned short*)four;
+                    v = make_uint2(__ldca(one) | (uint32_t)__ldca(one + 1) << 16, __ldca(one + 2) | (uint32_t)__ldca(one + 3) << 16);
+                }
+                q[b][w][0] = v.x;  // (bf16 as it was)
+                q[b][w][1] = v.y;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) most = max(most, on ? magnitude(widen(from[key_column<DIM>(t, w) + k])) : 0u);
+                for (int k = 0; k < 2; ++k)
+                    most = max(most, max(magnitude(widen_low(q[b][w][k])), magnitude(widen_high(q[b][w][k]))));
+            }
             most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
             most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
             uint32_t e = most >> 23;  // (biased exponent of the largest)
@@ -221,16 +392,15 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
             const float down = __uint_as_float((254 - e) << 23);
             q_factor[b] = __uint_as_float(e << 23) * a.p.scale * kLog2e;
 #pragma unroll
-            for (int w = 0; w < DIM / 16; ++w) {
-                float v[4];
+            for (int w = 0; w < DIM / 16; ++w)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = on ? widen(from[key_column<DIM>(t, w) + k]) * down : 0.0f;
-                q[b][w][0] = half2_of(v[0], v[1]);
-                q[b][w][1] = half2_of(v[2], v[3]);
-            }
+                for (int k = 0; k < 2; ++k) q[b][w][k] = half2_of(widen_low(q[b][w][k]) * down, widen_high(q[b][w][k]) * down);
         }
         __syncthreads();
-        const float far_bias[2] = {side > 0 ? bias[side - 1][g] : 0.0f, side > 0 && WIDE ? bias[side - 1][8 + g] : 0.0f};
+        const float far_bias[2] = {side > 0 ? sm.bias[side - 1][g] : 0.0f, side > 0 && WIDE ? sm.bias[side - 1][8 + g] : 0.0f};
+        // steps that begin before this key lie in the last bucket as a whole
+        const int64_t far_end = side == 0 ? (int64_t)end : pos - (T - 1) - sm.edges[side > 0 ? side - 1 : 0] + 1;
+        const uint32_t far_until = far_end < 0 ? 0 : far_end < (int64_t)end ? (uint32_t)far_end : end;
 
         float sum[N], most[N], out[N][DIM / 16][4];
 #pragma unroll
@@ -242,133 +412,96 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) out[b][m][k] = 0.0f;
         }
-
-        // a step's keys: lanes l and l + 16 know where key l lies
-        const int32_t* pages = a.p.at.pages + (int64_t)n * a.p.at.pages_ld;
-        auto page_of = [&](uint32_t first_key) -> int32_t {
-            const uint32_t j = first_key + (lane & 15);
-            if (first_key >= end || j >= end) return -1;
-            const uint32_t k = divide(j, a.p.at.page_rows, a.page_magic);
-            const int32_t page = __ldca(pages + k);
-            return page >= 0 && page < a.p.at.num_pages ? page : -1;
-        };
-        uint32_t keys[2][DIM / 16], values[4][DIM / 32];
-        float scale = 0.0f;
-        int64_t at = -1;
-        auto locate = [&](int32_t page, uint32_t first_key) {
-            const uint32_t j = first_key + (lane & 15);
-            const uint32_t k = divide(j, a.p.at.page_rows, a.page_magic);
-            const uint32_t row = j - k * a.p.at.page_rows;
-            at = page < 0 ? -1 : page * a.p.key_codes.page_ld + (int64_t)row * a.p.key_codes.ld + (int64_t)head * DIM;
-            return page < 0 ? -1 : page * a.p.key_scales.page_ld + (int64_t)row * a.p.key_scales.ld + (int64_t)head;
-        };
-        auto load_keys = [&](int64_t scale_at) {
-            scale = scale_at < 0 ? 0.0f : __ldca((const float*)(lane < 16 ? a.p.key_scales.p : a.p.value_scales.p) + scale_at);
+        uint32_t stage = 0, free_stage = S - 1;
+        for (; key0 < end; key0 += kStep) {
+            copies_wait(S - 2);
+            __syncwarp();  // every lane's copies of this step are there, every lane has read the step before
+            const unsigned here = there[0];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int64_t from = __shfl_sync(0xFFFFFFFFu, at, u * 8 + g);
+            for (int k = 0; k + 1 < S - 1; ++k) there[k] = there[k + 1];
+            there[S - 2] = copy_step(next_page, free_stage);
+            copies_close();
+            next_page = page_of(key0 + S * kStep);
+            const uint32_t from = stages + stage * (uint32_t)sizeof(AttendStage<DIM>);
+            free_stage = stage;
+            stage = stage + 1 < S ? stage + 1 : 0;
+            // scores of query heads g (and g + 8) with keys 2 t, 2 t + 1 of each eight
+            float s[T / 8][4];
 #pragma unroll
-                for (int w = 0; w < DIM / 16; ++w) keys[u][w] = 0;
-                if (from >= 0) load_key<DIM>(keys[u], (const uint8_t*)a.p.key_codes.p + from, t);
-            }
-        };
-        auto load_values = [&]() {
+            for (int u = 0; u < T / 8; ++u) {
+                uint32_t key[DIM / 16];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t from = __shfl_sync(0xFFFFFFFFu, at, 2 * t + (u & 1) + (u & 2) * 4);
-#pragma unroll
-                for (int w = 0; w < DIM / 32; ++w) values[u][w] = 0;
-                if (from >= 0) load_value<DIM>(values[u], (const uint8_t*)a.p.value_codes.p + from, g);
-            }
-        };
-        uint32_t key0 = begin + warp * kTile;
-        load_keys(locate(page_of(key0), key0));
-        load_values();
-        int32_t next_page = page_of(key0 + kSpanStep);
-        for (; key0 < end; key0 += kSpanStep) {
-            // what this step goes on with, before the next one's takes its place
-            const unsigned there = __ballot_sync(0xFFFFFFFFu, at >= 0);
-            const float log_scale = log2f(scale < kLeastScale ? kLeastScale : scale);  // (looked at for the values' only)
-            float key_scale[4], value_scale[4], value_log[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int key = 2 * t + (u & 1) + (u & 2) * 4;
-                key_scale[u] = __shfl_sync(0xFFFFFFFFu, scale, key);
-                value_scale[u] = __shfl_sync(0xFFFFFFFFu, scale, key + 16);
-                value_log[u] = __shfl_sync(0xFFFFFFFFu, log_scale, key + 16);
-            }
-            // scores of query heads g (and g + 8) with keys 2 t, 2 t + 1 of either eight
-            float s[2][4];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
+                for (int i = 0; i < kKeyReads<DIM>; ++i) read_words(key + 4 * i, from + key_at[i] + u * 8 * DIM, key_words<DIM>(i));
 #pragma unroll
                 for (int k = 0; k < 4; ++k) s[u][k] = 0.0f;
 #pragma unroll
                 for (int w = 0; w < DIM / 16; ++w) {
-                    const uint32_t c = signs_turned<I8>(keys[u][w]);
+                    const uint32_t c = signs_turned<I8>(key[w]);
                     multiply(s[u], q[0][w][0], WIDE ? q[N - 1][w][0] : 0u, q[0][w][1], WIDE ? q[N - 1][w][1] : 0u, pair_in_word<I8>(c, 0),
                              pair_in_word<I8>(c, 1));
                 }
             }
-            const uint32_t next = key0 + kSpanStep;
-            const int64_t next_scale = locate(next_page, next);
-            load_keys(next_scale);
-            next_page = page_of(next + kSpanStep);
-            uint32_t weights[N][2];
-            float bias_of[N][4];
-            const int64_t nearest = pos - (int64_t)(key0 + kTile - 1);  // distance of the step's last key
-            const bool far = side == 0 || nearest >= edges[side - 1];
-            if (!far) {
-                const int64_t d = pos - (int64_t)(key0 + (lane & 15));
-                uint32_t b = 0;
-                for (uint32_t hi = side; hi - b > 1;) {
-                    const uint32_t mid = (b + hi) / 2;
-                    if (edges[mid] <= d) b = mid;
+            float value_scale[T / 8][2], value_log[T / 8][2];
+#pragma unroll
+            for (int u = 0; u < T / 8; ++u) {
+                uint32_t k2[2], v2[2];
+                read_words(k2, from + 2 * T * DIM + (8 * u + 2 * t) * 4, 2);
+                read_words(v2, from + 2 * T * DIM + T * 4 + (8 * u + 2 * t) * 4, 2);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const bool in = here >> (8 * u + 2 * t + k) & 1;
+                    value_scale[u][k] = __uint_as_float(v2[k]);
+                    // (a scale that is no number has to come through: the comparison leaves it alone)
+                    value_log[u][k] = in ? log2_of(value_scale[u][k] < kLeastScale ? kLeastScale : value_scale[u][k]) : -INFINITY;
+#pragma unroll
+                    for (int b = 0; b < N; ++b) {
+                        float& x = s[u][2 * b + k];
+                        x = in ? x * __uint_as_float(k2[k]) * q_factor[b] + far_bias[b] : -INFINITY;
+                    }
+                }
+            }
+            if (key0 >= far_until) {
+                const int64_t d = pos - (int64_t)(key0 + lane % T);
+                uint32_t bucket = 0;
+                for (uint32_t hi = side; hi - bucket > 1;) {
+                    const uint32_t mid = (bucket + hi) / 2;
+                    if (sm.edges[mid] <= d) bucket = mid;
                     else hi = mid;
                 }
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t bucket = __shfl_sync(0xFFFFFFFFu, b, 2 * t + (u & 1) + (u & 2) * 4);
+                for (int u = 0; u < T / 8; ++u)
 #pragma unroll
-                    for (int x = 0; x < N; ++x) bias_of[x][u] = bias[bucket][x * 8 + g];
-                }
-            } else {
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t of = __shfl_sync(0xFFFFFFFFu, bucket, 8 * u + 2 * t + k);
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int x = 0; x < N; ++x) bias_of[x][u] = far_bias[x];
+                        for (int b = 0; b < N; ++b) s[u][2 * b + k] += sm.bias[of][b * 8 + g] - far_bias[b];
+                    }
             }
-            bool moved = false;
+            uint32_t weights[N][T / 8];
             float shift[N];
+            bool moved = false;
 #pragma unroll
             for (int b = 0; b < N; ++b) {
-                float x[4], top = -INFINITY;
-                bool nan = false;
+                float top = -INFINITY;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int key = 2 * t + (u & 1) + (u & 2) * 4;
-                    x[u] = there >> key & 1 ? fmaf(s[u / 2][b * 2 + u % 2] * key_scale[u], q_factor[b], bias_of[b][u]) : -INFINITY;
-                    const float with = there >> key & 1 ? x[u] + value_log[u] : -INFINITY;
-                    nan = nan || with != with;
-                    top = fmaxf(top, with);
-                }
-                if (nan) top = NAN;
+                for (int u = 0; u < T / 8; ++u)
 #pragma unroll
-                for (int o = 1; o < 4; o <<= 1) {
-                    const float other = __shfl_xor_sync(0xFFFFFFFFu, top, o);
-                    top = top != top || other != other ? NAN : fmaxf(top, other);
-                }
+                    for (int k = 0; k < 2; ++k) top = most_nan(top, s[u][2 * b + k] + value_log[u][k]);
+                top = most_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = most_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
                 const float old = most[b];
-                most[b] = old != old || top != top ? NAN : fmaxf(old, top);
-                const float base = most[b] == -INFINITY ? 0.0f : most[b];
-                shift[b] = old == -INFINITY ? 0.0f : exp2f(old - base);  // (nothing summed so far: whatever the factor)
+                most[b] = most_nan(old, top);
                 moved = moved || most[b] != old;
-                float e[4];
+                const float base = most[b] == -INFINITY ? 0.0f : most[b];
+                shift[b] = exp2_of(old - base);
+                float added = 0.0f;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) e[u] = exp2f(x[u] - base);
-                sum[b] = sum[b] * shift[b] + ((e[0] + e[1]) + (e[2] + e[3]));
-                weights[b][0] = half2_of(e[0] * value_scale[0], e[1] * value_scale[1]);
-                weights[b][1] = half2_of(e[2] * value_scale[2], e[3] * value_scale[3]);
+                for (int u = 0; u < T / 8; ++u) {
+                    const float e0 = exp2_of(s[u][2 * b] - base), e1 = exp2_of(s[u][2 * b + 1] - base);
+                    added += e0 + e1;
+                    weights[b][u] = half2_of(e0 * value_scale[u][0], e1 * value_scale[u][1]);
+                }
+                sum[b] = sum[b] * shift[b] + added;
             }
             if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
@@ -384,65 +517,74 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
                 }
             }
 #pragma unroll
-            for (int w = 0; w < DIM / 32; ++w) {
-                uint32_t c[4];
+            for (int half = 0; half < T / 16; ++half) {
+                uint32_t value[4][DIM / 32];  // of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
-                for (int u = 0; u < 4; ++u) c[u] = signs_turned<I8>(values[u][w]);
+                for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int k = 0; k < 4; k += 2) {
-                    const uint32_t a0 = pair_of_words<I8>(c[0], c[1], k), a1 = pair_of_words<I8>(c[0], c[1], k + 1),
-                                   a2 = pair_of_words<I8>(c[2], c[3], k), a3 = pair_of_words<I8>(c[2], c[3], k + 1);
+                    for (int i = 0; i < kValueReads<DIM>; ++i)
+                        read_words(value[u] + (i <= DIM / 128 ? 4 * i : DIM / 128 * 4 + i - DIM / 128),
+                                   from + value_at[u & 1][i] + (half * 16 + (u & 2) * 4) * DIM, value_words<DIM>(i));
 #pragma unroll
-                    for (int b = 0; b < N; ++b) multiply(out[b][w * 2 + k / 2], a0, a1, a2, a3, weights[b][0], weights[b][1]);
+                for (int w = 0; w < DIM / 32; ++w) {
+                    uint32_t c[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) c[u] = signs_turned<I8>(value[u][w]);
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        const uint32_t a0 = pair_of_words<I8>(c[0], c[1], k), a1 = pair_of_words<I8>(c[0], c[1], k + 1),
+                                       a2 = pair_of_words<I8>(c[2], c[3], k), a3 = pair_of_words<I8>(c[2], c[3], k + 1);
+#pragma unroll
+                        for (int b = 0; b < N; ++b)
+                            multiply(out[b][w * 2 + k / 2], a0, a1, a2, a3, weights[b][2 * half], weights[b][2 * half + 1]);
+                    }
                 }
             }
-            load_values();
         }
+        copies_wait(0);
         // the four warps' parts
 #pragma unroll
         for (int b = 0; b < N; ++b) {
             sum[b] += __shfl_xor_sync(0xFFFFFFFFu, sum[b], 1);
             sum[b] += __shfl_xor_sync(0xFFFFFFFFu, sum[b], 2);
             if (t == 0) {
-                warp_most[warp][b * 8 + g] = most[b];
-                warp_sum[warp][b * 8 + g] = sum[b];
+                sm.warp_most[warp][b * 8 + g] = most[b];
+                sm.warp_sum[warp][b * 8 + g] = sum[b];
             }
         }
         __syncthreads();
         auto most_of = [&](int h) {
-            float m = -INFINITY;
-            bool nan = false;
-            for (int w = 0; w < kAttendWarps; ++w) {
-                nan = nan || warp_most[w][h] != warp_most[w][h];
-                m = fmaxf(m, warp_most[w][h]);
-            }
-            return nan ? NAN : m;
+            float m = sm.warp_most[0][h];
+            for (int w = 1; w < kAttendWarps; ++w) m = most_nan(m, sm.warp_most[w][h]);
+            return m;
         };
-        auto factor_of = [&](int w, int h, float m) { return warp_most[w][h] == -INFINITY ? 0.0f : exp2f(warp_most[w][h] - m); };
-        for (int w = 0; w < kAttendWarps; ++w) {
-            if (warp == w) {
+        auto factor_of = [&](int w, int h, float m) { return sm.warp_most[w][h] == -INFINITY ? 0.0f : exp2_of(sm.warp_most[w][h] - m); };
+        // (this warp's own stages: nobody else reads or writes them)
 #pragma unroll
-                for (int b = 0; b < N; ++b) {
-                    const int h = b * 8 + 2 * t;
-                    const float f0 = factor_of(w, h, most_of(h)), f1 = factor_of(w, h + 1, most_of(h + 1));
+        for (int b = 0; b < N; ++b) {
+            const int h = b * 8 + 2 * t;
+            const float f0 = factor_of(warp, h, most_of(h)), f1 = factor_of(warp, h + 1, most_of(h + 1));
 #pragma unroll
-                    for (int m = 0; m < DIM / 16; ++m)
+            for (int m = 0; m < DIM / 16; ++m)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            float* to = &joined[h + (k & 1)][value_column<DIM>(g, 2 * m + k / 2)];
-                            const float v = out[b][m][k] * (k & 1 ? f1 : f0);
-                            *to = w == 0 ? v : *to + v;
-                        }
-                }
-            }
-            __syncthreads();
+                for (int k = 0; k < 4; ++k)
+                    sm.parts[warp][(h + (k & 1)) * (DIM + 4) + value_column<DIM>(g, 2 * m + k / 2)] = out[b][m][k] * (k & 1 ? f1 : f0);
         }
+        __syncthreads();
         for (uint32_t k = threadIdx.x; k < in_block * (DIM / 4); k += kAttendThreads) {
             const uint32_t h = k / (DIM / 4), col = k % (DIM / 4) * 4;
             const float m = most_of(h);
             float total = 0.0f;
-            for (int w = 0; w < kAttendWarps; ++w) total += warp_sum[w][h] * factor_of(w, h, m);
-            const float4 v = *(const float4*)&joined[h][col];
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kAttendWarps; ++w) {
+                total += sm.warp_sum[w][h] * factor_of(w, h, m);
+                const float4 p = *(const float4*)&sm.parts[w][h * (DIM + 4) + col];
+                v.x += p.x;
+                v.y += p.y;
+                v.z += p.z;
+                v.w += p.w;
+            }
             if (!ROBE_CHK(n < batch && head * a.group + q0 + h < (uint64_t)a.p.q_heads, ROBE_DBG_ROW_POS)) continue;
             if (pieces == 1) {
                 const float by = total == 0.0f ? 0.0f : 1.0f / total;
@@ -452,7 +594,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
                 to[2] = narrow<__nv_bfloat16>(v.z * by);
                 to[3] = narrow<__nv_bfloat16>(v.w * by);
             } else {
-                float* to = a.parts + ((uint64_t)item * kHeads + h) * (DIM + 4);
+                float* to = a.parts + ((uint64_t)item * a.rows + h) * (DIM + 4);
                 *(float4*)(to + col) = v;
                 if (col == 0) {
                     to[DIM] = m;
@@ -460,67 +602,84 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
                 }
             }
         }
-        __syncthreads();  // (the next item's bias and sums take their place)
+        __syncthreads();  // (the next item's bias, sums and stages take their place)
     }
 }
 
-// The spans of a sequence: a CTA per query head, warps taking spans in turn.  Sequences of one span are done already;
+// The spans of a sequence: a CTA per query head, its warps taking spans in turn.  Sequences of one span are done already;
 // those without keys get +0.
-constexpr int kJoinThreads = 256;
+constexpr int kSpanThreads = 256;
 template <int DIM>
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(AttendArgs a) {
-    constexpr int kWarps = kJoinThreads / 32, E = DIM / 32;
-    __shared__ float sums[kWarps][DIM], totals[kWarps], mosts[kWarps];
+__global__ void __launch_bounds__(kSpanThreads) attend_join_kernel(AttendArgs a) {
+    constexpr int kWarps = kSpanThreads / 32, E = DIM / 32, kAhead = 4;
+    __shared__ float sums[kWarps][DIM], words[kWarps], factors[kSpanThreads];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     follow();
     const uint32_t n = blockIdx.x / (uint32_t)a.p.q_heads, h = blockIdx.x - n * (uint32_t)a.p.q_heads;
-    const uint32_t first = __ldca(a.first + n), pieces = __ldca(a.first + n + 1) - first;
+    __shared__ uint32_t planned[kPlanWarp + 2];
+    if (a.plan == nullptr) plan_in_cta(a, planned);
+    const uint32_t* const firsts = a.plan == nullptr ? planned : a.first;
+    const uint32_t first = firsts[n], pieces = firsts[n + 1] - first;
     __nv_bfloat16* to = (__nv_bfloat16*)a.p.out.p + ((int64_t)n * a.p.q_heads + h) * a.p.out.ld;
     if (pieces == 1) return;
     if (pieces == 0) {
-        for (int k = threadIdx.x; k < DIM; k += kJoinThreads) to[k] = narrow<__nv_bfloat16>(0.0f);
+        for (int k = threadIdx.x; k < DIM; k += kSpanThreads) to[k] = narrow<__nv_bfloat16>(0.0f);
         return;
     }
     const uint32_t head = h / a.group, in_group = h - head * a.group;
     const uint32_t block = head * a.head_blocks + in_group / kHeads;
-    const float* parts = a.parts + (((uint64_t)first * a.blocks + block) * kHeads + in_group % kHeads) * (DIM + 4);
-    const uint64_t step = (uint64_t)a.blocks * kHeads * (DIM + 4);
-    float sum[E], total = 0.0f, most = -INFINITY;
+    const float* parts = a.parts + (((uint64_t)first * a.blocks + block) * a.rows + in_group % kHeads) * (DIM + 4);
+    const uint64_t step = (uint64_t)a.blocks * a.rows * (DIM + 4);
+    float most = -INFINITY;
+    for (uint32_t p = threadIdx.x; p < pieces; p += kSpanThreads) most = most_nan(most, __ldca(parts + p * step + DIM));
+    for (int o = 16; o > 0; o >>= 1) most = most_nan(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    if (lane == 0) words[warp] = most;
+    __syncthreads();
+    most = words[0];
+    for (int w = 1; w < kWarps; ++w) most = most_nan(most, words[w]);
+    float sum[E], total = 0.0f;
 #pragma unroll
     for (int k = 0; k < E; ++k) sum[k] = 0.0f;
-    bool nan = false;
-    for (uint32_t p = warp; p < pieces; p += kWarps) {
-        const float* from = parts + p * step;
-        const float m = __ldca(from + DIM), l = __ldca(from + DIM + 1);
-        float v[E];
+    for (uint32_t p0 = 0; p0 < pieces; p0 += kSpanThreads) {
+        const uint32_t count = pieces - p0 < (uint32_t)kSpanThreads ? pieces - p0 : (uint32_t)kSpanThreads;
+        float f = 0.0f;
+        if (threadIdx.x < count) {
+            const float* from = parts + (p0 + threadIdx.x) * step + DIM;
+            const float m = __ldca(from);
+            f = m == -INFINITY ? 0.0f : exp2_of(m - most);
+            total += __ldca(from + 1) * f;
+        }
+        __syncthreads();  // (the factors before have been read)
+        factors[threadIdx.x] = f;
+        __syncthreads();
+        for (uint32_t p = warp; p < count; p += kWarps * kAhead) {
+            float v[kAhead][E];
 #pragma unroll
-        for (int k = 0; k < E; ++k) v[k] = __ldca(from + k * 32 + lane);
-        nan = nan || m != m;
-        if (m == -INFINITY) continue;
-        const float up = fmaxf(most, m), f = most == -INFINITY ? 0.0f : exp2f(most - up), e = exp2f(m - up);
+            for (int u = 0; u < kAhead; ++u)
+                if (p + u * kWarps < count)
 #pragma unroll
-        for (int k = 0; k < E; ++k) sum[k] = sum[k] * f + v[k] * e;
-        total = total * f + l * e;
-        most = up;
+                    for (int k = 0; k < E; ++k) v[u][k] = __ldca(parts + (p0 + p + u * kWarps) * step + k * 32 + lane);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (p + u * kWarps < count) {
+                    const float e = factors[p + u * kWarps];
+#pragma unroll
+                    for (int k = 0; k < E; ++k) sum[k] = fmaf(v[u][k], e, sum[k]);
+                }
+        }
     }
-    if (nan) most = NAN;
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    __syncthreads();
+    if (lane == 0) words[warp] = total;
 #pragma unroll
     for (int k = 0; k < E; ++k) sums[warp][k * 32 + lane] = sum[k];
-    if (lane == 0) {
-        totals[warp] = total;
-        mosts[warp] = most;
-    }
     __syncthreads();
-    float m = -INFINITY;
-    for (int w = 0; w < kWarps; ++w) m = m != m || mosts[w] != mosts[w] ? NAN : fmaxf(m, mosts[w]);
-    for (int k = threadIdx.x; k < DIM; k += kJoinThreads) {
-        float v = 0.0f, l = 0.0f;
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = mosts[w] == -INFINITY ? 0.0f : exp2f(mosts[w] - m);
-            v += sums[w][k] * f;
-            l += totals[w] * f;
-        }
-        to[k] = narrow<__nv_bfloat16>(l == 0.0f ? 0.0f : v / l);
+    total = 0.0f;
+    for (int w = 0; w < kWarps; ++w) total += words[w];
+    for (int k = threadIdx.x; k < DIM; k += kSpanThreads) {
+        float v = 0.0f;
+        for (int w = 0; w < kWarps; ++w) v += sums[w][k];
+        to[k] = narrow<__nv_bfloat16>(total == 0.0f ? 0.0f : v / total);
     }
 }
 
@@ -528,31 +687,38 @@ uint32_t head_blocks_of(int64_t heads, int64_t q_heads) { return (uint32_t)((q_h
 
 template <int DIM>
 cudaError_t launch_attend_dim(AttendArgs& a, cudaStream_t st) {
+    cudaError_t e = cudaSuccess;
     auto launch = [&](auto kernel) {
+        const size_t bytes = sizeof(AttendSmem<DIM>) + (a.p.biased ? a.p.bk.side : 0) * (kHeads + 1) * sizeof(float);
         int resident = 1;
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, kAttendThreads, 0) != cudaSuccess || resident < 1) resident = 1;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, kAttendThreads, bytes);
+        if (e != cudaSuccess) return;
         a.ctas = 148u * (unsigned)resident < kAttendCtas ? 148u * (unsigned)resident : kAttendCtas;
-        launch_next(attend_plan_kernel, 1, kPlanThreads, 0, st, a);
-        launch_next(kernel, a.ctas, kAttendThreads, 0, st, a);
+        if (a.plan != nullptr) launch_next(attend_plan_kernel, 1, kPlanThreads, 0, st, a);
+        launch_next(kernel, a.ctas, kAttendThreads, bytes, st, a);
     };
     if (a.group > 8) a.p.i8 ? launch(attend_kernel<DIM, true, true>) : launch(attend_kernel<DIM, false, true>);
     else a.p.i8 ? launch(attend_kernel<DIM, true, false>) : launch(attend_kernel<DIM, false, false>);
-    launch_next(attend_join_kernel<DIM>, (unsigned)(a.p.at.batch * a.p.q_heads), kJoinThreads, 0, st, a);
+    if (e != cudaSuccess) return e;
+    launch_next(attend_join_kernel<DIM>, (unsigned)(a.p.at.batch * a.p.q_heads), kSpanThreads, 0, st, a);
     return cudaGetLastError();
 }
 
-// spans are made for at most kAttendCtas items; every sequence may have one more than its share, and no span is shorter than kSpanLeast
+// a sequence has at most one span more than its share of those that are made for the CTAs, and no span is shorter than kSpanLeast
 uint64_t most_items(int64_t batch, uint32_t blocks, int64_t positions) {
     const unsigned __int128 by_length = (unsigned __int128)batch * ((positions + kSpanLeast - 1) / kSpanLeast) * blocks;
-    const unsigned __int128 by_share = (unsigned __int128)kAttendCtas + (unsigned __int128)batch * blocks;
+    const unsigned __int128 by_share = (unsigned __int128)kAttendCtas * kSpansPerCta + (unsigned __int128)batch * blocks;
     return (uint64_t)(by_length < by_share ? by_length : by_share);
 }
+uint32_t rows_of(int64_t heads, int64_t q_heads) { return q_heads / heads < kHeads ? (uint32_t)(q_heads / heads) : (uint32_t)kHeads; }
+size_t plan_bytes(int64_t batch) { return sizeof(AttendPlan) + (((size_t)batch + 1) * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t attend_workspace_bytes(int64_t batch, int64_t heads, int64_t q_heads, int64_t dim, int64_t positions) {
-    const size_t first = sizeof(AttendPlan) + (((size_t)batch + 1) * 4 + 255) / 256 * 256;
-    return first + most_items(batch, (uint32_t)heads * head_blocks_of(heads, q_heads), positions) * kHeads * (dim + 4) * 4;
+    return plan_bytes(batch) +
+           most_items(batch, (uint32_t)heads * head_blocks_of(heads, q_heads), positions) * rows_of(heads, q_heads) * (dim + 4) * 4;
 }
 
 cudaError_t launch_attend(const AttendProblem& pb, void* workspace, cudaStream_t st) {
@@ -561,13 +727,26 @@ cudaError_t launch_attend(const AttendProblem& pb, void* workspace, cudaStream_t
     a.group = (uint32_t)(pb.q_heads / pb.heads);
     a.head_blocks = head_blocks_of(pb.heads, pb.q_heads);
     a.blocks = (uint32_t)pb.heads * a.head_blocks;
-    a.page_magic = magic_of(pb.at.page_rows);
+    a.rows = rows_of(pb.heads, pb.q_heads);
+    // positions below 2^31: the quotient is exact with magic = floor(2^(31 + l) / page_rows) + 1, l = ceil(log2(page_rows))
+    uint32_t l = 0;
+    while ((1ull << l) < pb.at.page_rows) ++l;
+    a.page_magic = pb.at.page_rows > 1 ? (uint32_t)((1ull << (31 + l)) / pb.at.page_rows + 1) : 0;
+    a.page_shift = l > 0 ? l - 1 : 0;
     a.positions = (uint32_t)(pb.at.max_pages * pb.at.page_rows);
-    a.plan = (AttendPlan*)workspace;
+    // places are numbered in 32 bits: pieces of 16 bytes, scales
+    const uint64_t pages = (uint64_t)(pb.at.num_pages > 0 ? pb.at.num_pages - 1 : 0), rows = pb.at.page_rows - 1;
+    const unsigned __int128 last = (unsigned __int128)pages * pb.key_codes.page_ld + rows * (uint64_t)pb.key_codes.ld + pb.heads * pb.dim;
+    const unsigned __int128 last_scale = (unsigned __int128)pages * pb.key_scales.page_ld + rows * (uint64_t)pb.key_scales.ld + pb.heads;
+    if (last / 16 >= (1ull << 32) - 1 || last_scale >= (1ull << 32)) return kGridTooSmall;
+    a.code_page = (uint32_t)(pb.key_codes.page_ld / 16);
+    a.code_ld = (uint32_t)(pb.key_codes.ld / 16);
+    a.scale_page = (uint32_t)pb.key_scales.page_ld;
+    a.scale_ld = (uint32_t)pb.key_scales.ld;
+    a.plan = pb.at.batch > kPlanWarp ? (AttendPlan*)workspace : nullptr;
     a.first = (uint32_t*)((char*)workspace + sizeof(AttendPlan));
-    a.parts = (float*)((char*)workspace + sizeof(AttendPlan) + (((size_t)pb.at.batch + 1) * 4 + 255) / 256 * 256);
-    if ((uint64_t)pb.at.batch * pb.q_heads >= (1ull << 31)) return kGridTooSmall;
-    if (most_items(pb.at.batch, a.blocks, a.positions) >= (1ull << 32) - 148 * 16) return kGridTooSmall;
+    a.parts = (float*)((char*)workspace + plan_bytes(pb.at.batch));
+    if (most_items(pb.at.batch, a.blocks, a.positions) >= (1ull << 32) - kAttendCtas) return kGridTooSmall;
     switch (pb.dim) {
         case 32: return launch_attend_dim<32>(a, st);
         case 64: return launch_attend_dim<64>(a, st);

@@ -16,25 +16,41 @@ constexpr int kJoinMost = 512;       // threads a row
 constexpr int64_t kGroupMost = 256;  // columns of a group that lanes of one warp hold; beyond: one scale a row
 
 // Eight columns of a row, loaded and stored by pieces of P elements; where fewer than eight are left, one by one.
+// (as words: kept apart, bf16 elements would take a register each)
 template <class T>
 struct Eight {
-    T e[8];
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ float get(int k) const {
+        if (sizeof(T) == 4) return __uint_as_float(w[k]);
+        return k % 2 ? widen_high(w[k / 2]) : widen_low(w[k / 2]);
+    }
 };
 template <class T, int P>
 constexpr int kStep = P * (int)sizeof(T) > 16 ? kPiece<T> : P;
 template <class T, int P>
 __device__ __forceinline__ void load_eight(Eight<T>& r, const T* p, int count) {
-    constexpr int S = kStep<T, P>;
-    if (count == 8) {
+    constexpr int S = kStep<T, P>, B = S * (int)sizeof(T);
+    if (count == 8 && B >= 4) {
+        using W = typename Word<B >= 4 ? B : 4>::type;
 #pragma unroll
         for (int q = 0; q < 8 / S; ++q) {
-            const Pack<T, S> e = load_pack<true, T, S>(p + q * S);
+            union {
+                W w;
+                uint32_t u[B >= 4 ? B / 4 : 1];
+            } e;
+            e.w = __ldcs((const W*)(p + q * S));
 #pragma unroll
-            for (int k = 0; k < S; ++k) r.e[q * S + k] = e.v[k];
+            for (int k = 0; k < B / 4; ++k) r.w[q * (B / 4) + k] = e.u[k];
         }
+    } else if (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r.w[k] = k < count ? __ldcs((const uint32_t*)p + k) : 0u;
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) r.e[k] = k < count ? p[k] : narrow<T>(0.0f);
+        for (int k = 0; k < 4; ++k) {
+            r.w[k] = 2 * k < count ? __ldcs((const unsigned short*)p + 2 * k) : 0u;
+            if (2 * k + 1 < count) r.w[k] |= (uint32_t)__ldcs((const unsigned short*)p + 2 * k + 1) << 16;
+        }
     }
 }
 template <class T, int P>
@@ -177,46 +193,42 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t threads, 
     return v;
 }
 
-// A row in the registers of its threads, K units each; the next row's loads are under way while one is worked on.
-template <class T, int P, int K, bool I8>
-__global__ void __launch_bounds__(kJoinMost) quantize_rows_kernel(QuantizeArgs a) {
-    __shared__ float sums[2][2][kJoinMost / 32];  // (two rows' turns: a barrier of the next row stands between a read and the next write)
-    __shared__ uint32_t most[2][kJoinMost / 32];
-    constexpr bool kAhead = K * sizeof(T) <= 8;
+// A row in the registers of its threads, K units each.  What hides the loads' latency is CTAs, not rows asked for ahead: at 16384 x
+// 4096 bf16 two CTAs an SM that asked for the next row took 252 us, five without LATER.
+template <class T, int P, int K, bool I8, int THREADS>
+__global__ void __launch_bounds__(THREADS, K == 4 ? 1 : 1024 / THREADS) quantize_rows_kernel(QuantizeArgs a) {
+    __shared__ float sums[2][2][THREADS / 32];  // (two rows' turns: a barrier of the next row stands between a read and the next write)
+    __shared__ uint32_t most[2][THREADS / 32];
     follow();
     const uint32_t per_cta = blockDim.x / a.threads;
     const uint32_t t = threadIdx.x % a.threads;
     const int64_t stride = (int64_t)gridDim.x * per_cta;
-    int64_t col[K];
-    int count[K];
-#pragma unroll
-    for (int j = 0; j < K; ++j) col[j] = columns_of(a.c, t + j * a.threads, count[j]);
-    Eight<T> x[K], y[K];
-    auto load = [&](int64_t r) {
-        if (r >= a.rows) return;
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            if (count[j] == 0) continue;
-            if (!ROBE_CHK(col[j] + count[j] <= a.c.d, ROBE_DBG_ROW_POS)) continue;
-            load_eight<T, P>(x[j], (const T*)a.x.p + r * a.x.ld + col[j], count[j]);
-            if (a.residual.p != nullptr) load_eight<T, P>(y[j], (const T*)a.residual.p + r * a.residual.ld + col[j], count[j]);
-        }
-    };
     int64_t r = (int64_t)blockIdx.x * per_cta + threadIdx.x / a.threads;
-    load(r);
     int turn = 0;
     for (int64_t base = (int64_t)blockIdx.x * per_cta; base < a.rows; base += stride, r += stride, turn ^= 1) {
         const bool on = r < a.rows;
+        int col[K], count[K];
+        Eight<T> x[K], y[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            col[j] = (int)columns_of(a.c, t + j * a.threads, count[j]);
+            if (!on || !ROBE_CHK(col[j] + count[j] <= a.c.d || count[j] == 0, ROBE_DBG_ROW_POS)) count[j] = 0;
+            if (count[j] > 0) load_eight<T, P>(x[j], (const T*)a.x.p + r * a.x.ld + col[j], count[j]);
+        }
+        if (a.residual.p != nullptr) {
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (count[j] > 0) load_eight<T, P>(y[j], (const T*)a.residual.p + r * a.residual.ld + col[j], count[j]);
+        }
         float v[K][8];
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float s = a.scale * widen(x[j].e[k]);
-                v[j][k] = !on || count[j] == 0 ? 0.0f : a.residual.p != nullptr ? widen(y[j].e[k]) + s : s;
+                const float s = a.scale * x[j].get(k);
+                v[j][k] = count[j] == 0 ? 0.0f : a.residual.p != nullptr ? y[j].get(k) + s : s;
             }
-        if (kAhead) load(r + stride);
-        if (a.out.p != nullptr && on) {
+        if (a.out.p != nullptr) {
 #pragma unroll
             for (int j = 0; j < K; ++j)
                 if (count[j] > 0) store_eight<T, P>(v[j], (T*)a.out.p + r * a.out.ld + col[j], count[j]);
@@ -249,16 +261,15 @@ __global__ void __launch_bounds__(kJoinMost) quantize_rows_kernel(QuantizeArgs a
                 for (int k = 0; k < 8; ++k) v[j][k] = v[j][k] * factor * w[k];
             }
         }
-        uint8_t* codes = nullptr;
-        float* scales = nullptr;
-        const bool to = on && codes_row(a, r, codes, scales);
+        uint8_t* const codes = (uint8_t*)a.codes.p + r * a.codes.ld;
+        float* const scales = (float*)a.scales.p + r * a.scales.ld;
         GroupScale whole{};
         if (a.c.whole) {
             uint32_t m = 0;
 #pragma unroll
             for (int j = 0; j < K; ++j) m = max(m, largest_of(v[j]));
             whole = group_scale(most_over_row(m, a.threads, most[turn]), I8 ? kLargestI8 : kLargestE4m3);
-            if (to && t == 0) scales[0] = whole.scale;
+            if (on && t == 0) scales[0] = whole.scale;
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -266,11 +277,10 @@ __global__ void __launch_bounds__(kJoinMost) quantize_rows_kernel(QuantizeArgs a
             if (!a.c.whole) {
                 g = group_scale(most_over(largest_of(v[j]), 1u << a.c.shift), I8 ? kLargestI8 : kLargestE4m3);
                 const uint32_t unit = t + j * a.threads;
-                if (to && count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
+                if (count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
             }
-            if (to && count[j] > 0) store_codes<I8>(codes + col[j], v[j], g.factor, count[j], a.code_piece);
+            if (count[j] > 0) store_codes<I8>(codes + col[j], v[j], g.factor, count[j], a.code_piece);
         }
-        if (!kAhead) load(r + stride);
     }
 }
 
@@ -296,8 +306,8 @@ __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a
             if (a.residual.p != nullptr) load_eight<T, P>(y, (const T*)a.residual.p + r * a.residual.ld + col, count);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float s = a.scale * widen(x.e[k]);
-                if (k < count) v[k] = a.residual.p != nullptr ? widen(y.e[k]) + s : s;
+                const float s = a.scale * x.get(k);
+                if (k < count) v[k] = a.residual.p != nullptr ? y.get(k) + s : s;
             }
             return count;
         };
@@ -396,15 +406,11 @@ cudaError_t launch_quantize(QuantizeArgs& a, bool in_registers, cudaStream_t st)
     const uint32_t block = threads >= 128 ? threads : 128 / threads * threads;
     const int64_t per = block / threads;
     const int64_t ctas = (a.rows + per - 1) / per;
-    auto launch = [&](auto kernel) {
-        int resident = 1;
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, (int)block, 0) != cudaSuccess || resident < 1) resident = 1;
-        const int64_t most = 148ll * resident;
-        launch_next(kernel, (unsigned)(ctas < most ? ctas : most), block, 0, st, a);
-    };
-    if (K == 1) launch(quantize_rows_kernel<T, P, 1, I8>);
-    else if (K == 2) launch(quantize_rows_kernel<T, P, 2, I8>);
-    else launch(quantize_rows_kernel<T, P, 4, I8>);
+    auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)(ctas < (1ll << 30) ? ctas : 1ll << 30), block, 0, st, a); };
+    if (K == 1) launch(quantize_rows_kernel<T, P, 1, I8, 256>);
+    else if (K == 2 && block <= 256) launch(quantize_rows_kernel<T, P, 2, I8, 256>);
+    else if (K == 2) launch(quantize_rows_kernel<T, P, 2, I8, 512>);
+    else launch(quantize_rows_kernel<T, P, 4, I8, 512>);
     return cudaGetLastError();
 }
 template <class T>
@@ -439,16 +445,20 @@ struct Place {
 };
 constexpr int kCacheRows = 256;  // most rows of a CTA
 
-// the places of the CTA's rows
+// the places of the CTA's rows: one warp finds the first row's sequence, from which the others are near
 __device__ __forceinline__ void find_places(const CacheArgs& a, Place* places, int64_t first, uint32_t rows) {
-    for (uint32_t k = threadIdx.x; k < rows; k += kCodeThreads) {
-        const CacheRow at = cache_row(a.c.at, first + k);
-        Place p{at.page, 0};
-        if (at.page >= 0) {
-            p.code = at.page * a.c.codes.page_ld + at.row * a.c.codes.ld;
-            p.scale = at.page * a.c.scales.page_ld + at.row * a.c.scales.ld;
+    if (threadIdx.x < 32) {
+        int64_t near = 0;
+        if (a.c.at.offsets != nullptr) near = sequence_of_warp(a.c.at, first);
+        for (uint32_t k = threadIdx.x; k < rows; k += 32) {
+            const CacheRow at = cache_row(a.c.at, first + k, near);
+            Place p{at.page, 0};
+            if (at.page >= 0) {
+                p.code = at.page * a.c.codes.page_ld + at.row * a.c.codes.ld;
+                p.scale = at.page * a.c.scales.page_ld + at.row * a.c.scales.ld;
+            }
+            places[k] = p;
         }
-        places[k] = p;
     }
     __syncthreads();
 }
@@ -459,7 +469,6 @@ __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) 
     follow();
     const int64_t first = (int64_t)blockIdx.x * a.per_cta;
     const uint32_t rows = a.n - first < a.per_cta ? (uint32_t)(a.n - first) : a.per_cta;
-    find_places(a, places, first, rows);
     const uint32_t items = rows * a.units;
     for (uint32_t base = 0; base < items; base += kCodeThreads * ITEMS) {
         Eight<T> e[ITEMS];
@@ -473,17 +482,18 @@ __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) 
             unit[i] = t - row[i] * a.units;
             count[i] = 0;
             if (t < items) col[i] = columns_of(a.cols, unit[i], count[i]);
-            if (count[i] > 0 && places[row[i]].code < 0) count[i] = 0;
             if (count[i] > 0) load_eight<T, P>(e[i], (const T*)a.rows.p + (first + row[i]) * a.rows.ld + col[i], count[i]);
         }
+        if (base == 0) find_places(a, places, first, rows);  // (while the rows are on their way)
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = count[i] > 0 ? widen(e[i].e[k]) : 0.0f;
+            for (int k = 0; k < 8; ++k) v[k] = count[i] > 0 ? e[i].get(k) : 0.0f;
             const GroupScale g = group_scale(most_over(largest_of(v), 1u << a.cols.shift), I8 ? kLargestI8 : kLargestE4m3);
             if (count[i] == 0) continue;
             const Place at = places[row[i]];
+            if (at.code < 0) continue;
             if (!ROBE_CHK(col[i] + count[i] <= a.cols.d, ROBE_DBG_ROW_POS)) continue;
             if ((unit[i] & ((1u << a.cols.shift) - 1u)) == 0) ((float*)a.c.scales.p)[at.scale + (unit[i] >> a.cols.shift)] = g.scale;
             store_codes<I8>((uint8_t*)a.c.codes.p + at.code + col[i], v, g.factor, count[i], a.code_piece);

@@ -91,16 +91,37 @@ __device__ __forceinline__ CacheRow cache_row_at(const CachePlaces& p, int64_t s
     at.row = (uint32_t)((uint64_t)pos - k * p.page_rows);
     return at;
 }
-// row r of the call
-__device__ __forceinline__ CacheRow cache_row(const CachePlaces& p, int64_t r) {
+// Sequence of row r of the call (offsets given): the last whose first row is at or before it, 0 where none is.  A warp looks at 32 places
+// at a time.
+__device__ __forceinline__ int64_t sequence_of_warp(const CachePlaces& p, int64_t r) {
+    const int64_t lane = threadIdx.x & 31;
+    int64_t lo = 0, hi = p.batch;  // offsets[lo] <= r, or lo is 0; offsets[hi] > r, or hi is batch
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+        const int hits = __popc(__ballot_sync(0xFFFFFFFFu, at < hi && __ldca(p.offsets + at) <= r));
+        const int64_t up = lo + (hits + 1) * step;
+        lo += hits * step;
+        if (up < hi) hi = up;
+    }
+    return lo;
+}
+// row r of the call; near: a sequence at or before its own (offsets given)
+__device__ __forceinline__ CacheRow cache_row(const CachePlaces& p, int64_t r, int64_t near = 0) {
     int64_t s, t;
     if (p.offsets == nullptr) {
         s = r / p.per;
         t = r - s * p.per;
     } else {
-        if (r < __ldca(p.offsets) || r >= __ldca(p.offsets + p.batch)) return CacheRow{-2, 0};
-        int64_t lo = 0, hi = p.batch;  // offsets[lo] <= r < offsets[hi]
-        while (hi - lo > 1) {
+        if (p.batch == 0 || r < __ldca(p.offsets) || r >= __ldca(p.offsets + p.batch)) return CacheRow{-2, 0};
+        int64_t lo = near, hi = p.batch;
+        for (int64_t step = 1; lo + step < p.batch; step *= 2) {  // (the next one's beginning first)
+            if (__ldca(p.offsets + lo + step) > r) {
+                hi = lo + step;
+                break;
+            }
+            lo += step;
+        }
+        while (hi - lo > 1) {  // offsets[lo] <= r < offsets[hi]
             const int64_t mid = (lo + hi) / 2;
             if (__ldca(p.offsets + mid) <= r) lo = mid;
             else hi = mid;
