@@ -279,6 +279,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     const uint32_t* const firsts = a.plan == nullptr ? sm.first : a.first;
     const uint32_t span = a.plan == nullptr ? sm.first[kPlanWarp + 1] : a.plan->span;
     const uint32_t items = firsts[batch] * a.blocks;
+    if (a.plan == nullptr && blockIdx.x == 0)
+        for (uint32_t k = threadIdx.x; k <= batch; k += kAttendThreads) a.first[k] = sm.first[k];  // for the join
     const uint32_t side = a.p.biased ? a.p.bk.side : 0;
     for (uint32_t k = threadIdx.x; k < side; k += kAttendThreads) sm.edges[k] = a.p.bk.edges[k];
     // where a lane copies to and reads from, in a stage
@@ -606,80 +608,78 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     }
 }
 
-// The spans of a sequence: a CTA per query head, its warps taking spans in turn.  Sequences of one span are done already;
-// those without keys get +0.
+// The spans of a sequence: a CTA per query head, its warps taking spans in turn, eight under way at a time.  Sequences of one
+// span are done already; those without keys get +0.
 constexpr int kSpanThreads = 256;
 template <int DIM>
 __global__ void __launch_bounds__(kSpanThreads) attend_join_kernel(AttendArgs a) {
-    constexpr int kWarps = kSpanThreads / 32, E = DIM / 32, kAhead = 4;
-    __shared__ float sums[kWarps][DIM], words[kWarps], factors[kSpanThreads];
+    constexpr int kWarps = kSpanThreads / 32, E = DIM / 32, kAhead = DIM > 128 ? 4 : 8;
+    __shared__ float sums[kWarps][DIM], totals[kWarps], mosts[kWarps];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    follow();
     const uint32_t n = blockIdx.x / (uint32_t)a.p.q_heads, h = blockIdx.x - n * (uint32_t)a.p.q_heads;
-    __shared__ uint32_t planned[kPlanWarp + 2];
-    if (a.plan == nullptr) plan_in_cta(a, planned);
-    const uint32_t* const firsts = a.plan == nullptr ? planned : a.first;
-    const uint32_t first = firsts[n], pieces = firsts[n + 1] - first;
+    const uint32_t head = h / a.group, in_group = h - head * a.group;
+    const uint32_t block = head * a.head_blocks + in_group / kHeads;
+    follow();
+    const uint32_t first = __ldca(a.first + n), pieces = __ldca(a.first + n + 1) - first;
     __nv_bfloat16* to = (__nv_bfloat16*)a.p.out.p + ((int64_t)n * a.p.q_heads + h) * a.p.out.ld;
     if (pieces == 1) return;
     if (pieces == 0) {
         for (int k = threadIdx.x; k < DIM; k += kSpanThreads) to[k] = narrow<__nv_bfloat16>(0.0f);
         return;
     }
-    const uint32_t head = h / a.group, in_group = h - head * a.group;
-    const uint32_t block = head * a.head_blocks + in_group / kHeads;
     const float* parts = a.parts + (((uint64_t)first * a.blocks + block) * a.rows + in_group % kHeads) * (DIM + 4);
     const uint64_t step = (uint64_t)a.blocks * a.rows * (DIM + 4);
-    float most = -INFINITY;
-    for (uint32_t p = threadIdx.x; p < pieces; p += kSpanThreads) most = most_nan(most, __ldca(parts + p * step + DIM));
-    for (int o = 16; o > 0; o >>= 1) most = most_nan(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-    if (lane == 0) words[warp] = most;
-    __syncthreads();
-    most = words[0];
-    for (int w = 1; w < kWarps; ++w) most = most_nan(most, words[w]);
-    float sum[E], total = 0.0f;
+    float sum[E], total = 0.0f, most = -INFINITY;
 #pragma unroll
     for (int k = 0; k < E; ++k) sum[k] = 0.0f;
-    for (uint32_t p0 = 0; p0 < pieces; p0 += kSpanThreads) {
-        const uint32_t count = pieces - p0 < (uint32_t)kSpanThreads ? pieces - p0 : (uint32_t)kSpanThreads;
-        float f = 0.0f;
-        if (threadIdx.x < count) {
-            const float* from = parts + (p0 + threadIdx.x) * step + DIM;
-            const float m = __ldca(from);
-            f = m == -INFINITY ? 0.0f : exp2_of(m - most);
-            total += __ldca(from + 1) * f;
+    for (uint32_t p = warp; p < pieces; p += kWarps * kAhead) {
+        float m[kAhead], l[kAhead], v[kAhead][E], top = most;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            m[u] = -INFINITY;
+            if (p + u * kWarps < pieces) {
+                const float* from = parts + (p + u * kWarps) * step;
+                m[u] = __ldca(from + DIM);
+                l[u] = __ldca(from + DIM + 1);
+#pragma unroll
+                for (int k = 0; k < E; ++k) v[u][k] = __ldca(from + k * 32 + lane);
+            }
         }
-        __syncthreads();  // (the factors before have been read)
-        factors[threadIdx.x] = f;
-        __syncthreads();
-        for (uint32_t p = warp; p < count; p += kWarps * kAhead) {
-            float v[kAhead][E];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (p + u * kWarps < count)
+        for (int u = 0; u < kAhead; ++u) top = most_nan(top, m[u]);
+        const float base = top == -INFINITY ? 0.0f : top, f = exp2_of(most - base);
+        total *= f;
 #pragma unroll
-                    for (int k = 0; k < E; ++k) v[u][k] = __ldca(parts + (p0 + p + u * kWarps) * step + k * 32 + lane);
+        for (int k = 0; k < E; ++k) sum[k] *= f;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (p + u * kWarps < count) {
-                    const float e = factors[p + u * kWarps];
+        for (int u = 0; u < kAhead; ++u) {
+            if (p + u * kWarps >= pieces) break;
+            const float e = exp2_of(m[u] - base);
+            total = fmaf(l[u], e, total);
 #pragma unroll
-                    for (int k = 0; k < E; ++k) sum[k] = fmaf(v[u][k], e, sum[k]);
-                }
+            for (int k = 0; k < E; ++k) sum[k] = fmaf(v[u][k], e, sum[k]);
         }
+        most = top;
     }
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-    __syncthreads();
-    if (lane == 0) words[warp] = total;
 #pragma unroll
     for (int k = 0; k < E; ++k) sums[warp][k * 32 + lane] = sum[k];
+    if (lane == 0) {
+        totals[warp] = total;
+        mosts[warp] = most;
+    }
     __syncthreads();
-    total = 0.0f;
-    for (int w = 0; w < kWarps; ++w) total += words[w];
     for (int k = threadIdx.x; k < DIM; k += kSpanThreads) {
-        float v = 0.0f;
-        for (int w = 0; w < kWarps; ++w) v += sums[w][k];
-        to[k] = narrow<__nv_bfloat16>(total == 0.0f ? 0.0f : v / total);
+        float m = mosts[0], v = 0.0f, l = 0.0f;
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) m = most_nan(m, mosts[w]);
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float f = exp2_of(mosts[w] - base);
+            v = fmaf(sums[w][k], f, v);
+            l = fmaf(totals[w], f, l);
+        }
+        to[k] = narrow<__nv_bfloat16>(l == 0.0f ? 0.0f : v / l);
     }
 }
 
