@@ -181,7 +181,7 @@ struct TableProblem {
     float scale;
 };
 cudaError_t launch_table_forward(const TableProblem& pb, void* out, int64_t out_ld, int out_dtype, cudaStream_t st);
-size_t table_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d);
+size_t table_grad_workspace_bytes(int64_t rows, int64_t d);
 cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int64_t grad_ld, int64_t skip, int accumulate, float* grad_table,
                                   int64_t grad_table_ld, void* workspace, cudaStream_t st);
 

@@ -121,7 +121,7 @@ int robe_table_forward(const void* table, int64_t table_ld, int64_t vocab, int64
 }
 
 size_t robe_table_backward_workspace_bytes(int64_t rows, int64_t vocab, int64_t d) {
-    return table_grad_sizes(rows, vocab, d) ? table_grad_workspace_bytes(rows, vocab, d) : 0;
+    return table_grad_sizes(rows, vocab, d) ? table_grad_workspace_bytes(rows, d) : 0;
 }
 
 int robe_table_backward(const void* grad, int64_t grad_ld, int dtype, const void* ids, int index_type, int64_t rows,
@@ -132,8 +132,9 @@ int robe_table_backward(const void* grad, int64_t grad_ld, int dtype, const void
     Span list;
     TableProblem pb;
     if (!ids_span(list, pb.ids, ids, index_type, rows)) return ROBE_ERR_INVALID_ARG;
-    const size_t need = table_grad_workspace_bytes(rows, vocab, d);
-    if (workspace == nullptr || workspace_bytes < need || ((uintptr_t)workspace & 255u) != 0) return ROBE_ERR_WORKSPACE;
+    const size_t need = table_grad_workspace_bytes(rows, d);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return ROBE_ERR_WORKSPACE;
+    if (((uintptr_t)workspace & 255u) != 0) return ROBE_ERR_WORKSPACE;
     const Span scratch{workspace, 1, 1, (int64_t)need, 1};
     Checked k;
     k.reads(from);

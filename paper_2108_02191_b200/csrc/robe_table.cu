@@ -15,23 +15,43 @@ namespace {
 
 constexpr int kTableThreads = 256;
 
-// V consecutive elements by accesses of at most 16 bytes
-template <class T, int V>
-constexpr int kAccess = V * (int)sizeof(T) > 16 ? kPiece<T> : V;
+// V consecutive elements by accesses of at most 16 bytes.  Held as words: bf16 elements kept apart would take a register each.
 template <class T, int V>
 struct Elements {
-    Pack<T, kAccess<T, V>> p[V / kAccess<T, V>];
-    __device__ __forceinline__ float get(int k) const { return widen(p[k / kAccess<T, V>].v[k % kAccess<T, V>]); }
-    __device__ __forceinline__ void set(int k, float v) { p[k / kAccess<T, V>].v[k % kAccess<T, V>] = narrow<T>(v); }
+    static constexpr int kBytes = V * (int)sizeof(T), kAccess = kBytes > 16 ? 16 : kBytes;
+    using W = typename Word<kAccess>::type;
+    union {
+        W access[kBytes / kAccess];
+        uint32_t word[(kBytes + 3) / 4];
+    } e;
+    __device__ __forceinline__ float get(int k) const {
+        if (sizeof(T) == 4) return __uint_as_float(e.word[k]);
+        if (V == 1) return widen_low((uint32_t) * (const unsigned short*)&e);
+        return k % 2 ? widen_high(e.word[k / 2]) : widen_low(e.word[k / 2]);
+    }
+    __device__ __forceinline__ void set(const float (&v)[V]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) e.word[k] = __float_as_uint(v[k]);
+        } else if constexpr (V == 1) {
+            e.word[0] = narrow2(v[0], 0.0f);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; k += 2) e.word[k / 2] = narrow2(v[k], v[k + 1]);
+        }
+    }
     template <bool STREAM>
     __device__ __forceinline__ void load(const T* from) {
 #pragma unroll
-        for (int q = 0; q < V / kAccess<T, V>; ++q) p[q] = load_pack<STREAM, T, kAccess<T, V>>(from + q * kAccess<T, V>);
+        for (int q = 0; q < kBytes / kAccess; ++q) e.access[q] = STREAM ? __ldcs((const W*)from + q) : __ldca((const W*)from + q);
     }
     template <bool STREAM>
     __device__ __forceinline__ void store(T* to) const {
 #pragma unroll
-        for (int q = 0; q < V / kAccess<T, V>; ++q) store_pack<STREAM, T, kAccess<T, V>>(to + q * kAccess<T, V>, p[q]);
+        for (int q = 0; q < kBytes / kAccess; ++q) {
+            if (STREAM) __stcs((W*)to + q, e.access[q]);
+            else ((W*)to)[q] = e.access[q];
+        }
     }
 };
 
@@ -50,34 +70,64 @@ struct LookupArgs {
     float scale;
 };
 
-// A thread takes ITEMS pieces of V elements, a CTA's width apart, all of their loads under way together.
-template <class TT, class TO, int V, int ITEMS>
-__global__ void __launch_bounds__(kTableThreads) lookup_kernel(LookupArgs a) {
+// A thread takes a piece of V elements: few pieces, spread over the SMs.
+template <class TT, class TO, int V>
+__global__ void __launch_bounds__(kTableThreads) lookup_few_kernel(LookupArgs a) {
     follow();
-    const uint32_t t0 = blockIdx.x * (uint32_t)(kTableThreads * ITEMS) + threadIdx.x;
-    Elements<TT, V> e[ITEMS];
-    uint32_t row[ITEMS], piece[ITEMS];
-    bool in[ITEMS];
+    const uint32_t t = blockIdx.x * (uint32_t)kTableThreads + threadIdx.x;
+    if (t >= a.items) return;
+    const uint32_t row = divide(t, a.pieces, a.magic), piece = t - row * a.pieces;
+    const int64_t id = a.ids.load(a.first + row);
+    const bool in = id >= 0 && id < a.vocab;
+    Elements<TT, V> e;
+    if (in) e.template load<false>((const TT*)a.table + id * a.table_ld + (uint64_t)piece * V);
+    float v[V];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t t = t0 + i * kTableThreads;
-        row[i] = divide(t, a.pieces, a.magic);
-        piece[i] = t - row[i] * a.pieces;
-        in[i] = false;
-        if (t < a.items) {
-            const int64_t id = a.ids.load(a.first + row[i]);
-            in[i] = id >= 0 && id < a.vocab;
-            if (in[i]) e[i].template load<false>((const TT*)a.table + id * a.table_ld + (uint64_t)piece[i] * V);
-        }
+    for (int k = 0; k < V; ++k) v[k] = in ? e.get(k) * a.scale : 0.0f;
+    Elements<TO, V> o;
+    o.set(v);
+    o.template store<false>((TO*)a.out + row * a.out_ld + (uint64_t)piece * V);
+}
+
+// Many pieces: a CTA takes the ids of its rows to shared memory first, so that the latency of an id is paid once for kTiles times ITEMS
+// rows of loads (852 K rows of 128, fp32 to bf16: ids by each thread for itself 79 us, four pieces a thread under way 62, two
+// 60).
+constexpr int kTiles = 8;
+constexpr int kLookupItems = 2;
+constexpr uint32_t kLookupPieces = kTableThreads * kTiles * kLookupItems;
+template <class TT, class TO, int V>
+__global__ void __launch_bounds__(kTableThreads) lookup_kernel(LookupArgs a) {
+    __shared__ uint32_t ids[kLookupPieces + 1];
+    follow();
+    const uint32_t t0 = blockIdx.x * kLookupPieces, end = a.items - t0 < kLookupPieces ? a.items : t0 + kLookupPieces;
+    const uint32_t row0 = divide(t0, a.pieces, a.magic), rows = divide(end - 1, a.pieces, a.magic) - row0 + 1;
+    for (uint32_t k = threadIdx.x; k < rows; k += kTableThreads) {
+        const int64_t id = a.ids.load(a.first + row0 + k);
+        if (ROBE_CHK(k < kLookupPieces + 1, ROBE_DBG_SHARED)) ids[k] = id >= 0 && id < a.vocab ? (uint32_t)id : 0xFFFFFFFFu;
     }
+    __syncthreads();
+    for (uint32_t base = t0 + threadIdx.x; base < end; base += kTableThreads * kLookupItems) {
+        Elements<TT, V> e[kLookupItems];
+        uint32_t row[kLookupItems], piece[kLookupItems], id[kLookupItems];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        if (t0 + i * kTableThreads >= a.items) return;
-        if (!ROBE_CHK(piece[i] < a.pieces && (uint64_t)row[i] * a.pieces + piece[i] < a.items, ROBE_DBG_ROW_POS)) return;
-        Elements<TO, V> o;
+        for (int i = 0; i < kLookupItems; ++i) {
+            const uint32_t t = base + i * kTableThreads;
+            row[i] = divide(t, a.pieces, a.magic);
+            piece[i] = t - row[i] * a.pieces;
+            id[i] = t < end ? ids[row[i] - row0] : 0xFFFFFFFFu;
+            if (id[i] != 0xFFFFFFFFu) e[i].template load<false>((const TT*)a.table + id[i] * a.table_ld + (uint64_t)piece[i] * V);
+        }
 #pragma unroll
-        for (int k = 0; k < V; ++k) o.set(k, in[i] ? e[i].get(k) * a.scale : 0.0f);
-        o.template store<false>((TO*)a.out + row[i] * a.out_ld + (uint64_t)piece[i] * V);
+        for (int i = 0; i < kLookupItems; ++i) {
+            if (base + i * kTableThreads >= end) break;
+            if (!ROBE_CHK(piece[i] < a.pieces && (uint64_t)row[i] * a.pieces + piece[i] < a.items, ROBE_DBG_ROW_POS)) return;
+            float v[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = id[i] != 0xFFFFFFFFu ? e[i].get(k) * a.scale : 0.0f;
+            Elements<TO, V> o;
+            o.set(v);
+            o.template store<false>((TO*)a.out + row[i] * a.out_ld + (uint64_t)piece[i] * V);
+        }
     }
 }
 
@@ -94,11 +144,9 @@ int piece_of(int most, int64_t d, const void* p, int64_t p_ld, int64_t p_size, c
 
 template <class TT, class TO, int V>
 void launch_lookup(const LookupArgs& a, cudaStream_t st) {
-    // few pieces: one a thread, spread over more SMs
-    constexpr int kItems = 4;
-    const bool few = a.items < 148u * 4 * kTableThreads * kItems;
-    const uint32_t per = kTableThreads * (few ? 1 : kItems);
-    launch_next(few ? lookup_kernel<TT, TO, V, 1> : lookup_kernel<TT, TO, V, kItems>, (a.items + per - 1) / per, kTableThreads, 0, st, a);
+    if (a.items < 148u * kLookupPieces)
+        launch_next(lookup_few_kernel<TT, TO, V>, (a.items + kTableThreads - 1) / kTableThreads, kTableThreads, 0, st, a);
+    else launch_next(lookup_kernel<TT, TO, V>, (a.items + kLookupPieces - 1) / kLookupPieces, kTableThreads, 0, st, a);
 }
 
 template <class TT, class TO>
@@ -112,22 +160,27 @@ void launch_lookup(const LookupArgs& a, int piece, cudaStream_t st) {
 
 // ---------------------------------------------------------------- gradient
 
-// Rows of a chunk of sorted positions.  Enough chunks for two waves of threads with eight columns each; at most 256 rows, so that
-// no fp32 sum has more terms than that.
+// Rows of a chunk of sorted positions: as many as make one full wave of CTAs (four an SM, eight columns a thread); at least 16, and at
+// most 256, so that no fp32 sum has more terms than that.  A border costs a row of sums for the run that crosses it, and CTAs
+// beyond a wave leave SMs empty: 16384 x 4096 bf16 (Zipf ids, accumulating) two waves 84 us, one and a half 81, one 71; 852 K x
+// 64 fp32 159, 153, 148; less than one 73 and 154.
 uint32_t chunk_rows(int64_t rows, int64_t d) {
-    const unsigned __int128 threads = (unsigned __int128)rows * (uint64_t)((d + 7) / 8);
-    uint32_t c = 16;
-    while (c < 256 && threads / (2 * c) >= 2u * 148u * 2048u) c *= 2;
-    return c;
+    const unsigned __int128 threads = (unsigned __int128)rows * (uint64_t)((d + 7) / 8), wanted = 4 * 148 * kTableThreads;
+    const unsigned __int128 c = (threads + wanted - 1) / wanted;
+    return c < 16 ? 16 : c > 256 ? 256 : (uint32_t)c;
 }
+// Where there are many chunks, the parts of a run that covers kFold of them are added up before the join.
+constexpr uint32_t kFold = 32;
+constexpr uint64_t kFoldFrom = 1024;
 
+constexpr int64_t kClusterRows = 65536;  // up to so many ids one cluster sorts in its shared memory
 struct GradLayout {
-    size_t keys[2], places[2], counts, totals, flags, parts, total;
+    size_t keys[2], places[2], counts, totals, parts, folds, total;
     uint32_t chunk;
     uint64_t chunks;
     int64_t parts_ld;
 };
-GradLayout grad_layout(int64_t rows, int64_t vocab, int64_t d) {
+GradLayout grad_layout(int64_t rows, int64_t d) {
     GradLayout L;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -136,16 +189,17 @@ GradLayout grad_layout(int64_t rows, int64_t vocab, int64_t d) {
         return here;
     };
     for (int k = 0; k < 2; ++k) {
-        L.keys[k] = take((size_t)rows * 4);
-        L.places[k] = take((size_t)rows * 4);
+        const bool used = k == 0 || rows > kClusterRows;
+        L.keys[k] = take(used ? (size_t)rows * 4 : 0);
+        L.places[k] = take(used ? (size_t)rows * 4 : 0);
     }
-    L.counts = take(sort_counts_bytes());
-    L.totals = take(sort_totals_bytes());
-    L.flags = take((size_t)vocab);
+    L.counts = take(rows > kClusterRows ? sort_counts_bytes() : 0);
+    L.totals = take(rows > kClusterRows ? sort_totals_bytes() : 0);
     L.chunk = chunk_rows(rows, d);
     L.chunks = ((uint64_t)rows + L.chunk - 1) / L.chunk;
     L.parts_ld = (d + 3) / 4 * 4;
     L.parts = take((size_t)L.chunks * 2 * L.parts_ld * 4);
+    L.folds = take(L.chunks >= kFoldFrom ? (size_t)(L.chunks / kFold) * L.parts_ld * 8 : 0);
     L.total = at;
     return L;
 }
@@ -160,38 +214,218 @@ struct GradArgs {
     float scale;
     int accumulate;
     uint32_t *keys, *places;  // sorted from grad_sums_kernel on
-    uint8_t* flags;           // [vocab] row has a gradient; not looked at when accumulating
     float* parts;             // [chunks][2]: what a chunk has of the run it begins in, and of the run it ends in
     int64_t parts_ld;
+    double* folds;            // [chunks / kFold]: the first parts of kFold chunks that lie in one run as a whole; nullptr: none
     uint32_t chunk;
     uint64_t chunks;
     uint32_t slices;       // of columns: CTAs per row (sums), warps per row (join)
-    uint32_t join_blocks;  // grad_join_kernel: CTAs that join; the others fill
-    uint32_t pieces;       // fill: of a row
-    uint64_t magic;        // of pieces
+    uint32_t lanes;        // join: that take a part's columns of a slice, four each
+    int flat;              // the table is one run of elements from a 16-byte boundary on
     int aligned;           // rows of `table` in pieces of four columns
 };
 
-// Sort keys: ids; what gets no gradient sorts behind them.
+// ---- ids and positions in the order of the ids, equal ids in the order of the call (least digit first, stable)
+
+// The sort key of a position: the id; what gets no gradient sorts behind all of them.
+__device__ __forceinline__ uint32_t key_of(const GradArgs& a, int64_t p) {
+    const int64_t id = a.ids.load(p);
+    return id >= 0 && id < a.vocab && id != a.skip ? (uint32_t)id : (uint32_t)a.vocab;
+}
+// +0 in every row of the table.  The sums write theirs over it: the order of kernels makes that safe, and knowing the rows without
+// an id would take a pass over flags for each (the rows written twice are as many as the ids have values).
+__device__ __forceinline__ void clear_table(const GradArgs& a, uint64_t thread, uint64_t threads) {
+    if (a.flat) {
+        const uint64_t elements = (uint64_t)a.vocab * (uint64_t)a.d;
+        for (uint64_t k = thread; k < elements / 4; k += threads) __stcs((float4*)a.table + k, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        if (thread < elements % 4) a.table[elements / 4 * 4 + thread] = 0.0f;
+    } else {
+        for (uint64_t row = thread / 32; row < (uint64_t)a.vocab; row += threads / 32)
+            for (int64_t col = thread % 32; col < a.d; col += 32) a.table[row * (uint64_t)a.table_ld + col] = 0.0f;
+    }
+}
+// Keys and positions of many ids.
 __global__ void __launch_bounds__(kTableThreads) grad_keys_kernel(GradArgs a) {
     follow<true>();
-    const uint64_t t = (uint64_t)blockIdx.x * kTableThreads + threadIdx.x;
-    if (t < (uint64_t)a.rows) {
-        const int64_t id = a.ids.load((int64_t)t);
-        a.keys[t] = id >= 0 && id < a.vocab && id != a.skip ? (uint32_t)id : (uint32_t)a.vocab;
-        a.places[t] = (uint32_t)t;
+    const uint64_t t = (uint64_t)blockIdx.x * kTableThreads + threadIdx.x, threads = (uint64_t)gridDim.x * kTableThreads;
+    for (uint64_t p = t; p < (uint64_t)a.rows; p += threads) {
+        a.keys[p] = key_of(a, (int64_t)p);
+        a.places[p] = (uint32_t)p;
     }
-    if (a.accumulate) return;
-    const uint64_t words = ((uint64_t)a.vocab + 15) / 16;  // (the workspace is in whole 256 bytes)
-    for (uint64_t k = t; k < words; k += (uint64_t)gridDim.x * kTableThreads) ((uint4*)a.flags)[k] = make_uint4(0, 0, 0, 0);
+    if (!a.accumulate) clear_table(a, t, threads);
 }
 
-// Sums of a chunk's runs, V columns a thread, `lanes` threads a row.
-template <class T, int V>
-__global__ void __launch_bounds__(kTableThreads) grad_sums_kernel(GradArgs a, uint32_t lanes) {
-    constexpr int kAhead = V * sizeof(T) > 16 ? 4 : 8;  // rows under way
-    extern __shared__ uint32_t staged[];  // keys, then places, of the CTA's chunks
+constexpr uint32_t kClusterMost = 8;  // CTAs
+constexpr int kClusterBits = 9;       // of a digit, at most
+// Ranks of a warp's ITEMS x 32 keys among its own by digit, in the order item, lane; counts[digit] is how many of each digit came before and
+// is counted up.  The lanes of a digit come of one ballot a bit.
+template <int ITEMS>
+__device__ __forceinline__ void rank_in_warp(const uint32_t (&key)[ITEMS], uint32_t shift, uint32_t bits, uint16_t* counts, uint32_t (&rank)[ITEMS]) {
+    const uint32_t lane = threadIdx.x & 31, mask = (1u << bits) - 1u;
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r) {
+        const uint32_t digit = (key[r] >> shift) & mask;
+        uint32_t peers = 0xFFFFFFFFu;
+#pragma unroll
+        for (uint32_t b = 0; b < kClusterBits; ++b) {
+            if (b >= bits) break;
+            const bool bit = (digit >> b) & 1u;
+            const uint32_t with = __ballot_sync(0xFFFFFFFFu, bit);
+            peers &= bit ? with : ~with;
+        }
+        const uint32_t below = peers & ((1u << lane) - 1u), before = counts[digit];
+        __syncwarp();
+        if (below == 0) counts[digit] = (uint16_t)(before + __popc(peers));
+        __syncwarp();
+        rank[r] = before + __popc(below);
+    }
+}
+// Exclusive scan of a value per thread of a CTA of kSortThreads; contains barriers.
+constexpr int kRankThreads = 1024, kRankWarps = kRankThreads / 32;
+__device__ __forceinline__ uint32_t scan_in_cta(uint32_t v, uint32_t* warp_sums) {
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    uint32_t upto = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= (uint32_t)o) upto += b;
+    }
+    if (lane == 31) warp_sums[warp] = upto;
+    __syncthreads();
+    if (warp == 0) {
+        uint32_t w = warp_sums[lane], sum = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= (uint32_t)o) sum += b;
+        }
+        warp_sums[lane] = sum - w;
+    }
+    __syncthreads();
+    const uint32_t before = warp_sums[warp] + upto - v;
+    __syncthreads();
+    return before;
+}
+
+// Up to 65536 ids: a cluster of up to eight CTAs sorts them in its shared memory, in one launch.  The other clusters clear the table.
+// (16384 ids of 17 bits: 11 us; keys, and three passes of three kernels each, 26.)
+template <int ITEMS>
+struct ClusterSmem {
+    uint2 pair[2][kRankThreads * ITEMS];
+    uint16_t warp_digit[kRankWarps][1 << kClusterBits];
+    uint32_t total[1 << kClusterBits], start[1 << kClusterBits], base[1 << kClusterBits];
+    uint32_t warp_sums[kRankWarps];
+};
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t address_in(const void* p, uint32_t rank) {  // the same place in another CTA of the cluster
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return at;
+}
+template <int ITEMS>
+__global__ void __launch_bounds__(kRankThreads) grad_cluster_sort_kernel(GradArgs a, uint32_t ctas, uint32_t passes, uint32_t bits) {
+    extern __shared__ __align__(16) uint8_t sort_memory[];
+    ClusterSmem<ITEMS>& sm = *(ClusterSmem<ITEMS>*)sort_memory;
+    constexpr uint32_t kTile = kRankThreads * ITEMS;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, rank_of_cta = blockIdx.x % ctas;
     follow<true>();
+    if (blockIdx.x >= ctas) {
+        clear_table(a, (uint64_t)(blockIdx.x - ctas) * kRankThreads + tid, (uint64_t)(gridDim.x - ctas) * kRankThreads);
+        return;
+    }
+    const uint32_t local = warp * (32 * ITEMS) + lane, first = rank_of_cta * kTile;
+    uint32_t key[ITEMS], place[ITEMS];
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r) {
+        place[r] = first + local + r * 32;
+        key[r] = place[r] < (uint64_t)a.rows ? key_of(a, place[r]) : 0xFFFFFFFFu;  // (behind all others, being the last)
+    }
+    for (uint32_t pass = 0; pass < passes; ++pass) {
+        const uint32_t shift = pass * bits, bins = 1u << bits;
+        if (pass > 0) {
+#pragma unroll
+            for (int r = 0; r < ITEMS; ++r) {
+                const uint2 p = sm.pair[pass & 1][local + r * 32];
+                key[r] = p.x;
+                place[r] = p.y;
+            }
+        }
+        for (uint32_t k = lane; k < bins / 2; k += 32) ((uint32_t*)sm.warp_digit[warp])[k] = 0;
+        __syncwarp();
+        uint32_t rank[ITEMS];
+        rank_in_warp(key, shift, bits, sm.warp_digit[warp], rank);
+        __syncthreads();
+        if (tid < bins / 2) {  // two digits in a word (a CTA has fewer pairs than 16 bits hold)
+            uint32_t sum = 0;
+#pragma unroll 16
+            for (int w = 0; w < kRankWarps; ++w) {
+                uint32_t* both = (uint32_t*)sm.warp_digit[w] + tid;
+                const uint32_t n = *both;
+                *both = sum;
+                sum += n;
+            }
+            sm.total[2 * tid] = sum & 0xFFFFu;
+            sm.total[2 * tid + 1] = sum >> 16;
+        }
+        cluster_barrier();
+        uint32_t all = 0, before = 0, own = 0;
+        if (tid < bins) {
+            uint32_t n[kClusterMost];
+#pragma unroll
+            for (uint32_t c = 0; c < kClusterMost; ++c) {
+                n[c] = 0;
+                if (c < ctas) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n[c]) : "r"(address_in(&sm.total[tid], c)));
+            }
+            own = sm.total[tid];
+#pragma unroll
+            for (uint32_t c = 0; c < kClusterMost; ++c) {
+                if (c < rank_of_cta) before += n[c];
+                all += n[c];
+            }
+        }
+        // where a digit starts among all pairs (at most 2^16) and among this CTA's, in one scan
+        const uint32_t start = scan_in_cta(all | own << 17, sm.warp_sums);
+        if (tid < bins) {
+            sm.start[tid] = start >> 17;
+            sm.base[tid] = (start & 0x1FFFFu) + before - (start >> 17);  // a pair at place k of this CTA goes to base + k
+        }
+        __syncthreads();
+        // laid out by digit in this CTA first: pairs that go to neighbouring places are then written by neighbouring lanes
+        uint2* const mine = sm.pair[pass & 1];
+#pragma unroll
+        for (int r = 0; r < ITEMS; ++r) {
+            const uint32_t digit = (key[r] >> shift) & (bins - 1u);
+            const uint32_t to = sm.start[digit] + sm.warp_digit[warp][digit] + rank[r];
+            if (ROBE_CHK(to < kTile, ROBE_DBG_SHARED)) mine[to] = make_uint2(key[r], place[r]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ITEMS; ++r) {
+            const uint32_t k = tid + r * kRankThreads;
+            const uint2 p = mine[k];
+            const uint32_t to = sm.base[(p.x >> shift) & (bins - 1u)] + k;
+            if (!ROBE_CHK(to < ctas * kTile, ROBE_DBG_SHARED)) continue;
+            const uint32_t at = address_in(&sm.pair[(pass + 1) & 1][to % kTile], to / kTile);
+            asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(p.x), "r"(p.y) : "memory");
+        }
+        cluster_barrier();
+    }
+    for (uint32_t k = tid; k < kTile && first + k < (uint64_t)a.rows; k += kRankThreads) {
+        const uint2 p = sm.pair[passes & 1][k];
+        a.keys[first + k] = p.x;
+        a.places[first + k] = p.y;
+    }
+}
+
+// Sums of a chunk's runs, V columns a thread, `lanes` threads a row.  ADD: to what is there, which is asked for together with the
+// rows of the run's end.
+template <class T, int V, bool ADD>
+__global__ void __launch_bounds__(kTableThreads, 4) grad_sums_kernel(GradArgs a, uint32_t lanes) {
+    constexpr int kAhead = ADD ? 2 : 4;  // rows under way: few, so that four CTAs are resident (16384 x 4096 bf16: 87 us with twice as many)
+    extern __shared__ uint32_t staged[];  // keys, then places, of the CTA's chunks
+    follow();
     const uint32_t groups = kTableThreads / lanes;
     const uint64_t block = blockIdx.x / a.slices;
     const uint32_t slice = blockIdx.x - (uint32_t)block * a.slices;
@@ -208,128 +442,136 @@ __global__ void __launch_bounds__(kTableThreads) grad_sums_kernel(GradArgs a, ui
     const int64_t col = ((int64_t)slice * lanes + threadIdx.x % lanes) * V;
     if (c >= a.chunks || col >= a.d) return;
     const uint64_t begin = c * a.chunk;
-    uint32_t count = (uint32_t)((uint64_t)a.rows - begin < a.chunk ? (uint64_t)a.rows - begin : a.chunk);
+    const uint32_t count = (uint32_t)((uint64_t)a.rows - begin < a.chunk ? (uint64_t)a.rows - begin : a.chunk);
+    const uint32_t vocab = (uint32_t)a.vocab;
     const uint32_t* keys = staged + group * a.chunk;
     const uint32_t* places = keys + staged_rows;
-    uint32_t key = keys[0];
-    if (key >= (uint32_t)a.vocab) return;
-    bool open = begin > 0 && a.keys[begin - 1] == key;  // the run began in an earlier chunk
+    if (keys[0] >= vocab) return;
+    bool open = begin > 0 && a.keys[begin - 1] == keys[0];  // the run began in an earlier chunk
+    const uint32_t after = begin + count < (uint64_t)a.rows ? a.keys[begin + count] : 0xFFFFFFFFu;
     float sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-    auto close = [&](bool goes_on) {
-        if (!open && !a.accumulate && col == 0) a.flags[key] = 1;
-        if (open || goes_on) {
-            float* to = a.parts + (c * 2 + (open ? 0 : 1)) * a.parts_ld + col;
+    // two groups of rows under way: while one is added up, the other is on its way
+    constexpr int G = kAhead / 2;
+    Elements<T, V> e[2][G];
+    Elements<float, V> old[2][ADD ? G : 1];
+    uint32_t key[2][G];
+    bool ends[2][G];  // its run ends with it
+    auto fetch = [&](int half, uint32_t i) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) to[v] = sum[v];
-            return;
+        for (int u = 0; u < G; ++u) {
+            key[half][u] = 0xFFFFFFFFu;
+            ends[half][u] = false;
+            if (i + u >= count || keys[i + u] >= vocab || !ROBE_CHK(places[i + u] < (uint64_t)a.rows && col + V <= a.d, ROBE_DBG_ROW_POS)) continue;
+            key[half][u] = keys[i + u];
+            e[half][u].template load<true>((const T*)a.grad + (int64_t)places[i + u] * a.grad_ld + col);
+            ends[half][u] = (i + u + 1 < count ? keys[i + u + 1] : after) != key[half][u];
+            if (ADD && ends[half][u]) old[half][ADD ? u : 0].template load<true>(a.table + (int64_t)key[half][u] * a.table_ld + col);
         }
-        float* to = a.table + (int64_t)key * a.table_ld + col;
-        if (!ROBE_CHK(key < (uint32_t)a.vocab && col + V <= a.d, ROBE_DBG_ROW_POS)) return;
-        Elements<float, V> o;
-        if (a.accumulate) o.template load<true>(to);
-#pragma unroll
-        for (int v = 0; v < V; ++v) o.set(v, a.accumulate ? fmaf(a.scale, sum[v], o.get(v)) : a.scale * sum[v]);
-        o.template store<true>(to);
     };
+    fetch(0, 0);
     for (uint32_t i = 0; i < count; i += kAhead) {
-        Elements<T, V> e[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (i + u < count && ROBE_CHK(places[i + u] < (uint64_t)a.rows, ROBE_DBG_ROW_POS))
-                e[u].template load<true>((const T*)a.grad + (int64_t)places[i + u] * a.grad_ld + col);
+        for (int half = 0; half < 2; ++half) {
+            fetch(half ^ 1, i + (half + 1) * G);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (i + u >= count) break;
-            const uint32_t k = keys[i + u];
-            if (k != key) {
-                close(false);
-                if (k >= (uint32_t)a.vocab) return;  // (these are the last)
-                key = k;
+            for (int u = 0; u < G; ++u) {
+                const uint32_t k = key[half][u];
+                if (k >= vocab) return;  // behind the chunk's end, or without a gradient as all that follow
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[v] += e[half][u].get(v);
+                if (!ends[half][u] && i + half * G + u + 1 < count) continue;
+                if (open || !ends[half][u]) {
+                    float* to = a.parts + (c * 2 + (open ? 0 : 1)) * a.parts_ld + col;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) to[v] = sum[v];
+                } else {
+                    float w[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) w[v] = ADD ? fmaf(a.scale, sum[v], old[half][ADD ? u : 0].get(v)) : a.scale * sum[v];
+                    Elements<float, V> o;
+                    o.set(w);
+                    o.template store<true>(a.table + (int64_t)k * a.table_ld + col);
+                }
                 open = false;
 #pragma unroll
                 for (int v = 0; v < V; ++v) sum[v] = 0.0f;
             }
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] += e[u].get(v);
         }
     }
-    close(begin + count < (uint64_t)a.rows && a.keys[begin + count] == key);
+}
+
+constexpr int kJoinWarps = kTableThreads / 32;
+constexpr uint32_t kJoinAlone = 16;       // parts that a warp adds by itself
+
+// Whether the chunks [g kFold, (g + 1) kFold) lie in the run of `key` as a whole, one that began before them.
+__device__ __forceinline__ bool folds_in(const GradArgs& a, uint64_t g, uint32_t key) {
+    const uint64_t end = (g + 1) * kFold * a.chunk;
+    return (g + 1) * kFold <= a.chunks && a.keys[(end < (uint64_t)a.rows ? end : (uint64_t)a.rows) - 1] == key;
+}
+// Sums of kFold first parts each, a CTA per group.
+__global__ void __launch_bounds__(kTableThreads) grad_fold_kernel(GradArgs a) {
+    follow();
+    const uint64_t g = blockIdx.x;
+    if (g == 0) return;
+    const uint64_t begin = g * kFold * a.chunk;
+    const uint32_t key = a.keys[begin];
+    if (key >= (uint32_t)a.vocab || a.keys[begin - 1] != key || !folds_in(a, g, key)) return;
+    for (int64_t col = threadIdx.x; col < a.d; col += kTableThreads) {
+        double s = 0.0;
+#pragma unroll 8
+        for (uint32_t k = 0; k < kFold; ++k) s += a.parts[(g * kFold + k) * 2 * a.parts_ld + col];
+        a.folds[g * a.parts_ld + col] = s;
+    }
 }
 
 // Runs that end in a later chunk than they begin in: the chunks' parts in order, in 64 bits.  A warp takes a chunk's last run and
-// 128 columns; runs over many chunks are shared by the CTA's warps.  The CTAs behind those write +0 where no id was.
-constexpr int kJoinWarps = kTableThreads / 32;
-constexpr uint32_t kJoinAlone = 16;  // parts that a warp adds by itself
-__global__ void __launch_bounds__(kTableThreads) grad_join_kernel(GradArgs a) {
-    follow();
-    if (blockIdx.x >= a.join_blocks) {
-        const uint64_t items = (uint64_t)a.vocab * a.pieces;
-        constexpr uint32_t kItems = 8;
-        const uint64_t first = (uint64_t)(blockIdx.x - a.join_blocks) * (kTableThreads * kItems);
-        const uint64_t row0 = first / a.pieces;
-        const uint32_t piece0 = (uint32_t)(first - row0 * a.pieces);
-#pragma unroll
-        for (uint32_t i = 0; i < kItems; ++i) {
-            const uint32_t k = i * kTableThreads + threadIdx.x;
-            if (first + k >= items) return;
-            const uint32_t r = divide(piece0 + k, a.pieces, a.magic), piece = piece0 + k - r * a.pieces;
-            const uint64_t row = row0 + r;
-            if (!ROBE_CHK(row < (uint64_t)a.vocab, ROBE_DBG_ROW_POS)) return;
-            if (__ldca(a.flags + row) != 0) continue;
-            if (a.aligned) __stcs((float4*)(a.table + row * a.table_ld) + piece, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-            else a.table[row * a.table_ld + piece] = 0.0f;
-        }
-        return;
-    }
+// a slice of columns, as many parts side by side as its lanes hold; runs over many chunks are shared by the CTA's warps.
+__global__ void __launch_bounds__(kTableThreads, 4) grad_join_kernel(GradArgs a) {
     __shared__ uint32_t shared_runs[kJoinWarps];  // parts of the runs that the warps share; 0: none
     __shared__ double sums[kJoinWarps][4][32];
+    follow();
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t blocks = blockIdx.x / a.slices;  // of kJoinWarps chunks
     const uint32_t slice = blockIdx.x - blocks * a.slices;
-    const int64_t col = (int64_t)slice * 128 + lane * 4;
+    const uint32_t side = 32 / a.lanes, sub = lane / a.lanes;  // parts side by side, the lane's among them
+    const int64_t col = (int64_t)slice * (a.lanes * 4) + lane % a.lanes * 4;
+    auto key_before = [&](uint64_t e) { return a.keys[(e < (uint64_t)a.rows ? e : (uint64_t)a.rows) - 1]; };
     auto parts_of = [&](uint64_t c) -> uint32_t {  // of the last run of chunk c, 0 where it ends there
         const uint64_t end = (c + 1) * a.chunk;
         if (c >= a.chunks || end >= (uint64_t)a.rows) return 0;
-        const uint32_t key = a.keys[end - 1];
-        if (key >= (uint32_t)a.vocab || a.keys[end] != key) return 0;
-        if (c > 0 && a.keys[end - a.chunk - 1] == key) return 0;  // it began earlier
         // it reaches the end of chunk c + k: true up to some k; 32 places at a time, first powers of two, then between
-        auto reaches = [&](uint64_t k) {
-            const uint64_t e = (c + k + 1) * a.chunk;
-            return a.keys[(e < (uint64_t)a.rows ? e : (uint64_t)a.rows) - 1] == key;
-        };
-        uint64_t yes = 0, no;  // it reaches the end of chunk c + yes and not of c + no
-        {
-            const uint64_t k = 1ull << lane;
-            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, c + k < a.chunks && reaches(k));
-            const int hits = __popc(hit);
-            if (hits > 0) yes = 1ull << (hits - 1);
-            no = 1ull << hits;
-            if (no > a.chunks - c) no = a.chunks - c;
-        }
+        const uint64_t far = c + (1ull << lane);
+        const uint32_t key = a.keys[end - 1], next_key = a.keys[end], old_key = c > 0 ? a.keys[end - a.chunk - 1] : 0xFFFFFFFFu;
+        const uint32_t far_key = far < a.chunks ? key_before((far + 1) * a.chunk) : 0xFFFFFFFFu;
+        if (key >= (uint32_t)a.vocab || next_key != key || old_key == key) return 0;  // (it began earlier)
+        const int first_hits = __popc(__ballot_sync(0xFFFFFFFFu, far_key == key));
+        if (first_hits == 0) return 2;  // (it ends in the next chunk)
+        uint64_t yes = 1ull << (first_hits - 1), no = 1ull << first_hits;  // it reaches the end of chunk c + yes and not of c + no
+        if (no > a.chunks - c) no = a.chunks - c;
         while (no - yes > 1) {
-            const uint64_t step = (no - yes + 31) / 32, k = yes + step * (lane + 1);
-            const uint32_t hits = __popc(__ballot_sync(0xFFFFFFFFu, k < no && reaches(k)));
-            const uint64_t up = yes + step * (hits + 1);
-            yes += step * hits;
+            const uint64_t apart = (no - yes + 31) / 32, k = yes + apart * (lane + 1);
+            const uint32_t hits = __popc(__ballot_sync(0xFFFFFFFFu, k < no && key_before((c + k + 1) * a.chunk) == key));
+            const uint64_t up = yes + apart * (hits + 1);
+            yes += apart * hits;
             if (up < no) no = up;
         }
         // chunks c .. c + yes end in it; it goes on into the next one if there is one and it begins with it
         const uint64_t next = (c + yes + 1) * a.chunk;
         return (uint32_t)(yes + 1 + (next < (uint64_t)a.rows && a.keys[next] == key ? 1 : 0));
     };
-    auto add = [&](double (&s)[4], uint64_t c, uint32_t begin, uint32_t end) {  // parts begin .. end - 1 of the run of chunk c
+    // parts begin, begin + apart, .. before end of the run that begins in chunk c (part 0: its own last one)
+    auto add = [&](double (&s)[4], uint64_t c, uint32_t begin, uint32_t end, uint32_t apart) {
         if (col >= a.d) return;
-        for (uint32_t k = begin; k < end; k += 8) {
-            float4 v[8];
+        for (uint32_t k = begin; k < end; k += 4 * apart) {
+            float4 v[4];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (k + u < end) v[u] = __ldca((const float4*)(a.parts + ((c + k + u) * 2 + (k + u == 0 ? 1 : 0)) * a.parts_ld + col));
+            for (int u = 0; u < 4; ++u)
+                if (k + u * apart < end) v[u] = __ldca((const float4*)(a.parts + ((c + k + u * apart) * 2 + (k + u * apart == 0 ? 1 : 0)) * a.parts_ld + col));
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (k + u < end) {
+            for (int u = 0; u < 4; ++u)
+                if (k + u * apart < end) {
                     s[0] += v[u].x;
                     s[1] += v[u].y;
                     s[2] += v[u].z;
@@ -337,20 +579,36 @@ __global__ void __launch_bounds__(kTableThreads) grad_join_kernel(GradArgs a) {
                 }
         }
     };
-    auto finish = [&](const double (&s)[4], uint64_t c) {
-        const uint32_t key = a.keys[(c + 1) * a.chunk - 1];
-        float* to = a.table + (int64_t)key * a.table_ld + col;
-        if (col >= a.d || !ROBE_CHK(key < (uint32_t)a.vocab, ROBE_DBG_ROW_POS)) return;
+    auto over_sides = [&](double (&s)[4]) {
+        for (uint32_t o = a.lanes; o < 32; o *= 2)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (col + q < a.d) to[q] = a.accumulate ? fmaf(a.scale, (float)s[q], to[q]) : a.scale * (float)s[q];
+            for (int q = 0; q < 4; ++q) s[q] += __shfl_xor_sync(0xFFFFFFFFu, s[q], o);
+    };
+    auto finish = [&](const double (&s)[4], uint64_t c) {
+        if (sub != 0 || col >= a.d) return;
+        const uint32_t key = a.keys[(c + 1) * a.chunk - 1];
+        if (!ROBE_CHK(key < (uint32_t)a.vocab, ROBE_DBG_ROW_POS)) return;
+        float* to = a.table + (int64_t)key * a.table_ld + col;
+        if (a.aligned) {
+            float4 o = a.accumulate ? *(const float4*)to : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            o.x = a.accumulate ? fmaf(a.scale, (float)s[0], o.x) : a.scale * (float)s[0];
+            o.y = a.accumulate ? fmaf(a.scale, (float)s[1], o.y) : a.scale * (float)s[1];
+            o.z = a.accumulate ? fmaf(a.scale, (float)s[2], o.z) : a.scale * (float)s[2];
+            o.w = a.accumulate ? fmaf(a.scale, (float)s[3], o.w) : a.scale * (float)s[3];
+            *(float4*)to = o;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (col + q < a.d) to[q] = a.accumulate ? fmaf(a.scale, (float)s[q], to[q]) : a.scale * (float)s[q];
+        }
     };
     const uint64_t mine = (uint64_t)blocks * kJoinWarps + warp;
     const uint32_t parts = parts_of(mine);
     if (lane == 0) shared_runs[warp] = parts > kJoinAlone ? parts : 0;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
     if (parts > 0 && parts <= kJoinAlone) {
-        double s[4] = {0.0, 0.0, 0.0, 0.0};
-        add(s, mine, 0, parts);
+        add(s, mine, sub, parts, side);
+        over_sides(s);
         finish(s, mine);
     }
     __syncthreads();
@@ -358,10 +616,26 @@ __global__ void __launch_bounds__(kTableThreads) grad_join_kernel(GradArgs a) {
         const uint32_t n = shared_runs[w];
         if (n == 0) continue;
         const uint64_t c = (uint64_t)blocks * kJoinWarps + w;
-        const uint32_t per = (n + kJoinWarps - 1) / kJoinWarps;
-        const uint32_t begin = warp * per < n ? warp * per : n, end = begin + per < n ? begin + per : n;
-        double s[4] = {0.0, 0.0, 0.0, 0.0};
-        add(s, c, begin, end);
+        const uint32_t who = warp * side + sub, all = kJoinWarps * side;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s[q] = 0.0;
+        uint32_t plain = n;  // parts from the beginning on that are added one by one; then folds, then the rest
+        if (a.folds != nullptr) {
+            const uint64_t g0 = (c + kFold) / kFold, end = (c + n) / kFold;  // groups behind chunk c, and up to the run's last whole one
+            const uint32_t key = a.keys[(c + 1) * a.chunk - 1];
+            if (g0 < end) {
+                plain = (uint32_t)(g0 * kFold - c);
+                // (the last group's last chunk may end with another run; the one behind it cannot be whole)
+                const uint64_t g1 = folds_in(a, end - 1, key) ? end : end - 1;
+                for (uint64_t g = g0 + who; g < g1; g += all)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (col + q < a.d) s[q] += a.folds[g * a.parts_ld + col + q];
+                add(s, c, (uint32_t)(g1 * kFold - c) + who, n, all);
+            }
+        }
+        add(s, c, who, plain, all);
+        over_sides(s);
 #pragma unroll
         for (int q = 0; q < 4; ++q) sums[warp][q][lane] = s[q];
         __syncthreads();
@@ -375,6 +649,32 @@ __global__ void __launch_bounds__(kTableThreads) grad_join_kernel(GradArgs a) {
     }
 }
 
+template <int ITEMS>
+cudaError_t launch_cluster_sort(const GradArgs& a, uint32_t bits, cudaStream_t st) {
+    const uint32_t passes = (bits + kClusterBits - 1) / kClusterBits, per = (bits + passes - 1) / passes;
+    const uint32_t ctas = a.rows <= kRankThreads ? 1 : kClusterMost;
+    const size_t bytes = sizeof(ClusterSmem<ITEMS>);
+    const cudaError_t e = cudaFuncSetAttribute(grad_cluster_sort_kernel<ITEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+    // the table: as many others as the SMs hold beside the sort
+    const unsigned __int128 pieces = (unsigned __int128)a.vocab * (uint64_t)a.d / (kRankThreads * 16) + 1;
+    uint64_t others = a.accumulate ? 0 : pieces < 2 * 148 - kClusterMost ? (uint64_t)pieces : 2 * 148 - kClusterMost;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas + (unsigned)((others + ctas - 1) / ctas * ctas));
+    cfg.blockDim = dim3(kRankThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, grad_cluster_sort_kernel<ITEMS>, a, ctas, passes, per);
+}
+
 template <class T, int V>
 cudaError_t launch_sums(GradArgs& a, cudaStream_t st) {
     uint32_t lanes = 4;
@@ -385,7 +685,8 @@ cudaError_t launch_sums(GradArgs& a, cudaStream_t st) {
     const uint64_t groups = kTableThreads / lanes;
     const uint64_t grid = (a.chunks + groups - 1) / groups * a.slices;
     if (grid >= (1ull << 31)) return kGridTooSmall;
-    launch_next(grad_sums_kernel<T, V>, (unsigned)grid, kTableThreads, groups * a.chunk * 8, st, a, lanes);
+    if (a.accumulate) launch_next(grad_sums_kernel<T, V, true>, (unsigned)grid, kTableThreads, groups * a.chunk * 8, st, a, lanes);
+    else launch_next(grad_sums_kernel<T, V, false>, (unsigned)grid, kTableThreads, groups * a.chunk * 8, st, a, lanes);
     return cudaSuccess;
 }
 template <class T>
@@ -427,12 +728,12 @@ cudaError_t launch_table_forward(const TableProblem& pb, void* out, int64_t out_
     return cudaSuccess;
 }
 
-size_t table_grad_workspace_bytes(int64_t rows, int64_t vocab, int64_t d) { return grad_layout(rows, vocab, d).total; }
+size_t table_grad_workspace_bytes(int64_t rows, int64_t d) { return grad_layout(rows, d).total; }
 
 cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int64_t grad_ld, int64_t skip, int accumulate, float* grad_table,
                                   int64_t grad_table_ld, void* workspace, cudaStream_t st) {
     if (accumulate && pb.rows == 0) return cudaSuccess;
-    const GradLayout L = grad_layout(pb.rows, pb.vocab, pb.d);
+    const GradLayout L = grad_layout(pb.rows, pb.d);
     char* ws = (char*)workspace;
     GradArgs a;
     a.grad = grad;
@@ -446,20 +747,20 @@ cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int6
     a.table_ld = grad_table_ld;
     a.scale = pb.scale;
     a.accumulate = accumulate;
-    a.flags = (uint8_t*)(ws + L.flags);
     a.parts = (float*)(ws + L.parts);
     a.parts_ld = L.parts_ld;
     a.chunk = L.chunk;
     a.chunks = L.chunks;
+    a.folds = L.chunks >= kFoldFrom ? (double*)(ws + L.folds) : nullptr;
     a.aligned = piece_of(4, pb.d, grad_table, grad_table_ld, 4, grad_table, grad_table_ld, 4, 2) == 4;
-    a.pieces = (uint32_t)(a.aligned ? pb.d / 4 : pb.d);
-    a.magic = magic_of(a.pieces);
+    a.flat = (uintptr_t)grad_table % 16 == 0 && (grad_table_ld == pb.d || pb.vocab == 1);
     const int64_t size = pb.dtype == 0 ? 4 : 2;
     // everything that is launched, before anything is
-    a.slices = (uint32_t)((pb.d + 127) / 128);
-    const uint64_t join = (L.chunks + kJoinWarps - 1) / kJoinWarps * a.slices;
-    const unsigned __int128 fill = accumulate ? 0 : ((unsigned __int128)pb.vocab * a.pieces + kTableThreads * 8 - 1) / (kTableThreads * 8);
-    if (join + fill >= (1ull << 31)) return kGridTooSmall;
+    a.lanes = 1;
+    while (a.lanes < 32 && (int64_t)a.lanes * 4 < pb.d) a.lanes *= 2;
+    const uint32_t join_slices = (uint32_t)((pb.d + a.lanes * 4 - 1) / (a.lanes * 4));
+    const uint64_t join = (L.chunks + kJoinWarps - 1) / kJoinWarps * join_slices;
+    if (join >= (1ull << 31)) return kGridTooSmall;
     const int piece = piece_of(size == 4 ? 4 : 8, pb.d, grad, grad_ld, size, grad_table, grad_table_ld, 4, pb.rows > 1 || pb.vocab > 1 ? 2 : 1);
     if (L.chunks * (uint64_t)((pb.d + (int64_t)kTableThreads * piece - 1) / ((int64_t)kTableThreads * piece)) >= (1ull << 31)) return kGridTooSmall;
 
@@ -467,20 +768,29 @@ cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int6
              *places[2] = {(uint32_t*)(ws + L.places[0]), (uint32_t*)(ws + L.places[1])};
     a.keys = keys[0];
     a.places = places[0];
-    const uint64_t threads = (uint64_t)pb.rows > (uint64_t)kTableThreads * 148 ? (uint64_t)pb.rows : (uint64_t)kTableThreads * 148;
-    launch_next(grad_keys_kernel, (unsigned)((threads + kTableThreads - 1) / kTableThreads), kTableThreads, 0, st, a);
+    uint32_t bits = 1;
+    while (((uint64_t)pb.vocab >> bits) != 0) ++bits;  // (vocab itself is a key)
+    if (pb.rows > 0 && pb.rows <= kClusterRows) {
+        const cudaError_t e = pb.rows <= kClusterRows / 8   ? launch_cluster_sort<1>(a, bits, st)
+                              : pb.rows <= kClusterRows / 4 ? launch_cluster_sort<2>(a, bits, st)
+                              : pb.rows <= kClusterRows / 2 ? launch_cluster_sort<4>(a, bits, st)
+                                                            : launch_cluster_sort<8>(a, bits, st);
+        if (e != cudaSuccess) return e;
+    } else {
+        launch_next(grad_keys_kernel, 148 * 8, kTableThreads, 0, st, a);
+        if (pb.rows > 0) {
+            const int in = launch_sort_pairs(keys, places, (uint64_t)pb.rows, bits, (uint32_t*)(ws + L.counts), (uint32_t*)(ws + L.totals), st);
+            a.keys = keys[in];
+            a.places = places[in];
+        }
+    }
     if (pb.rows > 0) {
-        uint32_t bits = 1;
-        while (((uint64_t)pb.vocab >> bits) != 0) ++bits;  // (vocab itself is a key)
-        const int in = launch_sort_pairs(keys, places, (uint64_t)pb.rows, bits, (uint32_t*)(ws + L.counts), (uint32_t*)(ws + L.totals), st);
-        a.keys = keys[in];
-        a.places = places[in];
         const cudaError_t e = pb.dtype == 0 ? launch_sums<float>(a, piece, st) : launch_sums<__nv_bfloat16>(a, piece, st);
         if (e != cudaSuccess) return e;
     }
-    a.slices = (uint32_t)((pb.d + 127) / 128);
-    a.join_blocks = (uint32_t)join;
-    launch_next(grad_join_kernel, (unsigned)(join + (uint64_t)fill), kTableThreads, 0, st, a);
+    if (a.folds != nullptr) launch_next(grad_fold_kernel, (unsigned)(L.chunks / kFold), kTableThreads, 0, st, a);
+    a.slices = join_slices;
+    if (join > 0) launch_next(grad_join_kernel, (unsigned)join, kTableThreads, 0, st, a);
     return cudaGetLastError();
 }
 
