@@ -121,16 +121,22 @@ Columns columns(int64_t d, int64_t group) {
     return c;
 }
 
+// every unit has eight columns of its group, their codes in one piece
+bool full_units(const Columns& c, int code_piece) {
+    return c.group == 8u << c.shift && c.d % c.group == 0 && code_piece == 8;
+}
+
 // ---------------------------------------------------------------- the join
 
 struct QuantizeArgs {
     int64_t rows;
     Columns c;
     int layer;
-    float eps, scale;
+    float eps, scale, per_column;  // per_column: 1 / d
     const float* w;
     RowsRef x, residual, out, codes, scales;
     int code_piece, w_pieces;
+    int full;  // every unit of a row has eight columns of its group, all in 16-byte pieces, codes in eights
     uint32_t threads;  // of a row
     // a cache takes the codes: rows of the call lie where `at` says
     int cached;
@@ -164,11 +170,15 @@ __device__ __forceinline__ void load_weights(float (&w)[8], const QuantizeArgs& 
 }
 
 __device__ __forceinline__ float add_over(float v, uint32_t lanes) {
-    for (uint32_t o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o <<= 1)
+        if (o < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
 __device__ __forceinline__ uint32_t most_over(uint32_t v, uint32_t lanes) {
-    for (uint32_t o = 1; o < lanes; o <<= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o <<= 1)
+        if (o < lanes) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
     return v;
 }
 // over the threads of a row: lanes of a warp, or whole warps that meet in shared memory (one word a warp)
@@ -193,8 +203,124 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t threads, 
     return v;
 }
 
-// A row in the registers of its threads, K units each.  What hides the loads' latency is CTAs, not rows asked for ahead: at 16384 x
-// 4096 bf16 two CTAs an SM that asked for the next row took 252 us, five without LATER.
+// The usual call: whole 16-byte pieces, groups of a power of two of columns that all rows are made of (or one scale a row).  No unit has less
+// than eight columns, so that two operations go in one instruction and nothing is asked per element; K units a thread.  What hides
+// the loads' latency is CTAs, not rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 87 us; 117 by the kernel for
+// any call, whose instructions bound it; 252 with two CTAs an SM that asked for the next row.)
+template <class T, int K, bool RESIDUAL, bool I8, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_full_kernel(QuantizeArgs a) {
+    __shared__ float sums[2][THREADS / 32];
+    __shared__ uint32_t most[THREADS / 32];
+    follow();
+    uint32_t t = threadIdx.x;
+    int64_t r = blockIdx.x;
+    if (a.threads != blockDim.x) {  // several rows a CTA
+        t = threadIdx.x % a.threads;
+        r = (int64_t)blockIdx.x * (blockDim.x / a.threads) + threadIdx.x / a.threads;
+    }
+    const bool on_row = r < a.rows;
+    Eight<T> x[K], y[RESIDUAL ? K : 1];
+    const T* from = (const T*)a.x.p + r * a.x.ld;
+    const T* beside = (const T*)a.residual.p + r * a.residual.ld;
+    bool on[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const uint32_t unit = t + j * a.threads;
+        on[j] = on_row && unit < a.c.units;
+        if (!ROBE_CHK(!on[j] || (unit + 1) * 8ll <= a.c.d, ROBE_DBG_ROW_POS)) on[j] = false;
+        if (on[j]) load_eight<T, kPiece<T>>(x[j], from + unit * 8, 8);
+        if (RESIDUAL && on[j]) load_eight<T, kPiece<T>>(y[RESIDUAL ? j : 0], beside + unit * 8, 8);
+    }
+    float2 v[K][4];
+    float2 sum = both(0.0f);
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[j][k] = both(0.0f);
+            if (on[j]) {
+                const float2 p = make_float2(x[j].get(2 * k), x[j].get(2 * k + 1));
+                const Eight<T>& q = y[RESIDUAL ? j : 0];
+                v[j][k] = RESIDUAL ? fma2(both(a.scale), p, make_float2(q.get(2 * k), q.get(2 * k + 1))) : mul2(both(a.scale), p);
+            }
+        }
+    if (a.out.p != nullptr) {
+        T* to = (T*)a.out.p + r * a.out.ld;
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (on[j]) store_eight<T, kPiece<T>>((const float(&)[8])v[j], to + (t + j * a.threads) * 8, 8);
+    }
+    if (a.w != nullptr) {
+        if (a.layer) {
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum = add2(sum, v[j][k]);
+            const float2 mean = both(-add_over_row(sum.x + sum.y, a.threads, sums[0]) * a.per_column);
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[j][k] = on[j] ? add2(v[j][k], mean) : both(0.0f);
+            sum = both(0.0f);
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum = fma2(v[j][k], v[j][k], sum);
+        const float2 factor = both(norm_factor(fmaf(add_over_row(sum.x + sum.y, a.threads, sums[1]), a.per_column, a.eps)));
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (!on[j]) continue;
+            const float4* w = (const float4*)(a.w + (t + j * a.threads) * 8);
+            const float4 p = __ldca(w), q = __ldca(w + 1);
+            v[j][0] = mul2(mul2(v[j][0], factor), make_float2(p.x, p.y));
+            v[j][1] = mul2(mul2(v[j][1], factor), make_float2(p.z, p.w));
+            v[j][2] = mul2(mul2(v[j][2], factor), make_float2(q.x, q.y));
+            v[j][3] = mul2(mul2(v[j][3], factor), make_float2(q.z, q.w));
+        }
+    }
+    uint8_t* const codes = (uint8_t*)a.codes.p + r * a.codes.ld;
+    float* const scales = (float*)a.scales.p + r * a.scales.ld;
+    constexpr float kQ = I8 ? kLargestI8 : kLargestE4m3;
+    auto largest = [&](int j) {
+        float m = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m = most_magnitude(m, v[j][k].x, v[j][k].y);
+        return __float_as_uint(m);
+    };
+    auto write = [&](int j, float f) {
+        float c[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 p = mul2(v[j][k], both(f));
+            c[2 * k] = p.x;
+            c[2 * k + 1] = p.y;
+        }
+        const uint2 w = I8 ? make_uint2(codes_i8(c[0], c[1], c[2], c[3]), codes_i8(c[4], c[5], c[6], c[7]))
+                           : make_uint2(codes_e4m3(c[0], c[1], c[2], c[3]), codes_e4m3(c[4], c[5], c[6], c[7]));
+        __stcs((uint2*)(codes + (t + j * a.threads) * 8), w);
+    };
+    if (a.c.whole) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < K; ++j) m = max(m, largest(j));
+        const GroupScale g = group_scale(most_over_row(m, a.threads, most), kQ);
+        if (on_row && t == 0) scales[0] = g.scale;
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (on[j]) write(j, g.factor);
+    } else {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const GroupScale g = group_scale(most_over(largest(j), 1u << a.c.shift), kQ);
+            const uint32_t unit = t + j * a.threads;
+            if (on[j] && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
+            if (on[j]) write(j, g.factor);
+        }
+    }
+}
+
+// Any call: a row in the registers of its threads, K units each.
 template <class T, int P, int K, bool I8, int THREADS>
 __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : 1024 / THREADS) quantize_rows_kernel(QuantizeArgs a) {
     __shared__ float sums[2][2][THREADS / 32];  // (two rows' turns: a barrier of the next row stands between a read and the next write)
@@ -225,8 +351,7 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : 1024 / THREADS) quantize
         for (int j = 0; j < K; ++j)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float s = a.scale * x[j].get(k);
-                v[j][k] = count[j] == 0 ? 0.0f : a.residual.p != nullptr ? y[j].get(k) + s : s;
+                v[j][k] = count[j] == 0 ? 0.0f : a.residual.p != nullptr ? fmaf(a.scale, x[j].get(k), y[j].get(k)) : a.scale * x[j].get(k);
             }
         if (a.out.p != nullptr) {
 #pragma unroll
@@ -240,7 +365,7 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : 1024 / THREADS) quantize
                 for (int j = 0; j < K; ++j)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) sum += v[j][k];
-                const float mean = add_over_row(sum, a.threads, sums[turn][0]) / (float)a.c.d;
+                const float mean = add_over_row(sum, a.threads, sums[turn][0]) * a.per_column;
 #pragma unroll
                 for (int j = 0; j < K; ++j)
 #pragma unroll
@@ -251,7 +376,7 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : 1024 / THREADS) quantize
             for (int j = 0; j < K; ++j)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum = fmaf(v[j][k], v[j][k], sum);
-            const float factor = 1.0f / sqrtf(add_over_row(sum, a.threads, sums[turn][1]) / (float)a.c.d + a.eps);
+            const float factor = norm_factor(fmaf(add_over_row(sum, a.threads, sums[turn][1]), a.per_column, a.eps));
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 if (count[j] == 0) continue;
@@ -306,8 +431,7 @@ __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a
             if (a.residual.p != nullptr) load_eight<T, P>(y, (const T*)a.residual.p + r * a.residual.ld + col, count);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float s = a.scale * x.get(k);
-                if (k < count) v[k] = a.residual.p != nullptr ? y.get(k) + s : s;
+                if (k < count) v[k] = a.residual.p != nullptr ? fmaf(a.scale, x.get(k), y.get(k)) : a.scale * x.get(k);
             }
             return count;
         };
@@ -321,7 +445,7 @@ __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a
 #pragma unroll
                     for (int k = 0; k < 8; ++k) sum += v[k];
                 }
-                mean = add_over_row(sum, kJoinMost, sums[0]) / (float)a.c.d;
+                mean = add_over_row(sum, kJoinMost, sums[0]) * a.per_column;
             }
             float sum = 0.0f, v[8];
             int64_t col;
@@ -331,7 +455,7 @@ __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a
                 for (int k = 0; k < 8; ++k)
                     if (k < count) sum = fmaf(v[k] - mean, v[k] - mean, sum);
             }
-            factor = 1.0f / sqrtf(add_over_row(sum, kJoinMost, sums[1]) / (float)a.c.d + a.eps);
+            factor = norm_factor(fmaf(add_over_row(sum, kJoinMost, sums[1]), a.per_column, a.eps));
         }
         auto normed = [&](float (&n)[8], const float (&v)[8], int64_t col, int count) {
 #pragma unroll
@@ -406,6 +530,21 @@ cudaError_t launch_quantize(QuantizeArgs& a, bool in_registers, cudaStream_t st)
     const uint32_t block = threads >= 128 ? threads : 128 / threads * threads;
     const int64_t per = block / threads;
     const int64_t ctas = (a.rows + per - 1) / per;
+    if constexpr (P == kPiece<T>) {
+        if (a.full && K <= 2 && ctas < (1ll << 31)) {
+            auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)ctas, block, 0, st, a); };
+            if (a.residual.p != nullptr) {
+                if (K == 1) launch(quantize_full_kernel<T, 1, true, I8, 256>);
+                else if (block <= 256) launch(quantize_full_kernel<T, 2, true, I8, 256>);
+                else launch(quantize_full_kernel<T, 2, true, I8, 512>);
+            } else {
+                if (K == 1) launch(quantize_full_kernel<T, 1, false, I8, 256>);
+                else if (block <= 256) launch(quantize_full_kernel<T, 2, false, I8, 256>);
+                else launch(quantize_full_kernel<T, 2, false, I8, 512>);
+            }
+            return cudaGetLastError();
+        }
+    }
     auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)(ctas < (1ll << 30) ? ctas : 1ll << 30), block, 0, st, a); };
     if (K == 1) launch(quantize_rows_kernel<T, P, 1, I8, 256>);
     else if (K == 2 && block <= 256) launch(quantize_rows_kernel<T, P, 2, I8, 256>);
@@ -463,26 +602,28 @@ __device__ __forceinline__ void find_places(const CacheArgs& a, Place* places, i
     __syncthreads();
 }
 
-template <class T, int P, bool I8, int ITEMS>
+// FULL: groups of a power of two of eights of columns, 16-byte pieces, codes in eights (QuantizeArgs::full).
+template <class T, int P, bool I8, int ITEMS, bool FULL>
 __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) {
     __shared__ Place places[kCacheRows];
     follow();
     const int64_t first = (int64_t)blockIdx.x * a.per_cta;
     const uint32_t rows = a.n - first < a.per_cta ? (uint32_t)(a.n - first) : a.per_cta;
-    const uint32_t items = rows * a.units;
+    const uint32_t items = rows * a.units, lanes = 1u << a.cols.shift;
+    const T* from = (const T*)a.rows.p + first * a.rows.ld;
     for (uint32_t base = 0; base < items; base += kCodeThreads * ITEMS) {
         Eight<T> e[ITEMS];
         int count[ITEMS];
-        int64_t col[ITEMS];
-        uint32_t row[ITEMS], unit[ITEMS];
+        uint32_t row[ITEMS], unit[ITEMS], col[ITEMS];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const uint32_t t = base + i * kCodeThreads + threadIdx.x;
             row[i] = divide(t, a.units, a.magic);
             unit[i] = t - row[i] * a.units;
-            count[i] = 0;
-            if (t < items) col[i] = columns_of(a.cols, unit[i], count[i]);
-            if (count[i] > 0) load_eight<T, P>(e[i], (const T*)a.rows.p + (first + row[i]) * a.rows.ld + col[i], count[i]);
+            count[i] = t < items ? 8 : 0;
+            col[i] = unit[i] * 8;
+            if (!FULL && t < items) col[i] = (uint32_t)columns_of(a.cols, unit[i], count[i]);
+            if (count[i] > 0) load_eight<T, P>(e[i], from + row[i] * a.rows.ld + col[i], FULL ? 8 : count[i]);
         }
         if (base == 0) find_places(a, places, first, rows);  // (while the rows are on their way)
 #pragma unroll
@@ -490,13 +631,18 @@ __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) 
             float v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = count[i] > 0 ? e[i].get(k) : 0.0f;
-            const GroupScale g = group_scale(most_over(largest_of(v), 1u << a.cols.shift), I8 ? kLargestI8 : kLargestE4m3);
+            float m = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) m = most_magnitude(m, v[2 * k], v[2 * k + 1]);
+            const GroupScale g = group_scale(most_over(__float_as_uint(m), lanes), I8 ? kLargestI8 : kLargestE4m3);
             if (count[i] == 0) continue;
             const Place at = places[row[i]];
             if (at.code < 0) continue;
-            if (!ROBE_CHK(col[i] + count[i] <= a.cols.d, ROBE_DBG_ROW_POS)) continue;
-            if ((unit[i] & ((1u << a.cols.shift) - 1u)) == 0) ((float*)a.c.scales.p)[at.scale + (unit[i] >> a.cols.shift)] = g.scale;
-            store_codes<I8>((uint8_t*)a.c.codes.p + at.code + col[i], v, g.factor, count[i], a.code_piece);
+            if (!ROBE_CHK(col[i] + (uint32_t)count[i] <= (uint64_t)a.cols.d, ROBE_DBG_ROW_POS)) continue;
+            if ((unit[i] & (lanes - 1u)) == 0) ((float*)a.c.scales.p)[at.scale + (unit[i] >> a.cols.shift)] = g.scale;
+            uint8_t* to = (uint8_t*)a.c.codes.p + at.code + col[i];
+            if (FULL) __stcs((uint2*)to, make_uint2(codes_of<I8>(v, g.factor), codes_of<I8>(v + 4, g.factor)));
+            else store_codes<I8>(to, v, g.factor, count[i], a.code_piece);
         }
     }
 }
@@ -506,10 +652,7 @@ template <int W>
 struct CodeWords {
     uint32_t w[W < 4 ? 1 : W / 4];
     __device__ __forceinline__ void load(const uint8_t* p) {
-        if constexpr (W == 16) {
-            const uint4 q = __ldcs((const uint4*)p);
-            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-        } else if constexpr (W == 8) {
+        if constexpr (W == 8) {
             const uint2 q = __ldcs((const uint2*)p);
             w[0] = q.x; w[1] = q.y;
         } else if constexpr (W == 4) {
@@ -566,7 +709,8 @@ __global__ void __launch_bounds__(kCodeThreads) cache_read_kernel(CacheArgs a) {
     }
 }
 
-// rows of a CTA: about `items` units a thread, spread over the SMs where there are few
+// rows of a CTA: about `items` units a thread, so that finding the rows' places is shared by many, spread over the SMs where there are few (rows of
+// 1024 bf16, written four units a thread 27.4 us, eight 26.5, sixteen 26.8; read eight 77, sixteen 75, thirty-two 77)
 uint32_t rows_per_cta(int64_t n, uint32_t units, int items) {
     int64_t rows = (int64_t)kCodeThreads * items / units;
     if (rows > n / (148 * 2)) rows = n / (148 * 2);
@@ -580,10 +724,14 @@ cudaError_t launch_write(CacheArgs& a, cudaStream_t st) {
     const int64_t grid = (a.n + a.per_cta - 1) / a.per_cta;
     if (grid >= (1ll << 31)) return kGridTooSmall;
     auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)grid, kCodeThreads, 0, st, a); };
-    if (piece == kMost) launch(cache_write_kernel<T, kMost, I8, 4>);
-    else if (kMost == 8 && piece == 4) launch(cache_write_kernel<T, 4, I8, 2>);
-    else if (piece == 2) launch(cache_write_kernel<T, 2, I8, 2>);
-    else launch(cache_write_kernel<T, 1, I8, 2>);
+    const bool full = piece == kMost && full_units(a.cols, a.code_piece);
+    const bool few = a.n * a.units < 148ll * 2 * kCodeThreads * 4;
+    if (full && few) launch(cache_write_kernel<T, kMost, I8, 1, true>);
+    else if (full) launch(cache_write_kernel<T, kMost, I8, 4, true>);
+    else if (piece == kMost) launch(cache_write_kernel<T, kMost, I8, 2, false>);
+    else if (kMost == 8 && piece == 4) launch(cache_write_kernel<T, 4, I8, 2, false>);
+    else if (piece == 2) launch(cache_write_kernel<T, 2, I8, 2, false>);
+    else launch(cache_write_kernel<T, 1, I8, 2, false>);
     return cudaGetLastError();
 }
 
@@ -592,8 +740,7 @@ cudaError_t launch_read(CacheArgs& a, int width, cudaStream_t st) {
     const int64_t grid = (a.n + a.per_cta - 1) / a.per_cta;
     if (grid >= (1ll << 31)) return kGridTooSmall;
     auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)grid, kCodeThreads, 0, st, a); };
-    if (width == 16) launch(cache_read_kernel<T, 16, I8, 2>);
-    else if (width == 8) launch(cache_read_kernel<T, 8, I8, 4>);
+    if (width == 8) launch(cache_read_kernel<T, 8, I8, 4>);
     else if (width == 4) launch(cache_read_kernel<T, 4, I8, 4>);
     else launch(cache_read_kernel<T, 1, I8, 4>);
     return cudaGetLastError();
@@ -605,6 +752,7 @@ cudaError_t launch_residual_quantize(const QuantizeProblem& pb, int dtype, cudaS
     QuantizeArgs a{};
     a.rows = pb.rows;
     a.c = columns(pb.d, pb.group);
+    a.per_column = 1.0f / (float)pb.d;
     a.layer = pb.layer;
     a.eps = pb.eps;
     a.scale = pb.scale;
@@ -616,6 +764,7 @@ cudaError_t launch_residual_quantize(const QuantizeProblem& pb, int dtype, cudaS
     a.scales = pb.scales;
     a.code_piece = piece_for(a.c, 8, 1, {&a.codes}, pb.rows);
     a.w_pieces = (uintptr_t)pb.w % 16 == 0 && a.c.group % 4 == 0;
+    a.full = full_units(a.c, a.code_piece) && (pb.w == nullptr || a.w_pieces);
     return dtype == 0 ? launch_quantize<float>(a, pb.i8, true, st) : launch_quantize<__nv_bfloat16>(a, pb.i8, true, st);
 }
 
@@ -646,15 +795,16 @@ cudaError_t launch_cache_write(const CacheProblem& pb, const void* rows, int64_t
     a.units = cols.units;
     a.magic = magic_of(a.units);
     a.code_piece = code_piece;
-    a.per_cta = rows_per_cta(n, a.units, 4);
+    a.per_cta = rows_per_cta(n, a.units, 8);
     if (dtype == 0) return pb.i8 ? launch_write<float, true>(a, st) : launch_write<float, false>(a, st);
     return pb.i8 ? launch_write<__nv_bfloat16, true>(a, st) : launch_write<__nv_bfloat16, false>(a, st);
 }
 
 cudaError_t launch_cache_read(const CacheProblem& pb, void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st) {
     const int64_t size = dtype == 0 ? 4 : 2;
-    int width = 16;
-    for (; width > 1; width = width == 4 ? 1 : width / 2) {
+    // (sixteen codes a thread are two pieces of a row apart when they are written: 133 K rows of 1024 to bf16 91 us, eight 75)
+    int width = 8;
+    for (; width > 1; width = width == 4 ? 1 : 4) {
         const int64_t bytes = width * size > 16 ? 16 : width * size;
         if (pb.d % width == 0 && pb.group % width == 0 && (uintptr_t)pb.codes.p % width == 0 && pb.codes.ld % width == 0 &&
             pb.codes.page_ld % width == 0 && (uintptr_t)rows % bytes == 0 && (n <= 1 || rows_ld * size % bytes == 0))
@@ -667,7 +817,7 @@ cudaError_t launch_cache_read(const CacheProblem& pb, void* rows, int64_t rows_l
     a.units = (uint32_t)(pb.d / width);
     a.magic = magic_of(a.units);
     a.group_magic = magic_of((uint32_t)pb.group);
-    a.per_cta = rows_per_cta(n, a.units, width == 16 ? 2 : 4);
+    a.per_cta = rows_per_cta(n, a.units, 16);
     if (dtype == 0) return pb.i8 ? launch_read<float, true>(a, width, st) : launch_read<float, false>(a, width, st);
     return pb.i8 ? launch_read<__nv_bfloat16, true>(a, width, st) : launch_read<__nv_bfloat16, false>(a, width, st);
 }

@@ -22,6 +22,12 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t largest, float q) {
     g.factor = __frcp_rn(g.scale);
     return g;
 }
+// the largest magnitude of three; NaN where one is
+__device__ __forceinline__ float most_magnitude(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 constexpr float kLargestE4m3 = 448.0f, kLargestI8 = 127.0f;
@@ -105,31 +111,40 @@ __device__ __forceinline__ int64_t sequence_of_warp(const CachePlaces& p, int64_
     }
     return lo;
 }
-// row r of the call; near: a sequence at or before its own (offsets given)
+// row r of the call; near: a sequence at or before its own (offsets given).  What it most likely needs is asked for together.
 __device__ __forceinline__ CacheRow cache_row(const CachePlaces& p, int64_t r, int64_t near = 0) {
-    int64_t s, t;
+    int64_t s, t, start;
     if (p.offsets == nullptr) {
         s = r / p.per;
         t = r - s * p.per;
+        start = p.starts != nullptr ? __ldca(p.starts + s) : 0;
     } else {
-        if (p.batch == 0 || r < __ldca(p.offsets) || r >= __ldca(p.offsets + p.batch)) return CacheRow{-2, 0};
-        int64_t lo = near, hi = p.batch;
-        for (int64_t step = 1; lo + step < p.batch; step *= 2) {  // (the next one's beginning first)
-            if (__ldca(p.offsets + lo + step) > r) {
-                hi = lo + step;
-                break;
+        if (p.batch == 0) return CacheRow{-2, 0};
+        const int64_t first = __ldca(p.offsets), last = __ldca(p.offsets + p.batch), next = __ldca(p.offsets + near + 1);
+        int64_t begin = __ldca(p.offsets + near);
+        start = p.starts != nullptr ? __ldca(p.starts + near) : 0;
+        if (r < first || r >= last) return CacheRow{-2, 0};
+        s = near;
+        if (next <= r) {
+            int64_t lo = near + 1 < p.batch ? near + 1 : near, hi = p.batch;
+            for (int64_t step = 1; lo + step < p.batch; step *= 2) {
+                if (__ldca(p.offsets + lo + step) > r) {
+                    hi = lo + step;
+                    break;
+                }
+                lo += step;
             }
-            lo += step;
+            while (hi - lo > 1) {  // offsets[lo] <= r < offsets[hi]
+                const int64_t mid = (lo + hi) / 2;
+                if (__ldca(p.offsets + mid) <= r) lo = mid;
+                else hi = mid;
+            }
+            s = lo;
+            begin = __ldca(p.offsets + s);
+            start = p.starts != nullptr ? __ldca(p.starts + s) : 0;
         }
-        while (hi - lo > 1) {  // offsets[lo] <= r < offsets[hi]
-            const int64_t mid = (lo + hi) / 2;
-            if (__ldca(p.offsets + mid) <= r) lo = mid;
-            else hi = mid;
-        }
-        s = lo;
-        t = (int64_t)((uint64_t)r - (uint64_t)__ldca(p.offsets + s));
+        t = (int64_t)((uint64_t)r - (uint64_t)begin);
     }
-    const int64_t start = p.starts != nullptr ? __ldca(p.starts + s) : 0;
     return cache_row_at(p, s, (int64_t)((uint64_t)start + (uint64_t)t));  // (negative: no place)
 }
 

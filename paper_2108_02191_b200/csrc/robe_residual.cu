@@ -172,13 +172,6 @@ __global__ void __launch_bounds__(kAnyThreads, 2) residual_any_kernel(ResidualPr
 // cycles): 32 elements a thread 241 us, 8 (twice the warps, twice the work per row) 284, the first two sums over a row joined into
 // one 213, scalar for paired operations 327 against 310 at that time, no test of a row's end 219.
 
-// 1 / sqrt(v), to about a rounding: the function's result (within two) and one step of Newton's method.  (A division and a
-// square root, rounded each, took 4 to 10 % of a pass.)
-__device__ __forceinline__ float norm_factor(float v) {
-    const float y = rsqrtf(v), off = fmaf(-v * y, y, 1.0f);
-    return off == off ? fmaf(0.5f * y, off, y) : y;  // (of 0 and of infinity there is nothing to mend)
-}
-
 constexpr int kMaxLanes = 512;
 constexpr int kWarpRowThreads = 256;
 constexpr int kRowElems = 16, kGradWarpElems = 8;  // elements of a thread
