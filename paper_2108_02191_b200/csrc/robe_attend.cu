@@ -62,9 +62,14 @@ struct AttendArgs {
     float* parts;     // [spans x blocks][rows][dim + 4]
 };
 
-__device__ __forceinline__ uint32_t length_of(const AttendArgs& a, int64_t n) {
-    const int64_t pos = __ldca(a.p.at.starts + n);
+// spans of a sequence: one for a sequence without keys, too, whose results are +0
+__device__ __forceinline__ uint32_t spans_of(uint32_t length, uint32_t span) { return length > span ? (length + span - 1) / span : 1; }
+// keys of a sequence whose new token stands at pos
+__device__ __forceinline__ uint32_t length_at(const AttendArgs& a, int64_t pos) {
     return pos < 0 ? 0 : pos >= (int64_t)a.positions ? a.positions : (uint32_t)pos + 1;
+}
+__device__ __forceinline__ uint32_t length_of(const AttendArgs& a, int64_t n) {
+    return length_at(a, __ldca(a.p.at.starts + n));
 }
 
 // length of the spans for that many keys in all
@@ -75,8 +80,9 @@ __device__ __forceinline__ uint32_t span_of(const AttendArgs& a, unsigned long l
     const unsigned long long span = ((each + many - 1) / many + kSpanStep - 1) / kSpanStep * kSpanStep;
     return span < kSpanLeast ? kSpanLeast : (uint32_t)span;
 }
-// The plan of a call of at most kPlanWarp sequences, by the CTA's first warp: first[0 .. batch] and behind them the spans' length.
-__device__ __forceinline__ void plan_in_cta(const AttendArgs& a, uint32_t* first) {
+// The plan of a call of at most kPlanWarp sequences, by the CTA's first warp: first[0 .. batch] and behind them the spans' length; where the
+// new tokens stand.
+__device__ __forceinline__ void plan_in_cta(const AttendArgs& a, uint32_t* first, int64_t* stands) {
     constexpr uint32_t kEach = kPlanWarp / 32;
     if (threadIdx.x < 32) {
         const uint32_t batch = (uint32_t)a.p.at.batch, n0 = threadIdx.x * kEach;
@@ -84,7 +90,11 @@ __device__ __forceinline__ void plan_in_cta(const AttendArgs& a, uint32_t* first
         unsigned long long keys = 0;
 #pragma unroll
         for (uint32_t k = 0; k < kEach; ++k) {
-            length[k] = n0 + k < batch ? length_of(a, n0 + k) : 0;
+            length[k] = 0;
+            if (n0 + k < batch) {
+                stands[n0 + k] = __ldca(a.p.at.starts + n0 + k);
+                length[k] = length_at(a, stands[n0 + k]);
+            }
             keys += length[k];
         }
         for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xFFFFFFFFu, keys, o);
@@ -92,7 +102,7 @@ __device__ __forceinline__ void plan_in_cta(const AttendArgs& a, uint32_t* first
         uint32_t mine = 0;
 #pragma unroll
         for (uint32_t k = 0; k < kEach; ++k) {
-            length[k] = (length[k] + span - 1) / span;
+            length[k] = n0 + k < batch ? spans_of(length[k], span) : 0;
             mine += length[k];
         }
         uint32_t before = mine;
@@ -131,7 +141,7 @@ __global__ void __launch_bounds__(kPlanThreads) attend_plan_kernel(AttendArgs a)
     if (threadIdx.x == 0) a.plan->span = span;
     for (int64_t base = 0; base < a.p.at.batch; base += kPlanThreads) {
         const int64_t n = base + threadIdx.x;
-        const uint32_t v = n < a.p.at.batch ? (length_of(a, n) + span - 1) / span : 0;
+        const uint32_t v = n < a.p.at.batch ? spans_of(length_of(a, n), span) : 0;
         uint32_t sum = v;
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, sum, o);
@@ -258,6 +268,7 @@ struct AttendSmem {
     static_assert(kStages * sizeof(AttendStage<DIM>) >= kHeads * (DIM + 4) * 4, "a warp's part has room in its stages");
     float warp_most[kAttendWarps][kHeads], warp_sum[kAttendWarps][kHeads];
     int32_t edges[kBiasMaxSide];
+    int64_t stands[kPlanWarp];
     uint32_t first[kPlanWarp + 2];
     float bias[][kHeads + 1];  // as many rows as a side has buckets
 };
@@ -275,7 +286,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     follow();
     const uint32_t batch = (uint32_t)a.p.at.batch;
-    if (a.plan == nullptr) plan_in_cta(a, sm.first);
+    if (a.plan == nullptr) plan_in_cta(a, sm.first, sm.stands);
     const uint32_t* const firsts = a.plan == nullptr ? sm.first : a.first;
     const uint32_t span = a.plan == nullptr ? sm.first[kPlanWarp + 1] : a.plan->span;
     const uint32_t items = firsts[batch] * a.blocks;
@@ -303,15 +314,15 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t piece = item / a.blocks, block = item - piece * a.blocks;
         uint32_t n = 0;
-        for (uint32_t hi = batch; hi - n > 1;) {  // first[n] <= piece < first[n + 1] (sequences without keys have no piece)
+        for (uint32_t hi = batch; hi - n > 1;) {  // first[n] <= piece < first[n + 1]
             const uint32_t mid = (n + hi) / 2;
             if (firsts[mid] <= piece) n = mid;
             else hi = mid;
         }
         const uint32_t pieces = firsts[n + 1] - firsts[n];
         const uint32_t split = piece - firsts[n];
-        const uint32_t length = length_of(a, n);
-        const int64_t pos = __ldca(a.p.at.starts + n);
+        const int64_t pos = a.plan == nullptr ? sm.stands[n] : __ldca(a.p.at.starts + n);
+        const uint32_t length = length_at(a, pos);
         const uint32_t begin = split * span, end = length - begin < span ? length : begin + span;
         const uint32_t head = block / a.head_blocks;  // of the cache
         const uint32_t q0 = (block - head * a.head_blocks) * kHeads;  // first of its query heads
@@ -608,58 +619,57 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     }
 }
 
-// The spans of a sequence: a CTA per query head, its warps taking spans in turn, eight under way at a time.  Sequences of one
-// span are done already; those without keys get +0.
+// The spans of a sequence: the warps of a query head take them in turn, eight under way at a time; a CTA has `each` query heads.
+// Sequences of one span are done already.
 constexpr int kSpanThreads = 256;
+constexpr uint32_t kSpanWarps = kSpanThreads / 32;
 template <int DIM>
-__global__ void __launch_bounds__(kSpanThreads) attend_join_kernel(AttendArgs a) {
-    constexpr int kWarps = kSpanThreads / 32, E = DIM / 32, kAhead = DIM > 128 ? 4 : 8;
-    __shared__ float sums[kWarps][DIM], totals[kWarps], mosts[kWarps];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const uint32_t n = blockIdx.x / (uint32_t)a.p.q_heads, h = blockIdx.x - n * (uint32_t)a.p.q_heads;
-    const uint32_t head = h / a.group, in_group = h - head * a.group;
-    const uint32_t block = head * a.head_blocks + in_group / kHeads;
+__global__ void __launch_bounds__(kSpanThreads) attend_join_kernel(AttendArgs a, uint32_t each) {
+    constexpr int E = DIM / 32, kAhead = DIM > 128 ? 4 : 8;
+    __shared__ float sums[kSpanWarps][DIM], totals[kSpanWarps], mosts[kSpanWarps];
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, q_heads = (uint32_t)a.p.q_heads;
+    const uint32_t per = kSpanWarps / each, sub = warp % per;  // warps of a query head
+    const uint32_t ctas = (q_heads + each - 1) / each, n = blockIdx.x / ctas, h = (blockIdx.x - n * ctas) * each + warp / per;
     follow();
     const uint32_t first = __ldca(a.first + n), pieces = __ldca(a.first + n + 1) - first;
-    __nv_bfloat16* to = (__nv_bfloat16*)a.p.out.p + ((int64_t)n * a.p.q_heads + h) * a.p.out.ld;
     if (pieces == 1) return;
-    if (pieces == 0) {
-        for (int k = threadIdx.x; k < DIM; k += kSpanThreads) to[k] = narrow<__nv_bfloat16>(0.0f);
-        return;
-    }
-    const float* parts = a.parts + (((uint64_t)first * a.blocks + block) * a.rows + in_group % kHeads) * (DIM + 4);
-    const uint64_t step = (uint64_t)a.blocks * a.rows * (DIM + 4);
     float sum[E], total = 0.0f, most = -INFINITY;
 #pragma unroll
     for (int k = 0; k < E; ++k) sum[k] = 0.0f;
-    for (uint32_t p = warp; p < pieces; p += kWarps * kAhead) {
-        float m[kAhead], l[kAhead], v[kAhead][E], top = most;
+    if (h < q_heads) {
+        const uint32_t head = h / a.group, in_group = h - head * a.group;
+        const uint32_t block = head * a.head_blocks + in_group / kHeads;
+        const float* parts = a.parts + (((uint64_t)first * a.blocks + block) * a.rows + in_group % kHeads) * (DIM + 4);
+        const uint64_t step = (uint64_t)a.blocks * a.rows * (DIM + 4);
+        for (uint32_t p = sub; p < pieces; p += per * kAhead) {
+            float m[kAhead], l[kAhead], v[kAhead][E], top = most;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            m[u] = -INFINITY;
-            if (p + u * kWarps < pieces) {
-                const float* from = parts + (p + u * kWarps) * step;
-                m[u] = __ldca(from + DIM);
-                l[u] = __ldca(from + DIM + 1);
+            for (int u = 0; u < kAhead; ++u) {
+                m[u] = -INFINITY;
+                if (p + u * per < pieces) {
+                    const float* from = parts + (p + u * per) * step;
+                    m[u] = __ldca(from + DIM);
+                    l[u] = __ldca(from + DIM + 1);
 #pragma unroll
-                for (int k = 0; k < E; ++k) v[u][k] = __ldca(from + k * 32 + lane);
+                    for (int k = 0; k < E; ++k) v[u][k] = __ldca(from + k * 32 + lane);
+                }
             }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) top = most_nan(top, m[u]);
+            const float base = top == -INFINITY ? 0.0f : top, f = exp2_of(most - base);
+            total *= f;
+#pragma unroll
+            for (int k = 0; k < E; ++k) sum[k] *= f;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (p + u * per >= pieces) break;
+                const float e = exp2_of(m[u] - base);
+                total = fmaf(l[u], e, total);
+#pragma unroll
+                for (int k = 0; k < E; ++k) sum[k] = fmaf(v[u][k], e, sum[k]);
+            }
+            most = top;
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) top = most_nan(top, m[u]);
-        const float base = top == -INFINITY ? 0.0f : top, f = exp2_of(most - base);
-        total *= f;
-#pragma unroll
-        for (int k = 0; k < E; ++k) sum[k] *= f;
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p + u * kWarps >= pieces) break;
-            const float e = exp2_of(m[u] - base);
-            total = fmaf(l[u], e, total);
-#pragma unroll
-            for (int k = 0; k < E; ++k) sum[k] = fmaf(v[u][k], e, sum[k]);
-        }
-        most = top;
     }
 #pragma unroll
     for (int k = 0; k < E; ++k) sums[warp][k * 32 + lane] = sum[k];
@@ -668,46 +678,56 @@ __global__ void __launch_bounds__(kSpanThreads) attend_join_kernel(AttendArgs a)
         mosts[warp] = most;
     }
     __syncthreads();
-    for (int k = threadIdx.x; k < DIM; k += kSpanThreads) {
-        float m = mosts[0], v = 0.0f, l = 0.0f;
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = most_nan(m, mosts[w]);
+    for (uint32_t k = threadIdx.x; k < each * DIM; k += kSpanThreads) {
+        const uint32_t of = k / DIM, col = k % DIM, w0 = of * per, head = (blockIdx.x - n * ctas) * each + of;
+        if (head >= q_heads) break;
+        float m = mosts[w0], v = 0.0f, l = 0.0f;
+        for (uint32_t w = 1; w < per; ++w) m = most_nan(m, mosts[w0 + w]);
         const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = exp2_of(mosts[w] - base);
-            v = fmaf(sums[w][k], f, v);
-            l = fmaf(totals[w], f, l);
+        for (uint32_t w = 0; w < per; ++w) {
+            const float f = exp2_of(mosts[w0 + w] - base);
+            v = fmaf(sums[w0 + w][col], f, v);
+            l = fmaf(totals[w0 + w], f, l);
         }
-        to[k] = narrow<__nv_bfloat16>(l == 0.0f ? 0.0f : v / l);
+        ((__nv_bfloat16*)a.p.out.p)[((int64_t)n * q_heads + head) * a.p.out.ld + col] = narrow<__nv_bfloat16>(l == 0.0f ? 0.0f : v / l);
     }
 }
 
 uint32_t head_blocks_of(int64_t heads, int64_t q_heads) { return (uint32_t)((q_heads / heads + kHeads - 1) / kHeads); }
 
+template <auto KERNEL>
+struct Kernel {
+    static constexpr auto value = KERNEL;
+};
 template <int DIM>
 cudaError_t launch_attend_dim(AttendArgs& a, cudaStream_t st) {
+    const size_t bytes = sizeof(AttendSmem<DIM>) + (a.p.biased ? a.p.bk.side : 0) * (kHeads + 1) * sizeof(float);
+    constexpr size_t kMostBytes = sizeof(AttendSmem<DIM>) + kBiasMaxSide * (kHeads + 1) * sizeof(float);
     cudaError_t e = cudaSuccess;
-    auto launch = [&](auto kernel) {
-        const size_t bytes = sizeof(AttendSmem<DIM>) + (a.p.biased ? a.p.bk.side : 0) * (kHeads + 1) * sizeof(float);
-        int resident = 1;
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, kAttendThreads, bytes);
+    auto launch = [&](auto of) {
+        constexpr auto kernel = decltype(of)::value;
+        unsigned resident = 1;
+        e = with_shared<kernel>(kMostBytes);
+        if (e == cudaSuccess) e = resident_ctas<kernel>(kAttendThreads, bytes, resident);
         if (e != cudaSuccess) return;
-        a.ctas = 148u * (unsigned)resident < kAttendCtas ? 148u * (unsigned)resident : kAttendCtas;
+        a.ctas = 148u * resident < kAttendCtas ? 148u * resident : kAttendCtas;
         if (a.plan != nullptr) launch_next(attend_plan_kernel, 1, kPlanThreads, 0, st, a);
         launch_next(kernel, a.ctas, kAttendThreads, bytes, st, a);
     };
-    if (a.group > 8) a.p.i8 ? launch(attend_kernel<DIM, true, true>) : launch(attend_kernel<DIM, false, true>);
-    else a.p.i8 ? launch(attend_kernel<DIM, true, false>) : launch(attend_kernel<DIM, false, false>);
+    if (a.group > 8) a.p.i8 ? launch(Kernel<attend_kernel<DIM, true, true>>{}) : launch(Kernel<attend_kernel<DIM, false, true>>{});
+    else a.p.i8 ? launch(Kernel<attend_kernel<DIM, true, false>>{}) : launch(Kernel<attend_kernel<DIM, false, false>>{});
     if (e != cudaSuccess) return e;
-    launch_next(attend_join_kernel<DIM>, (unsigned)(a.p.at.batch * a.p.q_heads), kSpanThreads, 0, st, a);
+    if (a.positions > kSpanLeast) {  // (a sequence within one span is done)
+        // few query heads: a CTA each, so that its warps share the spans; many: a warp each
+        const uint32_t q_heads = (uint32_t)a.p.q_heads, each = (uint64_t)a.p.at.batch * q_heads < 148 * 4 ? 1 : kSpanWarps;
+        launch_next(attend_join_kernel<DIM>, (unsigned)(a.p.at.batch * ((q_heads + each - 1) / each)), kSpanThreads, 0, st, a, each);
+    }
     return cudaGetLastError();
 }
 
 // a sequence has at most one span more than its share of those that are made for the CTAs, and no span is shorter than kSpanLeast
 uint64_t most_items(int64_t batch, uint32_t blocks, int64_t positions) {
-    const unsigned __int128 by_length = (unsigned __int128)batch * ((positions + kSpanLeast - 1) / kSpanLeast) * blocks;
+    const unsigned __int128 by_length = (unsigned __int128)batch * (positions > 0 ? (positions + kSpanLeast - 1) / kSpanLeast : 1) * blocks;
     const unsigned __int128 by_share = (unsigned __int128)kAttendCtas * kSpansPerCta + (unsigned __int128)batch * blocks;
     return (uint64_t)(by_length < by_share ? by_length : by_share);
 }

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "robe_device.cuh"
 
 namespace robe {
@@ -26,6 +28,41 @@ inline void launch_next(void (*kernel)(P...), unsigned grid, unsigned block, siz
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);  // (an error stays for cudaGetLastError)
+}
+
+// Lets a kernel have `most` bytes of dynamic shared memory; asked of the runtime once a device (the devices that have been asked for are
+// remembered, and asking again does no harm).
+template <auto KERNEL>
+inline cudaError_t with_shared(size_t most) {
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+// CTAs of a kernel that an SM holds, at least one; the last answer is remembered.
+template <auto KERNEL>
+inline cudaError_t resident_ctas(int threads, size_t bytes, unsigned& ctas) {
+    static std::atomic<uint64_t> last{0};  // bytes + 1, device, answer
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t asked = ((uint64_t)bytes + 1) << 32 | (uint64_t)(uint16_t)device << 16;
+    const uint64_t known = last.load(std::memory_order_relaxed);
+    if ((known & ~0xFFFFull) == asked) {
+        ctas = (unsigned)(known & 0xFFFFu);
+        return cudaSuccess;
+    }
+    int n = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERNEL, threads, bytes);
+    if (e != cudaSuccess) return e;
+    ctas = n < 1 ? 1u : (unsigned)n;
+    last.store(asked | ctas, std::memory_order_relaxed);
+    return cudaSuccess;
 }
 
 constexpr uint64_t kL2SizedBytes = 192ull << 20;  // arrays up to this size count as "of L2 size"

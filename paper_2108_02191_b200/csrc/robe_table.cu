@@ -171,9 +171,10 @@ uint32_t chunk_rows(int64_t rows, int64_t d) {
 }
 // Where there are many chunks, the parts of a run that covers kFold of them are added up before the join.
 constexpr uint32_t kFold = 32;
-constexpr uint64_t kFoldFrom = 1024;
+constexpr uint64_t kFoldFrom = 4096;
 
 constexpr int64_t kClusterRows = 65536;  // up to so many ids one cluster sorts in its shared memory
+constexpr int64_t kAloneRows = 512;      // up to so many every CTA that needs them sorts them for itself
 struct GradLayout {
     size_t keys[2], places[2], counts, totals, parts, folds, total;
     uint32_t chunk;
@@ -213,7 +214,7 @@ struct GradArgs {
     int64_t table_ld;
     float scale;
     int accumulate;
-    uint32_t *keys, *places;  // sorted from grad_sums_kernel on
+    uint32_t *keys, *places;  // sorted from grad_sums_kernel on, for few ids from the join on
     float* parts;             // [chunks][2]: what a chunk has of the run it begins in, and of the run it ends in
     int64_t parts_ld;
     double* folds;            // [chunks / kFold]: the first parts of kFold chunks that lie in one run as a whole; nullptr: none
@@ -419,23 +420,63 @@ __global__ void __launch_bounds__(kRankThreads) grad_cluster_sort_kernel(GradArg
     }
 }
 
+// The table alone.
+__global__ void __launch_bounds__(kTableThreads) grad_clear_kernel(GradArgs a) {
+    follow<true>();
+    clear_table(a, (uint64_t)blockIdx.x * kTableThreads + threadIdx.x, (uint64_t)gridDim.x * kTableThreads);
+}
+
 // Sums of a chunk's runs, V columns a thread, `lanes` threads a row.  ADD: to what is there, which is asked for together with the
-// rows of the run's end.
-template <class T, int V, bool ADD>
-__global__ void __launch_bounds__(kTableThreads, 4) grad_sums_kernel(GradArgs a, uint32_t lanes) {
-    constexpr int kAhead = ADD ? 2 : 4;  // rows under way: few, so that four CTAs are resident (16384 x 4096 bf16: 87 us with twice as many)
-    extern __shared__ uint32_t staged[];  // keys, then places, of the CTA's chunks
+// rows of the run's end.  HOW: kMany CTAs, a wave of them and more, kSome, so that a thread has more rows under way; kAlone: at most
+// kAloneRows ids, which each CTA sorts by counting for each how many come before it.
+enum SumsHow { kMany, kSome, kAlone };
+template <class T, int V, bool ADD, SumsHow HOW>
+__global__ void __launch_bounds__(kTableThreads, HOW == kMany ? 4 : 2) grad_sums_kernel(GradArgs a, uint32_t lanes) {
+    // rows under way: few where four CTAs are resident (16384 x 4096 bf16: 71 us, 87 with twice as many and two CTAs)
+    constexpr int kAhead = HOW == kMany ? (ADD ? 2 : 4) : (ADD ? 4 : 8);
+    extern __shared__ uint32_t staged[];  // keys, then places, of the CTA's chunks (kAlone: of all)
     follow();
     const uint32_t groups = kTableThreads / lanes;
     const uint64_t block = blockIdx.x / a.slices;
     const uint32_t slice = blockIdx.x - (uint32_t)block * a.slices;
-    const uint64_t from = block * groups * a.chunk;
-    const uint32_t staged_rows = groups * a.chunk;
-    for (uint32_t k = threadIdx.x; k < staged_rows; k += kTableThreads)
-        if (from + k < (uint64_t)a.rows) {
-            staged[k] = a.keys[from + k];
-            staged[staged_rows + k] = a.places[from + k];
+    const uint64_t from = HOW == kAlone ? 0 : block * groups * a.chunk;
+    const uint32_t staged_rows = HOW == kAlone ? (uint32_t)kAloneRows : groups * a.chunk;
+    if (HOW == kAlone) {
+        __shared__ __align__(16) uint32_t ids[kAloneRows];
+        constexpr int kIds = (int)kAloneRows / kTableThreads;
+        uint32_t mine[kIds], before[kIds];
+#pragma unroll
+        for (int r = 0; r < kIds; ++r) {
+            const uint32_t p = threadIdx.x + r * kTableThreads;
+            mine[r] = p < (uint64_t)a.rows ? key_of(a, p) : 0xFFFFFFFFu;  // (behind all others, being the last)
+            before[r] = 0;
+            ids[p] = mine[r];
         }
+        __syncthreads();
+        for (uint32_t k = 0; k < (uint32_t)a.rows; k += 4) {
+            const uint4 q = *(const uint4*)(ids + k);
+#pragma unroll
+            for (int r = 0; r < kIds; ++r) {
+                const uint32_t p = threadIdx.x + r * kTableThreads, m = mine[r];
+                before[r] += (q.x < m || (q.x == m && k < p)) + (q.y < m || (q.y == m && k + 1 < p)) + (q.z < m || (q.z == m && k + 2 < p)) +
+                             (q.w < m || (q.w == m && k + 3 < p));
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kIds; ++r) {
+            const uint32_t p = threadIdx.x + r * kTableThreads;
+            if (p >= (uint64_t)a.rows || !ROBE_CHK(before[r] < (uint64_t)a.rows, ROBE_DBG_SHARED)) continue;
+            staged[before[r]] = mine[r];
+            staged[staged_rows + before[r]] = p;
+            if (blockIdx.x == 0) a.keys[before[r]] = mine[r];  // for the join
+        }
+    } else {
+        for (uint32_t k = threadIdx.x; k < staged_rows; k += kTableThreads)
+            if (from + k < (uint64_t)a.rows) {
+                staged[k] = a.keys[from + k];
+                staged[staged_rows + k] = a.places[from + k];
+            }
+    }
     __syncthreads();
     const uint32_t group = threadIdx.x / lanes;
     const uint64_t c = block * groups + group;
@@ -444,11 +485,12 @@ __global__ void __launch_bounds__(kTableThreads, 4) grad_sums_kernel(GradArgs a,
     const uint64_t begin = c * a.chunk;
     const uint32_t count = (uint32_t)((uint64_t)a.rows - begin < a.chunk ? (uint64_t)a.rows - begin : a.chunk);
     const uint32_t vocab = (uint32_t)a.vocab;
-    const uint32_t* keys = staged + group * a.chunk;
+    const uint32_t* keys = staged + (begin - from);
     const uint32_t* places = keys + staged_rows;
     if (keys[0] >= vocab) return;
-    bool open = begin > 0 && a.keys[begin - 1] == keys[0];  // the run began in an earlier chunk
-    const uint32_t after = begin + count < (uint64_t)a.rows ? a.keys[begin + count] : 0xFFFFFFFFu;
+    const uint32_t* const all = HOW == kAlone ? staged : a.keys;
+    bool open = begin > 0 && all[begin - 1] == keys[0];  // the run began in an earlier chunk
+    const uint32_t after = begin + count < (uint64_t)a.rows ? all[begin + count] : 0xFFFFFFFFu;
     float sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.0f;
@@ -654,7 +696,7 @@ cudaError_t launch_cluster_sort(const GradArgs& a, uint32_t bits, cudaStream_t s
     const uint32_t passes = (bits + kClusterBits - 1) / kClusterBits, per = (bits + passes - 1) / passes;
     const uint32_t ctas = a.rows <= kRankThreads ? 1 : kClusterMost;
     const size_t bytes = sizeof(ClusterSmem<ITEMS>);
-    const cudaError_t e = cudaFuncSetAttribute(grad_cluster_sort_kernel<ITEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    const cudaError_t e = with_shared<grad_cluster_sort_kernel<ITEMS>>(bytes);
     if (e != cudaSuccess) return e;
     // the table: as many others as the SMs hold beside the sort
     const unsigned __int128 pieces = (unsigned __int128)a.vocab * (uint64_t)a.d / (kRankThreads * 16) + 1;
@@ -685,8 +727,11 @@ cudaError_t launch_sums(GradArgs& a, cudaStream_t st) {
     const uint64_t groups = kTableThreads / lanes;
     const uint64_t grid = (a.chunks + groups - 1) / groups * a.slices;
     if (grid >= (1ull << 31)) return kGridTooSmall;
-    if (a.accumulate) launch_next(grad_sums_kernel<T, V, true>, (unsigned)grid, kTableThreads, groups * a.chunk * 8, st, a, lanes);
-    else launch_next(grad_sums_kernel<T, V, false>, (unsigned)grid, kTableThreads, groups * a.chunk * 8, st, a, lanes);
+    auto launch = [&](auto kernel, uint64_t rows) { launch_next(kernel, (unsigned)grid, kTableThreads, rows * 8, st, a, lanes); };
+    const bool add = a.accumulate != 0;
+    if (a.rows <= kAloneRows) add ? launch(grad_sums_kernel<T, V, true, kAlone>, kAloneRows) : launch(grad_sums_kernel<T, V, false, kAlone>, kAloneRows);
+    else if (grid <= 148 * 2) add ? launch(grad_sums_kernel<T, V, true, kSome>, groups * a.chunk) : launch(grad_sums_kernel<T, V, false, kSome>, groups * a.chunk);
+    else add ? launch(grad_sums_kernel<T, V, true, kMany>, groups * a.chunk) : launch(grad_sums_kernel<T, V, false, kMany>, groups * a.chunk);
     return cudaSuccess;
 }
 template <class T>
@@ -770,7 +815,9 @@ cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int6
     a.places = places[0];
     uint32_t bits = 1;
     while (((uint64_t)pb.vocab >> bits) != 0) ++bits;  // (vocab itself is a key)
-    if (pb.rows > 0 && pb.rows <= kClusterRows) {
+    if (pb.rows <= kAloneRows) {
+        if (!accumulate) launch_next(grad_clear_kernel, 148 * 8, kTableThreads, 0, st, a);
+    } else if (pb.rows <= kClusterRows) {
         const cudaError_t e = pb.rows <= kClusterRows / 8   ? launch_cluster_sort<1>(a, bits, st)
                               : pb.rows <= kClusterRows / 4 ? launch_cluster_sort<2>(a, bits, st)
                               : pb.rows <= kClusterRows / 2 ? launch_cluster_sort<4>(a, bits, st)
@@ -778,11 +825,9 @@ cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int6
         if (e != cudaSuccess) return e;
     } else {
         launch_next(grad_keys_kernel, 148 * 8, kTableThreads, 0, st, a);
-        if (pb.rows > 0) {
-            const int in = launch_sort_pairs(keys, places, (uint64_t)pb.rows, bits, (uint32_t*)(ws + L.counts), (uint32_t*)(ws + L.totals), st);
-            a.keys = keys[in];
-            a.places = places[in];
-        }
+        const int in = launch_sort_pairs(keys, places, (uint64_t)pb.rows, bits, (uint32_t*)(ws + L.counts), (uint32_t*)(ws + L.totals), st);
+        a.keys = keys[in];
+        a.places = places[in];
     }
     if (pb.rows > 0) {
         const cudaError_t e = pb.dtype == 0 ? launch_sums<float>(a, piece, st) : launch_sums<__nv_bfloat16>(a, piece, st);
@@ -790,7 +835,7 @@ cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int6
     }
     if (a.folds != nullptr) launch_next(grad_fold_kernel, (unsigned)(L.chunks / kFold), kTableThreads, 0, st, a);
     a.slices = join_slices;
-    if (join > 0) launch_next(grad_join_kernel, (unsigned)join, kTableThreads, 0, st, a);
+    if (L.chunks > 1) launch_next(grad_join_kernel, (unsigned)join, kTableThreads, 0, st, a);
     return cudaGetLastError();
 }
 
