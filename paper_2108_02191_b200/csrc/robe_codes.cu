@@ -97,21 +97,21 @@ __device__ __forceinline__ uint32_t largest_of(const float (&v)[8]) {
 // ---- where columns lie: a unit is eight columns of one group; `lanes` units (a power of two) hold a group, those behind its end
 // nothing.  With one scale a row the units follow one another and the whole row is the group.
 struct Columns {
-    int64_t d;
-    uint32_t group, shift, units;  // shift: of lanes; units: of a row
-    int whole;                     // one scale a row
+    uint32_t d, group, shift, units;  // shift: of lanes; units: of a row
+    int whole;                        // one scale a row
 };
-__device__ __forceinline__ int64_t columns_of(const Columns& c, uint32_t unit, int& count) {
-    const int64_t begin = (int64_t)(unit >> c.shift) * c.group;
-    const int64_t end = begin + c.group < c.d ? begin + c.group : c.d;
-    const int64_t col = begin + (int64_t)(unit & ((1u << c.shift) - 1u)) * 8;
-    const int64_t left = end - col;
-    count = unit >= c.units || left <= 0 ? 0 : left < 8 ? (int)left : 8;
-    return col;
+// FULL: rows and groups are of whole eights of columns: a unit has eight or none
+template <bool FULL = false>
+__device__ __forceinline__ uint32_t columns_of(const Columns& c, uint32_t unit, int& count) {
+    const uint32_t begin = (unit >> c.shift) * c.group, in = (unit & ((1u << c.shift) - 1u)) * 8, col = begin + in;
+    const uint32_t end = begin + c.group < c.d ? begin + c.group : c.d;
+    if (FULL) count = in < c.group && col < c.d ? 8 : 0;
+    else count = col >= end ? 0 : end - col >= 8 ? 8 : (int)(end - col);
+    return col;  // (units behind the row's begin behind its end)
 }
 Columns columns(int64_t d, int64_t group) {
     Columns c;
-    c.d = d;
+    c.d = (uint32_t)d;
     c.whole = group > kGroupMost;
     if (c.whole) group = 8;
     c.group = (uint32_t)group;
@@ -121,10 +121,8 @@ Columns columns(int64_t d, int64_t group) {
     return c;
 }
 
-// every unit has eight columns of its group, their codes in one piece
-bool full_units(const Columns& c, int code_piece) {
-    return c.group == 8u << c.shift && c.d % c.group == 0 && code_piece == 8;
-}
+// rows and groups of whole eights of columns, whose codes are written in one piece
+bool full_units(const Columns& c, int code_piece) { return c.d % 8 == 0 && c.group % 8 == 0 && code_piece == 8; }
 
 // ---------------------------------------------------------------- the join
 
@@ -136,7 +134,7 @@ struct QuantizeArgs {
     const float* w;
     RowsRef x, residual, out, codes, scales;
     int code_piece, w_pieces;
-    int full;  // every unit of a row has eight columns of its group, all in 16-byte pieces, codes in eights
+    int i8;
     uint32_t threads;  // of a row
     // a cache takes the codes: rows of the call lie where `at` says
     int cached;
@@ -203,12 +201,13 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t threads, 
     return v;
 }
 
-// The usual call: whole 16-byte pieces, groups of a power of two of columns that all rows are made of (or one scale a row).  No unit has less
-// than eight columns, so that two operations go in one instruction and nothing is asked per element; K units a thread.  What hides
-// the loads' latency is CTAs, not rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 87 us; 117 by the kernel for
-// any call, whose instructions bound it; 252 with two CTAs an SM that asked for the next row.)
-template <class T, int K, bool RESIDUAL, bool I8, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_full_kernel(QuantizeArgs a) {
+// A row in the registers of its threads, K units each; two operations in one instruction.  What hides the loads' latency is CTAs, not
+// rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 87 us; elements one by one 117, bound by instructions; 252
+// with two CTAs an SM that asked for the next row.)
+// FULL: as columns_of has it, in 16-byte pieces and codes in eights, RESIDUAL and I8 known; otherwise these are asked for.
+template <class T, int P, int K, int THREADS, bool FULL, bool RESIDUAL, bool I8>
+__global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) quantize_rows_kernel(QuantizeArgs a) {
+    const bool joined = FULL ? RESIDUAL : a.residual.p != nullptr, i8 = FULL ? I8 : a.i8 != 0;
     __shared__ float sums[2][THREADS / 32];
     __shared__ uint32_t most[THREADS / 32];
     follow();
@@ -219,48 +218,50 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_full_kernel(
         r = (int64_t)blockIdx.x * (blockDim.x / a.threads) + threadIdx.x / a.threads;
     }
     const bool on_row = r < a.rows;
-    Eight<T> x[K], y[RESIDUAL ? K : 1];
+    Eight<T> x[K], y[K];
+    uint32_t col[K];
+    int count[K];
     const T* from = (const T*)a.x.p + r * a.x.ld;
     const T* beside = (const T*)a.residual.p + r * a.residual.ld;
-    bool on[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const uint32_t unit = t + j * a.threads;
-        on[j] = on_row && unit < a.c.units;
-        if (!ROBE_CHK(!on[j] || (unit + 1) * 8ll <= a.c.d, ROBE_DBG_ROW_POS)) on[j] = false;
-        if (on[j]) load_eight<T, kPiece<T>>(x[j], from + unit * 8, 8);
-        if (RESIDUAL && on[j]) load_eight<T, kPiece<T>>(y[RESIDUAL ? j : 0], beside + unit * 8, 8);
+        col[j] = columns_of<FULL>(a.c, t + j * a.threads, count[j]);
+        if (!on_row || !ROBE_CHK(count[j] == 0 || col[j] + (uint32_t)count[j] <= (uint64_t)a.c.d, ROBE_DBG_ROW_POS)) count[j] = 0;
+        if (count[j] > 0) load_eight<T, P>(x[j], from + col[j], FULL ? 8 : count[j]);
+        if (joined && count[j] > 0) load_eight<T, P>(y[j], beside + col[j], FULL ? 8 : count[j]);
     }
-    float2 v[K][4];
-    float2 sum = both(0.0f);
+    float2 v[K][4];  // (zeros behind the unit's columns)
 #pragma unroll
     for (int j = 0; j < K; ++j)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             v[j][k] = both(0.0f);
-            if (on[j]) {
+            if (count[j] > 0) {
                 const float2 p = make_float2(x[j].get(2 * k), x[j].get(2 * k + 1));
-                const Eight<T>& q = y[RESIDUAL ? j : 0];
-                v[j][k] = RESIDUAL ? fma2(both(a.scale), p, make_float2(q.get(2 * k), q.get(2 * k + 1))) : mul2(both(a.scale), p);
+                v[j][k] = joined ? fma2(both(a.scale), p, make_float2(y[j].get(2 * k), y[j].get(2 * k + 1))) : mul2(both(a.scale), p);
             }
         }
     if (a.out.p != nullptr) {
         T* to = (T*)a.out.p + r * a.out.ld;
 #pragma unroll
         for (int j = 0; j < K; ++j)
-            if (on[j]) store_eight<T, kPiece<T>>((const float(&)[8])v[j], to + (t + j * a.threads) * 8, 8);
+            if (count[j] > 0) store_eight<T, P>((const float(&)[8])v[j], to + col[j], FULL ? 8 : count[j]);
     }
     if (a.w != nullptr) {
+        float2 sum = both(0.0f);
         if (a.layer) {
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) sum = add2(sum, v[j][k]);
-            const float2 mean = both(-add_over_row(sum.x + sum.y, a.threads, sums[0]) * a.per_column);
+            const float mean = add_over_row(sum.x + sum.y, a.threads, sums[0]) * a.per_column;
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[j][k] = on[j] ? add2(v[j][k], mean) : both(0.0f);
+                for (int k = 0; k < 4; ++k) {
+                    v[j][k].x = (FULL ? 0 : 2 * k) < count[j] ? v[j][k].x - mean : 0.0f;
+                    v[j][k].y = (FULL ? 0 : 2 * k + 1) < count[j] ? v[j][k].y - mean : 0.0f;
+                }
             sum = both(0.0f);
         }
 #pragma unroll
@@ -270,147 +271,61 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) quantize_full_kernel(
         const float2 factor = both(norm_factor(fmaf(add_over_row(sum.x + sum.y, a.threads, sums[1]), a.per_column, a.eps)));
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            if (!on[j]) continue;
-            const float4* w = (const float4*)(a.w + (t + j * a.threads) * 8);
-            const float4 p = __ldca(w), q = __ldca(w + 1);
-            v[j][0] = mul2(mul2(v[j][0], factor), make_float2(p.x, p.y));
-            v[j][1] = mul2(mul2(v[j][1], factor), make_float2(p.z, p.w));
-            v[j][2] = mul2(mul2(v[j][2], factor), make_float2(q.x, q.y));
-            v[j][3] = mul2(mul2(v[j][3], factor), make_float2(q.z, q.w));
+            if (count[j] == 0) continue;
+            float w[8];
+            load_weights(w, a, col[j], FULL ? 8 : count[j]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[j][k] = mul2(mul2(v[j][k], factor), make_float2(w[2 * k], w[2 * k + 1]));
         }
     }
     uint8_t* const codes = (uint8_t*)a.codes.p + r * a.codes.ld;
     float* const scales = (float*)a.scales.p + r * a.scales.ld;
-    constexpr float kQ = I8 ? kLargestI8 : kLargestE4m3;
+    const float q = i8 ? kLargestI8 : kLargestE4m3;
     auto largest = [&](int j) {
         float m = 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) m = most_magnitude(m, v[j][k].x, v[j][k].y);
         return __float_as_uint(m);
     };
-    auto write = [&](int j, float f) {
-        float c[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 p = mul2(v[j][k], both(f));
-            c[2 * k] = p.x;
-            c[2 * k + 1] = p.y;
-        }
-        const uint2 w = I8 ? make_uint2(codes_i8(c[0], c[1], c[2], c[3]), codes_i8(c[4], c[5], c[6], c[7]))
-                           : make_uint2(codes_e4m3(c[0], c[1], c[2], c[3]), codes_e4m3(c[4], c[5], c[6], c[7]));
-        __stcs((uint2*)(codes + (t + j * a.threads) * 8), w);
-    };
+    GroupScale whole{};
     if (a.c.whole) {
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < K; ++j) m = max(m, largest(j));
-        const GroupScale g = group_scale(most_over_row(m, a.threads, most), kQ);
-        if (on_row && t == 0) scales[0] = g.scale;
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-            if (on[j]) write(j, g.factor);
-    } else {
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const GroupScale g = group_scale(most_over(largest(j), 1u << a.c.shift), kQ);
-            const uint32_t unit = t + j * a.threads;
-            if (on[j] && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
-            if (on[j]) write(j, g.factor);
-        }
+        whole = group_scale(most_over_row(m, a.threads, most), q);
+        if (on_row && t == 0) scales[0] = whole.scale;
     }
-}
-
-// Any call: a row in the registers of its threads, K units each.
-template <class T, int P, int K, bool I8, int THREADS>
-__global__ void __launch_bounds__(THREADS, K == 4 ? 1 : 1024 / THREADS) quantize_rows_kernel(QuantizeArgs a) {
-    __shared__ float sums[2][2][THREADS / 32];  // (two rows' turns: a barrier of the next row stands between a read and the next write)
-    __shared__ uint32_t most[2][THREADS / 32];
-    follow();
-    const uint32_t per_cta = blockDim.x / a.threads;
-    const uint32_t t = threadIdx.x % a.threads;
-    const int64_t stride = (int64_t)gridDim.x * per_cta;
-    int64_t r = (int64_t)blockIdx.x * per_cta + threadIdx.x / a.threads;
-    int turn = 0;
-    for (int64_t base = (int64_t)blockIdx.x * per_cta; base < a.rows; base += stride, r += stride, turn ^= 1) {
-        const bool on = r < a.rows;
-        int col[K], count[K];
-        Eight<T> x[K], y[K];
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            col[j] = (int)columns_of(a.c, t + j * a.threads, count[j]);
-            if (!on || !ROBE_CHK(col[j] + count[j] <= a.c.d || count[j] == 0, ROBE_DBG_ROW_POS)) count[j] = 0;
-            if (count[j] > 0) load_eight<T, P>(x[j], (const T*)a.x.p + r * a.x.ld + col[j], count[j]);
+    for (int j = 0; j < K; ++j) {
+        GroupScale g = whole;
+        if (!a.c.whole) {
+            g = group_scale(most_over(largest(j), 1u << a.c.shift), q);
+            const uint32_t unit = t + j * a.threads;
+            if (count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
         }
-        if (a.residual.p != nullptr) {
+        if (count[j] == 0) continue;
+        float c[8];
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (count[j] > 0) load_eight<T, P>(y[j], (const T*)a.residual.p + r * a.residual.ld + col[j], count[j]);
+        for (int k = 0; k < 4; ++k) {
+            const float2 p = mul2(v[j][k], both(g.factor));
+            c[2 * k] = p.x;
+            c[2 * k + 1] = p.y;
         }
-        float v[K][8];
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[j][k] = count[j] == 0 ? 0.0f : a.residual.p != nullptr ? fmaf(a.scale, x[j].get(k), y[j].get(k)) : a.scale * x[j].get(k);
-            }
-        if (a.out.p != nullptr) {
-#pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (count[j] > 0) store_eight<T, P>(v[j], (T*)a.out.p + r * a.out.ld + col[j], count[j]);
+        uint32_t low, high;
+        if (i8) {
+            low = codes_i8(c[0], c[1], c[2], c[3]);
+            high = codes_i8(c[4], c[5], c[6], c[7]);
+        } else {
+            low = codes_e4m3(c[0], c[1], c[2], c[3]);
+            high = codes_e4m3(c[4], c[5], c[6], c[7]);
         }
-        if (a.w != nullptr) {
-            if (a.layer) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < K; ++j)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) sum += v[j][k];
-                const float mean = add_over_row(sum, a.threads, sums[turn][0]) * a.per_column;
-#pragma unroll
-                for (int j = 0; j < K; ++j)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[j][k] = k < count[j] ? v[j][k] - mean : 0.0f;
-            }
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < K; ++j)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) sum = fmaf(v[j][k], v[j][k], sum);
-            const float factor = norm_factor(fmaf(add_over_row(sum, a.threads, sums[turn][1]), a.per_column, a.eps));
-#pragma unroll
-            for (int j = 0; j < K; ++j) {
-                if (count[j] == 0) continue;
-                float w[8];
-                load_weights(w, a, col[j], count[j]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[j][k] = v[j][k] * factor * w[k];
-            }
-        }
-        uint8_t* const codes = (uint8_t*)a.codes.p + r * a.codes.ld;
-        float* const scales = (float*)a.scales.p + r * a.scales.ld;
-        GroupScale whole{};
-        if (a.c.whole) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int j = 0; j < K; ++j) m = max(m, largest_of(v[j]));
-            whole = group_scale(most_over_row(m, a.threads, most[turn]), I8 ? kLargestI8 : kLargestE4m3);
-            if (on && t == 0) scales[0] = whole.scale;
-        }
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            GroupScale g = whole;
-            if (!a.c.whole) {
-                g = group_scale(most_over(largest_of(v[j]), 1u << a.c.shift), I8 ? kLargestI8 : kLargestE4m3);
-                const uint32_t unit = t + j * a.threads;
-                if (count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
-            }
-            if (count[j] > 0) store_codes<I8>(codes + col[j], v[j], g.factor, count[j], a.code_piece);
-        }
+        if (FULL) __stcs((uint2*)(codes + col[j]), make_uint2(low, high));
+        else store_codes(codes + col[j], low, high, count[j], a.code_piece);
     }
 }
 
 // Rows of any length, a CTA each, read again for every step: statistics, the largest magnitude of a whole row, codes.
-template <class T, int P, bool I8>
+template <class T, int P>
 __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a) {
     __shared__ float sums[2][kJoinMost / 32];
     __shared__ uint32_t most[kJoinMost / 32];
@@ -476,7 +391,7 @@ __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a
                 normed(n, v, col, count);
                 m = max(m, largest_of(n));
             }
-            whole = group_scale(most_over_row(m, kJoinMost, most), I8 ? kLargestI8 : kLargestE4m3);
+            whole = group_scale(most_over_row(m, kJoinMost, most), a.i8 ? kLargestI8 : kLargestE4m3);
             if (to && threadIdx.x == 0) scales[0] = whole.scale;
         }
         // (out may be the residual itself: every element is read for the last time by the thread that then writes it)
@@ -489,10 +404,13 @@ __global__ void __launch_bounds__(kJoinMost) quantize_long_kernel(QuantizeArgs a
             if (a.out.p != nullptr && count > 0) store_eight<T, P>(v, (T*)a.out.p + r * a.out.ld + col, count);
             GroupScale g = whole;
             if (!a.c.whole) {
-                g = group_scale(most_over(largest_of(n), 1u << a.c.shift), I8 ? kLargestI8 : kLargestE4m3);
+                g = group_scale(most_over(largest_of(n), 1u << a.c.shift), a.i8 ? kLargestI8 : kLargestE4m3);
                 if (to && count > 0 && (u & ((1u << a.c.shift) - 1u)) == 0) scales[u >> a.c.shift] = g.scale;
             }
-            if (to && count > 0) store_codes<I8>(codes + col, n, g.factor, count, a.code_piece);
+            if (to && count > 0) {
+                if (a.i8) store_codes<true>(codes + col, n, g.factor, count, a.code_piece);
+                else store_codes<false>(codes + col, n, g.factor, count, a.code_piece);
+            }
         }
         __syncthreads();  // the words of the sums are read until here
     }
@@ -509,14 +427,9 @@ int piece_for(const Columns& c, int most, int64_t size, std::initializer_list<co
     return 1;
 }
 
-template <class T, int P, bool I8>
+template <class T, int P>
 cudaError_t launch_quantize(QuantizeArgs& a, bool in_registers, cudaStream_t st) {
     const uint32_t units = a.c.units;
-    if (!in_registers || units > 4 * kJoinMost) {
-        const int64_t grid = a.rows < 148 * 8 ? a.rows : 148 * 8;
-        launch_next(quantize_long_kernel<T, P, I8>, (unsigned)grid, kJoinMost, 0, st, a);
-        return cudaGetLastError();
-    }
     const int K = units <= 64 ? 1 : units <= 2 * kJoinMost ? 2 : 4;
     uint32_t threads = (units + K - 1) / K;
     if (threads <= 32) {
@@ -530,40 +443,39 @@ cudaError_t launch_quantize(QuantizeArgs& a, bool in_registers, cudaStream_t st)
     const uint32_t block = threads >= 128 ? threads : 128 / threads * threads;
     const int64_t per = block / threads;
     const int64_t ctas = (a.rows + per - 1) / per;
+    if (!in_registers || units > 4 * kJoinMost || ctas >= (1ll << 31)) {
+        const int64_t grid = a.rows < 148 * 8 ? a.rows : 148 * 8;
+        launch_next(quantize_long_kernel<T, P>, (unsigned)grid, kJoinMost, 0, st, a);
+        return cudaGetLastError();
+    }
+    auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)ctas, block, 0, st, a); };
+    auto sized = [&](auto full, auto residual, auto eight) {
+        constexpr bool F = decltype(full)::value, R = decltype(residual)::value, E = decltype(eight)::value;
+        if (K == 1) launch(quantize_rows_kernel<T, P, 1, 256, F, R, E>);
+        else if (K == 2 && block <= 256) launch(quantize_rows_kernel<T, P, 2, 256, F, R, E>);
+        else if (K == 2) launch(quantize_rows_kernel<T, P, 2, 512, F, R, E>);
+        else launch(quantize_rows_kernel<T, P, 4, 512, F, R, E>);
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
     if constexpr (P == kPiece<T>) {
-        if (a.full && K <= 2 && ctas < (1ll << 31)) {
-            auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)ctas, block, 0, st, a); };
-            if (a.residual.p != nullptr) {
-                if (K == 1) launch(quantize_full_kernel<T, 1, true, I8, 256>);
-                else if (block <= 256) launch(quantize_full_kernel<T, 2, true, I8, 256>);
-                else launch(quantize_full_kernel<T, 2, true, I8, 512>);
-            } else {
-                if (K == 1) launch(quantize_full_kernel<T, 1, false, I8, 256>);
-                else if (block <= 256) launch(quantize_full_kernel<T, 2, false, I8, 256>);
-                else launch(quantize_full_kernel<T, 2, false, I8, 512>);
-            }
+        if (full_units(a.c, a.code_piece) && (a.w == nullptr || a.w_pieces)) {
+            if (a.residual.p != nullptr) a.i8 ? sized(yes, yes, yes) : sized(yes, yes, no);
+            else a.i8 ? sized(yes, no, yes) : sized(yes, no, no);
             return cudaGetLastError();
         }
     }
-    auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)(ctas < (1ll << 30) ? ctas : 1ll << 30), block, 0, st, a); };
-    if (K == 1) launch(quantize_rows_kernel<T, P, 1, I8, 256>);
-    else if (K == 2 && block <= 256) launch(quantize_rows_kernel<T, P, 2, I8, 256>);
-    else if (K == 2) launch(quantize_rows_kernel<T, P, 2, I8, 512>);
-    else launch(quantize_rows_kernel<T, P, 4, I8, 512>);
+    sized(no, no, no);
     return cudaGetLastError();
 }
 template <class T>
-cudaError_t launch_quantize(QuantizeArgs& a, int i8, bool in_registers, cudaStream_t st) {
+cudaError_t launch_quantize(QuantizeArgs& a, bool in_registers, cudaStream_t st) {
     constexpr int kMost = kPiece<T>;
     const int piece = piece_for(a.c, kMost, sizeof(T), {&a.x, &a.residual, &a.out}, a.rows);
-    auto go = [&](auto eight) {
-        constexpr bool I8 = decltype(eight)::value;
-        if (piece == kMost) return launch_quantize<T, kMost, I8>(a, in_registers, st);
-        if (kMost == 8 && piece == 4) return launch_quantize<T, 4, I8>(a, in_registers, st);
-        if (piece == 2) return launch_quantize<T, 2, I8>(a, in_registers, st);
-        return launch_quantize<T, 1, I8>(a, in_registers, st);
-    };
-    return i8 ? go(std::true_type{}) : go(std::false_type{});
+    if (piece == kMost) return launch_quantize<T, kMost>(a, in_registers, st);
+    if (kMost == 8 && piece == 4) return launch_quantize<T, 4>(a, in_registers, st);
+    if (piece == 2) return launch_quantize<T, 2>(a, in_registers, st);
+    return launch_quantize<T, 1>(a, in_registers, st);
 }
 
 // ---------------------------------------------------------------- the cache
@@ -602,7 +514,7 @@ __device__ __forceinline__ void find_places(const CacheArgs& a, Place* places, i
     __syncthreads();
 }
 
-// FULL: groups of a power of two of eights of columns, 16-byte pieces, codes in eights (QuantizeArgs::full).
+// FULL: rows and groups of whole eights of columns, 16-byte pieces, codes in eights: a unit has eight columns or none.
 template <class T, int P, bool I8, int ITEMS, bool FULL>
 __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) {
     __shared__ Place places[kCacheRows];
@@ -620,9 +532,8 @@ __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) 
             const uint32_t t = base + i * kCodeThreads + threadIdx.x;
             row[i] = divide(t, a.units, a.magic);
             unit[i] = t - row[i] * a.units;
-            count[i] = t < items ? 8 : 0;
-            col[i] = unit[i] * 8;
-            if (!FULL && t < items) col[i] = (uint32_t)columns_of(a.cols, unit[i], count[i]);
+            count[i] = 0;
+            if (t < items) col[i] = columns_of<FULL>(a.cols, unit[i], count[i]);
             if (count[i] > 0) load_eight<T, P>(e[i], from + row[i] * a.rows.ld + col[i], FULL ? 8 : count[i]);
         }
         if (base == 0) find_places(a, places, first, rows);  // (while the rows are on their way)
@@ -764,8 +675,8 @@ cudaError_t launch_residual_quantize(const QuantizeProblem& pb, int dtype, cudaS
     a.scales = pb.scales;
     a.code_piece = piece_for(a.c, 8, 1, {&a.codes}, pb.rows);
     a.w_pieces = (uintptr_t)pb.w % 16 == 0 && a.c.group % 4 == 0;
-    a.full = full_units(a.c, a.code_piece) && (pb.w == nullptr || a.w_pieces);
-    return dtype == 0 ? launch_quantize<float>(a, pb.i8, true, st) : launch_quantize<__nv_bfloat16>(a, pb.i8, true, st);
+    a.i8 = pb.i8;
+    return dtype == 0 ? launch_quantize<float>(a, true, st) : launch_quantize<__nv_bfloat16>(a, true, st);
 }
 
 cudaError_t launch_cache_write(const CacheProblem& pb, const void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st) {
@@ -784,8 +695,9 @@ cudaError_t launch_cache_write(const CacheProblem& pb, const void* rows, int64_t
         a.scales_page = pb.scales.page_ld;
         a.code_piece = code_piece;
         a.cached = 1;
+        a.i8 = pb.i8;
         a.at = pb.at;
-        return dtype == 0 ? launch_quantize<float>(a, pb.i8, false, st) : launch_quantize<__nv_bfloat16>(a, pb.i8, false, st);
+        return dtype == 0 ? launch_quantize<float>(a, false, st) : launch_quantize<__nv_bfloat16>(a, false, st);
     }
     CacheArgs a{};
     a.c = pb;
