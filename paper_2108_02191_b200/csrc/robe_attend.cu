@@ -19,6 +19,8 @@
 // Work is split over the cache's length by what is really there: the sequences, whose lengths only the device knows, are cut
 // into spans of equal length (by every CTA for itself, or by a kernel of its own where they are many), a CTA takes a span and a
 // head of the cache in turn, and another kernel joins the spans of a sequence.
+#include <initializer_list>
+
 #include "robe_codes.cuh"
 #include "robe_internal.h"
 
@@ -744,6 +746,8 @@ size_t attend_workspace_bytes(int64_t batch, int64_t heads, int64_t q_heads, int
 cudaError_t launch_attend(const AttendProblem& pb, void* workspace, cudaStream_t st) {
     AttendArgs a;
     a.p = pb;
+    if (pb.at.num_pages == 0)  // (copies of nothing name a place all the same)
+        for (CacheRef* c : {&a.p.key_codes, &a.p.key_scales, &a.p.value_codes, &a.p.value_scales}) c->p = workspace;
     a.group = (uint32_t)(pb.q_heads / pb.heads);
     a.head_blocks = head_blocks_of(pb.heads, pb.q_heads);
     a.blocks = (uint32_t)pb.heads * a.head_blocks;

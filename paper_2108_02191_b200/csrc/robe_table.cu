@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(kTableThreads) lookup_few_kernel(LookupArgs a)
     o.template store<false>((TO*)a.out + row * a.out_ld + (uint64_t)piece * V);
 }
 
-// Many pieces: a CTA takes the ids of its rows to shared memory first, so that the latency of an id is paid once for kTiles times ITEMS
-// rows of loads (852 K rows of 128, fp32 to bf16: ids by each thread for itself 79 us, four pieces a thread under way 62, two
+// Many pieces: a CTA takes the ids of its rows to shared memory first, so that the latency of an id is paid once for kTiles rounds of
+// loads (852 K rows of 128, fp32 to bf16: ids by each thread for itself 79 us, four pieces a thread under way 62, two
 // 60).
 constexpr int kTiles = 8;
 constexpr int kLookupItems = 2;
@@ -281,7 +281,7 @@ __device__ __forceinline__ void rank_in_warp(const uint32_t (&key)[ITEMS], uint3
         rank[r] = before + __popc(below);
     }
 }
-// Exclusive scan of a value per thread of a CTA of kSortThreads; contains barriers.
+// Exclusive scan of a value per thread of a CTA of kRankThreads; contains barriers.
 constexpr int kRankThreads = 1024, kRankWarps = kRankThreads / 32;
 __device__ __forceinline__ uint32_t scan_in_cta(uint32_t v, uint32_t* warp_sums) {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;

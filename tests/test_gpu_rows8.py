@@ -25,7 +25,7 @@ def code_bytes(shape, how="plain"):
 # ---------------------------------------------------------------- quantised rows and the join
 
 GROUPS = [(1, 1, 1), (1, 8, 0), (3, 64, 32), (5, 100, 32), (2, 100, 0), (33, 128, 128), (7, 1000, 128), (4, 1001, 0), (9, 96, 96), (2, 257, 256),
-          (3, 7, 1), (6, 80, 20), (2, 4096, 128), (3, 4100, 64), (70, 513, 0), (2, 16384, 128), (1, 16400, 0), (2, 40_000, 64), (2, 20_001, 5)]
+          (3, 7, 1), (6, 80, 20), (700, 104, 0), (5, 1000, 40), (64, 24, 24), (2, 4096, 128), (3, 4100, 64), (70, 513, 0), (2, 16384, 128), (1, 16400, 0), (2, 40_000, 64), (2, 20_001, 5)]
 
 
 @pytest.mark.parametrize("how", ["plain", "slice", "odd"])
@@ -200,7 +200,7 @@ def sequences(lengths, page_rows, starts, seed, spare=2):
 
 CASES = [([1], [0], 1, 8, 8), ([1, 1, 1], [5, 0, 17], 4, 64, 32), ([7, 0, 130, 1], [0, 3, 60, 9], 16, 256, 64), ([40, 3], [0, 1], 3, 100, 32),
          ([65, 64, 63], [1, 0, 2], 64, 160, 80), ([5, 6], [0, 0], 5, 1001, 0), ([30], [2], 16, 192, 96), ([9, 9], [7, 8], 8, 1024, 128), ([3, 4], [0, 0], 2, 20, 1),
-         ([300, 200], [0, 0], 32, 512, 256), ([12], [0], 16, 300, 0)]
+         ([300, 200], [0, 0], 32, 512, 256), ([12], [0], 16, 300, 0), ([3000, 0, 2500], [5, 1, 0], 64, 128, 64), ([2000], [0], 16, 1024, 128)]
 
 
 @pytest.mark.parametrize("how", ["plain", "pair", "odd"])
@@ -271,6 +271,23 @@ def test_cache_rows_without_a_place(group, equal):
         else:
             assert torch.equal(out[r].cpu(), back[r])
     assert {-1} <= {p for p in at if p < 0} and (equal or -2 in at)
+
+
+def test_cache_of_many_short_sequences():
+    # sequences of no rows between others, several to a block of rows, and a long one among them
+    lengths = [k * k % 4 * (k % 3) for k in range(1500)] + [700] + [0] * 500 + [1] * 40
+    pages, num, offsets = sequences(lengths, 4, [k % 5 for k in range(len(lengths))], 3)
+    starts = torch.tensor([k % 5 for k in range(len(lengths))])
+    n, d = int(offsets[-1]), 64
+    rows = torch.randn(n, d, generator=gen(1)).bfloat16()
+    cache = Cache(num, 4, d, 32, torch.int8)
+    robe.robe_cache_write(rows.cuda(), cache.codes, cache.scales, pages.cuda(), offsets.cuda(), starts.cuda(), 32)
+    at = torch.tensor(ref.places(pages, 4, num, n, offsets.tolist(), starts.tolist()))
+    codes, scales = ref.quantize(rows, 32, torch.int8)
+    assert torch.equal(cache.bytes.cpu().reshape(-1, d)[at], codes) and torch.equal(cache.scales.cpu().reshape(-1, 2)[at], scales)
+    out = blank((n, d), torch.float32)
+    robe.robe_cache_read(cache.codes, cache.scales, pages.cuda(), out, offsets.cuda(), starts.cuda(), 32)
+    assert torch.equal(out.cpu(), ref.values(codes, scales, 32, torch.int8).float())
 
 
 def test_cache_of_nothing():
@@ -366,7 +383,7 @@ def run_attention(made, pages, q, starts, heads, scale, bias=None, bias_rows=Non
     return out.cpu()
 
 
-ATTEND = [([1], 1, 1, 32, 1), ([1, 2, 15], 2, 4, 64, 16), ([16, 17, 33, 100], 4, 2, 128, 16), ([70, 300], 1, 8, 96, 64), ([257, 5, 64], 2, 16, 128, 7),
+ATTEND = [([1], 1, 1, 32, 1), ([256, 257], 1, 3, 64, 16), ([40] * 300, 1, 2, 32, 8), ([1, 2, 15], 2, 4, 64, 16), ([16, 17, 33, 100], 4, 2, 128, 16), ([70, 300], 1, 8, 96, 64), ([257, 5, 64], 2, 16, 128, 7),
           ([130], 2, 5, 256, 32), ([63, 65], 1, 16, 256, 64), ([500, 1, 129], 3, 12, 64, 128), ([1000], 1, 20, 96, 100), ([2049, 700], 2, 8, 128, 64),
           ([5000], 1, 33, 32, 1), ([3000, 4000], 8, 1, 128, 64)]
 
@@ -412,6 +429,20 @@ def test_attention_of_short_lengths_in_a_long_table_and_of_no_keys():
     for s, n in ((0, 40), (2, 151)):
         for h in range(8):
             attention_close(out[s, h], q[s, h], made["keys_rows"][s][:n, h // 4], made["values_rows"][s][:n, h // 4], 0.1, None, KINDS[0])
+
+
+@pytest.mark.parametrize("batch", [3, 300])
+def test_attention_over_a_cache_without_pages_and_of_no_keys_at_all(batch):
+    cache = Cache(2, 16, 64, 64, KINDS[0])
+    empty = dict(keys=type(cache).__new__(Cache), values=None)
+    empty["keys"].codes, empty["keys"].scales = cache.codes[:0], cache.scales[:0]
+    empty["values"] = empty["keys"]
+    pages = torch.zeros(batch, 40, dtype=torch.int32)
+    q = torch.ones(batch, 4, 64, dtype=torch.bfloat16)
+    out = run_attention(empty, pages, q, [600] * batch, 1, 0.1)
+    assert torch.equal(out, torch.zeros_like(out))
+    out = run_attention(dict(keys=cache, values=cache), pages, q, [-1] * batch, 1, 0.1)
+    assert torch.equal(out, torch.zeros_like(out))
 
 
 def test_attention_leaves_out_positions_without_a_place():

@@ -38,7 +38,7 @@ def ids_of(kind, n, vocab, seed=0):
 @pytest.mark.parametrize("table_type", TYPES)
 @pytest.mark.parametrize("out_type", TYPES)
 @pytest.mark.parametrize("n,vocab,d", [(1, 1, 1), (1, 5, 4096), (16, 1000, 64), (37, 50, 7), (129, 30, 100), (1000, 11, 12), (3, 9, 1001),
-                                       (5000, 400, 128), (2, 3, 8200)])
+                                       (5000, 400, 128), (2, 3, 8200), (41_000, 900, 128), (7001, 300, 101), (700_001, 40, 1)])
 def test_lookup(n, vocab, d, table_type, out_type, how):
     table = torch.randn(vocab, d, generator=gen(d)).to(table_type)
     ids = ids_of("outside" if n > 2 else "uniform", n, vocab)
@@ -98,6 +98,9 @@ def whole(n, d, most, seed, dtype):
 
 SIZES = [(1, 1, 1), (1, 3, 64), (2, 2, 3), (15, 4, 8), (16, 4, 8), (17, 4, 8), (33, 700, 100), (64, 5, 1001), (257, 2, 130), (1000, 300, 7),
          (4096, 100, 16), (5003, 2000, 36), (300, 4, 4100), (20_000, 3, 5), (3000, 70_000, 12)]
+# around the sizes at which the ids are sorted in another way, and with runs of many chunks
+SORTS = [(512, 600, 9), (513, 600, 9), (1024, 2, 4), (1025, 40_000, 4), (8192, 7, 8), (8193, 300, 8), (16_385, 5000, 3), (32_768, 2**20, 2), (32_769, 90, 4),
+         (65_536, 1, 4), (65_537, 20, 4), (70_001, 3000, 8), (200_000, 2, 6)]
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
@@ -116,6 +119,13 @@ def test_gradient_of_whole_numbers(n, vocab, d, kind, dtype, how, accumulate):
     s, _ = ref.table_sums(grad, ids, vocab)
     want = (0.5 * s + (old.double() if accumulate else 0.0)).float()
     assert torch.equal(table.cpu(), want) and surroundings_kept(table) and ws.kept_within()
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["uniform", "same", "few", "outside"])
+@pytest.mark.parametrize("n,vocab,d", SORTS)
+def test_gradient_of_many_ids(n, vocab, d, kind, accumulate):
+    test_gradient_of_whole_numbers(n, vocab, d, kind, torch.bfloat16, "plain", accumulate)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
