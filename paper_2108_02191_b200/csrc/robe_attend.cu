@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     constexpr int T = kTile<DIM>, S = kStages;
     constexpr uint32_t kStep = T * kAttendWarps;
     constexpr float kLog2e = 1.4426950408889634f;
+    constexpr float kMostFinite = 3.4028234663852886e38f;
     constexpr float kLeastScale = 7.8886090522101181e-31f;  // 2^-100: keys whose values have no scale count in the divisor too
     extern __shared__ __align__(128) uint8_t memory[];
     AttendSmem<DIM>& sm = *(AttendSmem<DIM>*)memory;
@@ -372,7 +373,9 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
 
         for (uint32_t k = threadIdx.x; k < side * kHeads; k += kAttendThreads) {
             const uint32_t b = k / kHeads, h = k % kHeads;
-            sm.bias[b][h] = h < in_block ? __ldca(a.p.bias + b * a.p.bias_ld + head * a.group + q0 + h) * kLog2e : 0.0f;
+            const float v = h < in_block ? __ldca(a.p.bias + b * a.p.bias_ld + head * a.group + q0 + h) : 0.0f;
+            // (what is finite stays finite: where all keys have the type's lowest value they count alike, where all have -inf none does)
+            sm.bias[b][h] = fabsf(v) < INFINITY ? fminf(fmaxf(v * kLog2e, -kMostFinite), kMostFinite) : v;
         }
         // queries: rows g and g + 8 of the instruction's first operand
         const bool q_pieces = ((uintptr_t)a.p.q.p | (uint64_t)a.p.q.ld * 2) % 8 == 0;
@@ -456,6 +459,11 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
                              pair_in_word<I8>(c, 1));
                 }
             }
+            // the last bucket's bias, or none yet (a bias may be infinite: what is added cannot be taken away again)
+            const bool far = key0 < far_until;
+            float first_bias[N];
+#pragma unroll
+            for (int b = 0; b < N; ++b) first_bias[b] = far ? far_bias[b] : 0.0f;
             float value_scale[T / 8][2], value_log[T / 8][2];
 #pragma unroll
             for (int u = 0; u < T / 8; ++u) {
@@ -471,11 +479,11 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
 #pragma unroll
                     for (int b = 0; b < N; ++b) {
                         float& x = s[u][2 * b + k];
-                        x = in ? x * __uint_as_float(k2[k]) * q_factor[b] + far_bias[b] : -INFINITY;
+                        x = in ? x * __uint_as_float(k2[k]) * q_factor[b] + first_bias[b] : -INFINITY;
                     }
                 }
             }
-            if (key0 >= far_until) {
+            if (!far) {
                 const int64_t d = pos - (int64_t)(key0 + lane % T);
                 uint32_t bucket = 0;
                 for (uint32_t hi = side; hi - bucket > 1;) {
@@ -488,8 +496,9 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const uint32_t of = __shfl_sync(0xFFFFFFFFu, bucket, 8 * u + 2 * t + k);
+                        if (!(here >> (8 * u + 2 * t + k) & 1)) continue;
 #pragma unroll
-                        for (int b = 0; b < N; ++b) s[u][2 * b + k] += sm.bias[of][b * 8 + g] - far_bias[b];
+                        for (int b = 0; b < N; ++b) s[u][2 * b + k] += sm.bias[of][b * 8 + g];
                     }
             }
             uint32_t weights[N][T / 8];

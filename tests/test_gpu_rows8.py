@@ -431,6 +431,71 @@ def test_attention_of_short_lengths_in_a_long_table_and_of_no_keys():
             attention_close(out[s, h], q[s, h], made["keys_rows"][s][:n, h // 4], made["values_rows"][s][:n, h // 4], 0.1, None, KINDS[0])
 
 
+def mean_close(got, v, kind):
+    """Equal weights: value scales here stay above 2^-14, so that a weight is off by 2^-11 of it, and the result by its own rounding."""
+    assert float(v.abs().amax(1).min()) / 448 > 2.0 ** -14
+    out = v.mean(0)
+    assert ((got.double() - out).abs() <= 2.0 ** -8 * out.abs() + (2.0 ** -11 + 2.0 ** -18) * (1 + 2.0 ** -8) * v.abs().mean(0) + 2.0 ** -130).all()
+
+
+@pytest.mark.parametrize("lengths", [[1, 20, 33, 700], [5000], [40, 0] * 150], ids=["some", "one", "many"])
+@pytest.mark.parametrize("open_buckets", [range(0, 1), range(0, 16), range(16, 31), range(31, 32), range(3, 32, 5), range(0)])
+def test_attention_with_buckets_masked_by_infinities(lengths, open_buckets):
+    # keys whose bias is -inf do not count, wherever they stand; where none counts the result is +0
+    heads, group, buckets = 2, 2, 32
+    made, pages, q, bias_rows = attention_case(lengths, heads, group, 64, 16, KINDS[0], buckets, 8)
+    closed = [b for b in range(buckets) if b not in open_buckets]
+    bias_rows[closed] = -math.inf
+    bias = robe.robe_bias_create(buckets, 100, False)
+    out = run_attention(made, pages, q, [n - 1 for n in lengths], heads, 0.1, bias, bias_rows)
+    robe.robe_bias_destroy(bias)
+    for s, n in list(enumerate(lengths))[:8]:
+        index = torch.tensor([rowref.bucket(j - (n - 1), buckets, 100, False) for j in range(n)], dtype=torch.int64)
+        seen = torch.tensor([int(i) in open_buckets for i in index], dtype=torch.bool)
+        for h in range(heads * group):
+            k, v = made["keys_rows"][s][seen, h // group], made["values_rows"][s][seen, h // group]
+            if k.shape[0] == 0:
+                assert torch.equal(out[s, h], torch.zeros(64, dtype=torch.bfloat16))
+            else:
+                attention_close(out[s, h], q[s, h], k, v, 0.1, bias_rows[:, h].double()[index[seen]], KINDS[0])
+
+
+@pytest.mark.parametrize("length", [7, 40, 900])
+@pytest.mark.parametrize("open_buckets", [range(0, 2), range(2, 31), range(31, 32), range(0)])
+def test_attention_with_buckets_of_the_lowest_value(length, open_buckets):
+    # next to any other bias the type's lowest value is a mask; alone it takes all keys alike
+    buckets = 32
+    made, pages, q, bias_rows = attention_case([length], 1, 3, 128, 16, KINDS[0], buckets, 4)
+    bias_rows[[b for b in range(buckets) if b not in open_buckets]] = torch.finfo(torch.float32).min
+    bias = robe.robe_bias_create(buckets, 100, False)
+    out = run_attention(made, pages, q, [length - 1], 1, 0.1, bias, bias_rows)
+    robe.robe_bias_destroy(bias)
+    index = torch.tensor([rowref.bucket(j - (length - 1), buckets, 100, False) for j in range(length)])
+    seen = torch.tensor([int(i) in open_buckets for i in index])
+    for h in range(3):
+        k, v = made["keys_rows"][0][:, 0], made["values_rows"][0][:, 0]
+        if seen.any():
+            attention_close(out[0, h], q[0, h], k[seen], v[seen], 0.1, bias_rows[:, h].double()[index[seen]], KINDS[0])
+        else:
+            mean_close(out[0, h], v, KINDS[0])
+
+
+def test_attention_does_not_read_the_bias_of_positions_without_a_place():
+    # the only key of bucket 3 has no page; its bias is no number
+    buckets, lengths = 32, [60]
+    made, pages, q, bias_rows = attention_case(lengths, 1, 2, 64, 1, KINDS[0], buckets, 5)
+    bias_rows[3] = NAN
+    pages[0, 60 - 1 - 3] = -1
+    bias = robe.robe_bias_create(buckets, 100, False)
+    out = run_attention(made, pages, q, [59], 1, 0.1, bias, bias_rows)
+    robe.robe_bias_destroy(bias)
+    index = torch.tensor([rowref.bucket(j - 59, buckets, 100, False) for j in range(60)])
+    seen = index != 3
+    assert int((~seen).sum()) == 1
+    for h in range(2):
+        attention_close(out[0, h], q[0, h], made["keys_rows"][0][seen, 0], made["values_rows"][0][seen, 0], 0.1, bias_rows[:, h].double()[index[seen]], KINDS[0])
+
+
 @pytest.mark.parametrize("batch", [3, 300])
 def test_attention_over_a_cache_without_pages_and_of_no_keys_at_all(batch):
     cache = Cache(2, 16, 64, 64, KINDS[0])
