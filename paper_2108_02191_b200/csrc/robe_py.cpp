@@ -262,7 +262,7 @@ struct Reader {
         if (!ok) return c;
         const Paged k = paged(codes), s = paged(scales);
         if (!ok) return c;
-        if (group < 0 || s.pages != k.pages || s.rows != k.rows || s.cols != (group == 0 ? 1 : (k.cols + group - 1) / group)) ok = false;
+        if (group < 0 || s.pages != k.pages || s.rows != k.rows || s.cols != (group == 0 ? 1 : k.cols / group + (k.cols % group != 0))) ok = false;
         if (pages->size(1) > 1 && pages->stride(1) != 1) ok = false;
         c.codes = k.p;
         c.codes_ld = k.ld;
