@@ -70,6 +70,72 @@ __device__ __forceinline__ void store_eight(const float (&v)[8], T* p, int count
             if (k < count) p[k] = narrow<T>(v[k]);
     }
 }
+// Eight elements of E bytes to an address that is no multiple of a piece: pieces are of what two lanes have, each lane stores the one that
+// ends among its own, and single elements are left at the ends of rows and warps.  The whole warp calls it.  count: of the lane,
+// chained: this lane and the one before have eight each that follow one another; given: this lane and the next.
+template <int E>
+__device__ __forceinline__ void store_chain(uint8_t* p, const uint32_t (&w)[2 * E], int count, bool chained, bool given) {
+    constexpr int N = 2 * E, PB = N >= 4 ? 16 : 8, PW = PB / 4;
+    const uint32_t off = (uint32_t)(uintptr_t)p & (PB - 1u);
+    uint32_t c[PW + N + 1];  // the last piece of the lane before, the lane's own
+#pragma unroll
+    for (int k = 0; k < PW; ++k) c[k] = __shfl_up_sync(0xFFFFFFFFu, w[N - PW + k], 1);
+#pragma unroll
+    for (int k = 0; k < N; ++k) c[PW + k] = w[k];
+    c[PW + N] = 0;
+    // from `PB - off` bytes on; off = 0: the lane's own
+    const uint32_t skip = PB - off;
+    uint32_t o[PW + N];
+    if (PW == 4) {
+#pragma unroll
+        for (int k = 0; k + 4 < PW + N + 1; ++k) c[k] = skip & 16 ? c[k + 4] : c[k];
+#pragma unroll
+        for (int k = 0; k + 2 < PW + N + 1; ++k) c[k] = skip & 8 ? c[k + 2] : c[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k + 2 < PW + N + 1; ++k) c[k] = skip & 8 ? c[k + 2] : c[k];
+    }
+#pragma unroll
+    for (int k = 0; k + 1 < PW + N + 1; ++k) c[k] = skip & 4 ? c[k + 1] : c[k];
+#pragma unroll
+    for (int k = 0; k < N; ++k) o[k] = E == 4 ? c[k] : __funnelshift_r(c[k], c[k + 1], (skip & 3) * 8);
+    const bool own = off == 0;
+    if (count == 8) {
+#pragma unroll
+        for (int q = 0; q < N / PW; ++q) {
+            if (q == 0 && !own && !chained) continue;
+            if (PW == 4) *(uint4*)(p - off + q * 16) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+            else *(uint2*)(p - off) = make_uint2(o[0], o[1]);
+        }
+    }
+    // elements before the first piece of the lane's own, behind its last, or all of a few
+    const uint32_t head = own || chained ? 0 : skip, tail = own || given ? 8 * E : 8 * E - off;
+    if (count > 0 && (count < 8 ? true : head > 0 || tail < 8 * E)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < count && (count < 8 || k * E < (int)head || k * E >= (int)tail)) {
+                if (E == 4) *(uint32_t*)(p + 4 * k) = w[k];
+                else if (E == 2) *(uint16_t*)(p + 2 * k) = (uint16_t)(w[k / 2] >> (16 * (k % 2)));
+                else p[k] = (uint8_t)(w[k / 4] >> (8 * (k % 4)));
+            }
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_chain(const float (&v)[8], T* p, int count, bool chained, bool given) {
+    uint32_t w[2 * sizeof(T)];
+#pragma unroll
+    for (int k = 0; k < 2 * (int)sizeof(T); ++k) {
+        if constexpr (sizeof(T) == 4) {
+            w[k] = __float_as_uint(v[k]);
+        } else {
+            Pack<T, 2> e;
+            e.v[0] = narrow<T>(v[2 * k]);
+            e.v[1] = narrow<T>(v[2 * k + 1]);
+            w[k] = *(const uint32_t*)&e;
+        }
+    }
+    store_chain<(int)sizeof(T)>((uint8_t*)p, w, count, chained, given);
+}
 // eight codes, by pieces of `piece` bytes
 __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t low, uint32_t high, int count, int piece) {
     if (count == 8 && piece == 8) {
@@ -134,6 +200,7 @@ struct QuantizeArgs {
     const float* w;
     RowsRef x, residual, out, codes, scales;
     int code_piece, w_pieces;
+    int chain;  // units follow one another in rows of many (store_chain)
     int i8;
     uint32_t threads;  // of a row
     // a cache takes the codes: rows of the call lie where `at` says
@@ -202,7 +269,7 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t threads, 
 }
 
 // A row in the registers of its threads, K units each; two operations in one instruction.  What hides the loads' latency is CTAs, not
-// rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 87 us; elements one by one 117, bound by instructions; 252
+// rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 91 us; elements one by one 117, bound by instructions; 252
 // with two CTAs an SM that asked for the next row.)
 // FULL: as columns_of has it, in 16-byte pieces and codes in eights, RESIDUAL and I8 known; otherwise these are asked for.
 template <class T, int P, int K, int THREADS, bool FULL, bool RESIDUAL, bool I8>
@@ -230,6 +297,16 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
         if (count[j] > 0) load_eight<T, P>(x[j], from + col[j], FULL ? 8 : count[j]);
         if (joined && count[j] > 0) load_eight<T, P>(y[j], beside + col[j], FULL ? 8 : count[j]);
     }
+    bool chained[K], given[K];  // (store_chain)
+    if (P == 1) {
+        const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, count[j] == 8 ? col[j] + 8 : 0u, 1);
+            chained[j] = lane > 0 && t > 0 && count[j] == 8 && before == col[j];
+            given[j] = __shfl_down_sync(0xFFFFFFFFu, chained[j], 1) && lane < 31;
+        }
+    }
     float2 v[K][4];  // (zeros behind the unit's columns)
 #pragma unroll
     for (int j = 0; j < K; ++j)
@@ -244,8 +321,10 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
     if (a.out.p != nullptr) {
         T* to = (T*)a.out.p + r * a.out.ld;
 #pragma unroll
-        for (int j = 0; j < K; ++j)
-            if (count[j] > 0) store_eight<T, P>((const float(&)[8])v[j], to + col[j], FULL ? 8 : count[j]);
+        for (int j = 0; j < K; ++j) {
+            if (P == 1 && a.chain) store_chain<T>((const float(&)[8])v[j], to + col[j], count[j], chained[j], given[j]);
+            else if (count[j] > 0) store_eight<T, P>((const float(&)[8])v[j], to + col[j], FULL ? 8 : count[j]);
+        }
     }
     if (a.w != nullptr) {
         float2 sum = both(0.0f);
@@ -303,7 +382,7 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
             const uint32_t unit = t + j * a.threads;
             if (count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
         }
-        if (count[j] == 0) continue;
+        if (P > 1 && count[j] == 0) continue;
         float c[8];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -320,7 +399,12 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
             high = codes_e4m3(c[4], c[5], c[6], c[7]);
         }
         if (FULL) __stcs((uint2*)(codes + col[j]), make_uint2(low, high));
-        else store_codes(codes + col[j], low, high, count[j], a.code_piece);
+        else if (P > 1 || !a.chain || a.code_piece >= 4) {
+            if (count[j] > 0) store_codes(codes + col[j], low, high, count[j], a.code_piece);
+        } else {
+            const uint32_t words[2] = {low, high};
+            store_chain<1>(codes + col[j], words, count[j], chained[j], given[j]);
+        }
     }
 }
 
@@ -674,6 +758,9 @@ cudaError_t launch_residual_quantize(const QuantizeProblem& pb, int dtype, cudaS
     a.codes = pb.codes;
     a.scales = pb.scales;
     a.code_piece = piece_for(a.c, 8, 1, {&a.codes}, pb.rows);
+    // (20 M elements bf16 in rows of 257 / 401 / 505 / 961 / 4099, element by element -> chained: 91 -> 106, 75 -> 75, 71 -> 61, 75 -> 61, 91 ->
+    // 65 us; fp32 505 / 4099 43 -> 35, 103 -> 73)
+    a.chain = a.c.units >= 64 && (a.c.group % 8 == 0 || pb.group == pb.d);
     a.w_pieces = (uintptr_t)pb.w % 16 == 0 && a.c.group % 4 == 0;
     a.i8 = pb.i8;
     return dtype == 0 ? launch_quantize<float>(a, true, st) : launch_quantize<__nv_bfloat16>(a, true, st);

@@ -25,7 +25,8 @@ def code_bytes(shape, how="plain"):
 # ---------------------------------------------------------------- quantised rows and the join
 
 GROUPS = [(1, 1, 1), (1, 8, 0), (3, 64, 32), (5, 100, 32), (2, 100, 0), (33, 128, 128), (7, 1000, 128), (4, 1001, 0), (9, 96, 96), (2, 257, 256),
-          (3, 7, 1), (6, 80, 20), (700, 104, 0), (5, 1000, 40), (64, 24, 24), (2, 4096, 128), (3, 4100, 64), (70, 513, 0), (2, 16384, 128), (1, 16400, 0), (2, 40_000, 64), (2, 20_001, 5)]
+          (3, 7, 1), (6, 80, 20), (700, 104, 0), (5, 1000, 40), (64, 24, 24), (2, 4096, 128), (3, 4100, 64), (70, 513, 0), (2, 16384, 128), (1, 16400, 0), (2, 40_000, 64), (2, 20_001, 5),
+          (4, 505, 64), (5, 961, 0), (2, 4099, 8), (3, 9001, 128), (2, 777, 16), (6, 519, 256)]
 
 
 @pytest.mark.parametrize("how", ["plain", "slice", "odd"])
@@ -82,7 +83,7 @@ def join_tolerance(d):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,d,group,how", [(1, 1, 0, "plain"), (3, 64, 32, "plain"), (5, 100, 0, "odd"), (300, 128, 128, "plain"), (7, 1000, 128, "slice"),
                                               (4, 1001, 0, "plain"), (2, 257, 100, "odd"), (2000, 40, 0, "plain"), (3, 4096, 128, "plain"),
-                                              (40, 5120, 64, "plain"), (2, 16384, 128, "plain"), (2, 16400, 0, "slice"), (2, 40_000, 64, "plain")])
+                                              (40, 5120, 64, "plain"), (6, 505, 64, "plain"), (5, 961, 0, "odd"), (3, 4099, 8, "plain"), (3, 9001, 128, "slice"), (2, 16384, 128, "plain"), (2, 16400, 0, "slice"), (2, 40_000, 64, "plain")])
 def test_join_with_a_norm_in_8_bits(rows, d, group, how, dtype, kind, layer):
     # numbers in steps of 1/64: the sum is exact, so `out` is known to the bit
     x = (torch.randn(rows, d, generator=gen(d)) * 64).round() / 64
@@ -116,7 +117,7 @@ def test_join_with_a_norm_in_8_bits(rows, d, group, how, dtype, kind, layer):
         assert ((back - normed).abs() <= half * (1 + 2.0 ** -20) + 2 * off + 2.0 ** -22 * normed.abs()).all()
 
 
-@pytest.mark.parametrize("rows,d", [(50, 128), (3, 4096), (2, 20_000)])
+@pytest.mark.parametrize("rows,d", [(50, 128), (3, 4096), (2, 20_000), (40, 1001), (9, 4099)])
 def test_join_in_place(rows, d):
     x, residual, w = torch.randn(rows, d, generator=gen(1)).cuda(), torch.randn(rows, d, generator=gen(2)).cuda(), torch.ones(d, device="cuda")
     def call(residual, out):
