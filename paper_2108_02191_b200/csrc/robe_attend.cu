@@ -55,6 +55,7 @@ struct AttendArgs {
     uint32_t group;        // query heads per head of the cache
     uint32_t rows;         // query heads of the largest block
     uint32_t ctas;         // that spans are made for, at most kAttendCtas
+    float share;           // of a CTA in a key of all: blocks / ctas, and a little more
     uint32_t page_magic, page_shift;  // key / page_rows = (key * magic >> 32) >> shift, for pages of more than one row
     uint32_t positions;    // that the page table has room for
     uint32_t code_page, code_ld;    // pieces of 16 bytes
@@ -64,8 +65,22 @@ struct AttendArgs {
     float* parts;     // [spans x blocks][rows][dim + 4]
 };
 
+// The spans' length and 2^7 over it, for counting them.  (Divisions by what only the device knows are what a plan would spend its time
+// on, so each is one product and a step of correction.)
+struct SpanLength {
+    uint32_t span;
+    float per_step;
+};
+__device__ __forceinline__ SpanLength span_length(uint32_t span) { return SpanLength{span, __frcp_rn((float)(span / kSpanStep))}; }
 // spans of a sequence: one for a sequence without keys, too, whose results are +0
-__device__ __forceinline__ uint32_t spans_of(uint32_t length, uint32_t span) { return length > span ? (length + span - 1) / span : 1; }
+__device__ __forceinline__ uint32_t spans_of(uint32_t length, const SpanLength& s) {
+    if (length <= s.span) return 1;
+    const uint32_t steps = (length - 1) / kSpanStep, each = s.span / kSpanStep;  // (below 2^24: exact as fp32)
+    uint32_t full = (uint32_t)((float)steps * s.per_step);
+    const int left = (int)(steps - full * each);
+    full = left < 0 ? full - 1 : left >= (int)each ? full + 1 : full;
+    return full + 1;
+}
 // keys of a sequence whose new token stands at pos
 __device__ __forceinline__ uint32_t length_at(const AttendArgs& a, int64_t pos) {
     return pos < 0 ? 0 : pos >= (int64_t)a.positions ? a.positions : (uint32_t)pos + 1;
@@ -74,54 +89,53 @@ __device__ __forceinline__ uint32_t length_of(const AttendArgs& a, int64_t n) {
     return length_at(a, __ldca(a.p.at.starts + n));
 }
 
-// length of the spans for that many keys in all
+// Length of the spans for that many keys in all: no less than a CTA's share, or what a share is cut into, which fp32 takes up by 2^-20 of it.
 __device__ __forceinline__ uint32_t span_of(const AttendArgs& a, unsigned long long keys) {
-    const unsigned long long each = (keys * a.blocks + a.ctas - 1) / a.ctas;
-    unsigned long long many = each < kSpanMany ? 1 : each / kSpanLong;
-    many = many < kSpansPerCta ? many : kSpansPerCta;
-    const unsigned long long span = ((each + many - 1) / many + kSpanStep - 1) / kSpanStep * kSpanStep;
-    return span < kSpanLeast ? kSpanLeast : (uint32_t)span;
+    const float share = (float)keys * a.share + 1.0f;
+    const float many = share < (float)kSpanMany ? 1.0f : fminf(floorf(share * (1.0f / kSpanLong)), (float)kSpansPerCta);
+    const float span = share * __frcp_ru(many) + 1.0f;
+    const uint32_t length = span < 2147483648.0f ? (uint32_t)span : 1u << 31;  // (longer than any sequence)
+    return length < kSpanLeast ? kSpanLeast : (length + kSpanStep - 1) / kSpanStep * kSpanStep;
 }
 // The plan of a call of at most kPlanWarp sequences, by the CTA's first warp: first[0 .. batch] and behind them the spans' length; where the
-// new tokens stand.
+// new tokens stand.  Lane l has the sequences l, l + 32 and so on.
 __device__ __forceinline__ void plan_in_cta(const AttendArgs& a, uint32_t* first, int64_t* stands) {
     constexpr uint32_t kEach = kPlanWarp / 32;
-    if (threadIdx.x < 32) {
-        const uint32_t batch = (uint32_t)a.p.at.batch, n0 = threadIdx.x * kEach;
-        uint32_t length[kEach];
-        unsigned long long keys = 0;
+    const uint32_t batch = (uint32_t)a.p.at.batch, lane = threadIdx.x;
+    uint32_t length[kEach], low = 0, high = 0;
 #pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k) {
-            length[k] = 0;
-            if (n0 + k < batch) {
-                stands[n0 + k] = __ldca(a.p.at.starts + n0 + k);
-                length[k] = length_at(a, stands[n0 + k]);
-            }
-            keys += length[k];
+    for (uint32_t k = 0; k < kEach; ++k) {
+        length[k] = 0;
+        if (k * 32 + lane < batch) {
+            const int64_t pos = __ldca(a.p.at.starts + k * 32 + lane);
+            stands[k * 32 + lane] = pos;
+            length[k] = length_at(a, pos);
         }
-        for (int o = 16; o > 0; o >>= 1) keys += __shfl_xor_sync(0xFFFFFFFFu, keys, o);
-        const uint32_t span = span_of(a, keys);
-        uint32_t mine = 0;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k) {
-            length[k] = n0 + k < batch ? spans_of(length[k], span) : 0;
-            mine += length[k];
-        }
-        uint32_t before = mine;
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, before, o);
-            if (threadIdx.x >= (uint32_t)o) before += b;
-        }
-        before -= mine;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k) {
-            if (n0 + k <= batch) first[n0 + k] = before;
-            before += length[k];
-        }
-        if (threadIdx.x == 31 && batch == kPlanWarp) first[batch] = before;
-        if (threadIdx.x == 0) first[kPlanWarp + 1] = span;
     }
-    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) {
+        low += length[k] & 0xFFFFu;
+        high += length[k] >> 16;
+    }
+    const unsigned long long keys = __reduce_add_sync(0xFFFFFFFFu, low) + ((unsigned long long)__reduce_add_sync(0xFFFFFFFFu, high) << 16);
+    const SpanLength s = span_length(span_of(a, keys));
+    uint32_t before = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) {
+        if (k * 32 >= batch) break;
+        const uint32_t spans = k * 32 + lane < batch ? spans_of(length[k], s) : 0;
+        uint32_t sum = spans;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= (uint32_t)o) sum += b;
+        }
+        if (k * 32 + lane < batch) first[k * 32 + lane + 1] = before + sum;
+        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    if (lane == 0) {
+        first[0] = 0;
+        first[kPlanWarp + 1] = s.span;
+    }
 }
 
 __global__ void __launch_bounds__(kPlanThreads) attend_plan_kernel(AttendArgs a) {
@@ -139,11 +153,11 @@ __global__ void __launch_bounds__(kPlanThreads) attend_plan_kernel(AttendArgs a)
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
     if (threadIdx.x % 32 == 0) atomicAdd(&keys, mine);  // (whole numbers: the order does not matter)
     __syncthreads();
-    const uint32_t span = span_of(a, keys);
-    if (threadIdx.x == 0) a.plan->span = span;
+    const SpanLength s = span_length(span_of(a, keys));
+    if (threadIdx.x == 0) a.plan->span = s.span;
     for (int64_t base = 0; base < a.p.at.batch; base += kPlanThreads) {
         const int64_t n = base + threadIdx.x;
-        const uint32_t v = n < a.p.at.batch ? spans_of(length_of(a, n), span) : 0;
+        const uint32_t v = n < a.p.at.batch ? spans_of(length_of(a, n), s) : 0;
         uint32_t sum = v;
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t b = __shfl_up_sync(0xFFFFFFFFu, sum, o);
@@ -288,15 +302,17 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     AttendSmem<DIM>& sm = *(AttendSmem<DIM>*)memory;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     follow();
-    const uint32_t batch = (uint32_t)a.p.at.batch;
-    if (a.plan == nullptr) plan_in_cta(a, sm.first, sm.stands);
+    const uint32_t batch = (uint32_t)a.p.at.batch, side = a.p.biased ? a.p.bk.side : 0;
+    for (uint32_t k = threadIdx.x; k < side; k += kAttendThreads) sm.edges[k] = a.p.bk.edges[k];
+    if (a.plan == nullptr) {
+        if (warp == 0) plan_in_cta(a, sm.first, sm.stands);
+        __syncthreads();
+    }
     const uint32_t* const firsts = a.plan == nullptr ? sm.first : a.first;
     const uint32_t span = a.plan == nullptr ? sm.first[kPlanWarp + 1] : a.plan->span;
     const uint32_t items = firsts[batch] * a.blocks;
     if (a.plan == nullptr && blockIdx.x == 0)
         for (uint32_t k = threadIdx.x; k <= batch; k += kAttendThreads) a.first[k] = sm.first[k];  // for the join
-    const uint32_t side = a.p.biased ? a.p.bk.side : 0;
-    for (uint32_t k = threadIdx.x; k < side; k += kAttendThreads) sm.edges[k] = a.p.bk.edges[k];
     // where a lane copies to and reads from, in a stage
     constexpr bool kPlain = 32 % (DIM / 16) == 0;  // (a lane's pieces are the same piece of different rows)
     const uint32_t stages = (uint32_t)__cvta_generic_to_shared(sm.stages[warp]);
@@ -722,6 +738,7 @@ cudaError_t launch_attend_dim(AttendArgs& a, cudaStream_t st) {
         if (e == cudaSuccess) e = resident_ctas<kernel>(kAttendThreads, bytes, resident);
         if (e != cudaSuccess) return;
         a.ctas = 148u * resident < kAttendCtas ? 148u * resident : kAttendCtas;
+        a.share = (float)((double)a.blocks / a.ctas * (1.0 + 1.0 / (1 << 20)));
         if (a.plan != nullptr) launch_next(attend_plan_kernel, 1, kPlanThreads, 0, st, a);
         launch_next(kernel, a.ctas, kAttendThreads, bytes, st, a);
     };
