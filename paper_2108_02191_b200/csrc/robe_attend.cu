@@ -40,7 +40,6 @@ constexpr uint32_t kSpanMany = 1536, kSpanLong = 1024;
 constexpr int kHeads = 16;                             // query heads of a CTA
 constexpr int kPlanThreads = 1024;
 constexpr uint32_t kPlanWarp = 256;                    // sequences of a call that a warp of each CTA plans for itself
-constexpr uint32_t kAttendCtas = 148 * 8;              // most CTAs
 constexpr uint32_t kSpansPerCta = 8;                   // most spans that are made for a CTA
 
 // What the first kernel leaves: the spans' length, and spans before sequence n in first[n].
@@ -54,7 +53,7 @@ struct AttendArgs {
     uint32_t head_blocks;  // blocks per head of the cache
     uint32_t group;        // query heads per head of the cache
     uint32_t rows;         // query heads of the largest block
-    uint32_t ctas;         // that spans are made for, at most kAttendCtas
+    uint32_t ctas;         // that spans are made for, at most most_ctas
     float share;           // of a CTA in a key of all: blocks / ctas, and a little more
     uint32_t page_magic, page_shift;  // key / page_rows = (key * magic >> 32) >> shift, for pages of more than one row
     uint32_t positions;    // that the page table has room for
@@ -289,7 +288,18 @@ struct AttendSmem {
     float bias[][kHeads + 1];  // as many rows as a side has buckets
 };
 
+// Most CTAs of a call: as many as the SMs' 228 KB of shared memory hold, at most eight an SM.
+template <int DIM>
+constexpr uint32_t kAttendCtas = 148 * (228 * 1024 / (sizeof(AttendSmem<DIM>) + 1024) < 8 ? 228 * 1024 / (sizeof(AttendSmem<DIM>) + 1024) : 8);
+uint32_t most_ctas(int64_t dim) {
+    return dim == 32 ? kAttendCtas<32> : dim == 64 ? kAttendCtas<64> : dim == 96 ? kAttendCtas<96> : dim == 128 ? kAttendCtas<128> : kAttendCtas<256>;
+}
+
 // WIDE: more than eight query heads to a CTA.
+// 64 sequences of up to 8191 keys, 8 heads of 128, e4m3, four query heads each (631 MB): 127 us with the join's 9, 76 % of what a copy
+// reaches; DRAM at 80 % while it runs, 11 warps an SM (shared memory, 167 registers) with 750 instructions for a warp's 32 keys. One of
+// 65521 keys, 4 heads: 21 us. A call of one key: 4.2 us.  The next item's first keys asked for before this one's sum is joined: 130 us
+// for the 127 (three CTAs an SM cover for one another).
 template <int DIM, bool I8, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     constexpr int N = WIDE ? 2 : 1;  // blocks of eight query heads
@@ -737,7 +747,7 @@ cudaError_t launch_attend_dim(AttendArgs& a, cudaStream_t st) {
         e = with_shared<kernel>(kMostBytes);
         if (e == cudaSuccess) e = resident_ctas<kernel>(kAttendThreads, bytes, resident);
         if (e != cudaSuccess) return;
-        a.ctas = 148u * resident < kAttendCtas ? 148u * resident : kAttendCtas;
+        a.ctas = 148u * resident < kAttendCtas<DIM> ? 148u * resident : kAttendCtas<DIM>;
         a.share = (float)((double)a.blocks / a.ctas * (1.0 + 1.0 / (1 << 20)));
         if (a.plan != nullptr) launch_next(attend_plan_kernel, 1, kPlanThreads, 0, st, a);
         launch_next(kernel, a.ctas, kAttendThreads, bytes, st, a);
@@ -754,9 +764,9 @@ cudaError_t launch_attend_dim(AttendArgs& a, cudaStream_t st) {
 }
 
 // a sequence has at most one span more than its share of those that are made for the CTAs, and no span is shorter than kSpanLeast
-uint64_t most_items(int64_t batch, uint32_t blocks, int64_t positions) {
+uint64_t most_items(int64_t batch, uint32_t blocks, int64_t positions, int64_t dim) {
     const unsigned __int128 by_length = (unsigned __int128)batch * (positions > 0 ? (positions + kSpanLeast - 1) / kSpanLeast : 1) * blocks;
-    const unsigned __int128 by_share = (unsigned __int128)kAttendCtas * kSpansPerCta + (unsigned __int128)batch * blocks;
+    const unsigned __int128 by_share = (unsigned __int128)most_ctas(dim) * kSpansPerCta + (unsigned __int128)batch * blocks;
     return (uint64_t)(by_length < by_share ? by_length : by_share);
 }
 uint32_t rows_of(int64_t heads, int64_t q_heads) { return q_heads / heads < kHeads ? (uint32_t)(q_heads / heads) : (uint32_t)kHeads; }
@@ -766,7 +776,7 @@ size_t plan_bytes(int64_t batch) { return sizeof(AttendPlan) + (((size_t)batch +
 
 size_t attend_workspace_bytes(int64_t batch, int64_t heads, int64_t q_heads, int64_t dim, int64_t positions) {
     return plan_bytes(batch) +
-           most_items(batch, (uint32_t)heads * head_blocks_of(heads, q_heads), positions) * rows_of(heads, q_heads) * (dim + 4) * 4;
+           most_items(batch, (uint32_t)heads * head_blocks_of(heads, q_heads), positions, dim) * rows_of(heads, q_heads) * (dim + 4) * 4;
 }
 
 cudaError_t launch_attend(const AttendProblem& pb, void* workspace, cudaStream_t st) {
@@ -796,7 +806,7 @@ cudaError_t launch_attend(const AttendProblem& pb, void* workspace, cudaStream_t
     a.plan = pb.at.batch > kPlanWarp ? (AttendPlan*)workspace : nullptr;
     a.first = (uint32_t*)((char*)workspace + sizeof(AttendPlan));
     a.parts = (float*)((char*)workspace + plan_bytes(pb.at.batch));
-    if (most_items(pb.at.batch, a.blocks, a.positions) >= (1ull << 32) - kAttendCtas) return kGridTooSmall;
+    if (most_items(pb.at.batch, a.blocks, a.positions, pb.dim) >= (1ull << 32) - most_ctas(pb.dim)) return kGridTooSmall;
     switch (pb.dim) {
         case 32: return launch_attend_dim<32>(a, st);
         case 64: return launch_attend_dim<64>(a, st);
