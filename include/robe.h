@@ -654,7 +654,8 @@ int robe_cache_read(const robe_cache_t* c, void* out, int64_t out_ld, int64_t n,
  * over the positions that have a place; +0 where there is none (starts[s] < 0, say).  bucket as in robe_bias_forward.
  *   keys, values   caches with the same code type, pages, sizes and strides; group = dim, d = heads * dim; offsets NULL;
  *                  codes 16-byte aligned (pointer, codes_ld and codes_page); scales as robe_cache_write leaves them.
- *   q, out         bf16 [batch * q_heads, dim], a row for every sequence and head, ld apart.  dim 32, 64, 96, 128 or 256; heads divides q_heads.
+ *   q, out         bf16 [batch, q_heads, dim]: heads ld apart, sequences seq (columns of a row that holds keys and values too, say).  dim 32,
+ *                  64, 96, 128 or 256; heads divides q_heads.
  *   bias           handle or NULL;  bias_rows  fp32 [num_buckets, q_heads], bias_ld apart.
  *   workspace      256-byte aligned, robe_cache_attention_workspace_bytes(batch, heads, q_heads, dim, max_pages * page_rows)
  *                  bytes (0 for bad arguments); one call at a time.
@@ -664,9 +665,9 @@ int robe_cache_read(const robe_cache_t* c, void* out, int64_t out_ld, int64_t n,
  * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_WORKSPACE, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
  */
 size_t robe_cache_attention_workspace_bytes(int64_t batch, int64_t heads, int64_t q_heads, int64_t dim, int64_t positions);
-int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, const void* q, int64_t q_ld, int64_t q_heads,
+int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, const void* q, int64_t q_ld, int64_t q_seq, int64_t q_heads,
                          float scale, robe_bias_t bias, const float* bias_rows, int64_t bias_ld, void* out, int64_t out_ld,
-                         void* workspace, size_t workspace_bytes, void* stream);
+                         int64_t out_seq, void* workspace, size_t workspace_bytes, void* stream);
 
 /* robe_status_string - static host string for a robe_status value. */
 const char* robe_status_string(int status);

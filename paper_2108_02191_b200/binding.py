@@ -157,8 +157,8 @@ _lib.robe_cache_write.argtypes = [C.POINTER(_Cache)] + _rows + [_i64, C.c_int, _
 _lib.robe_cache_read.argtypes = [C.POINTER(_Cache)] + _rows + [_i64, C.c_int, _vp]
 _lib.robe_cache_attention_workspace_bytes.argtypes = [_i64] * 5
 _lib.robe_cache_attention_workspace_bytes.restype = C.c_size_t
-_lib.robe_cache_attention.argtypes = ([C.POINTER(_Cache)] * 2 + _rows + [_i64, C.c_float, _BiasHandle] + _rows * 2
-                                      + [_vp, C.c_size_t, _vp])
+_lib.robe_cache_attention.argtypes = ([C.POINTER(_Cache)] * 2 + _rows + [_i64, _i64, C.c_float, _BiasHandle] + _rows * 2
+                                      + [_i64, _vp, C.c_size_t, _vp])
 _lib.robe_status_string.argtypes = [C.c_int]
 _lib.robe_status_string.restype = C.c_char_p
 for _name in EXPORTS:
@@ -753,23 +753,25 @@ def robe_cache_attention_workspace_bytes(batch: int, heads: int, q_heads: int, d
 def robe_cache_attention(q, keys, key_scales, values, value_scales, pages, starts, out, workspace, scale: float, bias=None,
                          bias_rows=None, stream=None) -> None:
     """Attention of the query at position starts[s] of each sequence over the rows 0 .. starts[s] of a cache of keys and one of values.
-    q, out bf16 [batch, q_heads, dim]; bias: a position-bias handle with bias_rows [buckets, q_heads]."""
+    q, out bf16 [batch, q_heads, dim] (columns of a wider tensor, too); bias: a position-bias handle with bias_rows [buckets, q_heads]."""
     rc = _native.cache_attention(q, keys, key_scales, values, value_scales, pages, starts, out, workspace, scale, bias, bias_rows, stream)
     if rc != _NOT_TAKEN:
         return _check(rc, "robe_cache_attention")
-    if _here(q, "q", torch.bfloat16).dim() != 3:
-        raise ValueError("q: expected [batch, query heads, columns of a head]")
-    p, ld, rows, dim = _matrix(q, "q")
-    batch, q_heads = q.shape[:2]
+    for t, what in ((q, "q"), (out, "out")):
+        if _here(t, what, torch.bfloat16).dim() != 3:
+            raise ValueError(f"{what}: expected [batch, query heads, columns of a head]")
+    if out.shape != q.shape:
+        raise ValueError(f"out: {tuple(out.shape)}, expected {tuple(q.shape)}")
+    p, ld, seq, batch, q_heads, dim = _paged(q, "q", (torch.bfloat16,))
+    to, to_ld, to_seq, *_ = _paged(out, "out", (torch.bfloat16,))
     if starts is None:
         raise ValueError("starts: expected int64 [batch]")
     k, v = (_cache(c, s, pages, None, starts, dim) for c, s in ((keys, key_scales), (values, value_scales)))
     if k.batch != batch:
         raise ValueError(f"pages: of {k.batch} sequences, expected {batch}")
-    to, to_ld = _matrix_like(_here(out, "out"), "out", torch.bfloat16, rows, dim)
     table, table_ld = (None, 0) if bias is None else _matrix_like(_here(bias_rows, "bias_rows"), "bias_rows", torch.float32,
                                                                   robe_bias_num_buckets(bias), q_heads)
-    _check(_lib.robe_cache_attention(C.byref(k), C.byref(v), p, ld, q_heads, scale, bias, table, table_ld, to, to_ld,
+    _check(_lib.robe_cache_attention(C.byref(k), C.byref(v), p, ld, seq, q_heads, scale, bias, table, table_ld, to, to_ld, to_seq,
                                      *_workspace(workspace), _stream_ptr(stream)), "robe_cache_attention")
 
 

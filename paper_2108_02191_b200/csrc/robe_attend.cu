@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
         const uint32_t head = block / a.head_blocks;  // of the cache
         const uint32_t q0 = (block - head * a.head_blocks) * kHeads;  // first of its query heads
         const uint32_t in_block = a.group - q0 < (uint32_t)kHeads ? a.group - q0 : (uint32_t)kHeads;
-        const int64_t q_row = (int64_t)n * a.p.q_heads + head * a.group + q0;
+        const uint32_t q_head = head * a.group + q0;
 
         // a step's copies: lane l knows where key l lies (of 16: l + 16 too)
         const int32_t* pages = a.p.at.pages + (int64_t)n * a.p.at.pages_ld;
@@ -404,14 +404,14 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
             sm.bias[b][h] = fabsf(v) < INFINITY ? fminf(fmaxf(v * kLog2e, -kMostFinite), kMostFinite) : v;
         }
         // queries: rows g and g + 8 of the instruction's first operand
-        const bool q_pieces = ((uintptr_t)a.p.q.p | (uint64_t)a.p.q.ld * 2) % 8 == 0;
+        const bool q_pieces = ((uintptr_t)a.p.q.p | (uint64_t)a.p.q.ld * 2 | (uint64_t)a.p.q.page_ld * 2) % 8 == 0;
         uint32_t q[N][DIM / 16][2];
         float q_factor[N];
 #pragma unroll
         for (int b = 0; b < N; ++b) {
             const uint32_t h = b * 8 + g;
             const bool on = h < in_block;
-            const __nv_bfloat16* from = (const __nv_bfloat16*)a.p.q.p + (q_row + h) * a.p.q.ld;
+            const __nv_bfloat16* from = (const __nv_bfloat16*)a.p.q.p + n * a.p.q.page_ld + (q_head + h) * a.p.q.ld;
             uint32_t most = 0;
 #pragma unroll
             for (int w = 0; w < DIM / 16; ++w) {
@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
             if (!ROBE_CHK(n < batch && head * a.group + q0 + h < (uint64_t)a.p.q_heads, ROBE_DBG_ROW_POS)) continue;
             if (pieces == 1) {
                 const float by = total == 0.0f ? 0.0f : 1.0f / total;
-                __nv_bfloat16* to = (__nv_bfloat16*)a.p.out.p + (q_row + h) * a.p.out.ld + col;
+                __nv_bfloat16* to = (__nv_bfloat16*)a.p.out.p + n * a.p.out.page_ld + (q_head + h) * a.p.out.ld + col;
                 to[0] = narrow<__nv_bfloat16>(v.x * by);
                 to[1] = narrow<__nv_bfloat16>(v.y * by);
                 to[2] = narrow<__nv_bfloat16>(v.z * by);
@@ -726,7 +726,7 @@ __global__ void __launch_bounds__(kSpanThreads) attend_join_kernel(AttendArgs a,
             v = fmaf(sums[w0 + w][col], f, v);
             l = fmaf(totals[w0 + w], f, l);
         }
-        ((__nv_bfloat16*)a.p.out.p)[((int64_t)n * q_heads + head) * a.p.out.ld + col] = narrow<__nv_bfloat16>(l == 0.0f ? 0.0f : v / l);
+        ((__nv_bfloat16*)a.p.out.p)[n * a.p.out.page_ld + head * a.p.out.ld + col] = narrow<__nv_bfloat16>(l == 0.0f ? 0.0f : v / l);
     }
 }
 

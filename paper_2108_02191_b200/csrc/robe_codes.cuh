@@ -148,7 +148,7 @@ __device__ __forceinline__ CacheRow cache_row(const CachePlaces& p, int64_t r, i
     return cache_row_at(p, s, (int64_t)((uint64_t)start + (uint64_t)t));  // (negative: no place)
 }
 
-struct CacheRef {  // codes or scales: rows ld elements apart, pages page_ld
+struct CacheRef {  // codes or scales: rows ld elements apart, pages page_ld; queries: heads and sequences
     void* p;
     int64_t ld, page_ld;
 };
@@ -175,7 +175,7 @@ struct AttendProblem {
     CacheRef key_codes, key_scales, value_codes, value_scales;
     int i8;
     int64_t heads, q_heads, dim;  // heads of the cache, of the queries
-    RowsRef q, out;               // bf16, a row per sequence and query head
+    CacheRef q, out;              // bf16
     float scale;
     int biased;
     BiasBuckets bk;

@@ -229,7 +229,7 @@ struct Reader {
         if (!t->is_contiguous() || t->numel() != n) ok = false;
         return t->data_ptr();
     }
-    // [pages, page_rows, ..] with contiguous rows
+    // [pages, page_rows, ..] with contiguous rows, or [sequences, heads, columns]
     struct Paged {
         void* p = nullptr;
         int64_t ld = 0, page = 0, pages = 0, rows = 0, cols = 1;
@@ -700,11 +700,11 @@ PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 13 || args[6] == Py_None) return not_taken();
     Reader r{args};
-    const Matrix q = r.matrix(0), out = r.matrix(7);
-    if (!r.ok || q.dtype != ROBE_BF16 || out.dtype != ROBE_BF16 || out.rows != q.rows || out.cols != q.cols) return not_taken();
-    const at::Tensor& t = THPVariable_Unpack(args[0]);
-    if (t.dim() != 3) return not_taken();
-    const int64_t q_heads = t.size(1);
+    const at::Tensor *tq = r.local(0), *to = r.local(7);
+    if (!r.ok || tq->scalar_type() != at::kBFloat16 || to->scalar_type() != at::kBFloat16 || tq->dim() != 3 || to->sizes() != tq->sizes()) return not_taken();
+    const Reader::Paged q = r.paged(tq), out = r.paged(to);
+    if (!r.ok) return not_taken();
+    const int64_t q_heads = q.rows;
     const robe_cache_t k = r.cache(1, 2, 5, -1, 6, q.cols), v = r.cache(3, 4, 5, -1, 6, q.cols);
     size_t ws_bytes = 0;
     void* ws = r.workspace(8, ws_bytes);
@@ -713,10 +713,11 @@ PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const robe_bias_t b = biased ? r.bias(10) : nullptr;
     const Matrix rows = biased ? r.matrix(11) : Matrix();
     void* st = r.stream(12);
-    if (!r.ok || k.batch != t.size(0)) return not_taken();
+    if (!r.ok || k.batch != q.pages) return not_taken();
     if (biased && (rows.dtype != ROBE_F32 || rows.cols != q_heads || rows.rows != row_calls.bias_num_buckets(b))) return not_taken();
     return made([&] {
-        return row_calls.cache_attention(&k, &v, q.p, q.ld, q_heads, scale, b, (const float*)rows.p, rows.ld, out.p, out.ld, ws, ws_bytes, st);
+        return row_calls.cache_attention(&k, &v, q.p, q.ld, q.page, q_heads, scale, b, (const float*)rows.p, rows.ld, out.p, out.ld, out.page, ws,
+                                         ws_bytes, st);
     });
 }
 

@@ -28,7 +28,7 @@ bool group_ok(int64_t d, int64_t& group) {
 struct CacheSpans {
     Span codes, scales, pages, offsets, starts;
 };
-// [pages, page_rows, cols]: equally far apart rows as a matrix, others as the block of memory they lie in
+// [pages, page_rows, cols] (of queries: sequences, heads, columns): equally far apart rows as a matrix, pages without gaps as its rows, others as the block of memory they lie in
 bool paged(Span& s, const void* p, int64_t ld, int64_t page, int64_t pages, int64_t page_rows, int64_t cols, int64_t size) {
     s = Span{p, cols, 0, cols, size};
     if (pages == 0) return true;
@@ -40,7 +40,7 @@ bool paged(Span& s, const void* p, int64_t ld, int64_t page, int64_t pages, int6
     const unsigned __int128 all = (unsigned __int128)(pages - 1) * page + in_page;
     if (all * size >= ((unsigned __int128)1 << 60)) return false;
     if (page_rows > 1 && (pages == 1 || (unsigned __int128)page == (unsigned __int128)ld * page_rows)) s = Span{p, ld, pages * page_rows, cols, size};
-    else if (page_rows == 1) s = Span{p, page, pages, cols, size};
+    else if (page_rows == 1 || ld == cols) s = Span{p, page, pages, cols * page_rows, size};
     else s = Span{p, (int64_t)all, 1, (int64_t)all, size};
     return true;
 }
@@ -215,9 +215,9 @@ size_t robe_cache_attention_workspace_bytes(int64_t batch, int64_t heads, int64_
     return attend_sizes(batch, heads, q_heads, dim, positions) ? attend_workspace_bytes(batch, heads, q_heads, dim, positions) : 0;
 }
 
-int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, const void* q, int64_t q_ld, int64_t q_heads,
+int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, const void* q, int64_t q_ld, int64_t q_seq, int64_t q_heads,
                          float scale, robe_bias_t bias, const float* bias_rows, int64_t bias_ld, void* out, int64_t out_ld,
-                         void* workspace, size_t workspace_bytes, void* stream) {
+                         int64_t out_seq, void* workspace, size_t workspace_bytes, void* stream) {
     CacheProblem pk, pv;
     CacheSpans sk, sv;
     if (!cache_problem(keys, pk, sk) || !cache_problem(values, pv, sv)) return ROBE_ERR_INVALID_ARG;
@@ -234,8 +234,9 @@ int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, c
     if (batch > 0 && keys->starts == nullptr) return ROBE_ERR_INVALID_ARG;
     for (const robe_cache_t* c : {keys, values})
         if (c->num_pages > 0 && (((uintptr_t)c->codes | (uint64_t)c->codes_ld | (uint64_t)c->codes_page) & 15u) != 0) return ROBE_ERR_INVALID_ARG;
-    const Span sq{q, q_ld, batch * q_heads, dim, 2}, so{out, out_ld, batch * q_heads, dim, 2},
-        sb{bias_rows, bias_ld, bias != nullptr ? (int64_t)bias->bk.buckets : 0, q_heads, 4};
+    Span sq, so;
+    if (!paged(sq, q, q_ld, q_seq, batch, q_heads, dim, 2) || !paged(so, out, out_ld, out_seq, batch, q_heads, dim, 2)) return ROBE_ERR_INVALID_ARG;
+    const Span sb{bias_rows, bias_ld, bias != nullptr ? (int64_t)bias->bk.buckets : 0, q_heads, 4};
     const size_t need = attend_workspace_bytes(batch, heads, q_heads, dim, (int64_t)room);
     if (workspace == nullptr || workspace_bytes < need || ((uintptr_t)workspace & 255u) != 0) return ROBE_ERR_WORKSPACE;
     const Span scratch{workspace, 1, 1, (int64_t)need, 1};
@@ -256,8 +257,8 @@ int robe_cache_attention(const robe_cache_t* keys, const robe_cache_t* values, c
     pb.heads = heads;
     pb.q_heads = q_heads;
     pb.dim = dim;
-    pb.q = ref(sq);
-    pb.out = ref(so);
+    pb.q = CacheRef{(void*)q, q_ld, q_seq};
+    pb.out = CacheRef{out, out_ld, out_seq};
     pb.scale = scale;
     pb.biased = bias != nullptr;
     if (bias != nullptr) pb.bk = bias->bk;

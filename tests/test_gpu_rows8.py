@@ -585,6 +585,42 @@ def test_attention_bits_and_strides():
         robe.robe_cache_attention(view(wide_q), made["keys"].codes, made["keys"].scales, made["values"].codes, made["values"].scales, pages.cuda(),
                                   torch.tensor([899, 349], device="cuda"), view(out), ws, 0.1)
         assert same_bits(out.cpu().reshape(2, 8, 128), a) and surroundings_kept(out)
+    # queries in a row with the new keys and values, results in a row of the same length or elsewhere in the queries' own
+    for left in (0, 4, 1):
+        qkv, wide = torch.randn(2, 12 * 128 + 8, generator=gen(left)).bfloat16().cuda(), torch.full((2, 12 * 128 + 8), NAN, dtype=torch.bfloat16, device="cuda")
+        view = lambda t: t[:, left:left + 8 * 128].unflatten(1, (8, 128))
+        view(qkv).copy_(q)
+        robe.robe_cache_attention(view(qkv), made["keys"].codes, made["keys"].scales, made["values"].codes, made["values"].scales, pages.cuda(),
+                                  torch.tensor([899, 349], device="cuda"), view(wide), ws, 0.1)
+        assert same_bits(view(wide).cpu(), a) and wide[:, :left].isnan().all() and wide[:, left + 8 * 128:].isnan().all()
+    both = torch.randn(2, 2, 8, 128, generator=gen(3)).bfloat16().cuda()
+    both[:, 0] = q.cuda()
+    robe.robe_cache_attention(both[:, 0], made["keys"].codes, made["keys"].scales, made["values"].codes, made["values"].scales, pages.cuda(),
+                              torch.tensor([899, 349], device="cuda"), both[:, 1], ws, 0.1)
+    assert same_bits(both[:, 1].cpu(), a) and same_bits(both[:, 0].cpu(), q)
+
+
+def test_two_captured_attentions_share_a_workspace():
+    # other lengths, caches and queries; each replayed after the other, and the second on what the first has left
+    calls, want = [], []
+    ws = torch.empty(robe.robe_cache_attention_workspace_bytes(3, 2, 8, 64, 60 * 32), dtype=torch.uint8, device="cuda")
+    for seed, lengths in ((1, [1900, 3, 700]), (2, [20, 1500, 0])):
+        made, pages, q, _ = attention_case(lengths, 2, 4, 64, 32, KINDS[seed - 1], 0, seed, room=1920)
+        out = torch.full(q.shape, NAN, dtype=torch.bfloat16, device="cuda")
+        args = (q.cuda(), made["keys"].codes, made["keys"].scales, made["values"].codes, made["values"].scales, pages.cuda(),
+                torch.tensor(lengths, device="cuda") - 1, out, ws, 0.1)
+        calls.append(args)
+        want.append(run_attention(made, pages, q, [n - 1 for n in lengths], 2, 0.1))
+    graphs = []
+    for args in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            robe.robe_cache_attention(*args)
+        graphs.append(graph)
+    for k in (0, 1, 0, 0, 1, 1, 0):
+        calls[k][7].fill_(NAN)
+        graphs[k].replay()
+        assert same_bits(calls[k][7].cpu(), want[k])
 
 
 # ---------------------------------------------------------------- together

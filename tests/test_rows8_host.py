@@ -180,13 +180,13 @@ def test_codes_and_scales_of_a_row_in_one_buffer_do_not_overlap():
 def attend(keys=None, values=None, **o):
     k = cache(group=32, starts=P[8], **(keys or {}))
     v = cache(group=32, starts=P[8], codes=P[3], scales=P[4], **(values or {}))
-    a = dict(q=P[5], q_ld=32, q_heads=4, bias=None, rows=None, rows_ld=4, out=P[6], out_ld=32, ws=P[7], bytes=1 << 40)
+    a = dict(q=P[5], q_ld=32, q_seq=128, q_heads=4, bias=None, rows=None, rows_ld=4, out=P[6], out_ld=32, out_seq=128, ws=P[7], bytes=1 << 40)
     a.update(o)
-    return lib().robe_cache_attention(C.byref(k), C.byref(v), a["q"], a["q_ld"], a["q_heads"], 1.0, a["bias"], a["rows"], a["rows_ld"], a["out"], a["out_ld"], a["ws"],
+    return lib().robe_cache_attention(C.byref(k), C.byref(v), a["q"], a["q_ld"], a["q_seq"], a["q_heads"], 1.0, a["bias"], a["rows"], a["rows_ld"], a["out"], a["out_ld"], a["out_seq"], a["ws"],
                                       a["bytes"], None)
 
 
-@pytest.mark.parametrize("o", [dict(q=None), dict(out=None), dict(q_heads=3), dict(q_heads=0), dict(q_heads=2**20), dict(q_ld=31), dict(out=P[5]), dict(out=P[0]), dict(out=P[7]),
+@pytest.mark.parametrize("o", [dict(q=None), dict(out=None), dict(q_heads=3), dict(q_heads=0), dict(q_heads=2**20), dict(q_ld=31), dict(q_seq=127), dict(out_seq=0), dict(out_seq=-128), dict(out=P[5]), dict(out=P[0]), dict(out=P[7]),
                                dict(keys=dict(code_type=robe.ROBE_E4M3)), dict(values=dict(num_pages=9)), dict(values=dict(codes_ld=80, codes_page=80 * 16)), dict(values=dict(pages=P[9])),
                                dict(keys=dict(offsets=P[9]), values=dict(offsets=P[9])), dict(keys=dict(d=48), values=dict(d=48)), dict(keys=dict(codes=C.c_void_p(0x10008))),
                                dict(keys=dict(codes_ld=72, codes_page=72 * 16), values=dict(codes_ld=72, codes_page=72 * 16)),
@@ -202,10 +202,10 @@ def test_attention_refuses_other_things():
     assert attend(bias=b, rows=P[9], rows_ld=3) == BAD and attend(bias=b, rows=P[6]) == BAD
     robe.robe_bias_destroy(b)
     k = cache(group=32)  # no positions
-    assert lib().robe_cache_attention(C.byref(k), C.byref(k), P[5], 32, 4, 1.0, None, None, 0, P[6], 32, P[7], 1 << 40, None) == BAD
+    assert lib().robe_cache_attention(C.byref(k), C.byref(k), P[5], 32, 128, 4, 1.0, None, None, 0, P[6], 32, 128, P[7], 1 << 40, None) == BAD
     for dim in (16, 33, 48, 512):
         k = cache(d=2 * dim, group=dim, codes_ld=2 * dim, codes_page=32 * dim, starts=P[8])
-        assert lib().robe_cache_attention(C.byref(k), C.byref(k), P[5], dim, 4, 1.0, None, None, 0, P[6], dim, P[7], 1 << 40, None) == BAD
+        assert lib().robe_cache_attention(C.byref(k), C.byref(k), P[5], dim, 4 * dim, 4, 1.0, None, None, 0, P[6], dim, 4 * dim, P[7], 1 << 40, None) == BAD
 
 
 def test_workspace_of_the_attention():
