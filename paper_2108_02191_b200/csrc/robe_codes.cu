@@ -692,14 +692,10 @@ __global__ void __launch_bounds__(kCodeThreads) cache_read_kernel(CacheArgs a) {
 #pragma unroll
             for (int q = 0; q < (W < 4 ? 1 : W / 4); ++q) values_of<I8>(e[i].w[q], v + 4 * q);
             T* to = (T*)a.rows.p + (first + row[i]) * a.rows.ld + col[i];
-            constexpr int S = W * (int)sizeof(T) > 16 ? kPiece<T> : W;
+            Pack<T, W> o;
 #pragma unroll
-            for (int q = 0; q < W / S; ++q) {
-                Pack<T, S> o;
-#pragma unroll
-                for (int k = 0; k < S; ++k) o.v[k] = narrow<T>(code[i] >= 0 ? v[q * S + k] * scale[i] : 0.0f);
-                store_pack<true, T, S>(to + q * S, o);
-            }
+            for (int k = 0; k < W; ++k) o.v[k] = narrow<T>(code[i] >= 0 ? v[k] * scale[i] : 0.0f);
+            store_pack<true, T, W>(to, o);
         }
     }
 }
@@ -735,8 +731,13 @@ cudaError_t launch_read(CacheArgs& a, int width, cudaStream_t st) {
     const int64_t grid = (a.n + a.per_cta - 1) / a.per_cta;
     if (grid >= (1ll << 31)) return kGridTooSmall;
     auto launch = [&](auto kernel) { launch_next(kernel, (unsigned)grid, kCodeThreads, 0, st, a); };
-    if (width == 8) launch(cache_read_kernel<T, 8, I8, 4>);
-    else if (width == 4) launch(cache_read_kernel<T, 4, I8, 4>);
+    if constexpr (sizeof(T) == 2) {
+        if (width == 8) {
+            launch(cache_read_kernel<T, 8, I8, 4>);
+            return cudaGetLastError();
+        }
+    }
+    if (width == 4) launch(cache_read_kernel<T, 4, I8, 4>);
     else launch(cache_read_kernel<T, 1, I8, 4>);
     return cudaGetLastError();
 }
@@ -801,10 +802,11 @@ cudaError_t launch_cache_write(const CacheProblem& pb, const void* rows, int64_t
 
 cudaError_t launch_cache_read(const CacheProblem& pb, void* rows, int64_t rows_ld, int64_t n, int dtype, cudaStream_t st) {
     const int64_t size = dtype == 0 ? 4 : 2;
-    // (sixteen codes a thread are two pieces of a row apart when they are written: 133 K rows of 1024 to bf16 91 us, eight 75)
-    int width = 8;
+    // (what is written in 16 bytes a thread: 133 K rows of 1024 to bf16 by sixteen codes a thread 91 us, eight 75; 100 K to fp32 by
+    // eight 108, four 86)
+    int width = dtype == 0 ? 4 : 8;
     for (; width > 1; width = width == 4 ? 1 : 4) {
-        const int64_t bytes = width * size > 16 ? 16 : width * size;
+        const int64_t bytes = width * size;
         if (pb.d % width == 0 && pb.group % width == 0 && (uintptr_t)pb.codes.p % width == 0 && pb.codes.ld % width == 0 &&
             pb.codes.page_ld % width == 0 && (uintptr_t)rows % bytes == 0 && (n <= 1 || rows_ld * size % bytes == 0))
             break;

@@ -151,7 +151,7 @@ void launch_lookup(const LookupArgs& a, cudaStream_t st) {
 
 template <class TT, class TO>
 void launch_lookup(const LookupArgs& a, int piece, cudaStream_t st) {
-    constexpr int kMost = sizeof(TT) == 4 && sizeof(TO) == 4 ? 4 : 8;
+    constexpr int kMost = sizeof(TO) == 4 ? 4 : 8;
     if (kMost == 8 && piece == 8) launch_lookup<TT, TO, kMost>(a, st);
     else if (piece == 4) launch_lookup<TT, TO, 4>(a, st);
     else if (piece == 2) launch_lookup<TT, TO, 2>(a, st);
@@ -160,12 +160,12 @@ void launch_lookup(const LookupArgs& a, int piece, cudaStream_t st) {
 
 // ---------------------------------------------------------------- gradient
 
-// Rows of a chunk of sorted positions: as many as make one full wave of CTAs (four an SM, eight columns a thread); at least 16, and at
+// Rows of a chunk of sorted positions: as many as make one full wave of CTAs (four an SM, four columns a thread); at least 16, and at
 // most 256, so that no fp32 sum has more terms than that.  A border costs a row of sums for the run that crosses it, and CTAs
-// beyond a wave leave SMs empty: 16384 x 4096 bf16 (Zipf ids, accumulating) two waves 84 us, one and a half 81, one 71; 852 K x
-// 64 fp32 159, 153, 148; less than one 73 and 154.
+// beyond a wave leave SMs empty (with eight columns a thread: 16384 x 4096 bf16, Zipf ids, accumulating, two waves 84 us, one
+// and a half 81, one 71; 852 K x 64 fp32 159, 153, 148; less than one 73 and 154).
 uint32_t chunk_rows(int64_t rows, int64_t d) {
-    const unsigned __int128 threads = (unsigned __int128)rows * (uint64_t)((d + 7) / 8), wanted = 4 * 148 * kTableThreads;
+    const unsigned __int128 threads = (unsigned __int128)rows * (uint64_t)((d + 3) / 4), wanted = 4 * 148 * kTableThreads;
     const unsigned __int128 c = (threads + wanted - 1) / wanted;
     return c < 16 ? 16 : c > 256 ? 256 : (uint32_t)c;
 }
@@ -432,8 +432,10 @@ __global__ void __launch_bounds__(kTableThreads) grad_clear_kernel(GradArgs a) {
 enum SumsHow { kMany, kSome, kAlone };
 template <class T, int V, bool ADD, SumsHow HOW>
 __global__ void __launch_bounds__(kTableThreads, HOW == kMany ? 4 : 2) grad_sums_kernel(GradArgs a, uint32_t lanes) {
-    // rows under way: few where four CTAs are resident (16384 x 4096 bf16: 71 us, 87 with twice as many and two CTAs)
-    constexpr int kAhead = HOW == kMany ? (ADD ? 2 : 4) : (ADD ? 4 : 8);
+    // rows under way: few where four CTAs are resident (16384 x 4096 bf16, Zipf ids, accumulating, four columns: two rows 82 us, four 70, eight
+    // 122; 852 K x 64 fp32: four 144, eight 148, bf16 149, 147; 5000 x 1000 bf16 36.9, 35.5; single elements gain nothing of more)
+    constexpr int kMany4 = ADD ? 4 : sizeof(T) == 2 ? 8 : 4;
+    constexpr int kAhead = HOW == kMany ? (V == 4 ? kMany4 : ADD ? 2 : 4) : (ADD ? 4 : 8);
     extern __shared__ uint32_t staged[];  // keys, then places, of the CTA's chunks (kAlone: of all)
     follow();
     const uint32_t groups = kTableThreads / lanes;
@@ -734,10 +736,10 @@ cudaError_t launch_sums(GradArgs& a, cudaStream_t st) {
     else add ? launch(grad_sums_kernel<T, V, true, kMany>, groups * a.chunk) : launch(grad_sums_kernel<T, V, false, kMany>, groups * a.chunk);
     return cudaSuccess;
 }
+// (at most four columns a thread, whose sums are stored in 16 bytes: 16384 x 4096 bf16, uniform ids, accumulating 132 us with eight, 122
+// with four, 5000 x 1000 43, 36)
 template <class T>
 cudaError_t launch_sums(GradArgs& a, int piece, cudaStream_t st) {
-    constexpr int kMost = kPiece<T>;
-    if (kMost == 8 && piece == 8) return launch_sums<T, kMost>(a, st);
     if (piece == 4) return launch_sums<T, 4>(a, st);
     if (piece == 2) return launch_sums<T, 2>(a, st);
     return launch_sums<T, 1>(a, st);
@@ -754,7 +756,9 @@ cudaError_t launch_table_forward(const TableProblem& pb, void* out, int64_t out_
     a.ids = pb.ids;
     a.out_ld = out_ld;
     a.scale = pb.scale;
-    const int piece = piece_of(ts + os == 8 ? 4 : 8, pb.d, pb.table, pb.table_ld, ts, out, out_ld, os, pb.rows > 1 || pb.vocab > 1 ? 2 : 1);
+    // (what is written in 16 bytes a thread: 852 K rows of 64 from bf16 to fp32 in pieces of eight 74 us, of four 58; from fp32 to bf16 in
+    // pieces of four 64 us for the 59 of eight, ids by Zipf)
+    const int piece = piece_of(os == 4 ? 4 : 8, pb.d, pb.table, pb.table_ld, ts, out, out_ld, os, pb.rows > 1 || pb.vocab > 1 ? 2 : 1);
     a.pieces = (uint32_t)(pb.d / piece);
     a.magic = magic_of(a.pieces);
     // pieces are numbered in 32 bits: as many rows a launch as that allows
@@ -806,7 +810,7 @@ cudaError_t launch_table_backward(const TableProblem& pb, const void* grad, int6
     const uint32_t join_slices = (uint32_t)((pb.d + a.lanes * 4 - 1) / (a.lanes * 4));
     const uint64_t join = (L.chunks + kJoinWarps - 1) / kJoinWarps * join_slices;
     if (join >= (1ull << 31)) return kGridTooSmall;
-    const int piece = piece_of(size == 4 ? 4 : 8, pb.d, grad, grad_ld, size, grad_table, grad_table_ld, 4, pb.rows > 1 || pb.vocab > 1 ? 2 : 1);
+    const int piece = piece_of(4, pb.d, grad, grad_ld, size, grad_table, grad_table_ld, 4, pb.rows > 1 || pb.vocab > 1 ? 2 : 1);
     if (L.chunks * (uint64_t)((pb.d + (int64_t)kTableThreads * piece - 1) / ((int64_t)kTableThreads * piece)) >= (1ull << 31)) return kGridTooSmall;
 
     uint32_t *keys[2] = {(uint32_t*)(ws + L.keys[0]), (uint32_t*)(ws + L.keys[1])},
