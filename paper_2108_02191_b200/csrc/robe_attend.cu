@@ -296,10 +296,10 @@ uint32_t most_ctas(int64_t dim) {
 }
 
 // WIDE: more than eight query heads to a CTA.
-// 64 sequences of up to 8191 keys, 8 heads of 128, e4m3, four query heads each (631 MB): 127 us with the join's 9, 76 % of what a copy
+// 64 sequences of up to 8191 keys, 8 heads of 128, e4m3, four query heads each (631 MB): 128-131 us with the join's 9, 74-76 % of what a copy
 // reaches; DRAM at 80 % while it runs, 11 warps an SM (shared memory, 167 registers) with 750 instructions for a warp's 32 keys. One of
-// 65521 keys, 4 heads: 21 us. A call of one key: 4.2 us.  The next item's first keys asked for before this one's sum is joined: 130 us
-// for the 127 (three CTAs an SM cover for one another).
+// 65521 keys, 4 heads: 21 us. A call of one key: 4.2 us.  The next item's first keys asked for before this one's sum is joined: no
+// faster (three CTAs an SM cover for one another).
 template <int DIM, bool I8, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads) attend_kernel(AttendArgs a) {
     constexpr int N = WIDE ? 2 : 1;  // blocks of eight query heads

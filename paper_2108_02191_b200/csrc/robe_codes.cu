@@ -269,7 +269,7 @@ __device__ __forceinline__ uint32_t most_over_row(uint32_t v, uint32_t threads, 
 }
 
 // A row in the registers of its threads, K units each; two operations in one instruction.  What hides the loads' latency is CTAs, not
-// rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 91 us; elements one by one 117, bound by instructions; 252
+// rows asked for ahead.  (16384 x 4096 bf16, groups of 128, 472 MB: 87 us, 91 with the two units in different groups; elements one by one 117, bound by instructions; 252
 // with two CTAs an SM that asked for the next row.)
 // FULL: as columns_of has it, in 16-byte pieces and codes in eights, RESIDUAL and I8 known; otherwise these are asked for.
 template <class T, int P, int K, int THREADS, bool FULL, bool RESIDUAL, bool I8>
@@ -285,6 +285,9 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
         r = (int64_t)blockIdx.x * (blockDim.x / a.threads) + threadIdx.x / a.threads;
     }
     const bool on_row = r < a.rows;
+    // two units of a thread are one in each half of a group where it has two: they share its scale
+    const bool paired = FULL && K == 2 && a.c.shift > 0;
+    const uint32_t half = paired ? 1u << (a.c.shift - 1) : 0;
     Eight<T> x[K], y[K];
     uint32_t col[K];
     int count[K];
@@ -292,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
     const T* beside = (const T*)a.residual.p + r * a.residual.ld;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        col[j] = columns_of<FULL>(a.c, t + j * a.threads, count[j]);
+        col[j] = columns_of<FULL>(a.c, paired ? t + (t & ~(half - 1u)) + j * half : t + j * a.threads, count[j]);
         if (!on_row || !ROBE_CHK(count[j] == 0 || col[j] + (uint32_t)count[j] <= (uint64_t)a.c.d, ROBE_DBG_ROW_POS)) count[j] = 0;
         if (count[j] > 0) load_eight<T, P>(x[j], from + col[j], FULL ? 8 : count[j]);
         if (joined && count[j] > 0) load_eight<T, P>(y[j], beside + col[j], FULL ? 8 : count[j]);
@@ -373,11 +376,14 @@ __global__ void __launch_bounds__(THREADS, K == 4 ? 1 : THREADS == 256 ? 5 : 2) 
         for (int j = 0; j < K; ++j) m = max(m, largest(j));
         whole = group_scale(most_over_row(m, a.threads, most), q);
         if (on_row && t == 0) scales[0] = whole.scale;
+    } else if (paired) {
+        whole = group_scale(most_over(max(largest(0), largest(K - 1)), half), q);
+        if (count[0] > 0 && (t & (half - 1u)) == 0) scales[t >> (a.c.shift - 1)] = whole.scale;
     }
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         GroupScale g = whole;
-        if (!a.c.whole) {
+        if (!a.c.whole && !paired) {
             g = group_scale(most_over(largest(j), 1u << a.c.shift), q);
             const uint32_t unit = t + j * a.threads;
             if (count[j] > 0 && (unit & ((1u << a.c.shift) - 1u)) == 0) scales[unit >> a.c.shift] = g.scale;
@@ -642,6 +648,61 @@ __global__ void __launch_bounds__(kCodeThreads) cache_write_kernel(CacheArgs a) 
     }
 }
 
+// The same where groups have two units and more: a thread has one in each half of its group, so that places, shuffles and the scale are had
+// once for sixteen columns.  (33 K rows of 1024 bf16, groups of 128: 27.5 us a unit at a time, 21.8 so, with one or two pairs under way, 25.7 with
+// three; 100 K bf16 79 -> 61, fp32 92 -> 79)
+template <class T, bool I8, int ITEMS>
+__global__ void __launch_bounds__(kCodeThreads) cache_write_pairs_kernel(CacheArgs a) {
+    constexpr int P = kPiece<T>;
+    __shared__ Place places[kCacheRows];
+    follow();
+    const int64_t first = (int64_t)blockIdx.x * a.per_cta;
+    const uint32_t rows = a.n - first < a.per_cta ? (uint32_t)(a.n - first) : a.per_cta;
+    const uint32_t items = rows * a.units, shift = a.cols.shift - 1, lanes = 1u << shift;
+    const T* from = (const T*)a.rows.p + first * a.rows.ld;
+    for (uint32_t base = 0; base < items; base += kCodeThreads * ITEMS) {
+        Eight<T> e[ITEMS][2];
+        bool on[ITEMS][2];
+        uint32_t row[ITEMS], group[ITEMS], col[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t t = base + i * kCodeThreads + threadIdx.x;
+            row[i] = divide(t, a.units, a.magic);
+            const uint32_t unit = t - row[i] * a.units, in = (unit & (lanes - 1u)) * 8;
+            group[i] = unit >> shift;
+            col[i] = group[i] * a.cols.group + in;
+            const T* const p = from + row[i] * a.rows.ld + col[i];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                on[i][h] = t < items && in + h * lanes * 8 < a.cols.group && col[i] + h * lanes * 8 < a.cols.d;
+                if (on[i][h]) load_eight<T, P>(e[i][h], p + h * lanes * 8, 8);
+            }
+        }
+        if (base == 0) find_places(a, places, first, rows);  // (while the rows are on their way)
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float v[2][8], m = 0.0f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[h][k] = on[i][h] ? e[i][h].get(k) : 0.0f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m = most_magnitude(m, v[h][2 * k], v[h][2 * k + 1]);
+            }
+            const GroupScale g = group_scale(most_over(__float_as_uint(m), lanes), I8 ? kLargestI8 : kLargestE4m3);
+            if (!on[i][0]) continue;  // (its second half is none either)
+            const Place at = places[row[i]];
+            if (at.code < 0) continue;
+            if (!ROBE_CHK(col[i] + 8 + (on[i][1] ? lanes * 8 : 0) <= (uint64_t)a.cols.d, ROBE_DBG_ROW_POS)) continue;
+            if ((threadIdx.x & (lanes - 1u)) == 0) ((float*)a.c.scales.p)[at.scale + group[i]] = g.scale;
+            uint8_t* const to = (uint8_t*)a.c.codes.p + at.code + col[i];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (on[i][h]) __stcs((uint2*)(to + h * lanes * 8), make_uint2(codes_of<I8>(v[h], g.factor), codes_of<I8>(v[h] + 4, g.factor)));
+        }
+    }
+}
+
 // W columns a thread: one access of W bytes, W a power of two that divides the group
 template <int W>
 struct CodeWords {
@@ -718,7 +779,11 @@ cudaError_t launch_write(CacheArgs& a, cudaStream_t st) {
     const bool full = piece == kMost && full_units(a.cols, a.code_piece);
     const bool few = a.n * a.units < 148ll * 2 * kCodeThreads * 4;
     if (full && few) launch(cache_write_kernel<T, kMost, I8, 1, true>);
-    else if (full) launch(cache_write_kernel<T, kMost, I8, 4, true>);
+    else if (full && a.cols.shift > 0) {
+        a.units /= 2;
+        a.magic = magic_of(a.units);
+        launch(cache_write_pairs_kernel<T, I8, 2>);
+    } else if (full) launch(cache_write_kernel<T, kMost, I8, 4, true>);
     else if (piece == kMost) launch(cache_write_kernel<T, kMost, I8, 2, false>);
     else if (kMost == 8 && piece == 4) launch(cache_write_kernel<T, 4, I8, 2, false>);
     else if (piece == 2) launch(cache_write_kernel<T, 2, I8, 2, false>);

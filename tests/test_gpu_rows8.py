@@ -26,7 +26,8 @@ def code_bytes(shape, how="plain"):
 
 GROUPS = [(1, 1, 1), (1, 8, 0), (3, 64, 32), (5, 100, 32), (2, 100, 0), (33, 128, 128), (7, 1000, 128), (4, 1001, 0), (9, 96, 96), (2, 257, 256),
           (3, 7, 1), (6, 80, 20), (700, 104, 0), (5, 1000, 40), (64, 24, 24), (2, 4096, 128), (3, 4100, 64), (70, 513, 0), (2, 16384, 128), (1, 16400, 0), (2, 40_000, 64), (2, 20_001, 5),
-          (4, 505, 64), (5, 961, 0), (2, 4099, 8), (3, 9001, 128), (2, 777, 16), (6, 519, 256)]
+          (4, 505, 64), (5, 961, 0), (2, 4099, 8), (3, 9001, 128), (2, 777, 16), (6, 519, 256),
+          (3, 1040, 96), (3, 2056, 64), (5, 1032, 24), (2, 8192, 256), (3, 680, 8), (4, 1280, 160)]
 
 
 @pytest.mark.parametrize("how", ["plain", "slice", "odd"])
@@ -201,7 +202,8 @@ def sequences(lengths, page_rows, starts, seed, spare=2):
 
 CASES = [([1], [0], 1, 8, 8), ([1, 1, 1], [5, 0, 17], 4, 64, 32), ([7, 0, 130, 1], [0, 3, 60, 9], 16, 256, 64), ([40, 3], [0, 1], 3, 100, 32),
          ([65, 64, 63], [1, 0, 2], 64, 160, 80), ([5, 6], [0, 0], 5, 1001, 0), ([30], [2], 16, 192, 96), ([9, 9], [7, 8], 8, 1024, 128), ([3, 4], [0, 0], 2, 20, 1),
-         ([300, 200], [0, 0], 32, 512, 256), ([12], [0], 16, 300, 0), ([3000, 0, 2500], [5, 1, 0], 64, 128, 64), ([2000], [0], 16, 1024, 128)]
+         ([300, 200], [0, 0], 32, 512, 256), ([12], [0], 16, 300, 0), ([3000, 0, 2500], [5, 1, 0], 64, 128, 64), ([2000], [0], 16, 1024, 128),
+         ([3000, 0, 2500, 700], [5, 1, 0, 70], 64, 512, 128), ([6200], [0], 16, 512, 8), ([2500], [3], 32, 960, 96), ([5000], [0], 64, 520, 64), ([5000], [9], 64, 512, 16)]
 
 
 @pytest.mark.parametrize("how", ["plain", "pair", "odd"])
