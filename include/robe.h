@@ -576,7 +576,8 @@ int robe_table_forward(const void* table, int64_t table_ld, int64_t vocab, int64
  *   grad        [rows, d], fp32 or bf16 (dtype), grad_ld apart.
  *   skip        an id whose row gets no gradient (-1: none); ids outside the table never do.
  *   grad_table  fp32 [vocab, d], grad_table_ld apart.
- *   workspace   256-byte aligned, robe_table_backward_workspace_bytes(rows, vocab, d) (0 for bad arguments).
+ *   workspace   256-byte aligned, robe_table_backward_workspace_bytes(rows, vocab, d) (0 for bad arguments); the figure never falls
+ *               as rows or d grows, so one for the largest call serves every smaller one.
  *   rows < 2^31.
  * A sum's order follows from the sizes and ids alone: fp32 sums of at most 256 rows in the order of the call, joined in fp64.
  * Errors: as above, and ROBE_ERR_WORKSPACE.

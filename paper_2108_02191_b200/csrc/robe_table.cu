@@ -164,10 +164,20 @@ void launch_lookup(const LookupArgs& a, int piece, cudaStream_t st) {
 // most 256, so that no fp32 sum has more terms than that.  A border costs a row of sums for the run that crosses it, and CTAs
 // beyond a wave leave SMs empty (with eight columns a thread: 16384 x 4096 bf16, Zipf ids, accumulating, two waves 84 us, one
 // and a half 81, one 71; 852 K x 64 fp32 159, 153, 148; less than one 73 and 154).
+constexpr uint32_t kChunkLeast = 16, kChunkMost = 256;
+constexpr uint64_t kWave = 4 * 148 * kTableThreads;  // threads
 uint32_t chunk_rows(int64_t rows, int64_t d) {
-    const unsigned __int128 threads = (unsigned __int128)rows * (uint64_t)((d + 3) / 4), wanted = 4 * 148 * kTableThreads;
-    const unsigned __int128 c = (threads + wanted - 1) / wanted;
-    return c < 16 ? 16 : c > 256 ? 256 : (uint32_t)c;
+    const unsigned __int128 threads = (unsigned __int128)rows * (uint64_t)((d + 3) / 4);
+    const unsigned __int128 c = (threads + kWave - 1) / kWave;
+    return c < kChunkLeast ? kChunkLeast : c > kChunkMost ? kChunkMost : (uint32_t)c;
+}
+// Chunks x columns by fours, at least: what the largest of all calls with at most so many rows of at most so many columns has, so that a
+// workspace for the largest call serves every smaller one.  (Chunks get longer with a call, so there may be fewer of them: but of c rows, c
+// between the limits, there are at most ceil(kWave / fours), for c fours of such a row make up a wave at most.)
+uint64_t most_parts(int64_t rows, int64_t d) {
+    const uint64_t n = (uint64_t)rows, fours = (uint64_t)((d + 3) / 4), most = (n + kChunkMost - 1) / kChunkMost * fours;
+    if (chunk_rows(rows, d) == kChunkLeast) return (n + kChunkLeast - 1) / kChunkLeast * fours;
+    return most > kWave + fours ? most : kWave + fours;
 }
 // Where there are many chunks, the parts of a run that covers kFold of them are added up before the join.
 constexpr uint32_t kFold = 32;
@@ -199,8 +209,9 @@ GradLayout grad_layout(int64_t rows, int64_t d) {
     L.chunk = chunk_rows(rows, d);
     L.chunks = ((uint64_t)rows + L.chunk - 1) / L.chunk;
     L.parts_ld = (d + 3) / 4 * 4;
-    L.parts = take((size_t)L.chunks * 2 * L.parts_ld * 4);
-    L.folds = take(L.chunks >= kFoldFrom ? (size_t)(L.chunks / kFold) * L.parts_ld * 8 : 0);
+    const size_t most = most_parts(rows, d);
+    L.parts = take(most * 2 * 4 * sizeof(float));
+    L.folds = take(most * 4 * sizeof(double) / kFold);
     L.total = at;
     return L;
 }

@@ -167,6 +167,20 @@ def test_gradient_in_longer_chunks(n, d):
         assert torch.equal(table[:, c].double(), want)
 
 
+@pytest.mark.parametrize("n,largest,d", [(75_776, 79_000, 128), (151_552, 157_000, 64), (9472, 10_000, 1024), (2368, 2500, 4096), (16, 2369, 4096)])
+def test_gradient_with_the_workspace_of_a_larger_call(n, largest, d):
+    # calls of which the larger ones have fewer, longer chunks
+    vocab = 50
+    g = torch.Generator(device="cuda").manual_seed(n)
+    grad = torch.randint(-3, 4, (n, d), generator=g, device="cuda").float()
+    ids = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    ws = Workspace(robe.robe_table_backward_workspace_bytes(largest, vocab, d))
+    table = torch.full((vocab, d), NAN, device="cuda")
+    robe.robe_table_backward(grad, ids, table, ws.own)
+    want = torch.zeros(vocab, d, device="cuda").index_add_(0, ids, grad)  # (whole numbers: exact in any order)
+    assert torch.equal(table, want) and ws.kept_within()
+
+
 def test_gradient_skips_one_id_and_keeps_rows_without_ids():
     n, vocab, d = 500, 40, 24
     ids = torch.randint(0, 20, (n,), generator=gen(1))

@@ -114,6 +114,26 @@ def test_workspace_of_the_table_gradient():
     assert need(10**6, 100, 8192) >= 10**6 // 256 * 2 * 8192 * 4
 
 
+def test_workspace_of_the_table_gradient_never_falls_as_a_call_grows():
+    # one sized for the largest batch serves every smaller one; chunks of rows get longer where a call has more than a wave of them
+    need = robe.robe_table_backward_workspace_bytes
+    for d in (1, 3, 4, 64, 100, 128, 1000, 1024, 4096, 4099, 8192, 2**20):
+        for rows in (range(0, 3000), range(9000, 12_000), range(65_000, 66_000), range(75_000, 80_000, 3), range(150_000, 160_000, 7), range(0, 3_000_000, 1237),
+                     range(2**31 - 9000, 2**31, 11)):
+            sizes = [need(n, 10**6, d) for n in rows]
+            assert all(a <= b for a, b in zip(sizes, sizes[1:])), (d, rows)
+    for n in (1, 16, 17, 149, 512, 5003, 16_384, 65_536, 65_537, 100_000, 2 * 10**6, 2**31 - 1):
+        sizes = [need(n, 10**6, d) for d in list(range(1, 9000)) + list(range(9000, 2**20 + 1, 997))]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), n
+    # sizes at which it fell: the row counts at which chunks become longer
+    for n, d in [(75_776, 128), (151_552, 64), (9472, 1024), (2368, 4096)]:
+        assert need(n + 1, 10**6, d) >= need(n, 10**6, d)
+    # a call with the workspace of a larger one; one byte less than its own is refused (checked before anything is launched)
+    for n, d in [(75_777, 128), (2369, 4096)]:
+        assert backward(rows=n, vocab=10**6, d=d, ld=d, table_ld=d, grad=C.c_void_p(1 << 40), ids=C.c_void_p(2 << 40), table=C.c_void_p(3 << 40), ws=C.c_void_p(4 << 40),
+                        bytes=need(n, 10**6, d) - 1) == WORK
+
+
 # ---------------------------------------------------------------- rows in 8 bits: argument checks
 
 
