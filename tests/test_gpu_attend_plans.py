@@ -152,3 +152,13 @@ LONG = [
 @pytest.mark.parametrize("heads,group,dim,page_rows,lengths", LONG, ids=[f"{c[0]}x{c[1]}x{c[2]}-{len(c[4])}-{max(c[4])}" for c in LONG])
 def test_spans_of_long_sequences(heads, group, dim, page_rows, lengths, kind, buckets):
     check_call(lengths, heads, group, dim, page_rows, kind, buckets, room=0 if buckets else 1 << 19)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("buckets", [0, 32])
+@pytest.mark.parametrize("batch", [31, 32, 33, 64, 255, 256, 257, 600, 1025])
+def test_calls_of_many_sequences(batch, buckets):
+    # sequences of none, one, two and three spans in every group of 32
+    some = [0, 1, 256, 257, 700, 33, 512, 513, 128, 129, 64]
+    lengths = [some[(k * 7 + k // 32) % len(some)] for k in range(batch)]
+    check_call(lengths, 2, 2, 64, 16, KINDS[batch % 2], buckets, sample=sorted({*range(0, batch, 1 + batch // 40), *range(max(0, batch - 4), batch)}))
