@@ -162,3 +162,12 @@ def test_calls_of_many_sequences(batch, buckets):
     some = [0, 1, 256, 257, 700, 33, 512, 513, 128, 129, 64]
     lengths = [some[(k * 7 + k // 32) % len(some)] for k in range(batch)]
     check_call(lengths, 2, 2, 64, 16, KINDS[batch % 2], buckets, sample=sorted({*range(0, batch, 1 + batch // 40), *range(max(0, batch - 4), batch)}))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("buckets", [0, 32])
+@pytest.mark.parametrize("length,batch", [(96, 5), (1024, 5), (8192, 5), (320, 300)])
+def test_starts_beyond_the_page_table(length, batch, buckets):
+    # all positions of the table, whose distances go by where the token stands; no row is written behind the table's last
+    beyond = [length - 1, length, length + 5, 10**12, 2**63 - 1]
+    check_call([length] * batch, 2, 3, 64, 32, KINDS[1], buckets, starts=[beyond[s % 5] for s in range(batch)], sample=range(10 if batch > 10 else batch))

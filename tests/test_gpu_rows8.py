@@ -425,6 +425,7 @@ def test_attention_with_a_two_sided_bias_takes_its_earlier_side():
 
 def test_attention_of_short_lengths_in_a_long_table_and_of_no_keys():
     # page tables with room for far more than there is; a sequence without a key, one whose start is beyond the table
+    # (two without a key, in fact; starts beyond the table: test_gpu_attend_plans.py)
     lengths = [40, 3, 200, 64]
     made, pages, q, _ = attention_case(lengths, 2, 4, 128, 16, KINDS[0], 0, 11, room=20_000)
     out = run_attention(made, pages, q, [39, -1, 150, -2**63], 2, 0.1)
@@ -524,6 +525,7 @@ def test_attention_leaves_out_positions_without_a_place():
     for h in range(8):
         attention_close(out[0, h], q[0, h], made["keys_rows"][0][keep, 0], made["values_rows"][0][keep, 0], 0.2, None, KINDS[1])
     # a start beyond the table: all positions that the table has
+    # (that it runs and leaves the other sequence alone; the values of such a call: test_gpu_attend_plans.py)
     out = run_attention(made, pages, q, [pages.shape[1] * 16 + 10**12, 89], 1, 0.2)
     assert torch.isfinite(out[1].float()).all()
 
