@@ -10,9 +10,9 @@
 // Keys and values are copied ahead to shared memory, each warp for itself, in pieces of 16 bytes that are shuffled so that both
 // ways of reading them meet no bank twice.  Keys' scales multiply the scores; values' scales go into the weights:
 //     w_j = exp2(x_j - m) sv_j with m the running maximum of x_j + log2(sv_j)  (x_j = s_j log2(e)),
-// so that weights are at most 1 and are rounded to fp16 relative to the largest CONTRIBUTION (half a step is 2^-12 of a
-// weight down to 2^-14 of the largest, 2^-25 of the largest below: the result is bf16), while the divisor
-// sum exp2(x_j - m) stays in fp32.
+// so that weights are at most 1 and are rounded to fp16 relative to the largest CONTRIBUTION (half a step is at most 2^-11 of a
+// weight down to 2^-14 of the largest, 2^-25 of the largest below, where a weight of half a step and less is 0: the result is
+// bf16), while the divisor sum exp2(x_j - m) stays in fp32.
 // The new tokens' queries are taken to fp16 after an exact division by a power of two (of the row's largest element):
 // bf16 has fewer fraction bits than fp16, so elements down to 2^-16 of the largest stay exact.
 //
