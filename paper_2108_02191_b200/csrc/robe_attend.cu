@@ -3,8 +3,10 @@
 //     out = sum_j exp(s_j) V_j / sum_j exp(s_j).
 //
 // Bound by memory: 2 (dim + 4) bytes per key and head of the cache, each read once, for 4 dim operations per query head.  A warp
-// works on 32 keys at a time (16 where heads have 256 columns) with m16n8k16 instructions (fp16, fp32 sums): a single token has at most as many query heads to a head
-// of the cache as such an instruction has rows, so the tensor cores' larger tiles would stay empty.  Codes of 8 bits are exact in
+// works on 32 keys at a time (16 where heads have 256 columns) with m16n8k16 instructions (fp16, fp32 sums): a single token seldom has more query heads to a head
+// of the cache than such an instruction has rows, so the tensor cores' larger tiles would stay empty.  (More are taken in blocks of 16, each
+// of which copies and widens the keys and values anew: 64 sequences of up to 8191 keys, one head of 128, 16 / 32 / 64 query heads 34 / 54 / 82
+// us.)  Codes of 8 bits are exact in
 // fp16.  Since the order of a sum's terms is free, a thread reads 16 consecutive bytes of a key and calls them what the instruction
 // wants of it, and the transposed values come of one byte permutation per pair of keys, which the widening needs anyway.
 // Keys and values are copied ahead to shared memory, each warp for itself, in pieces of 16 bytes that are shuffled so that both
@@ -296,7 +298,7 @@ uint32_t most_ctas(int64_t dim) {
 }
 
 // WIDE: more than eight query heads to a CTA.
-// 64 sequences of up to 8191 keys, 8 heads of 128, e4m3, four query heads each (631 MB): 128-131 us with the join's 9, 74-76 % of what a copy
+// 64 sequences of up to 8191 keys, 8 heads of 128, e4m3, four query heads each (631 MB): 130 us with the join's 9, 74 % of what a copy
 // reaches; DRAM at 80 % while it runs, 11 warps an SM (shared memory, 167 registers) with 750 instructions for a warp's 32 keys. One of
 // 65521 keys, 4 heads: 21 us. A call of one key: 4.2 us.  The next item's first keys asked for before this one's sum is joined: no
 // faster (three CTAs an SM cover for one another).

@@ -4,8 +4,8 @@
 // S_v = sum of the gradient rows whose id is v needs them by id: ids and positions are sorted (stable radix sort, so the
 // order of a sum is the order of the rows in the call), the sorted positions are cut into chunks of equal length however
 // the ids repeat, a chunk sums its runs of equal ids in registers, and runs that cross a border between chunks are
-// joined afterwards from one partial row per chunk.  No atomics on floating-point data, no waits between CTAs:
-// the result is bit-reproducible.
+// joined afterwards from one partial row per chunk.  No atomics on floating-point data, and CTAs wait for one another only
+// within the cluster that sorts up to 65536 ids: the result is bit-reproducible.
 #include "robe_internal.h"
 #include "robe_rowops.cuh"
 
@@ -162,8 +162,8 @@ void launch_lookup(const LookupArgs& a, int piece, cudaStream_t st) {
 
 // Rows of a chunk of sorted positions: as many as make one full wave of CTAs (four an SM, four columns a thread); at least 16, and at
 // most 256, so that no fp32 sum has more terms than that.  A border costs a row of sums for the run that crosses it, and CTAs
-// beyond a wave leave SMs empty (with eight columns a thread: 16384 x 4096 bf16, Zipf ids, accumulating, two waves 84 us, one
-// and a half 81, one 71; 852 K x 64 fp32 159, 153, 148; less than one 73 and 154).
+// beyond a wave leave SMs empty (16384 x 4096 bf16, Zipf ids, accumulating: two waves 77 us, one
+// and a half 79, one 72, three quarters of one 80; 852 K x 64 fp32 147, 153, 144, 146; with uniform ids, and 5000 x 1000 bf16, all alike).
 constexpr uint32_t kChunkLeast = 16, kChunkMost = 256;
 constexpr uint64_t kWave = 4 * 148 * kTableThreads;  // threads
 uint32_t chunk_rows(int64_t rows, int64_t d) {

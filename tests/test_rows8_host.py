@@ -106,6 +106,7 @@ def test_workspace_of_the_table_gradient():
         assert need(*bad) == 0
     assert backward(bytes=need(4, 100, 8) - 1) == WORK
     # ids and positions twice, a byte an id of the table, two rows of sums for 16 rows of the gradient
+    # (there is no byte an id any more: the figure does not go by the table, and stays within the bound all the same)
     n, vocab, d = 16384, 65536, 4096
     assert need(n, vocab, d) <= 16 * n + vocab + n // 16 * 2 * d * 4 + 400_000
     # nothing overflows at the limits
