@@ -18,3 +18,13 @@ def test_tables_and_rows_in_8_bits_run_clean_on_the_index_check_build():
                        env=dict(os.environ, ROBE_LIBRARY=build.build_debug()), cwd=ROOT, capture_output=True, text=True, timeout=3000)
     assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
     assert " passed" in r.stdout
+
+
+def test_plans_of_the_attention_run_clean_on_the_index_check_build():
+    if os.environ.get("ROBE_LIBRARY"):
+        pytest.skip("already inside the child run")
+    from paper_2108_02191_b200 import build
+    r = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_attend_plans.py", "-m", "gpu", "-x", "-q"],
+                       env=dict(os.environ, ROBE_LIBRARY=build.build_debug()), cwd=ROOT, capture_output=True, text=True, timeout=3000)
+    assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
+    assert " passed" in r.stdout
