@@ -663,7 +663,7 @@ int robe_cache_read(const robe_cache_t* c, void* out, int64_t out_ld, int64_t n,
  *   max_pages * page_rows < 2^31 - 2^16;  batch * q_heads < 2^31;  codes of a cache within 64 GB, scales within 16 (ROBE_ERR_UNSUPPORTED).
  * Scores, the divisor and the sums are fp32.  Weights are rounded to fp16 with their value's scale in them: with c_j = exp(x_j) times
  * V_j's scale and c the largest of a span's, c_j is off by at most 2^-11 of itself from 2^-14 c on and by at most 2^-25 c below,
- * so that a key of at most 2^-25 c adds nothing to the sum, while the divisor counts it exactly.  A result is off by that times codes: small
+ * so that a key of at most 2^-25 c adds nothing to the sum, while the divisor, in fp32, counts it.  A result is off by that times codes: small
  * next to the largest contribution to its row, not next to a column's own sum where the keys of large c_j have a code of 0 there.
  * How the sum over a sequence is cut follows from all lengths of the call; the same call gives the same bits.
  * Errors: ROBE_ERR_INVALID_ARG, ROBE_ERR_WORKSPACE, ROBE_ERR_UNSUPPORTED, ROBE_ERR_CUDA.
